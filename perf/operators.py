@@ -325,7 +325,7 @@ def _plain_norm_backward(case, s):
     xhat = (x - s["mean"][:, None]) * rstd
     g = dy * s["gamma"].float()
     dx = rstd * (g - g.mean(dim=1, keepdim=True) - xhat * (g * xhat).mean(dim=1, keepdim=True))
-    return [dx.to(dy.dtype), (dy * xhat).sum(dim=0).to(s["gamma"].dtype), dy.sum(dim=0).to(s["gamma"].dtype)]
+    return [dx.to(s["dy"].dtype), (dy * xhat).sum(dim=0).to(s["gamma"].dtype), dy.sum(dim=0).to(s["gamma"].dtype)]
 
 
 # ---- the package's calls --------------------------------------------------------------------------
