@@ -339,6 +339,97 @@ int fh_plan_measure(const fh_tensor_desc* descs, int32_t n, const fh_params* par
                     void* d_work, size_t work_bytes, int32_t repeats, fh_plan_tensor* out, void* stream);
 
 /*
+ * Matrices in microscaled 4-bit floating point.
+ *
+ * The paper's quantiser (Section 4.4.1) keeps uniform codes between a plane's minimum and maximum, which suits feature maps.  The
+ * saved inputs of linear layers are matrices, which the backward pass multiplies; in the form here they need not be restored first:
+ * the tensor cores multiply the codes.
+ *
+ * A value is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign (E2M1), times the scale of its block.  Blocks are runs of consecutive
+ * elements of a row; a row's last block is filled up with zeros.
+ *   FH_MX_B32   blocks of 32, scales 2^k, k = -127 ... 125 (E8M0, the OCP microscaling format MXFP4)
+ *   FH_MX_B16   blocks of 16, scales E4M3 (2^-9 ... 448) times 2^exponent, one exponent for the matrix, -64 ... 64
+ * A block's scale is the smallest of its type that is at least a sixth of the block's largest magnitude (the largest, if none is;
+ * the smallest for a block of zeros).  Values are divided by their scale and rounded to nearest, ties to even; what is beyond 6
+ * becomes 6, which happens only where the largest scale was too small.  rounding = 1: a value between two neighbours goes up (in
+ * magnitude) iff its distance from the lower one exceeds (r + 1/2) / 2^16 of the step, r the low (even columns) or high half of
+ * word (column mod 8) / 2 of Philox-4x32-10 with key (seed low, seed high) and counter (column / 8, row, tensor_id low, high):
+ * the restored value is unbiased to within 2^-17 of a step.  All of this is exact: containers are pure functions of the input and the parameters.
+ * A block with a NaN or an infinity gets the scale NaN (byte 255 or 127) and codes 0, and is restored as NaN.
+ *
+ * Container of a rows x cols matrix (little-endian): 128 bytes of header: u32 magic "FHM4" | u16 version (1) | u8 format | u8 rounding |
+ * i32 rows | i32 cols | i32 exponent | u32 0 | u64 total bytes | u64 tensor_id | zeros.  Then the codes, rows padded to a multiple of 8 and
+ * columns to Kp, a multiple of 64, with zeros: for each 128 rows (the last ones: as many as there are), for each 32 columns, 16 bytes a row,
+ * columns 2i and 2i + 1 in the low and high half of byte i.  Then the scales: for each 128 rows, for each four blocks, 512 bytes, those of
+ * row r at 16 (r mod 32) + 4 (r mod 128 / 32); zeros where there is no row or no block.
+ */
+typedef enum { FH_MX_B32 = 0, FH_MX_B16 = 1 } fh_mx_format;
+
+/* A dense matrix: element (r, c) at r * ld + c; pointers need the element's alignment only (16-byte aligned rows are faster). */
+typedef struct {
+  int32_t dtype; /* fh_dtype */
+  int32_t rows, cols;
+  int32_t reserved; /* 0 */
+  int64_t ld;       /* >= cols */
+} fh_matrix;
+
+typedef struct {
+  int32_t format;   /* fh_mx_format                                                            */
+  int32_t exponent; /* B16: the matrix's exponent, its largest magnitude is held when it is
+                       at most 2688 * 2^exponent; B32: 0                                         */
+  int32_t rounding; /* 0 = to nearest, 1 = random                                              */
+  int32_t reserved; /* 0                                                                       */
+  uint64_t seed;    /* key of the random draws                                                 */
+  uint64_t tensor_id;
+} fh_mx_params;
+
+/* Size of a container; 0 for invalid arguments.  Host-only, no CUDA call. */
+size_t fh_mx_bytes(int32_t rows, int32_t cols, int32_t format);
+
+/*
+ * Compress a matrix: one kernel, one pass over d_src.
+ *   d_rows   container of the matrix (blocks along its rows), 16-byte aligned, rows_capacity bytes; may be NULL
+ *   d_cols   container of its transpose (blocks along its columns), cols_capacity bytes; may be NULL, but not both.  It is the container
+ *            that compressing the transposed matrix gives, draws included.
+ * A matrix product needs its operands' blocks along the axis it sums over; forward and backward pass sum over different ones.
+ * FH_ERR_CAPACITY when a container has less than fh_mx_bytes.  Input and containers must not overlap.
+ */
+int fh_mx_compress(const fh_matrix* matrix, const fh_mx_params* params, const void* d_src, void* d_rows, size_t rows_capacity,
+                   void* d_cols, size_t cols_capacity, void* stream);
+
+/*
+ * Restore a matrix from its container: one kernel.  Values are exact in fp32 and in bf16.
+ *   expect, format   what the caller expects; another header is FH_ERR_CORRUPT (through d_status; nothing is written then)
+ *   d_dst            the matrix; elements between cols and ld are left alone
+ *   d_status         optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
+ */
+int fh_mx_decompress(const void* d_src, size_t src_bytes, const fh_matrix* expect, int32_t format, void* d_dst, uint64_t* d_status,
+                     void* stream);
+
+/*
+ * C = alpha * A B^T, or C + alpha * A B^T, of matrices held in containers of one format: A m x k, B n x k, C m x n, dense.  One kernel.
+ * The products of codes are exact, sums and scales are fp32, C is rounded once.  A linear layer y = x W^T with W out x in: forward
+ * A = x by rows, B = W by rows; the input's gradient A = dy by rows, B = W by columns; the weight's gradient A = dy by columns, B = x by
+ * columns.  Where the blocks along k of a row of A or B hold a NaN scale, that row (column) of C is NaN.
+ *   d_a, d_b    containers of an m x k and an n x k matrix; another header is FH_ERR_CORRUPT (through d_status; C is not written then)
+ *   d_c         element (i, j) at i * ldc + j; must not overlap the containers
+ *   d_status    optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
+ * Results do not depend on the call's place among others: equal inputs give equal bits.
+ */
+typedef struct {
+  int32_t format;     /* fh_mx_format of both                     */
+  int32_t m, n, k;
+  int32_t dtype;      /* fh_dtype of C                            */
+  int32_t accumulate; /* 1: C is added to                         */
+  int64_t ldc;        /* >= n                                     */
+  float alpha;        /* finite                                   */
+  int32_t reserved;   /* 0                                        */
+} fh_mx_product_desc;
+
+int fh_mx_product(const fh_mx_product_desc* desc, const void* d_a, size_t a_bytes, const void* d_b, size_t b_bytes, void* d_c,
+                  uint64_t* d_status, void* stream);
+
+/*
  * Fault injection on the host side, for tests of the error path of the device-side waits.  (The paper has no
  * counterpart.)  Compressing places the overflow parts of outlier-rich planes in plane order: a tile of
  * planes waits, with a limit, until every earlier tile has published its size; a wait that runs out ends the

@@ -19,6 +19,7 @@ FH_OK, FH_ERR_ARG, FH_ERR_UNSUPPORTED, FH_ERR_CAPACITY, FH_ERR_NONFINITE, FH_ERR
 FH_F32, FH_BF16 = 0, 1
 FH_SALIENT_AUTO, FH_SALIENT_OFF, FH_SALIENT_ALL, FH_SALIENT_CHANNEL, FH_SALIENT_TENSOR = 0, 1, 2, 3, 4
 FH_KEEP, FH_COMPRESS, FH_EVICT = 0, 1, 2
+FH_MX_B32, FH_MX_B16 = 0, 1
 FH_STATIC_MAX_PLANES = 131072
 FH_DEBUG_WAIT_POLLS, FH_DEBUG_SILENT_TILE = 0, 1
 
@@ -26,7 +27,7 @@ EXPORTS = ["fh_default_params", "fh_version", "fh_device_count", "fh_compressed_
            "fh_decompress", "fh_run_schedule", "fh_host_work_bytes", "fh_compress_host",
            "fh_decompress_host", "fh_compress_static", "fh_plan_generate", "fh_plan_measure", "fh_debug_set",
            "fh_kernel_launches",
-           "fh_shutdown"]
+           "fh_shutdown", "fh_mx_bytes", "fh_mx_compress", "fh_mx_decompress", "fh_mx_product"]
 
 
 class FhError(RuntimeError):
@@ -81,6 +82,20 @@ class fh_plan_report(C.Structure):
                 ("n_over_budget", C.c_int32)]
 
 
+class fh_matrix(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("reserved", C.c_int32), ("ld", C.c_int64)]
+
+
+class fh_mx_params(C.Structure):
+    _fields_ = [("format", C.c_int32), ("exponent", C.c_int32), ("rounding", C.c_int32), ("reserved", C.c_int32),
+                ("seed", C.c_uint64), ("tensor_id", C.c_uint64)]
+
+
+class fh_mx_product_desc(C.Structure):
+    _fields_ = [("format", C.c_int32), ("m", C.c_int32), ("n", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32),
+                ("accumulate", C.c_int32), ("ldc", C.c_int64), ("alpha", C.c_float), ("reserved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -128,6 +143,16 @@ def lib() -> C.CDLL:
         L.fh_debug_set.restype = C.c_int
         L.fh_kernel_launches.restype = C.c_uint64
         L.fh_shutdown.restype = None
+        L.fh_mx_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+        L.fh_mx_bytes.restype = C.c_size_t
+        L.fh_mx_compress.argtypes = [C.POINTER(fh_matrix), C.POINTER(fh_mx_params), C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p,
+                                     C.c_size_t, C.c_void_p]
+        L.fh_mx_compress.restype = C.c_int
+        L.fh_mx_decompress.argtypes = [C.c_void_p, C.c_size_t, C.POINTER(fh_matrix), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.fh_mx_decompress.restype = C.c_int
+        L.fh_mx_product.argtypes = [C.POINTER(fh_mx_product_desc), C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p,
+                                    C.c_void_p]
+        L.fh_mx_product.restype = C.c_int
         _lib = L
     return _lib
 
@@ -267,6 +292,66 @@ def plan_measure(descs, p: fh_params, dense, work, repeats: int = 5, t_recompute
                                _stream_ptr(stream))
     return int(rc), [dict(bytes=int(o.bytes), packed_bytes=int(o.packed_bytes), t_compress=float(o.t_compress),
                           t_decompress=float(o.t_decompress), t_recompute=float(o.t_recompute)) for o in out]
+
+
+# ---- matrices in microscaled 4-bit floating point ------------------------------------------------
+
+def matrix(rows: int, cols: int, dtype: int = FH_F32, ld: Optional[int] = None) -> fh_matrix:
+    return fh_matrix(dtype, rows, cols, 0, cols if ld is None else ld)
+
+
+def mx_params(format: int = FH_MX_B32, exponent: int = 0, rounding: int = 0, seed: int = 0, tensor_id: int = 0) -> fh_mx_params:
+    return fh_mx_params(format, exponent, rounding, 0, seed, tensor_id)
+
+
+def mx_bytes(rows: int, cols: int, format: int) -> int:
+    return int(lib().fh_mx_bytes(rows, cols, format))
+
+
+def _ptr(t, elements: int = 0, esize: int = 1) -> Optional[int]:
+    """A tensor's address, once it is known to hold `elements` of `esize` bytes on the current device (the library takes
+    addresses and cannot see what they belong to)."""
+    if t is None:
+        return None
+    import torch
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"a tensor on {t.device}, where cuda:{torch.cuda.current_device()} is the current device")
+    if elements and (t.element_size() != esize or t.untyped_storage().nbytes() < (t.storage_offset() + elements) * esize):
+        raise ValueError(f"a tensor of {t.dtype} and shape {tuple(t.shape)}, where {elements} elements of {esize} bytes are wanted")
+    return t.data_ptr()
+
+
+def _extent(m) -> int:
+    """Elements from a matrix's first to its last, 0 where the library will refuse it."""
+    return max(0, (m.rows - 1) * m.ld + m.cols)
+
+
+def _esize(dtype: int) -> int:
+    return 4 if dtype == FH_F32 else 2
+
+
+def fh_mx_compress(m: fh_matrix, p: fh_mx_params, src, rows=None, cols=None, stream=None) -> int:
+    """Enqueue compression of the matrix `src` (a CUDA tensor that `m` describes) into the uint8 CUDA tensors `rows` (blocks
+    along its rows) and `cols` (the transpose, blocks along the columns); either may be None."""
+    return lib().fh_mx_compress(C.byref(m), C.byref(p), _ptr(src, _extent(m), _esize(m.dtype)), _ptr(rows), 0 if rows is None else rows.nbytes,
+                                _ptr(cols), 0 if cols is None else cols.nbytes, _stream_ptr(stream))
+
+
+def fh_mx_decompress(src, m: fh_matrix, format: int, dst, status=None, stream=None) -> int:
+    """Enqueue restoring the container `src` (uint8) into `dst`, which `m` describes."""
+    return lib().fh_mx_decompress(_ptr(src), src.nbytes, C.byref(m), format, _ptr(dst, _extent(m), _esize(m.dtype)),
+                                  _ptr(status), _stream_ptr(stream))
+
+
+def mx_product_desc(m: int, n: int, k: int, format: int = FH_MX_B32, dtype: int = FH_F32, ldc: Optional[int] = None, alpha: float = 1.0,
+                    accumulate: bool = False) -> fh_mx_product_desc:
+    return fh_mx_product_desc(format, m, n, k, dtype, int(accumulate), n if ldc is None else ldc, alpha, 0)
+
+
+def fh_mx_product(d: fh_mx_product_desc, a, b, c, status=None, stream=None) -> int:
+    """Enqueue the product of the containers `a` (m x k) and `b` (n x k), uint8 CUDA tensors, into the matrix `c` (m x n)."""
+    return lib().fh_mx_product(C.byref(d), _ptr(a), a.nbytes, _ptr(b), b.nbytes,
+                               _ptr(c, max(0, (d.m - 1) * d.ldc + d.n), _esize(d.dtype)), _ptr(status), _stream_ptr(stream))
 
 
 def debug_set(what: int, value: int) -> int:

@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "fh_launch.cuh"
+#include "fh_mx_launch.cuh"
 
 namespace fh {
 
@@ -530,6 +531,10 @@ int enqueue_decompress(const void* d_src, size_t src_bytes, const fh_tensor_desc
 bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
 }  // namespace
+
+namespace fh {
+void count_launch(int kernels) { g_launches.fetch_add((uint64_t)kernels); }
+}  // namespace fh
 
 extern "C" {
 

@@ -1,0 +1,107 @@
+// Host side of the C ABI's functions on microscaled 4-bit matrices: argument checks and launches.  None of them keeps anything between
+// calls, so that they can be captured, replayed and called from several threads.
+#include "../../include/fh.h"
+
+#include <cuda_runtime.h>
+
+#include "fh_launch.cuh"
+#include "fh_mx.cuh"
+#include "fh_mx_launch.cuh"
+
+namespace {
+
+bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+size_t esize_of(int dtype) { return dtype == FH_F32 ? 4 : 2; }
+bool is_dtype(int dtype) { return dtype == FH_F32 || dtype == FH_BF16; }
+bool is_format(int format) { return format == FH_MX_B32 || format == FH_MX_B16; }
+
+int check_matrix(const fh_matrix* m) {
+  if (!m || !is_dtype(m->dtype) || m->rows < 1 || m->cols < 1 || m->reserved != 0) return FH_ERR_ARG;
+  // (addresses are formed in 64 bits of bytes)
+  if (m->ld < m->cols || m->ld > (INT64_MAX >> 3) / m->rows) return FH_ERR_ARG;
+  return FH_OK;
+}
+
+int check_mx(const fh_mx_params* p) {
+  if (!p || !is_format(p->format) || p->reserved != 0) return FH_ERR_ARG;
+  if (p->rounding != 0 && p->rounding != 1) return FH_ERR_UNSUPPORTED;
+  if (p->format == FH_MX_B32 ? p->exponent != 0 : (p->exponent < -64 || p->exponent > 64)) return FH_ERR_ARG;
+  return FH_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fh_mx_bytes(int32_t rows, int32_t cols, int32_t format) {
+  // (padded extents stay below 2^32)
+  if (rows < 1 || cols < 1 || !is_format(format)) return 0;
+  return (size_t)fh::MxLayout((uint32_t)rows, (uint32_t)cols, (uint32_t)format).total;
+}
+
+int fh_mx_compress(const fh_matrix* matrix, const fh_mx_params* params, const void* d_src, void* d_rows, size_t rows_capacity,
+                   void* d_cols, size_t cols_capacity, void* stream) {
+  int rc = check_matrix(matrix);
+  if (rc != FH_OK) return rc;
+  rc = check_mx(params);
+  if (rc != FH_OK) return rc;
+  if (!d_src || (!d_rows && !d_cols) || misaligned(d_src, esize_of(matrix->dtype)) || misaligned(d_rows, 16) || misaligned(d_cols, 16))
+    return FH_ERR_ARG;
+  if (d_rows && rows_capacity < fh_mx_bytes(matrix->rows, matrix->cols, params->format)) return FH_ERR_CAPACITY;
+  if (d_cols && cols_capacity < fh_mx_bytes(matrix->cols, matrix->rows, params->format)) return FH_ERR_CAPACITY;
+  fh::MxSaveArgs a = {};
+  a.src = (const uint8_t*)d_src;
+  a.by_rows = (uint8_t*)d_rows;
+  a.by_cols = (uint8_t*)d_cols;
+  a.rows = (uint32_t)matrix->rows;
+  a.cols = (uint32_t)matrix->cols;
+  a.ld = (uint64_t)matrix->ld;
+  a.exponent = params->exponent;
+  a.seed = params->seed;
+  a.tensor_id = params->tensor_id;
+  return fh::launch_mx_save(a, matrix->dtype, params->format, true, params->rounding == 1, (cudaStream_t)stream);
+}
+
+int fh_mx_decompress(const void* d_src, size_t src_bytes, const fh_matrix* expect, int32_t format, void* d_dst, uint64_t* d_status,
+                     void* stream) {
+  const int rc = check_matrix(expect);
+  if (rc != FH_OK) return rc;
+  if (!is_format(format) || !d_src || !d_dst || misaligned(d_src, 16) || misaligned(d_dst, esize_of(expect->dtype)) || misaligned(d_status, 8))
+    return FH_ERR_ARG;
+  fh::MxSaveArgs a = {};
+  a.src = (const uint8_t*)d_src;
+  a.src_bytes = src_bytes;
+  a.dst = (uint8_t*)d_dst;
+  a.status = (unsigned long long*)d_status;
+  a.rows = (uint32_t)expect->rows;
+  a.cols = (uint32_t)expect->cols;
+  a.ld = (uint64_t)expect->ld;
+  return fh::launch_mx_save(a, expect->dtype, format, false, false, (cudaStream_t)stream);
+}
+
+int fh_mx_product(const fh_mx_product_desc* desc, const void* d_a, size_t a_bytes, const void* d_b, size_t b_bytes, void* d_c,
+                  uint64_t* d_status, void* stream) {
+  if (!desc || !is_format(desc->format) || !is_dtype(desc->dtype) || desc->m < 1 || desc->n < 1 || desc->k < 1) return FH_ERR_ARG;
+  if ((desc->accumulate != 0 && desc->accumulate != 1) || desc->reserved != 0 || desc->ldc < desc->n ||
+      desc->ldc > (INT64_MAX >> 3) / desc->m)
+    return FH_ERR_ARG;
+  if (!(desc->alpha >= -3.4028235e38f && desc->alpha <= 3.4028235e38f)) return FH_ERR_ARG;
+  if (!d_a || !d_b || !d_c || misaligned(d_a, 16) || misaligned(d_b, 16) || misaligned(d_c, esize_of(desc->dtype)) || misaligned(d_status, 8))
+    return FH_ERR_ARG;
+  fh::MxProductArgs a = {};
+  a.a = (const uint8_t*)d_a;
+  a.b = (const uint8_t*)d_b;
+  a.a_bytes = a_bytes;
+  a.b_bytes = b_bytes;
+  a.c = (uint8_t*)d_c;
+  a.status = (unsigned long long*)d_status;
+  a.m = (uint32_t)desc->m;
+  a.n = (uint32_t)desc->n;
+  a.k = (uint32_t)desc->k;
+  a.ldc = (uint64_t)desc->ldc;
+  a.alpha = desc->alpha;
+  a.accumulate = desc->accumulate == 1;
+  return fh::launch_mx_product(a, desc->dtype, desc->format, (cudaStream_t)stream);
+}
+
+}  // extern "C"

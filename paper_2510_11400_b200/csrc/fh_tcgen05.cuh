@@ -1,0 +1,86 @@
+// Tensor-core instructions of sm_100a as the product kernels use them: tensor memory, scale copies, block-scaled matrix
+// instructions on 4-bit operands, clusters.
+#pragma once
+
+#include <stdint.h>
+
+#include "fh_device.cuh"
+
+namespace fh {
+
+__device__ __forceinline__ void tmem_alloc(uint32_t* at, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(at)), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t base, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tmem_last_alloc() { asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Arrives at `bar` when all matrix instructions and scale copies that this thread has issued are complete.
+__device__ __forceinline__ void tc_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+// Shared-memory descriptor without swizzle: the operand is made of pieces of 8 rows x 16 bytes, each 128 bytes in a row; `lead`
+// bytes from a piece to the next along a row, `stride` bytes to the next eight rows.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint32_t stride) {
+  return (uint64_t)(addr >> 4 & 0x3FFFu) | (uint64_t)(lead >> 4 & 0x3FFFu) << 16 | (uint64_t)(stride >> 4 & 0x3FFFu) << 32 | 1ull << 46;
+}
+
+// 512 bytes of scales (128 rows, four blocks) to four columns of tensor memory, repeated for each 32 lanes.
+__device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+
+// Instruction descriptor: both operands E2M1, M x N, scales E8M0 or E4M3; `id`: which of a word's scales come first.
+__host__ __device__ constexpr uint32_t mx_idesc(uint32_t m, uint32_t n, bool e8m0, uint32_t id) {
+  return id << 4 | 1u << 7 | 1u << 10 | n / 8u << 17 | (e8m0 ? 1u : 0u) << 23 | m / 16u << 24 | id << 29;
+}
+
+// D (+)= A B^T over 64 elements: block-scaled, blocks of 32 (two scales to a row) or 16 (four).
+template <bool B32>
+__device__ __forceinline__ void tc_mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool add) {
+  if (B32)
+    asm volatile(
+        "{ .reg .pred p; setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p; }" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)add)
+        : "memory");
+  else
+    asm volatile(
+        "{ .reg .pred p; setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p; }" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)add)
+        : "memory");
+}
+
+// 16 columns of the warp's 32 lanes: lane i gets its row's.  The values are there after tc_load_wait().
+__device__ __forceinline__ void tc_load16(uint32_t tmem, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+        "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(tmem)
+      : "memory");
+}
+__device__ __forceinline__ void tc_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// Word at `addr` of the shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ float ld_cluster(uint32_t addr, uint32_t rank) {
+  uint32_t there;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+  return v;
+}
+
+}  // namespace fh

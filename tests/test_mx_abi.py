@@ -1,0 +1,79 @@
+"""Refusals of the microscaled matrices' functions and their size formula: host-side, before any CUDA call."""
+import ctypes as C
+
+import pytest
+
+from oracle import mx
+from paper_2510_11400_b200 import api, build
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return api.lib()
+
+
+A = 4096    # an aligned address that nothing reads
+
+
+def test_struct_sizes_match_the_header():
+    assert C.sizeof(api.fh_matrix) == 24 and C.sizeof(api.fh_mx_params) == 32 and C.sizeof(api.fh_mx_product_desc) == 40
+
+
+@pytest.mark.parametrize("fmt", [mx.B32, mx.B16])
+@pytest.mark.parametrize("shape", [(1, 1), (8, 64), (9, 65), (128, 256), (129, 257), (1000, 40), (2 ** 31 - 1, 1), (1, 2 ** 31 - 1),
+                                   (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_sizes(lib, shape, fmt):
+    assert api.mx_bytes(*shape, fmt) == mx.sizes(*shape, fmt)[3]
+
+
+def test_sizes_of_nothing(lib):
+    assert api.mx_bytes(0, 5, 0) == api.mx_bytes(5, 0, 0) == api.mx_bytes(-1, 5, 0) == api.mx_bytes(5, 5, 2) == api.mx_bytes(5, 5, -1) == 0
+
+
+def compress(lib, m, p, src=A, rows=A, rcap=1 << 40, cols=A, ccap=1 << 40):
+    return lib.fh_mx_compress(C.byref(m) if m is not None else None, C.byref(p) if p is not None else None, src, rows, rcap, cols, ccap, None)
+
+
+def test_compress_refuses(lib):
+    m, p, ARG = api.matrix(10, 40), api.mx_params(), api.FH_ERR_ARG
+    assert compress(lib, None, p) == ARG and compress(lib, m, None) == ARG
+    for bad in (api.matrix(0, 40), api.matrix(10, 0), api.matrix(10, -4), api.matrix(10, 40, 2), api.matrix(10, 40, 0, 39),
+                api.matrix(2 ** 31 - 1, 40, 0, 2 ** 40), api.matrix(2 ** 31 - 1, 2 ** 31 - 1), api.fh_matrix(0, 10, 40, 1, 40)):
+        assert compress(lib, bad, p) == ARG
+    for bad in (api.mx_params(2), api.mx_params(-1), api.mx_params(mx.B32, 1), api.mx_params(mx.B16, 65), api.mx_params(mx.B16, -65),
+                api.fh_mx_params(0, 0, 0, 1, 0, 0)):
+        assert compress(lib, m, bad) == ARG
+    assert compress(lib, m, api.mx_params(rounding=2)) == api.FH_ERR_UNSUPPORTED
+    assert compress(lib, m, p, src=None) == ARG and compress(lib, m, p, rows=None, cols=None) == ARG
+    assert compress(lib, m, p, src=A + 2) == ARG and compress(lib, m, p, rows=A + 8) == ARG and compress(lib, m, p, cols=A + 8) == ARG
+    assert compress(lib, api.matrix(10, 40, api.FH_BF16), p, src=A + 1) == ARG
+    assert compress(lib, m, p, rcap=api.mx_bytes(10, 40, 0) - 1) == api.FH_ERR_CAPACITY
+    assert compress(lib, m, p, ccap=api.mx_bytes(40, 10, 0) - 1) == api.FH_ERR_CAPACITY
+    assert compress(lib, api.matrix(2 ** 29, 2 ** 29), p, rcap=1 << 62, ccap=1 << 62) == api.FH_ERR_UNSUPPORTED
+
+
+def test_decompress_refuses(lib):
+    def call(m, fmt=0, src=A, n=1 << 40, dst=A, status=None):
+        return lib.fh_mx_decompress(src, n, C.byref(m) if m is not None else None, fmt, dst, status, None)
+    m, ARG = api.matrix(10, 40), api.FH_ERR_ARG
+    assert call(None) == ARG and call(m, 2) == ARG and call(m, src=None) == ARG and call(m, dst=None) == ARG
+    assert call(m, src=A + 8) == ARG and call(m, dst=A + 2) == ARG and call(m, status=A + 4) == ARG
+    assert call(api.matrix(10, 40, 3)) == ARG and call(api.matrix(10, 40, 0, 8)) == ARG and call(api.matrix(0, 1)) == ARG
+
+
+def test_product_refuses(lib):
+    def call(d, a=A, b=A, c=A, status=None):
+        return lib.fh_mx_product(C.byref(d) if d is not None else None, a, 1 << 40, b, 1 << 40, c, status, None)
+    ARG, good = api.FH_ERR_ARG, api.mx_product_desc(5, 6, 7)
+    assert call(None) == ARG
+    for bad in (dict(m=0), dict(n=0), dict(k=-1), dict(format=2), dict(dtype=2), dict(ldc=5), dict(alpha=float("nan")), dict(alpha=float("inf")),
+                dict(ldc=2 ** 62)):
+        kw = dict(m=5, n=6, k=7) | bad
+        assert call(api.mx_product_desc(**kw)) == ARG, bad
+    for field in ("accumulate", "reserved"):
+        d = api.mx_product_desc(5, 6, 7)
+        setattr(d, field, 2)
+        assert call(d) == ARG
+    assert call(good, a=None) == ARG and call(good, b=None) == ARG and call(good, c=None) == ARG
+    assert call(good, a=A + 8) == ARG and call(good, b=A + 8) == ARG and call(good, c=A + 2) == ARG and call(good, status=A + 4) == ARG
