@@ -430,6 +430,51 @@ int fh_mx_product(const fh_mx_product_desc* desc, const void* d_a, size_t a_byte
                   uint64_t* d_status, void* stream);
 
 /*
+ * Layer norm with its output, and its saved input, in 4 bits.
+ *
+ * y = (x - mean) * rstd * gamma + beta over each row, mean and variance (divisor cols) of the row, rstd = 1 / sqrt(variance + eps).  A
+ * linear layer behind it reads y from the container that the same kernel writes; the backward pass reads x from a container, so that
+ * neither has to be kept dense.
+ */
+typedef struct {
+  int32_t dtype;    /* fh_dtype of x, y, dy, dx                                                */
+  int32_t wdtype;   /* fh_dtype of gamma, beta and their gradients                             */
+  int32_t rows, cols; /* cols <= 28672 (FH_ERR_UNSUPPORTED beyond)                              */
+  float eps;        /* >= 0                                                                    */
+  int32_t reserved; /* 0                                                                       */
+  int64_t ldx;      /* elements from one row of x (and of dx) to the next, >= cols            */
+  int64_t ldy;      /* ... of y (and of dy)                                                    */
+} fh_norm_desc;
+
+/*
+ * Forward pass: one kernel, x is read once (rows of more than 2048 16-byte vectors: three times).
+ *   d_gamma, d_beta   cols weights, either may be NULL (1, 0)
+ *   d_y               dense output, may be NULL if d_packed is not; may be d_x when ldx = ldy
+ *   d_mean, d_rstd    rows floats for the backward pass, either may be NULL
+ *   params, d_packed  container of y (blocks along its rows, rounding to nearest), packed_capacity bytes; byte for byte what
+ *                     fh_mx_compress makes of the dense y in its type; may be NULL
+ */
+int fh_layer_norm(const fh_norm_desc* desc, const void* d_x, const void* d_gamma, const void* d_beta, void* d_y, float* d_mean,
+                  float* d_rstd, const fh_mx_params* params, void* d_packed, size_t packed_capacity, void* stream);
+
+/*
+ * Backward pass, with xhat = (x - mean) * rstd and g = dy * gamma:
+ *   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)), dgamma = sum over the rows of dy * xhat, dbeta = sum over the rows of dy.
+ *   d_x, x_bytes      x_bytes = 0: dense x; otherwise a container of x, of format x_format, of x_bytes readable bytes (another header
+ *                     is FH_ERR_CORRUPT through d_status, and nothing is written)
+ *   d_gamma           as in the forward pass, may be NULL;  d_mean, d_rstd  rows floats each
+ *   d_dx, d_dgamma, d_dbeta   any may be NULL, but not all; d_dx may be d_dy when ldx = ldy, or the dense d_x
+ *   d_work            caller-owned workspace, 16-byte aligned, at least fh_layer_norm_work_bytes(desc) bytes, needed when d_dgamma or
+ *                     d_dbeta is given; calls that may run at the same time need one each
+ *   d_status          optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
+ * One kernel, and a second, small one for dgamma and dbeta.  Sums are fp32 in a fixed order: equal inputs give equal bits.
+ */
+size_t fh_layer_norm_work_bytes(const fh_norm_desc* desc);
+int fh_layer_norm_backward(const fh_norm_desc* desc, const void* d_dy, const void* d_x, size_t x_bytes, int32_t x_format, const void* d_gamma,
+                           const float* d_mean, const float* d_rstd, void* d_dx, void* d_dgamma, void* d_dbeta, void* d_work,
+                           size_t work_bytes, uint64_t* d_status, void* stream);
+
+/*
  * Fault injection on the host side, for tests of the error path of the device-side waits.  (The paper has no
  * counterpart.)  Compressing places the overflow parts of outlier-rich planes in plane order: a tile of
  * planes waits, with a limit, until every earlier tile has published its size; a wait that runs out ends the

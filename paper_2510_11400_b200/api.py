@@ -27,7 +27,8 @@ EXPORTS = ["fh_default_params", "fh_version", "fh_device_count", "fh_compressed_
            "fh_decompress", "fh_run_schedule", "fh_host_work_bytes", "fh_compress_host",
            "fh_decompress_host", "fh_compress_static", "fh_plan_generate", "fh_plan_measure", "fh_debug_set",
            "fh_kernel_launches",
-           "fh_shutdown", "fh_mx_bytes", "fh_mx_compress", "fh_mx_decompress", "fh_mx_product"]
+           "fh_shutdown", "fh_mx_bytes", "fh_mx_compress", "fh_mx_decompress", "fh_mx_product", "fh_layer_norm",
+           "fh_layer_norm_work_bytes", "fh_layer_norm_backward"]
 
 
 class FhError(RuntimeError):
@@ -96,6 +97,11 @@ class fh_mx_product_desc(C.Structure):
                 ("accumulate", C.c_int32), ("ldc", C.c_int64), ("alpha", C.c_float), ("reserved", C.c_int32)]
 
 
+class fh_norm_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("wdtype", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("eps", C.c_float),
+                ("reserved", C.c_int32), ("ldx", C.c_int64), ("ldy", C.c_int64)]
+
+
 _lib = None
 
 
@@ -153,6 +159,13 @@ def lib() -> C.CDLL:
         L.fh_mx_product.argtypes = [C.POINTER(fh_mx_product_desc), C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p,
                                     C.c_void_p]
         L.fh_mx_product.restype = C.c_int
+        N, V = C.POINTER(fh_norm_desc), C.c_void_p
+        L.fh_layer_norm.argtypes = [N, V, V, V, V, V, V, C.POINTER(fh_mx_params), V, C.c_size_t, V]
+        L.fh_layer_norm.restype = C.c_int
+        L.fh_layer_norm_work_bytes.argtypes = [N]
+        L.fh_layer_norm_work_bytes.restype = C.c_size_t
+        L.fh_layer_norm_backward.argtypes = [N, V, V, C.c_size_t, C.c_int32, V, V, V, V, V, V, V, C.c_size_t, V, V]
+        L.fh_layer_norm_backward.restype = C.c_int
         _lib = L
     return _lib
 
@@ -352,6 +365,42 @@ def fh_mx_product(d: fh_mx_product_desc, a, b, c, status=None, stream=None) -> i
     """Enqueue the product of the containers `a` (m x k) and `b` (n x k), uint8 CUDA tensors, into the matrix `c` (m x n)."""
     return lib().fh_mx_product(C.byref(d), _ptr(a), a.nbytes, _ptr(b), b.nbytes,
                                _ptr(c, max(0, (d.m - 1) * d.ldc + d.n), _esize(d.dtype)), _ptr(status), _stream_ptr(stream))
+
+
+def norm_desc(rows: int, cols: int, dtype: int = FH_F32, wdtype: int = FH_F32, eps: float = 1e-5, ldx: Optional[int] = None,
+              ldy: Optional[int] = None) -> fh_norm_desc:
+    return fh_norm_desc(dtype, wdtype, rows, cols, eps, 0, cols if ldx is None else ldx, cols if ldy is None else ldy)
+
+
+def _spans(d: fh_norm_desc) -> Tuple[int, int, int, int]:
+    """Elements of x and of y from the first to the last, their size and that of a weight."""
+    return max(0, (d.rows - 1) * d.ldx + d.cols), max(0, (d.rows - 1) * d.ldy + d.cols), _esize(d.dtype), _esize(d.wdtype)
+
+
+def fh_layer_norm(d: fh_norm_desc, x, gamma, beta, y, mean=None, rstd=None, packed=None, params: Optional[fh_mx_params] = None,
+                  stream=None) -> int:
+    """Enqueue the layer norm of `x` into `y` (may be None) and, in 4 bits as `params` says, into the uint8 tensor `packed`; gamma, beta, mean
+    and rstd may be None."""
+    nx, ny, es, ws = _spans(d)
+    return lib().fh_layer_norm(C.byref(d), _ptr(x, nx, es), _ptr(gamma, d.cols, ws), _ptr(beta, d.cols, ws), _ptr(y, ny, es),
+                               _ptr(mean, d.rows, 4), _ptr(rstd, d.rows, 4), None if params is None else C.byref(params), _ptr(packed),
+                               0 if packed is None else packed.nbytes, _stream_ptr(stream))
+
+
+def norm_work_bytes(d: fh_norm_desc) -> int:
+    return int(lib().fh_layer_norm_work_bytes(C.byref(d)))
+
+
+def fh_layer_norm_backward(d: fh_norm_desc, dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, work=None, packed: Optional[int] = None,
+                           status=None, stream=None) -> int:
+    """Enqueue the layer norm's backward pass; `x` is dense, or with `packed` a container (uint8) of that format.  `work`: uint8, at
+    least norm_work_bytes, where dgamma or dbeta is wanted."""
+    nx, ny, es, ws = _spans(d)
+    return lib().fh_layer_norm_backward(C.byref(d), _ptr(dy, ny, es), _ptr(x, *((nx, es) if packed is None else ())),
+                                        0 if packed is None else x.nbytes, 0 if packed is None else packed, _ptr(gamma, d.cols, ws),
+                                        _ptr(mean, d.rows, 4), _ptr(rstd, d.rows, 4), _ptr(dx, nx, es), _ptr(dgamma, d.cols, ws),
+                                        _ptr(dbeta, d.cols, ws), _ptr(work), 0 if work is None else work.nbytes, _ptr(status),
+                                        _stream_ptr(stream))
 
 
 def debug_set(what: int, value: int) -> int:

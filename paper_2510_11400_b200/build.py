@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfh_sm100a.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("fh_warp_f32.cu", "fh_warp_bf16.cu", "fh_warp_f32_plain.cu", "fh_warp_bf16_plain.cu",
                                           "fh_warp_f32_random.cu", "fh_warp_bf16_random.cu", "fh_cta_f32.cu", "fh_cta_bf16.cu",
-                                          "fh_generic.cu", "fh_decompress.cu", "fh_mx_save.cu", "fh_mx_product.cu", "fh_mx.cu", "fh.cu", "fh_plan.cpp")]
+                                          "fh_generic.cu", "fh_decompress.cu", "fh_mx_save.cu", "fh_mx_product.cu", "fh_norm.cu", "fh_mx.cu", "fh.cu", "fh_plan.cpp")]
 HEADERS = [os.path.join(CSRC, f) for f in ("fh_device.cuh", "fh_blocks.cuh", "fh_channel.cuh", "fh_compress.cuh",
                                           "fh_decompress.cuh", "fh_launch.cuh", "fh_launch_cta.cuh",
                                           "fh_launch_warp.cuh", "fh_mx.cuh", "fh_mx_launch.cuh", "fh_tcgen05.cuh")] + \

@@ -29,6 +29,24 @@ int check_mx(const fh_mx_params* p) {
   return FH_OK;
 }
 
+int check_norm(const fh_norm_desc* d) {
+  if (!d || !is_dtype(d->dtype) || !is_dtype(d->wdtype) || d->rows < 1 || d->cols < 1 || d->reserved != 0) return FH_ERR_ARG;
+  if (d->ldx < d->cols || d->ldy < d->cols || d->ldx > (INT64_MAX >> 3) / d->rows || d->ldy > (INT64_MAX >> 3) / d->rows) return FH_ERR_ARG;
+  if (!(d->eps >= 0.0f && d->eps <= 3.4028235e38f)) return FH_ERR_ARG;
+  return (uint32_t)d->cols > fh::kNormCols ? FH_ERR_UNSUPPORTED : FH_OK;
+}
+
+fh::NormArgs norm_args(const fh_norm_desc* d) {
+  fh::NormArgs a = {};
+  a.rows = (uint32_t)d->rows;
+  a.cols = (uint32_t)d->cols;
+  a.ldx = (uint64_t)d->ldx;
+  a.ldy = (uint64_t)d->ldy;
+  a.wdtype = d->wdtype;
+  a.eps = d->eps;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -102,6 +120,69 @@ int fh_mx_product(const fh_mx_product_desc* desc, const void* d_a, size_t a_byte
   a.alpha = desc->alpha;
   a.accumulate = desc->accumulate == 1;
   return fh::launch_mx_product(a, desc->dtype, desc->format, (cudaStream_t)stream);
+}
+
+int fh_layer_norm(const fh_norm_desc* desc, const void* d_x, const void* d_gamma, const void* d_beta, void* d_y, float* d_mean,
+                  float* d_rstd, const fh_mx_params* params, void* d_packed, size_t packed_capacity, void* stream) {
+  int rc = check_norm(desc);
+  if (rc != FH_OK) return rc;
+  const size_t es = esize_of(desc->dtype), ws = esize_of(desc->wdtype);
+  if (!d_x || (!d_y && !d_packed) || misaligned(d_x, es) || misaligned(d_y, es) || misaligned(d_gamma, ws) || misaligned(d_beta, ws) ||
+      misaligned(d_mean, 4) || misaligned(d_rstd, 4) || misaligned(d_packed, 16))
+    return FH_ERR_ARG;
+  fh::NormArgs a = norm_args(desc);
+  if (d_packed) {
+    rc = check_mx(params);
+    if (rc != FH_OK) return rc;
+    if (params->rounding != 0) return FH_ERR_UNSUPPORTED;
+    if (packed_capacity < fh_mx_bytes(desc->rows, desc->cols, params->format)) return FH_ERR_CAPACITY;
+    a.packed = (uint8_t*)d_packed;
+    a.format = (uint32_t)params->format;
+    a.exponent = params->exponent;
+    a.tensor_id = params->tensor_id;
+  }
+  a.x = (const uint8_t*)d_x;
+  a.gamma = (const uint8_t*)d_gamma;
+  a.beta = (const uint8_t*)d_beta;
+  a.y = (uint8_t*)d_y;
+  a.mean = d_mean;
+  a.rstd = d_rstd;
+  return fh::launch_norm_forward(a, desc->dtype, (cudaStream_t)stream);
+}
+
+size_t fh_layer_norm_work_bytes(const fh_norm_desc* desc) {
+  if (check_norm(desc) != FH_OK) return 0;
+  return (size_t)fh::norm_parts((uint32_t)desc->rows, (uint32_t)desc->cols, desc->dtype) * 2 * (size_t)desc->cols * sizeof(float);
+}
+
+int fh_layer_norm_backward(const fh_norm_desc* desc, const void* d_dy, const void* d_x, size_t x_bytes, int32_t x_format, const void* d_gamma,
+                           const float* d_mean, const float* d_rstd, void* d_dx, void* d_dgamma, void* d_dbeta, void* d_work,
+                           size_t work_bytes, uint64_t* d_status, void* stream) {
+  const int rc = check_norm(desc);
+  if (rc != FH_OK) return rc;
+  const size_t es = esize_of(desc->dtype), ws = esize_of(desc->wdtype);
+  if (!d_dy || !d_x || !d_mean || !d_rstd || (!d_dx && !d_dgamma && !d_dbeta) || (x_bytes && !is_format(x_format))) return FH_ERR_ARG;
+  if (misaligned(d_dy, es) || misaligned(d_x, x_bytes ? 16 : es) || misaligned(d_gamma, ws) || misaligned(d_mean, 4) || misaligned(d_rstd, 4) ||
+      misaligned(d_dx, es) || misaligned(d_dgamma, ws) || misaligned(d_dbeta, ws) || misaligned(d_work, 16) || misaligned(d_status, 8))
+    return FH_ERR_ARG;
+  fh::NormArgs a = norm_args(desc);
+  if (d_dgamma || d_dbeta) {
+    if (!d_work) return FH_ERR_ARG;
+    if (work_bytes < fh_layer_norm_work_bytes(desc)) return FH_ERR_CAPACITY;
+    a.work = (float*)d_work;
+  }
+  a.dy = (const uint8_t*)d_dy;
+  a.x = (const uint8_t*)d_x;
+  a.x_bytes = x_bytes;
+  a.format = x_bytes ? (uint32_t)x_format : 0u;
+  a.gamma = (const uint8_t*)d_gamma;
+  a.mean = const_cast<float*>(d_mean);
+  a.rstd = const_cast<float*>(d_rstd);
+  a.dx = (uint8_t*)d_dx;
+  a.dgamma = (uint8_t*)d_dgamma;
+  a.dbeta = (uint8_t*)d_dbeta;
+  a.status = (unsigned long long*)d_status;
+  return fh::launch_norm_backward(a, desc->dtype, (cudaStream_t)stream);
 }
 
 }  // extern "C"

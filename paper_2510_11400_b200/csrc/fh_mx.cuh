@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -149,20 +150,33 @@ __device__ __forceinline__ uint32_t mx_codes8(const float (&v)[8]) {
   return r;
 }
 
-// Four codes (16 bits) to values, two halves of fp16 each: exact.
-__device__ __forceinline__ void mx_values4(uint32_t codes, float (&v)[4]) {
-  uint32_t lo, hi;
+// Eight codes to values, by way of fp16, which holds them: exact.
+__device__ __forceinline__ void mx_values8(uint32_t codes, float (&v)[8]) {
+  uint32_t h[4];
   asm("{ .reg .b8 a, b, c, d;\n\t"
-      "mov.b32 {a, b, c, d}, %2;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
       "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %1, b; }"
-      : "=r"(lo), "=r"(hi)
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d; }"
+      : "=&r"(h[0]), "=&r"(h[1]), "=&r"(h[2]), "=&r"(h[3])
       : "r"(codes));
-  const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&lo)), q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-  v[0] = p.x;
-  v[1] = p.y;
-  v[2] = q.x;
-  v[3] = q.y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+    v[2 * i] = p.x;
+    v[2 * i + 1] = p.y;
+  }
+}
+
+// Four codes (the low 16 bits) to values: the upper two bytes of an fp32 number picked from tables of the eight magnitudes, and the
+// sign.  (The conversion instruction, asked for two bytes out of four, was compiled into one that took the upper two.)
+__device__ __forceinline__ void mx_values4(uint32_t codes, float (&v)[4]) {
+  const uint32_t m = codes & 0x7777u;
+  const uint32_t hi = __byte_perm(0x3F3F3F00u, 0x40404040u, m), lo = __byte_perm(0xC0800000u, 0xC0804000u, m);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    v[e] = bits_f((__byte_perm(lo, hi, (uint32_t)((4 + e) << 12 | e << 8)) & 0xFFFF0000u) | (codes << (28 - 4 * e) & 0x80000000u));
 }
 
 // A scale byte as a factor; `scale`: 2^exponent (B16).

@@ -37,7 +37,28 @@ struct MxProductArgs {
 };
 int launch_mx_product(const MxProductArgs& a, int dtype, int format, cudaStream_t stream);
 
-constexpr size_t kMxSmemLimit = 227 * 1024;  // dynamic shared memory a CTA may have
+struct NormArgs {
+  const uint8_t *x, *gamma, *beta, *dy;  // x: dense, or a container of x_bytes bytes (backward, x_bytes > 0)
+  uint64_t x_bytes;
+  uint8_t *y, *dx, *dgamma, *dbeta;      // any may be null
+  float *mean, *rstd;                    // forward: may be null
+  uint8_t* packed;                       // forward: container of y, may be null
+  float* work;                           // backward: sums of each CTA's rows, null when no weight's gradient is wanted
+  unsigned long long* status;            // backward: may be null
+  uint64_t ldx, ldy;                     // of x and dx, of y and dy
+  uint64_t tensor_id;
+  uint32_t rows, cols, format;
+  int32_t exponent, wdtype;
+  uint32_t parts;                        // backward: CTAs (set where the kernel is launched)
+  float eps;
+};
+constexpr uint32_t kNormCols = 28672;    // longest row: two sums a column in an SM's shared memory
+// CTAs among which the rows are dealt out in the backward pass.
+uint32_t norm_parts(uint32_t rows, uint32_t cols, int dtype);
+int launch_norm_forward(const NormArgs& a, int dtype, cudaStream_t stream);
+int launch_norm_backward(const NormArgs& a, int dtype, cudaStream_t stream);
+
+constexpr size_t kMxSmemLimit = 226 * 1024;  // dynamic shared memory a CTA may have, next to a little that a kernel declares
 
 // Counts a kernel for fh_kernel_launches().
 void count_launch(int kernels = 1);

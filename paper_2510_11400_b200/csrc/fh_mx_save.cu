@@ -222,15 +222,10 @@ __global__ void __launch_bounds__(kSaveThreads) mx_decompress_kernel(const MxSav
     uint4* p = reinterpret_cast<uint4*>(smem + r * kPitch<DT> + 32 * ES * j);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float v[8], lo[4], hi[4];
-      const float f = i < 2 ? f0 : f1;
-      mx_values4(w[i] & 0xFFFFu, lo);
-      mx_values4(w[i] >> 16, hi);
+      float v[8];
+      mx_values8(w[i], v);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = lo[e] * f;
-        v[4 + e] = hi[e] * f;
-      }
+      for (int e = 0; e < 8; ++e) v[e] *= i < 2 ? f0 : f1;
       if (DT == kF32) {
         p[2 * i] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
         p[2 * i + 1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));

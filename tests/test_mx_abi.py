@@ -77,3 +77,35 @@ def test_product_refuses(lib):
         assert call(d) == ARG
     assert call(good, a=None) == ARG and call(good, b=None) == ARG and call(good, c=None) == ARG
     assert call(good, a=A + 8) == ARG and call(good, b=A + 8) == ARG and call(good, c=A + 2) == ARG and call(good, status=A + 4) == ARG
+
+
+def test_layer_norm_refuses(lib):
+    assert C.sizeof(api.fh_norm_desc) == 40
+    ARG, good, p = api.FH_ERR_ARG, api.norm_desc(10, 40), api.mx_params()
+
+    def fwd(d=good, x=A, g=A, b=A, y=A, mean=A, rstd=A, prm=None, packed=None, cap=0):
+        return lib.fh_layer_norm(C.byref(d) if d is not None else None, x, g, b, y, mean, rstd, C.byref(prm) if prm is not None else None, packed, cap, None)
+
+    def bwd(d=good, dy=A, x=A, xb=0, xf=0, g=A, mean=A, rstd=A, dx=A, dg=A, db=A, work=A, wb=1 << 40, status=None):
+        return lib.fh_layer_norm_backward(C.byref(d) if d is not None else None, dy, x, xb, xf, g, mean, rstd, dx, dg, db, work, wb, status, None)
+
+    bad = [None, api.norm_desc(0, 40), api.norm_desc(10, 0), api.norm_desc(10, 40, 2), api.norm_desc(10, 40, 0, 2), api.norm_desc(10, 40, eps=-1.0),
+           api.norm_desc(10, 40, eps=float("nan")), api.norm_desc(10, 40, eps=float("inf")), api.norm_desc(10, 40, ldx=39), api.norm_desc(10, 40, ldy=39),
+           api.norm_desc(2 ** 31 - 1, 40, ldx=2 ** 40), api.fh_norm_desc(0, 0, 10, 40, 0.0, 1, 40, 40)]
+    for d in bad:
+        assert fwd(d) == ARG and bwd(d) == ARG
+        assert lib.fh_layer_norm_work_bytes(C.byref(d) if d is not None else None) == 0
+    assert fwd(api.norm_desc(10, 28673)) == bwd(api.norm_desc(10, 28673)) == api.FH_ERR_UNSUPPORTED
+    assert fwd(x=None) == ARG and fwd(y=None) == ARG
+    for name in ("x", "g", "b", "y", "mean", "rstd"):
+        assert fwd(**{name: A + 2}) == ARG, name
+    assert fwd(packed=A) == ARG and fwd(prm=p, packed=A + 8, cap=1 << 40) == ARG and fwd(prm=api.mx_params(3), packed=A, cap=1 << 40) == ARG
+    assert fwd(prm=api.mx_params(rounding=1), packed=A, cap=1 << 40) == api.FH_ERR_UNSUPPORTED
+    assert fwd(prm=p, packed=A, cap=api.mx_bytes(10, 40, 0) - 1) == api.FH_ERR_CAPACITY
+    for name in ("dy", "x", "mean", "rstd"):
+        assert bwd(**{name: None}) == ARG, name
+    for name in ("dy", "x", "g", "mean", "rstd", "dx", "dg", "db"):
+        assert bwd(**{name: A + 2}) == ARG, name
+    assert bwd(dx=None, dg=None, db=None) == ARG and bwd(x=A + 8, xb=1 << 20) == ARG and bwd(xb=1 << 20, xf=2) == ARG and bwd(status=A + 4) == ARG
+    assert bwd(work=None) == ARG and bwd(work=A + 8) == ARG and bwd(wb=api.norm_work_bytes(good) - 1) == api.FH_ERR_CAPACITY
+    assert api.norm_work_bytes(api.norm_desc(10 ** 6, 4096)) == 296 * 2 * 4096 * 4 and api.norm_work_bytes(api.norm_desc(1, 1)) == 8
