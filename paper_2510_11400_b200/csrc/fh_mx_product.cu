@@ -1,5 +1,6 @@
 // Products of microscaled 4-bit matrices on the tensor cores.
 #include <algorithm>
+#include <type_traits>
 
 #include "fh_launch.cuh"
 #include "fh_mx.cuh"
@@ -32,21 +33,50 @@ struct ProductShape {
   static constexpr uint32_t kCols = kAcc + kStages * 2 * kScaleCols <= 128 ? 128 : 256;
   static_assert(kAcc + kStages * 2 * kScaleCols <= kCols, "tensor memory");
   static constexpr size_t kSmem = 128 + kStages * kStage + 256;
-  static_assert(kStages * kStage >= QT * 512, "partial sums");
+  static_assert(kStages * kStage >= (QT + 8) * 512, "partial sums, and rows read behind them");
 };
 
+// NR rows of a column of C from row `row` on, those below `end`.  What is added to is asked for all at once.
+template <int DT, int NR>
+__device__ __forceinline__ void store_c(uint8_t* c, uint64_t ldc, uint32_t row, uint32_t end, uint32_t col, const float (&v)[NR], bool add) {
+  using T = typename std::conditional<DT == kF32, float, __nv_bfloat16>::type;
+  T* p = reinterpret_cast<T*>(c) + (uint64_t)row * ldc + col;
+  float old[NR];
+  if (add) {
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+      old[x] = 0.0f;
+      if (row + x < end) old[x] = (float)p[x * ldc];
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < NR; ++x)
+    if (row + x < end) p[x * ldc] = (T)(add ? old[x] + v[x] : v[x]);
+}
+
+// What the sums are multiplied by, one after the other: 2^(ea + eb) in two steps, so that neither over- nor underflows where the result
+// does not, and alpha.
 struct ProductScale {
-  float a, b, alpha;
+  float f1, f2, alpha;
+  __device__ __forceinline__ ProductScale(int ea, int eb, float alpha_) : alpha(alpha_) {
+    const int e = ea + eb, e1 = e / 2;
+    f1 = pow2_f(e1);
+    f2 = pow2_f(e - e1);
+  }
+  __device__ __forceinline__ float operator()(float v) const { return v * f1 * f2 * alpha; }
 };
 
-template <int DT>
-__device__ __forceinline__ void store_c(uint8_t* c, uint64_t at, float v, bool add) {
-  if (DT == kF32) {
-    float* p = reinterpret_cast<float*>(c) + at;
-    *p = add ? *p + v : v;
-  } else {
-    __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(c) + at;
-    *p = __float2bfloat16_rn(add ? __bfloat162float(*p) + v : v);
+// Sums a row of partial sums over the parts of a cluster (CTAs `stride` apart, from `first` on), NR rows at a time, in the order of the parts.
+template <int NR>
+__device__ __forceinline__ void sum_parts(uint32_t at, uint32_t row_bytes, uint32_t first, uint32_t stride, uint32_t parts, float (&v)[NR]) {
+#pragma unroll
+  for (int x = 0; x < NR; ++x) v[x] = 0.0f;
+  for (uint32_t r = 0; r < parts; ++r) {
+    float w[NR];
+#pragma unroll
+    for (int x = 0; x < NR; ++x) w[x] = ld_cluster(at + x * row_bytes, first + r * stride);
+#pragma unroll
+    for (int x = 0; x < NR; ++x) v[x] += w[x];
   }
 }
 
@@ -152,20 +182,18 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
     tc_fence_after();
   }
   const uint32_t col = tp * 128u + warp * 32u + lane;
-  const int e = ea + eb, e1 = e / 2;
-  const float f1 = pow2_f(e1), f2 = pow2_f(e - e1);  // (in two steps: neither over- nor underflows where the result does not)
+  const ProductScale scaled(ea, eb, g.alpha);
   if (g.split == 1u) {
     if (good) {
 #pragma unroll 1
       for (uint32_t q0 = 0; q0 < (uint32_t)QT; q0 += 16u) {
         uint32_t v[16];
+        float f[16];
         tc_load16(tmem + (warp * 32u << 16) + q0, v);
         tc_load_wait();
 #pragma unroll
-        for (uint32_t x = 0; x < 16u; ++x) {
-          const uint32_t row = tq * 128u + q0 + x;
-          if (row < g.m && col < g.n) store_c<DT>(g.c, (uint64_t)row * g.ldc + col, bits_f(v[x]) * f1 * f2 * g.alpha, g.accumulate);
-        }
+        for (uint32_t x = 0; x < 16u; ++x) f[x] = scaled(bits_f(v[x]));
+        if (col < g.n) store_c<DT, 16>(g.c, g.ldc, tq * 128u + q0, g.m, col, f, g.accumulate);
       }
     }
   } else {
@@ -184,11 +212,14 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
     }
     cluster_sync();
     if (good && col < g.n) {
-      const uint32_t rows = min((uint32_t)QT, g.m - tq * 128u);
-      for (uint32_t q = rows * rank / g.split; q < rows * (rank + 1u) / g.split; ++q) {
-        float v = 0.0f;
-        for (uint32_t r = 0; r < g.split; ++r) v += ld_cluster(smem_u32(part + q * 128u + tid), r);
-        store_c<DT>(g.c, (uint64_t)(tq * 128u + q) * g.ldc + col, v * f1 * f2 * g.alpha, g.accumulate);
+      const uint32_t rows = min((uint32_t)QT, g.m - tq * 128u), end = rows * (rank + 1u) / g.split;
+      constexpr int NR = QT < 32 ? 2 : 8;
+      for (uint32_t q = rows * rank / g.split; q < end; q += NR) {
+        float f[NR];
+        sum_parts<NR>(smem_u32(part + q * 128u + tid), 512u, 0u, 1u, g.split, f);  // (rows behind the last: stage bytes)
+#pragma unroll
+        for (int x = 0; x < NR; ++x) f[x] = scaled(f[x]);
+        store_c<DT, NR>(g.c, g.ldc, tq * 128u + q, tq * 128u + end, col, f, g.accumulate);
       }
     }
     cluster_sync();
@@ -197,6 +228,219 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
   tc_fence_before();
   __syncthreads();
   if (warp == 5) tmem_free(tmem, S::kCols);
+}
+
+// Large products: a pair of CTAs on a tile of 256 columns and 256 rows of C, 128 rows of B and 128 of A in the shared memory of each.
+// A tile of 128 x 128 moves 34 KB from L2 to an SM for 256 cycles of matrix instructions; this one 36 KB for 512.  Pairs take
+// tiles one after the other; the eight warps for the result take the accumulator into registers at once, so that the next tile's matrix
+// instructions start while they write.  With a split, a cluster's pairs share one tile.
+constexpr int kPairThreads = 320;  // eight warps for the result, one for copies, one for matrix instructions
+
+template <int F>
+struct PairShape {
+  static constexpr int kAtoms = F == kMxB32 ? 2 : 4;
+  static constexpr uint32_t kOp = 128 * 128, kS = kAtoms * 512;
+  static constexpr uint32_t kStage = 2 * kOp + 3 * kS;  // codes of B and A, scales of B, scales of both halves of A
+  static constexpr int kStages = F == kMxB32 ? 6 : 5;
+  static constexpr uint32_t kScaleCols = kAtoms * 12;   // columns of tensor memory: B's four and A's eight to a word
+  static constexpr uint32_t kCols = 512;
+  static_assert(256 + kStages * kScaleCols <= kCols, "tensor memory");
+  static constexpr size_t kSmem = 128 + (size_t)kStages * kStage + 256;
+  static_assert(kStages * kStage >= (256 + 8) * 512, "partial sums, and rows read behind them");
+};
+
+template <int DT, int F>
+__global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const MxProductArgs g) {
+  using S = PairShape<F>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);
+  uint64_t* empty = full + S::kStages;
+  uint64_t* peer = empty + S::kStages;  // even CTA: the odd one's stage has arrived
+  uint64_t* sums = peer + S::kStages;   // the accumulator is complete
+  uint64_t* taken = sums + 1;           // even CTA: both CTAs' warps have taken it
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(taken + 1);
+  volatile uint32_t* abort = tmem_at + 1;
+  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const uint32_t crank = cluster_rank(), half = crank & 1u, even = crank & ~1u, rank = crank / 2u;
+  const uint32_t pairs = gridDim.x / (2u * g.split), pair = blockIdx.x / (2u * g.split);  // clusters, each on tiles of its own
+  const MxLayout lp(g.n, g.k, F), lq(g.m, g.k, F);
+  if (tid == 0) {
+    for (int i = 0; i < S::kStages; ++i) {
+      mbar_init(full + i, 1);
+      mbar_init(empty + i, 1);
+      mbar_init(peer + i, 1);
+    }
+    mbar_init(sums, 1);
+    mbar_init(taken, 16);
+    *abort = 0u;
+    fence_mbar_init();
+  }
+  if (warp == 9) {
+    tmem_alloc_pair(tmem_at, S::kCols);
+    tmem_last_alloc_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // (both CTAs' barriers stand)
+  tc_fence_after();
+  const uint32_t tmem = *tmem_at;
+  dep_trigger();  // (behind the allocation: no later kernel takes tensor memory that this one still wants)
+  dep_wait();
+  int32_t ea = 0, eb = 0;
+  const bool ok_a = mx_header_ok(g.a, g.a_bytes, lq, &ea), ok_b = mx_header_ok(g.b, g.b_bytes, lp, &eb), ok = ok_a && ok_b;
+  if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
+  const uint32_t chunks = lp.kp / 32u, steps = (chunks + kStepChunks - 1u) / kStepChunks;
+  const uint32_t first = (uint32_t)((uint64_t)steps * rank / g.split), last = (uint32_t)((uint64_t)steps * (rank + 1u) / g.split);
+  const uint32_t blocks_p = (g.n + 127u) / 128u, blocks_q = (g.m + 127u) / 128u;
+  const uint32_t tiles = ok ? g.tiles_m * g.tiles_n : 0u;
+  bool good = true;
+  if (warp == 8) {
+    if (lane == 0) {
+      uint32_t i = 0;
+      for (uint32_t tile = pair; tile < tiles && good; tile += pairs) {
+        const uint32_t bp = tile % g.tiles_n * 2u + half, bq0 = tile / g.tiles_n * 2u, bq = bq0 + half;
+        const uint32_t rp = bp < blocks_p ? lp.block_rows(bp) : 0u, rq = bq < blocks_q ? lq.block_rows(bq) : 0u;
+        const uint8_t* p = g.b + (rp ? lp.code_at(bp * 128u, 0) : 0u);
+        const uint8_t* q = g.a + (rq ? lq.code_at(bq * 128u, 0) : 0u);
+        const uint8_t* sp = g.b + (rp ? lp.atom_at(bp, 0) : 0u);
+        const uint8_t* sq0 = g.a + lq.atom_at(bq0, 0);
+        const bool two = bq0 + 1u < blocks_q;
+        const uint8_t* sq1 = g.a + (two ? lq.atom_at(bq0 + 1u, 0) : 0u);
+        // a block of codes: one piece if it has all its rows; otherwise its chunks go where those of a whole one would be
+        auto codes = [&](uint8_t* dst, const uint8_t* src, uint32_t rows, uint32_t it, uint32_t nc, uint64_t* bar) {
+          if (rows == 128u) {
+            bulk_g2s(dst, src + (uint64_t)it * kStepChunks * 2048u, nc * 2048u, bar);
+          } else if (rows) {
+            for (uint32_t j = 0; j < nc; ++j) bulk_g2s(dst + j * 2048u, src + ((uint64_t)it * kStepChunks + j) * 16u * rows, 16u * rows, bar);
+          }
+        };
+        for (uint32_t it = first; it < last; ++it, ++i) {
+          const uint32_t s = i % S::kStages;
+          if (i >= (uint32_t)S::kStages && !mbar_wait_cluster(empty + s, (i / S::kStages - 1u) & 1u, kWaitPolls, abort)) {
+            *abort = 1u;
+            good = false;
+            break;
+          }
+          const uint32_t nc = min((uint32_t)kStepChunks, chunks - it * kStepChunks);
+          const uint32_t na = min((uint32_t)S::kAtoms, lp.atoms - it * S::kAtoms);
+          uint8_t* st = smem + s * S::kStage;
+          const uint64_t at = (uint64_t)it * S::kAtoms * 512u;
+          mbar_expect_tx(full + s, nc * 16u * (rp + rq) + na * 512u * ((rp ? 1u : 0u) + (two ? 2u : 1u)));
+          codes(st, p, rp, it, nc, full + s);
+          codes(st + S::kOp, q, rq, it, nc, full + s);
+          if (rp) bulk_g2s(st + 2 * S::kOp, sp + at, na * 512u, full + s);
+          bulk_g2s(st + 2 * S::kOp + S::kS, sq0 + at, na * 512u, full + s);
+          if (two) bulk_g2s(st + 2 * S::kOp + 2 * S::kS, sq1 + at, na * 512u, full + s);
+        }
+      }
+      // nothing may be in flight when the CTA ends
+      for (uint32_t w = i > (uint32_t)S::kStages ? i - S::kStages : 0u; w < i; ++w) mbar_wait(full + w % S::kStages, w / S::kStages & 1u, kWaitPolls);
+    }
+  } else if (warp == 9) {
+    if (lane == 0) {
+      const uint16_t both = (uint16_t)(3u << even);
+      uint32_t i = 0, n = 0;
+      for (uint32_t tile = pair; tile < tiles && good; tile += pairs, ++n) {
+        if (half == 0u && n && !mbar_wait_cluster(taken, (n - 1u) & 1u, kWaitPolls, abort)) {
+          *abort = 1u;
+          break;
+        }
+        tc_fence_after();
+        for (uint32_t it = first; it < last; ++it, ++i) {
+          const uint32_t s = i % S::kStages, ph = i / S::kStages & 1u;
+          if (!mbar_wait_abortable(full + s, ph, kWaitPolls, abort) || (half == 0u && !mbar_wait_cluster(peer + s, ph, kWaitPolls, abort))) {
+            *abort = 1u;
+            good = false;
+            break;
+          }
+          if (half) {  // the odd CTA's stage is there: tell the even one, which issues for both
+            mbar_arrive_at(peer + s, even);
+            continue;
+          }
+          tc_fence_after();
+          const uint32_t nc = min((uint32_t)kStepChunks, chunks - it * kStepChunks);
+          const uint32_t na = min((uint32_t)S::kAtoms, lp.atoms - it * S::kAtoms);
+          const uint32_t st = smem_u32(smem + s * S::kStage), sc = st + 2u * S::kOp;
+          const uint32_t sa = tmem + 256u + s * S::kScaleCols, sb = sa + S::kAtoms * 4u;
+          for (uint32_t x = 0; x < na; ++x) {
+            tc_copy_scales_pair(sa + 4u * x, smem_desc(sc + 512u * x, 128u, 128u));
+            tc_copy_scales_pair(sb + 8u * x, smem_desc(sc + S::kS + 512u * x, 128u, 128u));
+            tc_copy_scales_pair(sb + 8u * x + 4u, smem_desc(sc + 2u * S::kS + 512u * x, 128u, 128u));
+          }
+          for (uint32_t x = 0; x < nc / 2u; ++x) {
+            const uint64_t da = smem_desc(st + x * 4096u, 2048u, 128u), db = smem_desc(st + S::kOp + x * 4096u, 2048u, 128u);
+            const uint32_t word = F == kMxB32 ? x / 2u : x, id = F == kMxB32 ? x % 2u * 2u : 0u;
+            tc_mma_mx_pair<F == kMxB32>(tmem, da, db, mx_idesc(256u, 256u, F == kMxB32, id), sa + 4u * word, sb + 8u * word, it > first || x > 0u);
+          }
+          tc_commit_pair(empty + s, both);
+        }
+        if (half == 0u) tc_commit_pair(sums, both);
+      }
+    }
+  } else {
+    const ProductScale scaled(ea, eb, g.alpha);
+    const uint32_t side = warp / 4u * 128u;  // columns of the accumulator: rows of A
+    uint32_t n = 0;
+    for (uint32_t tile = pair; tile < tiles && good; tile += pairs, ++n) {
+      good = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(sums, n & 1u, kWaitPolls, abort) && !*abort);
+      if (!good) break;
+      tc_fence_after();
+      const uint32_t col = tile % g.tiles_n * 256u + half * 128u + warp % 4u * 32u + lane, row = tile / g.tiles_n * 256u + side;
+      uint32_t v[8][16];
+#pragma unroll
+      for (uint32_t x = 0; x < 8u; ++x) tc_load16(tmem + (warp % 4u * 32u << 16) + side + 16u * x, v[x]);
+      tc_load_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_at(taken, even);
+      if (g.split == 1u) {
+        if (col < g.n) {
+#pragma unroll
+          for (uint32_t x = 0; x < 8u; ++x) {
+            float f[16];
+#pragma unroll
+            for (uint32_t y = 0; y < 16u; ++y) f[y] = scaled(bits_f(v[x][y]));
+            store_c<DT, 16>(g.c, g.ldc, row + 16u * x, g.m, col, f, g.accumulate);
+          }
+        }
+      } else {  // (one tile only: all copies into shared memory have been used)
+        float* part = reinterpret_cast<float*>(smem) + side * 128u + warp % 4u * 32u + lane;
+#pragma unroll
+        for (uint32_t x = 0; x < 8u; ++x)
+#pragma unroll
+          for (uint32_t y = 0; y < 16u; ++y) part[(16u * x + y) * 128u] = bits_f(v[x][y]);
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  if (g.split > 1u) {
+    cluster_sync();
+    if (warp < 8u && good && tiles) {
+      const ProductScale scaled(ea, eb, g.alpha);
+      const uint32_t p = warp % 4u * 32u + lane, col = pair % g.tiles_n * 256u + half * 128u + p, row = pair / g.tiles_n * 256u;
+      const uint32_t rows = min(256u, g.m - row), from = rows * rank / g.split, end = rows * (rank + 1u) / g.split, mid = (from + end) / 2u;
+      const uint32_t stop = warp < 4u ? mid : end;
+      if (col < g.n)
+        for (uint32_t q = warp < 4u ? from : mid; q < stop; q += 8u) {
+          float f[8];
+          sum_parts<8>(smem_u32(reinterpret_cast<float*>(smem) + q * 128u + p), 512u, half, 2u, g.split, f);
+#pragma unroll
+          for (int x = 0; x < 8; ++x) f[x] = scaled(f[x]);
+          store_c<DT, 8>(g.c, g.ldc, row + q, row + stop, col, f, g.accumulate);
+        }
+    }
+  }
+  if (*abort && lane == 0 && g.status) *g.status = status_word(kErrTimeout);
+  __syncthreads();
+  cluster_sync();  // (a pair's memory serves both until both are done)
+  if (warp == 9) tmem_free_pair(tmem, S::kCols);
+}
+
+template <int DT, int F>
+int launch_product_pair(const MxProductArgs& a, uint32_t clusters, cudaStream_t stream) {
+  return launch_plain<mx_product_pair_kernel<DT, F>>(clusters * 2u * a.split, kPairThreads, PairShape<F>::kSmem, (int)(2u * a.split), stream, a);
 }
 
 template <int DT, int F, int QT>
@@ -216,14 +460,23 @@ int launch_product_df(const MxProductArgs& a, cudaStream_t stream) {
 
 int launch_mx_product(const MxProductArgs& a0, int dtype, int format, cudaStream_t stream) {
   MxProductArgs a = a0;
-  const uint64_t tm = ((uint64_t)a.m + 127) / 128, tn = ((uint64_t)a.n + 127) / 128;
   const int sms = sm_count();
   if (sms < 1) return FH_ERR_CUDA;
-  // parts of the common axis while that leaves SMs idle, each of at least two stages
   const uint64_t steps = ((uint64_t)a.k + 255) / 256;
-  uint64_t split = std::min<uint64_t>({8, (uint64_t)sms / (tm * tn), steps / 2});
-  if (split < 1) split = 1;
-  if (tm * tn * split > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
+  const uint64_t pm = ((uint64_t)a.m + 255) / 256, pn = ((uint64_t)a.n + 255) / 256, tm = ((uint64_t)a.m + 127) / 128, tn = ((uint64_t)a.n + 127) / 128;
+  if (tm * tn > 0x7FFFFFFFull / 8) return FH_ERR_UNSUPPORTED;
+  if (a.m > 128) {
+    const uint64_t split = std::max<uint64_t>(1, std::min<uint64_t>({4, (uint64_t)sms / 2 / (pm * pn), steps / 2}));
+    a.tiles_m = (uint32_t)pm;
+    a.tiles_n = (uint32_t)pn;
+    a.split = (uint32_t)split;
+    const uint32_t clusters = (uint32_t)(split > 1 ? pm * pn : std::min<uint64_t>(pm * pn, (uint64_t)sms / 2));
+    if (dtype == kF32)
+      return format == kMxB32 ? launch_product_pair<kF32, kMxB32>(a, clusters, stream) : launch_product_pair<kF32, kMxB16>(a, clusters, stream);
+    return format == kMxB32 ? launch_product_pair<kBF16, kMxB32>(a, clusters, stream) : launch_product_pair<kBF16, kMxB16>(a, clusters, stream);
+  }
+  // parts of the common axis while that leaves SMs idle, each of at least two stages
+  const uint64_t split = std::max<uint64_t>(1, std::min<uint64_t>({8, (uint64_t)sms / (tm * tn), steps / 2}));
   a.tiles_m = (uint32_t)tm;
   a.tiles_n = (uint32_t)tn;
   a.split = (uint32_t)split;

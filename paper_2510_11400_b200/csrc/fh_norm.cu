@@ -15,38 +15,88 @@ struct NormVec {
   static constexpr int kE = DT == kF32 ? 4 : 8;  // elements of a 16-byte vector
 };
 
-// A vector of a row as it lies in memory, zeros behind the last column.  VEC: on a 16-byte boundary.
-template <int DT, bool VEC>
-__device__ __forceinline__ uint4 load_vec(const uint8_t* row, uint32_t col, uint32_t cols) {
+// Which of a row's columns are element e of vector i of thread t of its team: E neighbours, so that they are one access of 16 bytes, or,
+// where rows lie off the 16-byte grid (LINES), elements TEAM apart, so that a warp's accesses of one element each are neighbours.
+template <int E, int TEAM, bool LINES>
+__device__ __forceinline__ uint32_t column(uint32_t i, uint32_t t, int e) {
+  return LINES ? (i * E + e) * TEAM + t : (i * TEAM + t) * E + e;
+}
+template <int DT>
+__device__ __forceinline__ uint32_t load_elem(const uint8_t* row, uint32_t col) {
+  return DT == kF32 ? reinterpret_cast<const uint32_t*>(row)[col] : reinterpret_cast<const uint16_t*>(row)[col];
+}
+// Vector i of a row as it lies in memory, zeros behind the last column.  VEC: rows are on the 16-byte grid.
+template <int DT, int TEAM, bool VEC, bool LINES>
+__device__ __forceinline__ uint4 load_vec(const uint8_t* row, uint32_t i, uint32_t t, uint32_t cols) {
   constexpr int E = NormVec<DT>::kE;
+  const uint32_t col = column<E, TEAM, LINES>(i, t, 0);
   if (VEC && col + E <= cols) return *reinterpret_cast<const uint4*>(row + (uint64_t)col * (16 / E));
   uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (col + e < cols) {
-      if (DT == kF32)
-        w[e] = reinterpret_cast<const uint32_t*>(row)[col + e];
-      else
-        w[e / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(row)[col + e] << (e % 2 * 16);
-    }
+  for (int e = 0; e < E; ++e) {
+    const uint32_t c = column<E, TEAM, LINES>(i, t, e);
+    if (c < cols) w[DT == kF32 ? e : e / 2] |= load_elem<DT>(row, c) << (DT == kF32 ? 0 : e % 2 * 16);
+  }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-template <int DT, bool VEC>
-__device__ __forceinline__ void store_vec(uint8_t* row, uint32_t col, uint32_t cols, const uint4& v) {
+template <int DT, int TEAM, bool VEC, bool LINES>
+__device__ __forceinline__ void store_vec(uint8_t* row, uint32_t i, uint32_t t, uint32_t cols, const uint4& v) {
   constexpr int E = NormVec<DT>::kE;
+  const uint32_t col = column<E, TEAM, LINES>(i, t, 0);
   if (VEC && col + E <= cols) {
     *reinterpret_cast<uint4*>(row + (uint64_t)col * (16 / E)) = v;
     return;
   }
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (col + e < cols) {
+  for (int e = 0; e < E; ++e) {
+    const uint32_t c = column<E, TEAM, LINES>(i, t, e);
+    if (c < cols) {
       if (DT == kF32)
-        reinterpret_cast<uint32_t*>(row)[col + e] = w[e];
+        reinterpret_cast<uint32_t*>(row)[c] = w[e];
       else
-        reinterpret_cast<uint16_t*>(row)[col + e] = (uint16_t)(w[e / 2] >> (e % 2 * 16));
+        reinterpret_cast<uint16_t*>(row)[c] = (uint16_t)(w[e / 2] >> (e % 2 * 16));
     }
+  }
+}
+// The same into the thread's own 16 bytes of shared memory, later: what a thread has asked for so it alone reads, so that no barrier
+// stands between.  `ok`: there is such a row.  (An element of bf16 is too small for such a copy: off the grid it is loaded when it is used.)
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4u : 0u) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+template <int DT, int TEAM, bool VEC, bool LINES>
+__device__ __forceinline__ void copy_vec(uint32_t dst, const uint8_t* row, uint32_t i, uint32_t t, uint32_t cols, bool ok) {
+  constexpr int E = NormVec<DT>::kE;
+  const uint32_t col = column<E, TEAM, LINES>(i, t, 0);
+  if (VEC) {
+    const uint32_t n = ok && col < cols ? min((uint32_t)E, cols - col) : 0u;
+    copy16(dst, row + (n ? (uint64_t)col * (16 / E) : 0u), n * (16 / E));
+  } else if (DT == kF32) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const uint32_t c = column<E, TEAM, LINES>(i, t, e);
+      const bool there = ok && c < cols;
+      copy4(dst + 4 * e, row + (there ? (uint64_t)c * 4u : 0u), there);
+    }
+  }
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 ld_shared8(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
 }
 template <int DT, int E>
 __device__ __forceinline__ void unpack(const uint4& v, float (&f)[E]) {
@@ -68,30 +118,69 @@ __device__ __forceinline__ uint4 pack(const float (&f)[E]) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// E weights from `col` on, in fp32; `none` where there are none.
-template <int E>
-__device__ __forceinline__ void load_weights(const uint8_t* p, int wdt, uint32_t col, uint32_t cols, float none, float (&f)[E]) {
+// The weights of vector i in fp32; `none` where there are none.
+template <int E, int TEAM, bool LINES>
+__device__ __forceinline__ void load_weights(const uint8_t* p, int wdt, uint32_t i, uint32_t t, uint32_t cols, float none, float (&f)[E]) {
+  const uint32_t col = column<E, TEAM, LINES>(i, t, 0);
+  if (!LINES && p && (uintptr_t)p % 16 == 0 && col + E <= cols) {
+    if (wdt == kF32) {
+#pragma unroll
+      for (int h = 0; h < E / 4; ++h) {
+        const float4 v = reinterpret_cast<const float4*>(p)[col / 4u + h];
+        f[4 * h] = v.x;
+        f[4 * h + 1] = v.y;
+        f[4 * h + 2] = v.z;
+        f[4 * h + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < E / 4; ++h) {
+        const uint2 v = reinterpret_cast<const uint2*>(p)[col / 4u + h];
+        f[4 * h] = bits_f(v.x << 16);
+        f[4 * h + 1] = bits_f(v.x & 0xFFFF0000u);
+        f[4 * h + 2] = bits_f(v.y << 16);
+        f[4 * h + 3] = bits_f(v.y & 0xFFFF0000u);
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < E; ++e) {
+    const uint32_t c = column<E, TEAM, LINES>(i, t, e);
     f[e] = none;
-    if (p && col + e < cols)
-      f[e] = wdt == kF32 ? reinterpret_cast<const float*>(p)[col + e] : bits_f((uint32_t) reinterpret_cast<const uint16_t*>(p)[col + e] << 16);
+    if (p && c < cols) f[e] = wdt == kF32 ? reinterpret_cast<const float*>(p)[c] : bits_f((uint32_t) reinterpret_cast<const uint16_t*>(p)[c] << 16);
   }
 }
 
-// Sum over the TEAM threads that share a row, in a fixed order, the same in every thread.  `slot`: kNormWarps floats that the CTA
-// uses for nothing else until two more of its barriers have passed.
+// Barrier of the TEAM threads that share a row.
 template <int TEAM>
-__device__ __forceinline__ float team_sum(float v, float* slot) {
+__device__ __forceinline__ void team_barrier() {
+  if (TEAM == kNormThreads)
+    __syncthreads();
+  else if (TEAM > 32)
+    asm volatile("bar.sync %0, %1;" ::"r"(1u + threadIdx.x / TEAM), "n"(TEAM) : "memory");
+}
+
+// Sums over the TEAM threads that share a row, in a fixed order, the same in every thread.  `slot`: TEAM / 32 pairs that the team uses for
+// nothing else until another of its barriers has passed.
+template <int TEAM>
+__device__ __forceinline__ float2 team_sum(float a, float b, float2* slot) {
 #pragma unroll
-  for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-  if (TEAM == 32) return v;
-  if (threadIdx.x % 32 == 0) slot[threadIdx.x / 32] = v;
-  __syncthreads();
-  float s = 0.0f;
+  for (int d = 16; d; d /= 2) {
+    a += __shfl_xor_sync(0xFFFFFFFFu, a, d);
+    b += __shfl_xor_sync(0xFFFFFFFFu, b, d);
+  }
+  if (TEAM == 32) return make_float2(a, b);
+  if (threadIdx.x % 32 == 0) slot[threadIdx.x % TEAM / 32] = make_float2(a, b);
+  team_barrier<TEAM>();
+  a = b = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kNormWarps; ++w) s += slot[w];
-  return s;
+  for (int w = 0; w < TEAM / 32; ++w) {
+    const float2 v = slot[w];
+    a += v.x;
+    b += v.y;
+  }
+  return make_float2(a, b);
 }
 
 // ---- codes of a row of the output, E of its columns from `col` on in each lane (neighbouring lanes hold neighbouring columns)
@@ -133,19 +222,27 @@ __device__ __forceinline__ void store_codes(const NormArgs& a, const MxLayout& l
     store_codes_f<DT, kMxB16, E>(a, l, row, col, v, unscale);
 }
 
-// Forward.  y = (x - mean) * rstd * gamma + beta, mean and variance from the row as it is held in registers (the squares of the
-// distances from the mean, not of the values), sums in fp32.  TEAM threads to a row, V vectors to a thread; V = 0: any number, the row is
-// read again for each of the three sweeps.
+// Forward.  y = (x - mean) * rstd * gamma + beta, mean and variance from the row as it is held on the chip (the squares of the
+// distances from the mean, not of the values), sums in fp32.  TEAM threads to a row, V vectors to a thread, each team with the weights
+// of its columns in registers and the next rows on their way into shared memory; V = 0: any number of vectors, each sweep reads the row
+// and the weights again.  What bounds it is memory, once enough rows are on their way: with weights read again for every row, element by
+// element, and nothing asked for ahead, 16384 x 4096 bf16 took 153 us.
+constexpr int kAhead = 4;  // rows of a team in shared memory
+
 template <int DT, int TEAM, int V, bool VEC>
 __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormArgs a) {
   constexpr int E = NormVec<DT>::kE, N = V ? V : 1;
-  __shared__ float slots[4][kNormWarps];
-  const uint32_t t = threadIdx.x % TEAM, team = blockIdx.x * (kNormThreads / TEAM) + threadIdx.x / TEAM, teams = gridDim.x * (kNormThreads / TEAM);
+  constexpr bool kCopies = V && (VEC || DT == kF32);
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float2 slots[kNormThreads / TEAM][4][TEAM / 32];
+  const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
+                 teams = gridDim.x * (kNormThreads / TEAM);
   const MxLayout l(a.rows, a.cols, a.format);
   const uint32_t rows = a.packed ? (a.rows + 127u) / 128u * 128u : a.rows;  // (the padding of a container belongs to it)
   const uint32_t sweeps = V ? V : (a.cols + TEAM * E - 1u) / (TEAM * E);
-  const uint32_t psweeps = a.packed ? sweeps : 0u;
   const float inv = __frcp_rn((float)a.cols), unscale = a.format == kMxB32 ? 1.0f : pow2_f(-a.exponent);
+  const uint32_t ring = smem_u32(smem) + threadIdx.x * 16u;
+  auto row_of = [&](uint32_t row) { return a.x + (uint64_t)row * a.ldx * (16 / E); };
   dep_trigger();
   dep_wait();
   if (a.packed && blockIdx.x == 0 && threadIdx.x < 8) {
@@ -155,20 +252,41 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
     if (threadIdx.x == 2) v = make_uint4((uint32_t)a.tensor_id, (uint32_t)(a.tensor_id >> 32), 0u, 0u);
     reinterpret_cast<uint4*>(a.packed)[threadIdx.x] = v;
   }
-  uint32_t turn = 0;
-  for (uint32_t row = team; row < rows; row += teams, turn ^= 2u) {
+  auto ask = [&](uint64_t row, uint32_t slot) {
+    if (kCopies) {
+      const bool ok = row < a.rows;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        copy_vec<DT, TEAM, VEC, false>(ring + (slot * N + i) * (kNormThreads * 16u), ok ? row_of((uint32_t)row) : a.x, i, t, a.cols, ok);
+      copy_commit();
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < kAhead - 1; ++k) ask((uint64_t)team + (uint64_t)k * teams, k);
+  float gamma[N][E], beta[N][E];
+  if (V) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      load_weights<E, TEAM, false>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, gamma[i]);
+      load_weights<E, TEAM, false>(a.beta, a.wdtype, i, t, a.cols, 0.0f, beta[i]);
+    }
+  }
+  uint32_t turn = 0, slot = 0;
+  for (uint32_t row = team; row < rows; row += teams, turn ^= 2u, slot = slot + 1u == kAhead ? 0u : slot + 1u) {
+    ask((uint64_t)row + (uint64_t)(kAhead - 1) * teams, slot ? slot - 1u : kAhead - 1u);
     if (row >= a.rows) {
       const float zero[E] = {};
-      for (uint32_t i = 0; i < psweeps; ++i) store_codes<DT, E>(a, l, row, (i * TEAM + t) * E, zero, unscale);
+      for (uint32_t i = 0; i < sweeps; ++i) store_codes<DT, E>(a, l, row, (i * TEAM + t) * E, zero, unscale);
       continue;
     }
-    const uint8_t* x = a.x + (uint64_t)row * a.ldx * (16 / E);
+    const uint8_t* x = row_of(row);
     uint4 raw[N];
-    float sum = 0.0f;
+    if (kCopies) copy_wait<kAhead - 1>();
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (V) raw[i] = load_vec<DT, VEC>(x, (i * TEAM + t) * E, a.cols);
-    auto vec = [&](uint32_t i) { return V ? raw[i % N] : load_vec<DT, VEC>(x, (i * TEAM + t) * E, a.cols); };
+      if (V) raw[i] = kCopies ? ld_shared16(ring + (slot * N + i) * (kNormThreads * 16u)) : load_vec<DT, TEAM, VEC, false>(x, i, t, a.cols);
+    auto vec = [&](uint32_t i) { return V ? raw[i % N] : load_vec<DT, TEAM, VEC, false>(x, i, t, a.cols); };
+    float sum = 0.0f;
 #pragma unroll
     for (uint32_t i = 0; i < sweeps; ++i) {
       float f[E];
@@ -176,7 +294,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
 #pragma unroll
       for (int e = 0; e < E; ++e) sum += f[e];
     }
-    const float mean = team_sum<TEAM>(sum, slots[turn]) * inv;
+    const float mean = team_sum<TEAM>(sum, 0.0f, slots[in_cta][turn]).x * inv;
     float sq = 0.0f;
 #pragma unroll
     for (uint32_t i = 0; i < sweeps; ++i) {
@@ -188,7 +306,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
         sq = __fmaf_rn(d, d, sq);
       }
     }
-    const float rstd = __frsqrt_rn(team_sum<TEAM>(sq, slots[turn + 1]) * inv + a.eps);
+    const float rstd = __frsqrt_rn(team_sum<TEAM>(sq, 0.0f, slots[in_cta][turn + 1]).x * inv + a.eps);
     if (t == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
@@ -199,12 +317,14 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
       const uint32_t col = (i * TEAM + t) * E;
       float f[E], g[E], b[E];
       unpack<DT, E>(vec(i), f);
-      load_weights<E>(a.gamma, a.wdtype, col, a.cols, 1.0f, g);
-      load_weights<E>(a.beta, a.wdtype, col, a.cols, 0.0f, b);
+      if (!V) {
+        load_weights<E, TEAM, false>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, g);
+        load_weights<E, TEAM, false>(a.beta, a.wdtype, i, t, a.cols, 0.0f, b);
+      }
 #pragma unroll
-      for (int e = 0; e < E; ++e) f[e] = __fmaf_rn((f[e] - mean) * rstd, g[e], b[e]);
+      for (int e = 0; e < E; ++e) f[e] = __fmaf_rn((f[e] - mean) * rstd, V ? gamma[i % N][e] : g[e], V ? beta[i % N][e] : b[e]);
       const uint4 out = pack<DT, E>(f);
-      if (y && col < a.cols) store_vec<DT, VEC>(y, col, a.cols, out);
+      if (y && col < a.cols) store_vec<DT, TEAM, VEC, false>(y, i, t, a.cols, out);
       if (a.packed) {
         // codes of what y is in its type, so that they are those that compressing y gives
         unpack<DT, E>(out, f);
@@ -215,6 +335,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
       }
     }
   }
+  if (kCopies) copy_wait<0>();
 }
 
 // ---- backward -----------------------------------------------------------------------------------------
@@ -223,46 +344,55 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
 // where there are too many; a CTA's teams are added up at the end, and the CTAs' sums, which lie in the caller's workspace, by a second kernel:
 // all in a fixed order.
 
-// x of a row's columns from `col` on: dense, or four bits and the scale.
-template <int DT, bool VEC, int X>
-__device__ __forceinline__ uint4 load_x(const NormArgs& a, const MxLayout& l, uint32_t row, uint32_t col) {
+// x of vector i: dense as it lies there, or the word with its codes and the one with its scale.
+template <int DT, int TEAM, bool VEC, bool LINES, int X>
+__device__ __forceinline__ uint4 load_x(const NormArgs& a, const MxLayout& l, uint32_t row, uint32_t i, uint32_t t) {
   constexpr int E = NormVec<DT>::kE;
-  if (X == 0) return load_vec<DT, VEC>(a.x + (uint64_t)row * a.ldx * (16 / E), col, a.cols);
+  if (X == 0) return load_vec<DT, TEAM, VEC, LINES>(a.x + (uint64_t)row * a.ldx * (16 / E), i, t, a.cols);
+  const uint32_t col = column<E, TEAM, LINES>(i, t, 0);
   uint4 v = make_uint4(0u, 0u, 0u, 0u);
   if (col < a.cols) {
-    constexpr int F = X - 1;
-    v.x = *reinterpret_cast<const uint32_t*>(a.x + l.code_at(row, col / 32u) + col % 32u / 8u * 4u) >> (col % 8u * 4u);
-    const uint32_t b = col / (F == kMxB32 ? 32u : 16u);
-    v.y = a.x[l.atom_at(row / 128u, b / 4u) + MxLayout::scale_in_atom(row) + b % 4u];
+    v.x = *reinterpret_cast<const uint32_t*>(a.x + l.code_at(row, col / 32u) + col % 32u / 8u * 4u);
+    v.y = *reinterpret_cast<const uint32_t*>(a.x + l.atom_at(row / 128u, col / (X > 1 ? 64u : 128u)) + MxLayout::scale_in_atom(row));
   }
   return v;
 }
 template <int DT, int X, int E>
-__device__ __forceinline__ void unpack_x(const uint4& v, float scale, float (&f)[E]) {
+__device__ __forceinline__ void unpack_x(const uint4& v, uint32_t col, float scale, float (&f)[E]) {
   if (X == 0) {
     unpack<DT, E>(v, f);
     return;
   }
-  const float s = mx_factor<(X > 1 ? kMxB16 : kMxB32)>(v.y, scale);
+  const float s = mx_factor<(X > 1 ? kMxB16 : kMxB32)>(v.y >> (col / (X > 1 ? 16u : 32u) % 4u * 8u) & 255u, scale);
   if constexpr (E == 8)
     mx_values8(v.x, f);
   else
-    mx_values4(v.x, f);
+    mx_values4(v.x >> (col % 8u * 4u), f);
 #pragma unroll
   for (int e = 0; e < E; ++e) f[e] *= s;
 }
 
+template <int V, int X>
+struct BackRing {  // bytes of a slot: dy, x, and the row's mean and rstd
+  static constexpr uint32_t kX = kNormThreads * 16 * V, kStat = kX + kNormThreads * (X ? 8 : 16) * V, kSlot = kStat + kNormThreads * 8;
+  static constexpr int kRows = V < 4 ? 4 : 3;
+};
+
 template <int DT, int TEAM, int V, bool VEC, int X>
-__global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_kernel(const NormArgs a) {
   constexpr int E = NormVec<DT>::kE, N = V ? V : 1;
+  constexpr bool kLines = !VEC && X == 0;
+  constexpr bool kCopies = V && (VEC || DT == kF32);
+  using R = BackRing<N, X>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float slots[4][kNormWarps];
+  __shared__ float2 slots[kNormThreads / TEAM][2][TEAM / 32];
   float* acc = reinterpret_cast<float*>(smem);  // V = 0: dgamma and dbeta of the CTA; otherwise room for the other teams' sums
   const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
                  teams = gridDim.x * (kNormThreads / TEAM);
   const MxLayout l(a.rows, a.cols, a.format);
   const uint32_t sweeps = V ? V : (a.cols + TEAM * E - 1u) / (TEAM * E), wide = sweeps * TEAM * E;
   const float inv = __frcp_rn((float)a.cols);
+  const uint32_t ring = smem_u32(smem);
   dep_trigger();
   dep_wait();
   int32_t exponent = 0;
@@ -273,38 +403,78 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const NormA
   } else if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) {
     *a.status = 0ull;
   }
+  auto ask = [&](uint64_t r, uint32_t slot) {
+    if (kCopies) {
+      const bool ok = r < a.rows;
+      const uint32_t row = ok ? (uint32_t)r : 0u, at = ring + slot * R::kSlot;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        copy_vec<DT, TEAM, VEC, kLines>(at + (i * kNormThreads + threadIdx.x) * 16u, a.dy + (uint64_t)row * a.ldy * (16 / E), i, t, a.cols, ok);
+        if (X == 0) {
+          copy_vec<DT, TEAM, VEC, kLines>(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u, a.x + (uint64_t)row * a.ldx * (16 / E), i, t, a.cols, ok);
+        } else {
+          const uint32_t col = column<E, TEAM, kLines>(i, t, 0), to = at + R::kX + (i * kNormThreads + threadIdx.x) * 8u;
+          const bool there = ok && col < a.cols;
+          copy4(to, there ? a.x + l.code_at(row, col / 32u) + col % 32u / 8u * 4u : a.x, there);
+          copy4(to + 4u, there ? a.x + l.atom_at(row / 128u, col / (X > 1 ? 64u : 128u)) + MxLayout::scale_in_atom(row) : a.x, there);
+        }
+      }
+      copy4(at + R::kStat + threadIdx.x * 8u, a.mean + row, ok);
+      copy4(at + R::kStat + threadIdx.x * 8u + 4u, a.rstd + row, ok);
+      copy_commit();
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < R::kRows - 1; ++k) ask((uint64_t)team + (uint64_t)k * teams, k);
   const float scale = X == 1 + kMxB16 ? pow2_f(exponent) : 1.0f;
   float dg[N][E] = {}, db[N][E] = {}, gamma[N][E];
   if (V) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) load_weights<E>(a.gamma, a.wdtype, (i * TEAM + t) * E, a.cols, 1.0f, gamma[i]);
+    for (int i = 0; i < N; ++i) load_weights<E, TEAM, kLines>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, gamma[i]);
   } else {
     for (uint32_t i = threadIdx.x; i < 2u * wide; i += kNormThreads) acc[i] = 0.0f;
     __syncthreads();
   }
-  uint32_t turn = 0;
-  for (uint32_t row = team; row < a.rows; row += teams, turn ^= 2u) {
+  uint32_t turn = 0, slot = 0;
+  for (uint32_t row = team; row < a.rows; row += teams, turn ^= 1u, slot = slot + 1u == R::kRows ? 0u : slot + 1u) {
+    ask((uint64_t)row + (uint64_t)(R::kRows - 1) * teams, slot ? slot - 1u : R::kRows - 1u);
     const uint8_t* dyr = a.dy + (uint64_t)row * a.ldy * (16 / E);
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    const uint32_t at = ring + slot * R::kSlot;
+    float mean, rstd;
     uint4 rx[N], ry[N];
+    if (kCopies) {
+      copy_wait<R::kRows - 1>();
+      const uint2 st = ld_shared8(at + R::kStat + threadIdx.x * 8u);
+      mean = bits_f(st.x);
+      rstd = bits_f(st.y);
+    } else {
+      mean = a.mean[row];
+      rstd = a.rstd[row];
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (V) {
-        const uint32_t col = (i * TEAM + t) * E;
-        ry[i] = load_vec<DT, VEC>(dyr, col, a.cols);
-        rx[i] = load_x<DT, VEC, X>(a, l, row, col);
+      if (V && kCopies) {
+        ry[i] = ld_shared16(at + (i * kNormThreads + threadIdx.x) * 16u);
+        if (X == 0) {
+          rx[i] = ld_shared16(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u);
+        } else {
+          const uint2 w = ld_shared8(at + R::kX + (i * kNormThreads + threadIdx.x) * 8u);
+          rx[i] = make_uint4(w.x, w.y, 0u, 0u);
+        }
+      } else if (V) {
+        ry[i] = load_vec<DT, TEAM, VEC, kLines>(dyr, i, t, a.cols);
+        rx[i] = load_x<DT, TEAM, VEC, kLines, X>(a, l, row, i, t);
       }
     // xhat, dy and g = dy * gamma of vector i (zeros behind the last column, as dy is zero there)
     auto vec = [&](uint32_t i, float(&xh)[E], float(&dy)[E], float(&g)[E]) {
-      const uint32_t col = (i * TEAM + t) * E;
-      unpack<DT, E>(V ? ry[i % N] : load_vec<DT, VEC>(dyr, col, a.cols), dy);
-      unpack_x<DT, X, E>(V ? rx[i % N] : load_x<DT, VEC, X>(a, l, row, col), scale, xh);
-      if (!V) load_weights<E>(a.gamma, a.wdtype, col, a.cols, 1.0f, g);
+      unpack<DT, E>(V ? ry[i % N] : load_vec<DT, TEAM, VEC, kLines>(dyr, i, t, a.cols), dy);
+      unpack_x<DT, X, E>(V ? rx[i % N] : load_x<DT, TEAM, VEC, kLines, X>(a, l, row, i, t), column<E, TEAM, kLines>(i, t, 0), scale, xh);
+      if (!V) load_weights<E, TEAM, kLines>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         xh[e] = (xh[e] - mean) * rstd;
         g[e] = dy[e] * (V ? gamma[i % N][e] : g[e]);
-        if (col + e >= a.cols) xh[e] = 0.0f;  // (a NaN mean or rstd must not come back through 0 * NaN)
+        if (column<E, TEAM, kLines>(i, t, e) >= a.cols) xh[e] = 0.0f;  // (a NaN mean or rstd must not come back through 0 * NaN)
       }
     };
     float s1 = 0.0f, s2 = 0.0f;
@@ -316,68 +486,64 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward_kernel(const NormA
       for (int e = 0; e < E; ++e) {
         s1 += g[e];
         s2 = __fmaf_rn(g[e], xh[e], s2);
-      }
-    }
-    const float m1 = team_sum<TEAM>(s1, slots[turn]) * inv, m2 = team_sum<TEAM>(s2, slots[turn + 1]) * inv;
-    uint8_t* dxr = a.dx ? a.dx + (uint64_t)row * a.ldx * (16 / E) : nullptr;
-#pragma unroll
-    for (uint32_t i = 0; i < sweeps; ++i) {
-      const uint32_t col = (i * TEAM + t) * E;
-      float xh[E], dy[E], g[E];
-      vec(i, xh, dy, g);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
         if (V) {
           dg[i % N][e] = __fmaf_rn(dy[e], xh[e], dg[i % N][e]);
           db[i % N][e] += dy[e];
         } else {  // (a team is the CTA; thread t alone has these columns)
-          acc[col + e] = __fmaf_rn(dy[e], xh[e], acc[col + e]);
-          acc[wide + col + e] += dy[e];
+          const uint32_t c = column<E, TEAM, kLines>(i, t, e);
+          acc[c] = __fmaf_rn(dy[e], xh[e], acc[c]);
+          acc[wide + c] += dy[e];
         }
-        g[e] = rstd * (g[e] - m1 - xh[e] * m2);
       }
-      if (dxr && col < a.cols) store_vec<DT, VEC>(dxr, col, a.cols, pack<DT, E>(g));
+    }
+    if (!a.dx) continue;
+    const float2 m = team_sum<TEAM>(s1, s2, slots[in_cta][turn]);
+    const float m1 = m.x * inv, m2 = m.y * inv;
+    uint8_t* dxr = a.dx + (uint64_t)row * a.ldx * (16 / E);
+#pragma unroll
+    for (uint32_t i = 0; i < sweeps; ++i) {
+      float xh[E], dy[E], g[E];
+      vec(i, xh, dy, g);
+#pragma unroll
+      for (int e = 0; e < E; ++e) g[e] = rstd * (g[e] - m1 - xh[e] * m2);
+      if (column<E, TEAM, kLines>(i, t, 0) < a.cols) store_vec<DT, TEAM, VEC, kLines>(dxr, i, t, a.cols, pack<DT, E>(g));
     }
   }
+  if (kCopies) copy_wait<0>();
   if (!a.work) return;
   float* out = a.work + (uint64_t)blockIdx.x * 2u * a.cols;
-  if (V == 0) {
-    __syncthreads();
-    for (uint32_t c = threadIdx.x; c < a.cols; c += kNormThreads) {
-      out[c] = acc[c];
-      out[a.cols + c] = acc[wide + c];
-    }
-    return;
-  }
-  if (TEAM == 32) {  // the CTA's teams one after the other
-    for (uint32_t w = 0; w < (uint32_t)kNormWarps; ++w) {
+  if (V && TEAM < kNormThreads) {  // the CTA's teams one after the other
+    for (uint32_t w = 0; w < (uint32_t)(kNormThreads / TEAM); ++w) {
+      __syncthreads();  // (the first one: nobody reads its rows any more)
       if (in_cta == w) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
           for (int e = 0; e < E; ++e) {
-            const uint32_t at = (i * TEAM + t) * E + e;
-            acc[at] = w ? acc[at] + dg[i][e] : dg[i][e];
-            acc[wide + at] = w ? acc[wide + at] + db[i][e] : db[i][e];
+            const uint32_t c = column<E, TEAM, kLines>(i, t, e);
+            acc[c] = w ? acc[c] + dg[i][e] : dg[i][e];
+            acc[wide + c] = w ? acc[wide + c] + db[i][e] : db[i][e];
           }
       }
-      __syncthreads();
     }
-    for (uint32_t c = threadIdx.x; c < a.cols; c += kNormThreads) {
-      out[c] = acc[c];
-      out[a.cols + c] = acc[wide + c];
-    }
-  } else {
+  }
+  if (V && TEAM == kNormThreads) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const uint32_t at = (i * TEAM + t) * E + e;
-        if (at < a.cols) {
-          out[at] = dg[i][e];
-          out[a.cols + at] = db[i][e];
+        const uint32_t c = column<E, TEAM, kLines>(i, t, e);
+        if (c < a.cols) {
+          out[c] = dg[i][e];
+          out[a.cols + c] = db[i][e];
         }
       }
+  } else {
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < a.cols; c += kNormThreads) {
+      out[c] = acc[c];
+      out[a.cols + c] = acc[wide + c];
+    }
   }
 }
 
@@ -412,18 +578,18 @@ __global__ void __launch_bounds__(kNormThreads) norm_columns_kernel(const NormAr
 template <int DT, int TEAM, int V, bool VEC>
 int launch_forward_t(const NormArgs& a, cudaStream_t stream) {
   const uint64_t rows = a.packed ? ((uint64_t)a.rows + 127) / 128 * 128 : a.rows;
-  const uint32_t grid = (uint32_t)std::min<uint64_t>((rows * TEAM + kNormThreads - 1) / kNormThreads, (uint64_t)sm_count() * 8);
-  return launch_plain<norm_forward_kernel<DT, TEAM, V, VEC>>(grid, kNormThreads, 0, 1, stream, a);
+  const uint32_t grid = (uint32_t)std::min<uint64_t>((rows * TEAM + kNormThreads - 1) / kNormThreads, (uint64_t)sm_count() * 4);
+  const size_t smem = V && (VEC || DT == kF32) ? (size_t)kAhead * V * kNormThreads * 16 : 0;
+  return launch_plain<norm_forward_kernel<DT, TEAM, V, VEC>>(grid, kNormThreads, smem, 1, stream, a);
 }
 template <int DT, bool VEC>
 int launch_forward_dv(const NormArgs& a, cudaStream_t stream) {
   const uint32_t vecs = (a.cols + NormVec<DT>::kE - 1) / NormVec<DT>::kE;
   if (vecs <= 32) return launch_forward_t<DT, 32, 1, VEC>(a, stream);
-  if (vecs <= 128) return launch_forward_t<DT, 32, 4, VEC>(a, stream);
+  if (vecs <= 128) return launch_forward_t<DT, 128, 1, VEC>(a, stream);
   if (vecs <= 256) return launch_forward_t<DT, 256, 1, VEC>(a, stream);
   if (vecs <= 512) return launch_forward_t<DT, 256, 2, VEC>(a, stream);
   if (vecs <= 1024) return launch_forward_t<DT, 256, 4, VEC>(a, stream);
-  if (vecs <= 2048) return launch_forward_t<DT, 256, 8, VEC>(a, stream);
   return launch_forward_t<DT, 256, 0, VEC>(a, stream);
 }
 
@@ -431,14 +597,15 @@ template <int DT, int TEAM, int V, bool VEC, int X>
 int launch_backward_t(const NormArgs& a, cudaStream_t stream) {
   constexpr uint32_t E = NormVec<DT>::kE;
   const uint32_t sweeps = V ? V : (a.cols + TEAM * E - 1u) / (TEAM * E);
-  const size_t smem = V == 0 || TEAM == 32 ? (size_t)8 * sweeps * TEAM * E : 0;
-  return launch_plain<norm_backward_kernel<DT, TEAM, V, VEC, X>>(a.parts, kNormThreads, smem, 1, stream, a);
+  constexpr size_t ring = V && (VEC || DT == kF32) ? (size_t)BackRing<V ? V : 1, X>::kRows * BackRing<V ? V : 1, X>::kSlot : 0;
+  const size_t sums = V == 0 || TEAM < kNormThreads ? (size_t)8 * sweeps * TEAM * E : 0;
+  return launch_plain<norm_backward_kernel<DT, TEAM, V, VEC, X>>(a.parts, kNormThreads, std::max(ring, sums), 1, stream, a);
 }
 template <int DT, bool VEC, int X>
 int launch_backward_dx(const NormArgs& a, cudaStream_t stream) {
   const uint32_t vecs = (a.cols + NormVec<DT>::kE - 1) / NormVec<DT>::kE;
   if (vecs <= 32) return launch_backward_t<DT, 32, 1, VEC, X>(a, stream);
-  if (vecs <= 128) return launch_backward_t<DT, 32, 4, VEC, X>(a, stream);
+  if (vecs <= 128) return launch_backward_t<DT, 128, 1, VEC, X>(a, stream);
   if (vecs <= 256) return launch_backward_t<DT, 256, 1, VEC, X>(a, stream);
   if (vecs <= 512) return launch_backward_t<DT, 256, 2, VEC, X>(a, stream);
   if (vecs <= 1024) return launch_backward_t<DT, 256, 4, VEC, X>(a, stream);
@@ -456,7 +623,8 @@ bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
 }  // namespace
 
 uint32_t norm_parts(uint32_t rows, uint32_t cols, int dtype) {
-  const uint32_t each = cols <= (dtype == kF32 ? 512u : 1024u) ? 32u : 4u;  // rows that make a CTA worth its sums (a warp or a CTA to a row)
+  // rows that make a CTA worth its sums: four to a team of a warp, of half a CTA, of a CTA (see launch_backward_dx)
+  const uint32_t vecs = (cols + (dtype == kF32 ? 3u : 7u)) / (dtype == kF32 ? 4u : 8u), each = vecs <= 32u ? 32u : (vecs <= 128u ? 8u : 4u);
   const uint32_t n = rows / each + (rows % each ? 1u : 0u);
   return n < 296u ? n : 296u;
 }

@@ -128,12 +128,14 @@ def test_strides_alignments_and_in_place(cols, ldx, ldy, offset, dtype):
     assert api.fh_layer_norm_backward(d, vdy, vx, tg, tmean, trstd, vdx, dgamma, dbeta, work) == api.FH_OK
     check_backward(num(vdx), num(dgamma), num(dbeta), dy, x, g, num(tmean), num(trstd), dtype, api.FH_F32)
     assert around(fdx, vdx)
-    # in place: y over x, dx over dy, dx over x (of equal strides)
+    # in place: y over x, dx over dy, dx over x (of equal strides): what the same call gives out of place
     d = api.norm_desc(rows, cols, dtype, api.FH_F32, 1e-5, ldx, ldx)
-    _, vdy = apart(tdy, ldx, offset)
-    assert api.fh_layer_norm_backward(d, vdy, vx, tg, tmean, trstd, vdy) == api.FH_OK and torch.equal(vdy, vdx)
-    _, vdy, _, over = *apart(tdy, ldx, offset), *apart(tx, ldx, offset)
+    (_, vdy), (_, vdx), (_, vy) = apart(tdy, ldx, offset), apart(torch.zeros_like(tx), ldx, offset), apart(torch.zeros_like(tx), ldx, offset)
+    assert api.fh_layer_norm_backward(d, vdy, vx, tg, tmean, trstd, vdx) == api.FH_OK and api.fh_layer_norm(d, vx, tg, tb, vy) == api.FH_OK
+    check_backward(num(vdx), None, None, dy, x, g, num(tmean), num(trstd), dtype, api.FH_F32)
+    _, over = apart(tx, ldx, offset)
     assert api.fh_layer_norm_backward(d, vdy, over, tg, tmean, trstd, over) == api.FH_OK and torch.equal(over, vdx)
+    assert api.fh_layer_norm_backward(d, vdy, vx, tg, tmean, trstd, vdy) == api.FH_OK and torch.equal(vdy, vdx)
     assert api.fh_layer_norm(d, vx, tg, tb, vx) == api.FH_OK and torch.equal(vx, vy)
 
 
