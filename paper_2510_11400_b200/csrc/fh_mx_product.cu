@@ -1,4 +1,6 @@
 // Products of microscaled 4-bit matrices on the tensor cores.
+#include <cuda.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -20,7 +22,20 @@ namespace {
 // rows that come of it are not looked at: a code is always finite, and a NaN scale stays in its row.
 constexpr int kProductThreads = 192;  // four warps for the result, one for copies, one for matrix instructions
 constexpr int kStepChunks = 8;        // 8 x 32 elements to a stage
-constexpr uint32_t kWaitPolls = 1u << 20;
+constexpr uint32_t kWaitPolls = 1u << 26;   // some seconds
+constexpr uint32_t kDrainPolls = 1u << 20;  // waits of up to 2 us each, for copies under way
+
+// Stage of a ring and the parity of its round.
+template <int STAGES>
+struct Turn {
+  uint32_t stage = 0, round = 0;
+  __device__ __forceinline__ void next() {
+    if (++stage == (uint32_t)STAGES) {
+      stage = 0;
+      round ^= 1u;
+    }
+  }
+};
 
 template <int F, int QT>
 struct ProductShape {
@@ -127,9 +142,10 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
       const uint8_t* sp = g.b + lp.atom_at(tp, 0);
       const uint8_t* sq = g.a + lq.atom_at(tq, 0);
       uint32_t i = 0;
-      for (uint32_t it = first; it < last; ++it, ++i) {
-        const uint32_t s = i % S::kStages;
-        if (i >= (uint32_t)S::kStages && !mbar_wait(empty + s, (i / S::kStages - 1u) & 1u, kWaitPolls)) {
+      Turn<S::kStages> at;
+      for (uint32_t it = first; it < last; ++it, ++i, at.next()) {
+        const uint32_t s = at.stage;
+        if (i >= (uint32_t)S::kStages && !mbar_poll<false>(empty + s, at.round ^ 1u, kWaitPolls, abort)) {
           *abort = 1u;
           break;
         }
@@ -143,31 +159,36 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
         bulk_g2s(st + S::kP + S::kQ + S::kS, sq + (uint64_t)it * S::kAtoms * 512u, na * 512u, full + s);
       }
       // nothing may be in flight when the CTA ends
-      for (uint32_t w = i > (uint32_t)S::kStages ? i - S::kStages : 0u; w < i; ++w) mbar_wait(full + w % S::kStages, w / S::kStages & 1u, kWaitPolls);
+      for (uint32_t w = i > (uint32_t)S::kStages ? i - S::kStages : 0u; w < i; ++w) mbar_wait(full + w % S::kStages, w / S::kStages & 1u, kDrainPolls);
     }
   } else if (ok && warp == 5) {
     if (lane == 0) {
-      uint32_t i = 0;
-      for (uint32_t it = first; it < last; ++it, ++i) {
-        const uint32_t s = i % S::kStages;
-        if (!mbar_wait_abortable(full + s, i / S::kStages & 1u, kWaitPolls, abort)) {
+      Turn<S::kStages> at;
+      for (uint32_t it = first; it < last; ++it, at.next()) {
+        const uint32_t s = at.stage;
+        if (!mbar_poll<false>(full + s, at.round, kWaitPolls, abort)) {
           *abort = 1u;
           break;
         }
         tc_fence_after();
         const uint32_t nc = min((uint32_t)kStepChunks, chunks - it * kStepChunks);
         const uint32_t na = min((uint32_t)S::kAtoms, lp.atoms - it * S::kAtoms);
-        const uint32_t st = smem_u32(smem + s * S::kStage);
+        const uint32_t st = smem_u32(smem) + s * S::kStage;
         const uint32_t sa = tmem + S::kAcc + s * 2u * S::kScaleCols, sb = sa + S::kScaleCols;
-        for (uint32_t x = 0; x < na; ++x) {
-          tc_copy_scales(sa + 4u * x, smem_desc(st + S::kP + S::kQ + 512u * x, 128u, 128u));
-          tc_copy_scales(sb + 4u * x, smem_desc(st + S::kP + S::kQ + S::kS + 512u * x, 128u, 128u));
-        }
-        for (uint32_t x = 0; x < nc / 2u; ++x) {
-          const uint64_t da = smem_desc(st + x * 32u * rp, rp * 16u, 128u), db = smem_desc(st + S::kP + x * 32u * rq, rq * 16u, 128u);
-          const uint32_t word = F == kMxB32 ? x / 2u : x, id = F == kMxB32 ? x % 2u * 2u : 0u;
-          tc_mma_mx<F == kMxB32>(tmem, da, db, mx_idesc(128u, QT, F == kMxB32, id), sa + 4u * word, sb + 4u * word, i > 0u || x > 0u);
-        }
+        const uint64_t da = smem_desc(st, rp * 16u, 128u), db = smem_desc(st + S::kP, rq * 16u, 128u), ds = smem_desc(st + S::kP + S::kQ, 128u, 128u);
+#pragma unroll
+        for (uint32_t x = 0; x < (uint32_t)S::kAtoms; ++x)
+          if (x < na) {
+            tc_copy_scales(sa + 4u * x, ds + 32u * x);
+            tc_copy_scales(sb + 4u * x, ds + S::kS / 16u + 32u * x);
+          }
+#pragma unroll
+        for (uint32_t x = 0; x < kStepChunks / 2u; ++x)
+          if (2u * x < nc) {
+            const uint32_t word = F == kMxB32 ? x / 2u : x, id = F == kMxB32 ? x % 2u * 2u : 0u;
+            tc_mma_mx<F == kMxB32>(tmem, da + 2u * x * rp, db + 2u * x * rq, mx_idesc(128u, QT, F == kMxB32, id), sa + 4u * word, sb + 4u * word,
+                                   it > first || x > 0u);
+          }
         tc_commit(empty + s);
       }
       tc_commit(done);
@@ -178,7 +199,7 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
   const bool mine = ok && warp < 4;
   bool good = mine;
   if (mine) {
-    good = __all_sync(0xFFFFFFFFu, mbar_wait_abortable(done, 0u, kWaitPolls, abort) && !*abort);
+    good = mbar_wait_warp(done, 0u, kDrainPolls, abort);
     tc_fence_after();
   }
   const uint32_t col = tp * 128u + warp * 32u + lane;
@@ -249,15 +270,27 @@ struct PairShape {
   static_assert(kStages * kStage >= (256 + 8) * 512, "partial sums, and rows read behind them");
 };
 
+// How the codes and scales of an operand are laid out for the copies, which tell the even CTA's barrier of both CTAs' stages: a plain
+// bulk copy cannot reach the other CTA's, and a thread that passed the word on took 0.3 us a stage.
+struct OperandMaps {
+  CUtensorMap codes;   // of the blocks of 128 rows: 128 bytes (eight rows), 16 of them, every 32 columns
+  CUtensorMap rest;    // of the last block, if it has fewer rows: the copies fill up with zeros
+  CUtensorMap scales;  // 128 bytes, four to a group
+};
+struct PairArgs {
+  OperandMaps a, b;
+  MxProductArgs g;
+};
+
 template <int DT, int F>
-__global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const MxProductArgs g) {
+__global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const __grid_constant__ PairArgs pa) {
+  const MxProductArgs& g = pa.g;
   using S = PairShape<F>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);  // even CTA: both CTAs' stages have arrived
   uint64_t* empty = full + S::kStages;
-  uint64_t* peer = empty + S::kStages;  // even CTA: the odd one's stage has arrived
-  uint64_t* sums = peer + S::kStages;   // the accumulator is complete
+  uint64_t* sums = empty + S::kStages;  // the accumulator is complete
   uint64_t* taken = sums + 1;           // even CTA: both CTAs' warps have taken it
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(taken + 1);
   volatile uint32_t* abort = tmem_at + 1;
@@ -269,7 +302,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(full + i, 1);
       mbar_init(empty + i, 1);
-      mbar_init(peer + i, 1);
     }
     mbar_init(sums, 1);
     mbar_init(taken, 16);
@@ -298,84 +330,75 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
   if (warp == 8) {
     if (lane == 0) {
       uint32_t i = 0;
+      Turn<S::kStages> turn;
       for (uint32_t tile = pair; tile < tiles && good; tile += pairs) {
-        const uint32_t bp = tile % g.tiles_n * 2u + half, bq0 = tile / g.tiles_n * 2u, bq = bq0 + half;
-        const uint32_t rp = bp < blocks_p ? lp.block_rows(bp) : 0u, rq = bq < blocks_q ? lq.block_rows(bq) : 0u;
-        const uint8_t* p = g.b + (rp ? lp.code_at(bp * 128u, 0) : 0u);
-        const uint8_t* q = g.a + (rq ? lq.code_at(bq * 128u, 0) : 0u);
-        const uint8_t* sp = g.b + (rp ? lp.atom_at(bp, 0) : 0u);
-        const uint8_t* sq0 = g.a + lq.atom_at(bq0, 0);
-        const bool two = bq0 + 1u < blocks_q;
-        const uint8_t* sq1 = g.a + (two ? lq.atom_at(bq0 + 1u, 0) : 0u);
-        // a block of codes: one piece if it has all its rows; otherwise its chunks go where those of a whole one would be
-        auto codes = [&](uint8_t* dst, const uint8_t* src, uint32_t rows, uint32_t it, uint32_t nc, uint64_t* bar) {
-          if (rows == 128u) {
-            bulk_g2s(dst, src + (uint64_t)it * kStepChunks * 2048u, nc * 2048u, bar);
-          } else if (rows) {
-            for (uint32_t j = 0; j < nc; ++j) bulk_g2s(dst + j * 2048u, src + ((uint64_t)it * kStepChunks + j) * 16u * rows, 16u * rows, bar);
-          }
-        };
-        for (uint32_t it = first; it < last; ++it, ++i) {
-          const uint32_t s = i % S::kStages;
-          if (i >= (uint32_t)S::kStages && !mbar_wait_cluster(empty + s, (i / S::kStages - 1u) & 1u, kWaitPolls, abort)) {
+        const uint32_t bp0 = tile % g.tiles_n * 2u, bq0 = tile / g.tiles_n * 2u, bp = bp0 + half, bq = bq0 + half;
+        const uint32_t np = min(2u, blocks_p - bp0), nq = min(2u, blocks_q - bq0);  // blocks that there are
+        const bool p_whole = lp.block_rows(min(bp, blocks_p - 1u)) == 128u, q_whole = lq.block_rows(min(bq, blocks_q - 1u)) == 128u;
+        const uint32_t bytes = (np + nq) * S::kOp + (np + 2u * nq) * S::kS;  // of both CTAs
+        const uint32_t zp = p_whole ? bp * chunks : 0u, zq = q_whole ? bq * chunks : 0u;
+        for (uint32_t it = first; it < last; ++it, ++i, turn.next()) {
+          const uint32_t s = turn.stage;
+          if (i >= (uint32_t)S::kStages && !mbar_poll<true>(empty + s, turn.round ^ 1u, kWaitPolls, abort)) {
             *abort = 1u;
             good = false;
             break;
           }
-          const uint32_t nc = min((uint32_t)kStepChunks, chunks - it * kStepChunks);
-          const uint32_t na = min((uint32_t)S::kAtoms, lp.atoms - it * S::kAtoms);
-          uint8_t* st = smem + s * S::kStage;
-          const uint64_t at = (uint64_t)it * S::kAtoms * 512u;
-          mbar_expect_tx(full + s, nc * 16u * (rp + rq) + na * 512u * ((rp ? 1u : 0u) + (two ? 2u : 1u)));
-          codes(st, p, rp, it, nc, full + s);
-          codes(st + S::kOp, q, rq, it, nc, full + s);
-          if (rp) bulk_g2s(st + 2 * S::kOp, sp + at, na * 512u, full + s);
-          bulk_g2s(st + 2 * S::kOp + S::kS, sq0 + at, na * 512u, full + s);
-          if (two) bulk_g2s(st + 2 * S::kOp + 2 * S::kS, sq1 + at, na * 512u, full + s);
+          const uint32_t st = smem_u32(smem) + s * S::kStage, sc = st + 2u * S::kOp, bar = at_rank(full + s, even);
+          if (half == 0u) mbar_expect_tx(full + s, bytes);
+          if (half < np) tma_pair_3d(st, p_whole ? &pa.b.codes : &pa.b.rest, 0u, 0u, zp + it * kStepChunks, bar);
+          if (half < nq) tma_pair_3d(st + S::kOp, q_whole ? &pa.a.codes : &pa.a.rest, 0u, 0u, zq + it * kStepChunks, bar);
+          const uint32_t word = it * S::kAtoms;
+          if (half < np) tma_pair_2d(sc, &pa.b.scales, 0u, (bp * lp.atoms + word) * 4u, bar);
+          tma_pair_2d(sc + S::kS, &pa.a.scales, 0u, (bq0 * lq.atoms + word) * 4u, bar);
+          if (nq > 1u) tma_pair_2d(sc + 2u * S::kS, &pa.a.scales, 0u, ((bq0 + 1u) * lq.atoms + word) * 4u, bar);
         }
       }
-      // nothing may be in flight when the CTA ends
-      for (uint32_t w = i > (uint32_t)S::kStages ? i - S::kStages : 0u; w < i; ++w) mbar_wait(full + w % S::kStages, w / S::kStages & 1u, kWaitPolls);
+      // nothing may be in flight when a CTA ends
+      if (half == 0u)
+        for (uint32_t w = i > (uint32_t)S::kStages ? i - S::kStages : 0u; w < i; ++w) mbar_wait(full + w % S::kStages, w / S::kStages & 1u, kDrainPolls);
     }
   } else if (warp == 9) {
-    if (lane == 0) {
+    if (lane == 0 && half == 0u) {  // (issues for both)
       const uint16_t both = (uint16_t)(3u << even);
-      uint32_t i = 0, n = 0;
+      uint32_t n = 0;
+      Turn<S::kStages> turn;
       for (uint32_t tile = pair; tile < tiles && good; tile += pairs, ++n) {
-        if (half == 0u && n && !mbar_wait_cluster(taken, (n - 1u) & 1u, kWaitPolls, abort)) {
+        if (n && !mbar_poll<true>(taken, (n - 1u) & 1u, kWaitPolls, abort)) {
           *abort = 1u;
           break;
         }
         tc_fence_after();
-        for (uint32_t it = first; it < last; ++it, ++i) {
-          const uint32_t s = i % S::kStages, ph = i / S::kStages & 1u;
-          if (!mbar_wait_abortable(full + s, ph, kWaitPolls, abort) || (half == 0u && !mbar_wait_cluster(peer + s, ph, kWaitPolls, abort))) {
+        for (uint32_t it = first; it < last; ++it, turn.next()) {
+          const uint32_t s = turn.stage, ph = turn.round;
+          if (!mbar_poll<true>(full + s, ph, kWaitPolls, abort)) {
             *abort = 1u;
             good = false;
             break;
           }
-          if (half) {  // the odd CTA's stage is there: tell the even one, which issues for both
-            mbar_arrive_at(peer + s, even);
-            continue;
-          }
           tc_fence_after();
           const uint32_t nc = min((uint32_t)kStepChunks, chunks - it * kStepChunks);
           const uint32_t na = min((uint32_t)S::kAtoms, lp.atoms - it * S::kAtoms);
-          const uint32_t st = smem_u32(smem + s * S::kStage), sc = st + 2u * S::kOp;
+          const uint32_t st = smem_u32(smem) + s * S::kStage;
           const uint32_t sa = tmem + 256u + s * S::kScaleCols, sb = sa + S::kAtoms * 4u;
-          for (uint32_t x = 0; x < na; ++x) {
-            tc_copy_scales_pair(sa + 4u * x, smem_desc(sc + 512u * x, 128u, 128u));
-            tc_copy_scales_pair(sb + 8u * x, smem_desc(sc + S::kS + 512u * x, 128u, 128u));
-            tc_copy_scales_pair(sb + 8u * x + 4u, smem_desc(sc + 2u * S::kS + 512u * x, 128u, 128u));
-          }
-          for (uint32_t x = 0; x < nc / 2u; ++x) {
-            const uint64_t da = smem_desc(st + x * 4096u, 2048u, 128u), db = smem_desc(st + S::kOp + x * 4096u, 2048u, 128u);
-            const uint32_t word = F == kMxB32 ? x / 2u : x, id = F == kMxB32 ? x % 2u * 2u : 0u;
-            tc_mma_mx_pair<F == kMxB32>(tmem, da, db, mx_idesc(256u, 256u, F == kMxB32, id), sa + 4u * word, sb + 8u * word, it > first || x > 0u);
-          }
+          const uint64_t da = smem_desc(st, 2048u, 128u), db = smem_desc(st + S::kOp, 2048u, 128u), ds = smem_desc(st + 2u * S::kOp, 128u, 128u);
+#pragma unroll
+          for (uint32_t x = 0; x < (uint32_t)S::kAtoms; ++x)
+            if (x < na) {
+              tc_copy_scales_pair(sa + 4u * x, ds + 32u * x);
+              tc_copy_scales_pair(sb + 8u * x, ds + S::kS / 16u + 32u * x);
+              tc_copy_scales_pair(sb + 8u * x + 4u, ds + 2u * S::kS / 16u + 32u * x);
+            }
+#pragma unroll
+          for (uint32_t x = 0; x < kStepChunks / 2u; ++x)
+            if (2u * x < nc) {
+              const uint32_t word = F == kMxB32 ? x / 2u : x, id = F == kMxB32 ? x % 2u * 2u : 0u;
+              tc_mma_mx_pair<F == kMxB32>(tmem, da + 256u * x, db + 256u * x, mx_idesc(256u, 256u, F == kMxB32, id), sa + 4u * word, sb + 8u * word,
+                                          it > first || x > 0u);
+            }
           tc_commit_pair(empty + s, both);
         }
-        if (half == 0u) tc_commit_pair(sums, both);
+        tc_commit_pair(sums, both);
       }
     }
   } else {
@@ -383,7 +406,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
     const uint32_t side = warp / 4u * 128u;  // columns of the accumulator: rows of A
     uint32_t n = 0;
     for (uint32_t tile = pair; tile < tiles && good; tile += pairs, ++n) {
-      good = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(sums, n & 1u, kWaitPolls, abort) && !*abort);
+      good = mbar_wait_warp(sums, n & 1u, kDrainPolls, abort);
       if (!good) break;
       tc_fence_after();
       const uint32_t col = tile % g.tiles_n * 256u + half * 128u + warp % 4u * 32u + lane, row = tile / g.tiles_n * 256u + side;
@@ -438,9 +461,44 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
   if (warp == 9) tmem_free_pair(tmem, S::kCols);
 }
 
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+  static std::atomic<void*> fn{nullptr};
+  void* f = fn.load();
+  if (!f) {
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) return nullptr;
+    fn.store(f);
+  }
+  return (EncodeTiled)f;
+}
+
+// A map of `dims` boxes of 128 bytes, `strides` bytes apart, as bytes.
+bool encode_map(CUtensorMap* map, const uint8_t* base, uint32_t rank, const cuuint64_t (&dims)[3], const cuuint64_t (&strides)[2], const cuuint32_t (&box)[3]) {
+  const EncodeTiled f = encode_tiled();
+  const cuuint32_t ones[3] = {1, 1, 1};
+  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, const_cast<uint8_t*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int F>
+bool encode_operand(OperandMaps* m, const uint8_t* c, uint32_t rows, uint32_t k) {
+  const MxLayout l(rows, k, F);
+  const uint32_t whole = l.r8 / 128u, rest = l.r8 % 128u, chunks = l.kp / 32u;
+  const cuuint32_t box[3] = {128, 16, (cuuint32_t)kStepChunks}, sbox[3] = {128, 4 * PairShape<F>::kAtoms, 1};
+  bool ok = true;
+  if (whole) ok = encode_map(&m->codes, c + kMxHeadBytes, 3, {128, 16, (cuuint64_t)whole * chunks}, {128, 2048}, box);
+  if (rest) ok = ok && encode_map(&m->rest, c + l.code_at(whole * 128u, 0), 3, {128, rest / 8u, chunks}, {128, rest * 16u}, box);
+  return ok && encode_map(&m->scales, c + l.atom_at(0, 0), 2, {128, (cuuint64_t)(whole + (rest ? 1u : 0u)) * l.atoms * 4u, 1}, {128, 0}, sbox);
+}
+
 template <int DT, int F>
 int launch_product_pair(const MxProductArgs& a, uint32_t clusters, cudaStream_t stream) {
-  return launch_plain<mx_product_pair_kernel<DT, F>>(clusters * 2u * a.split, kPairThreads, PairShape<F>::kSmem, (int)(2u * a.split), stream, a);
+  PairArgs p = {};
+  p.g = a;
+  if (!encode_operand<F>(&p.a, a.a, a.m, a.k) || !encode_operand<F>(&p.b, a.b, a.n, a.k)) return FH_ERR_UNSUPPORTED;
+  return launch_plain<mx_product_pair_kernel<DT, F>>(clusters * 2u * a.split, kPairThreads, PairShape<F>::kSmem, (int)(2u * a.split), stream, p);
 }
 
 template <int DT, int F, int QT>

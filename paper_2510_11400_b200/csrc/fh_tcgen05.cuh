@@ -89,21 +89,65 @@ __device__ __forceinline__ void tc_mma_mx_pair(uint32_t d, uint64_t a, uint64_t 
         "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)add)
         : "memory");
 }
+// Address of this CTA's `p` in the shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
+  uint32_t there;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_u32(p)), "r"(rank));
+  return there;
+}
+// A box of a tensor map to this CTA's memory, told to a barrier that may be the pair's other CTA's (`bar`: its cluster address).
+__device__ __forceinline__ void tma_pair_3d(uint32_t dst, const void* map, uint32_t x, uint32_t y, uint32_t z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void tma_pair_2d(uint32_t dst, const void* map, uint32_t x, uint32_t y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(bar)
+               : "memory");
+}
 // Arrival at the same barrier of CTA `rank`, after all that this thread has seen; and the wait that sees it (bounded).
 __device__ __forceinline__ void mbar_arrive_at(uint64_t* bar, uint32_t rank) {
-  uint32_t there;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_u32(bar)), "r"(rank));
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(there) : "memory");
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(bar, rank)) : "memory");
 }
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, uint32_t limit, const volatile uint32_t* abort) {
+// Bounded wait of a whole warp for something far off: one lane looks, suspended in between, so that the warps that wait for a result
+// leave the barriers of those that work on it alone.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, uint32_t limit, const volatile uint32_t* abort) {
+  bool ok = true;
+  if (threadIdx.x % 32 == 0) {
+    ok = false;
+    for (uint32_t i = 0; i < limit && !ok; ++i) {
+      uint32_t done;
+      asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
+                   : "=r"(done)
+                   : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs)
+                   : "memory");
+      ok = done != 0;
+      if ((i & 7u) == 7u && *abort) break;
+    }
+    ok = ok && !*abort;
+  }
+  return __all_sync(0xFFFFFFFFu, ok);
+}
+
+// Polls without pause: a suspended thread wakes up late, and a stage of these kernels takes less than that (see mx_product_kernel).
+// CLUSTER: what is waited for was written by another CTA's thread.
+template <bool CLUSTER>
+__device__ __forceinline__ bool mbar_poll(uint64_t* bar, uint32_t parity, uint32_t limit, const volatile uint32_t* abort) {
   for (uint32_t i = 0; i < limit; ++i) {
     uint32_t ok;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
-                 : "=r"(ok)
-                 : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs)
-                 : "memory");
+    if (CLUSTER)
+      asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                   : "=r"(ok)
+                   : "r"(smem_u32(bar)), "r"(parity)
+                   : "memory");
+    else
+      asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                   : "=r"(ok)
+                   : "r"(smem_u32(bar)), "r"(parity)
+                   : "memory");
     if (ok) return true;
-    if ((i & 7u) == 7u && *abort) return false;
+    if ((i & 63u) == 63u && *abort) return false;
   }
   return false;
 }
