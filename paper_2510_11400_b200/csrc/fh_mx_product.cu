@@ -51,34 +51,47 @@ struct ProductShape {
   static_assert(kStages * kStage >= (QT + 8) * 512, "partial sums, and rows read behind them");
 };
 
-// NR rows of a column of C from row `row` on, those below `end`.  What is added to is asked for all at once.
+// NR rows of a column of C from row `row` on, those below `end`.  What is added to is asked for all at once.  (Addresses step from row
+// to row: a product with ldc for each of them made a tile of 128 x 256 take 4 us.)
 template <int DT, int NR>
 __device__ __forceinline__ void store_c(uint8_t* c, uint64_t ldc, uint32_t row, uint32_t end, uint32_t col, const float (&v)[NR], bool add) {
   using T = typename std::conditional<DT == kF32, float, __nv_bfloat16>::type;
-  T* p = reinterpret_cast<T*>(c) + (uint64_t)row * ldc + col;
+  T* const p0 = reinterpret_cast<T*>(c) + (uint64_t)row * ldc + col;
+  if (!add && row + NR <= end) {
+    T* p = p0;
+#pragma unroll
+    for (int x = 0; x < NR; ++x, p += ldc) *p = (T)v[x];
+    return;
+  }
   float old[NR];
   if (add) {
+    const T* p = p0;
 #pragma unroll
-    for (int x = 0; x < NR; ++x) {
+    for (int x = 0; x < NR; ++x, p += ldc) {
       old[x] = 0.0f;
-      if (row + x < end) old[x] = (float)p[x * ldc];
+      if (row + x < end) old[x] = (float)*p;
     }
   }
+  T* p = p0;
 #pragma unroll
-  for (int x = 0; x < NR; ++x)
-    if (row + x < end) p[x * ldc] = (T)(add ? old[x] + v[x] : v[x]);
+  for (int x = 0; x < NR; ++x, p += ldc)
+    if (row + x < end) *p = (T)(add ? old[x] + v[x] : v[x]);
 }
 
-// What the sums are multiplied by, one after the other: 2^(ea + eb) in two steps, so that neither over- nor underflows where the result
-// does not, and alpha.
+// What the sums are multiplied by: 2^(ea + eb) and alpha, as one factor where that is exact and no product of it leaves the range of normal
+// numbers that the result is in; otherwise one after the other, the power in two steps.
 struct ProductScale {
   float f1, f2, alpha;
+  bool one;
   __device__ __forceinline__ ProductScale(int ea, int eb, float alpha_) : alpha(alpha_) {
     const int e = ea + eb, e1 = e / 2;
     f1 = pow2_f(e1);
     f2 = pow2_f(e - e1);
+    const float m = fabsf(alpha_);
+    one = (e >= -32 && e <= 32 && m >= 0x1p-60f && m <= 0x1p60f) || e == 0;
+    if (one) alpha = alpha_ * f1 * f2;
   }
-  __device__ __forceinline__ float operator()(float v) const { return v * f1 * f2 * alpha; }
+  __device__ __forceinline__ float operator()(float v) const { return one ? v * alpha : v * f1 * f2 * alpha; }
 };
 
 // Sums a row of partial sums over the parts of a cluster (CTAs `stride` apart, from `first` on), NR rows at a time, in the order of the parts.
@@ -199,7 +212,7 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
   const bool mine = ok && warp < 4;
   bool good = mine;
   if (mine) {
-    good = mbar_wait_warp(done, 0u, kDrainPolls, abort);
+    good = mbar_poll_warp(done, 0u, kWaitPolls, abort);
     tc_fence_after();
   }
   const uint32_t col = tp * 128u + warp * 32u + lane;
@@ -406,7 +419,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
     const uint32_t side = warp / 4u * 128u;  // columns of the accumulator: rows of A
     uint32_t n = 0;
     for (uint32_t tile = pair; tile < tiles && good; tile += pairs, ++n) {
-      good = mbar_wait_warp(sums, n & 1u, kDrainPolls, abort);
+      good = mbar_poll_warp(sums, n & 1u, kWaitPolls, abort);
       if (!good) break;
       tc_fence_after();
       const uint32_t col = tile % g.tiles_n * 256u + half * 128u + warp % 4u * 32u + lane, row = tile / g.tiles_n * 256u + side;
@@ -418,14 +431,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
       __syncwarp();
       if (lane == 0) mbar_arrive_at(taken, even);
       if (g.split == 1u) {
-        if (col < g.n) {
 #pragma unroll
-          for (uint32_t x = 0; x < 8u; ++x) {
-            float f[16];
+        for (uint32_t x = 0; x < 8u; ++x) {
+          float f[16];
 #pragma unroll
-            for (uint32_t y = 0; y < 16u; ++y) f[y] = scaled(bits_f(v[x][y]));
-            store_c<DT, 16>(g.c, g.ldc, row + 16u * x, g.m, col, f, g.accumulate);
-          }
+          for (uint32_t y = 0; y < 16u; ++y) f[y] = scaled(bits_f(v[x][y]));
+          if (col < g.n) store_c<DT, 16>(g.c, g.ldc, row + 16u * x, g.m, col, f, g.accumulate);
         }
       } else {  // (one tile only: all copies into shared memory have been used)
         float* part = reinterpret_cast<float*>(smem) + side * 128u + warp % 4u * 32u + lane;
@@ -533,8 +544,8 @@ int launch_mx_product(const MxProductArgs& a0, int dtype, int format, cudaStream
       return format == kMxB32 ? launch_product_pair<kF32, kMxB32>(a, clusters, stream) : launch_product_pair<kF32, kMxB16>(a, clusters, stream);
     return format == kMxB32 ? launch_product_pair<kBF16, kMxB32>(a, clusters, stream) : launch_product_pair<kBF16, kMxB16>(a, clusters, stream);
   }
-  // parts of the common axis while that leaves SMs idle, each of at least two stages
-  const uint64_t split = std::max<uint64_t>(1, std::min<uint64_t>({8, (uint64_t)sms / (tm * tn), steps / 2}));
+  // parts of the common axis while that leaves room (two CTAs fit an SM while a tile has few rows of A), each of at least two stages
+  const uint64_t split = std::max<uint64_t>(1, std::min<uint64_t>({8, (uint64_t)sms * (a.m <= 32 ? 2 : 1) / (tm * tn), steps / 2}));
   a.tiles_m = (uint32_t)tm;
   a.tiles_n = (uint32_t)tn;
   a.split = (uint32_t)split;

@@ -110,26 +110,6 @@ __device__ __forceinline__ void tma_pair_2d(uint32_t dst, const void* map, uint3
 __device__ __forceinline__ void mbar_arrive_at(uint64_t* bar, uint32_t rank) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_rank(bar, rank)) : "memory");
 }
-// Bounded wait of a whole warp for something far off: one lane looks, suspended in between, so that the warps that wait for a result
-// leave the barriers of those that work on it alone.
-__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, uint32_t limit, const volatile uint32_t* abort) {
-  bool ok = true;
-  if (threadIdx.x % 32 == 0) {
-    ok = false;
-    for (uint32_t i = 0; i < limit && !ok; ++i) {
-      uint32_t done;
-      asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
-                   : "=r"(done)
-                   : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs)
-                   : "memory");
-      ok = done != 0;
-      if ((i & 7u) == 7u && *abort) break;
-    }
-    ok = ok && !*abort;
-  }
-  return __all_sync(0xFFFFFFFFu, ok);
-}
-
 // Polls without pause: a suspended thread wakes up late, and a stage of these kernels takes less than that (see mx_product_kernel).
 // CLUSTER: what is waited for was written by another CTA's thread.
 template <bool CLUSTER>
@@ -150,6 +130,13 @@ __device__ __forceinline__ bool mbar_poll(uint64_t* bar, uint32_t parity, uint32
     if ((i & 63u) == 63u && *abort) return false;
   }
   return false;
+}
+
+// The same for a whole warp, one lane of which looks.
+__device__ __forceinline__ bool mbar_poll_warp(uint64_t* bar, uint32_t parity, uint32_t limit, const volatile uint32_t* abort) {
+  bool ok = true;
+  if (threadIdx.x % 32 == 0) ok = mbar_poll<true>(bar, parity, limit, abort) && !*abort;
+  return __all_sync(0xFFFFFFFFu, ok);
 }
 
 // 16 columns of the warp's 32 lanes: lane i gets its row's.  The values are there after tc_load_wait().
