@@ -47,7 +47,7 @@ struct ProductShape {
   static constexpr uint32_t kAcc = QT < 32 ? 32 : QT;
   static constexpr uint32_t kCols = kAcc + kStages * 2 * kScaleCols <= 128 ? 128 : 256;
   static_assert(kAcc + kStages * 2 * kScaleCols <= kCols, "tensor memory");
-  static constexpr size_t kSmem = 128 + kStages * kStage + 256;
+  static constexpr size_t kSmem = 128 + (size_t)kStages * kStage + 256;
   static_assert(kStages * kStage >= (QT + 8) * 512, "partial sums, and rows read behind them");
 };
 
@@ -295,6 +295,17 @@ struct PairArgs {
   MxProductArgs g;
 };
 
+// Tile `t` of the pairs' order: eight rows of tiles at a time, column by column, so that the tiles under way together share rows of A and of B
+// in L2 (row by row, 8192 x 16384 x 8192 took 595 us).
+struct PairTile {
+  uint32_t m, n;
+  __device__ __forceinline__ PairTile(uint32_t t, uint32_t tiles_m, uint32_t tiles_n) {
+    const uint32_t band = t / (8u * tiles_n), at = t % (8u * tiles_n), high = min(8u, tiles_m - 8u * band);
+    m = 8u * band + at % high;
+    n = at / high;
+  }
+};
+
 template <int DT, int F>
 __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const __grid_constant__ PairArgs pa) {
   const MxProductArgs& g = pa.g;
@@ -345,7 +356,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
       uint32_t i = 0;
       Turn<S::kStages> turn;
       for (uint32_t tile = pair; tile < tiles && good; tile += pairs) {
-        const uint32_t bp0 = tile % g.tiles_n * 2u, bq0 = tile / g.tiles_n * 2u, bp = bp0 + half, bq = bq0 + half;
+        const PairTile where(tile, g.tiles_m, g.tiles_n);
+        const uint32_t bp0 = where.n * 2u, bq0 = where.m * 2u, bp = bp0 + half, bq = bq0 + half;
         const uint32_t np = min(2u, blocks_p - bp0), nq = min(2u, blocks_q - bq0);  // blocks that there are
         const bool p_whole = lp.block_rows(min(bp, blocks_p - 1u)) == 128u, q_whole = lq.block_rows(min(bq, blocks_q - 1u)) == 128u;
         const uint32_t bytes = (np + nq) * S::kOp + (np + 2u * nq) * S::kS;  // of both CTAs
@@ -422,7 +434,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
       good = mbar_poll_warp(sums, n & 1u, kWaitPolls, abort);
       if (!good) break;
       tc_fence_after();
-      const uint32_t col = tile % g.tiles_n * 256u + half * 128u + warp % 4u * 32u + lane, row = tile / g.tiles_n * 256u + side;
+      const PairTile where(tile, g.tiles_m, g.tiles_n);
+      const uint32_t col = where.n * 256u + half * 128u + warp % 4u * 32u + lane, row = where.m * 256u + side;
       uint32_t v[8][16];
 #pragma unroll
       for (uint32_t x = 0; x < 8u; ++x) tc_load16(tmem + (warp % 4u * 32u << 16) + side + 16u * x, v[x]);
@@ -453,7 +466,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
     cluster_sync();
     if (warp < 8u && good && tiles) {
       const ProductScale scaled(ea, eb, g.alpha);
-      const uint32_t p = warp % 4u * 32u + lane, col = pair % g.tiles_n * 256u + half * 128u + p, row = pair / g.tiles_n * 256u;
+      const PairTile where(pair, g.tiles_m, g.tiles_n);
+      const uint32_t p = warp % 4u * 32u + lane, col = where.n * 256u + half * 128u + p, row = where.m * 256u;
       const uint32_t rows = min(256u, g.m - row), from = rows * rank / g.split, end = rows * (rank + 1u) / g.split, mid = (from + end) / 2u;
       const uint32_t stop = warp < 4u ? mid : end;
       if (col < g.n)
@@ -504,51 +518,96 @@ bool encode_operand(OperandMaps* m, const uint8_t* c, uint32_t rows, uint32_t k)
   return ok && encode_map(&m->scales, c + l.atom_at(0, 0), 2, {128, (cuuint64_t)(whole + (rest ? 1u : 0u)) * l.atoms * 4u, 1}, {128, 0}, sbox);
 }
 
+// Clusters of `size` CTAs of a kernel that the device holds at once (0: an error): fewer than CTAs divided by size, as a cluster stays within
+// a part of the device (of 148 CTAs of the pair kernel, 33 clusters of four, 22 of six, 15 of eight).
+template <auto Kernel>
+int clusters_at_once(int size, int threads, size_t smem) {
+  static std::atomic<int> known[64][9];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || size < 1 || size > 8) return 0;
+  if (dev < 64 && known[dev][size].load()) return known[dev][size].load();
+  if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMxSmemLimit) != cudaSuccess) return 0;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)size);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)size;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, Kernel, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  if (dev < 64) known[dev][size].store(n);
+  return n;
+}
+
+// Into how many parts to split the common axis: what takes the fewest rounds of stages, where a round of clusters costs `fixed` stages besides and a
+// split two more than that.  At least two stages to a part.
+template <typename AtOnce>
+uint32_t choose_split(uint64_t tiles, uint64_t steps, uint32_t most, uint64_t fixed, AtOnce at_once) {
+  uint32_t best = 1;
+  uint64_t least = ~0ull;
+  for (uint32_t s = 1; s <= most && (s == 1 || 2 * s <= steps); ++s) {
+    const int n = at_once(s);
+    if (n < 1) continue;
+    const uint64_t cost = (tiles + n - 1) / n * ((steps + s - 1) / s + fixed + (s > 1 ? fixed / 2 : 0));
+    if (cost < least) {
+      least = cost;
+      best = s;
+    }
+  }
+  return best;
+}
+
 template <int DT, int F>
-int launch_product_pair(const MxProductArgs& a, uint32_t clusters, cudaStream_t stream) {
+int launch_product_pair(const MxProductArgs& a, cudaStream_t stream) {
   PairArgs p = {};
   p.g = a;
+  p.g.tiles_m = (a.m + 255u) / 256u;
+  p.g.tiles_n = (a.n + 255u) / 256u;
   if (!encode_operand<F>(&p.a, a.a, a.m, a.k) || !encode_operand<F>(&p.b, a.b, a.n, a.k)) return FH_ERR_UNSUPPORTED;
-  return launch_plain<mx_product_pair_kernel<DT, F>>(clusters * 2u * a.split, kPairThreads, PairShape<F>::kSmem, (int)(2u * a.split), stream, p);
+  const uint64_t tiles = (uint64_t)p.g.tiles_m * p.g.tiles_n;
+  auto at_once = [](uint32_t s) { return clusters_at_once<mx_product_pair_kernel<DT, F>>((int)(2 * s), kPairThreads, PairShape<F>::kSmem); };
+  // (a tile's start and end take about as long as ten stages)
+  p.g.split = choose_split(tiles, ((uint64_t)a.k + 255) / 256, 4, 10, at_once);
+  const int n = at_once(1);
+  if (n < 1) return FH_ERR_CUDA;
+  const uint32_t clusters = (uint32_t)(p.g.split > 1 ? tiles : std::min<uint64_t>(tiles, (uint64_t)n));
+  return launch_plain<mx_product_pair_kernel<DT, F>>(clusters * 2u * p.g.split, kPairThreads, PairShape<F>::kSmem, (int)(2u * p.g.split), stream, p);
 }
 
 template <int DT, int F, int QT>
-int launch_product_t(const MxProductArgs& a, cudaStream_t stream) {
-  return launch_plain<mx_product_kernel<DT, F, QT>>(a.tiles_m * a.tiles_n * a.split, kProductThreads, ProductShape<F, QT>::kSmem,
-                                                    (int)a.split, stream, a);
+int launch_product_t(const MxProductArgs& a0, cudaStream_t stream) {
+  MxProductArgs a = a0;
+  a.tiles_m = (a.m + 127u) / 128u;
+  a.tiles_n = (a.n + 127u) / 128u;
+  const uint64_t tiles = (uint64_t)a.tiles_m * a.tiles_n;
+  // (the runtime counts one CTA of a cluster to an SM; these fit by shared and by tensor memory)
+  using S = ProductShape<F, QT>;
+  constexpr int kPerSm = std::min<int>((int)(kSmemPerSm / (S::kSmem + 1024)), (int)(512 / S::kCols));
+  auto at_once = [](uint32_t s) { return kPerSm * clusters_at_once<mx_product_kernel<DT, F, QT>>((int)s, kProductThreads, S::kSmem); };
+  // (a tile's start and end take about as long as eight stages)
+  a.split = choose_split(tiles, ((uint64_t)a.k + 255) / 256, 8, 8, at_once);
+  return launch_plain<mx_product_kernel<DT, F, QT>>((uint32_t)tiles * a.split, kProductThreads, ProductShape<F, QT>::kSmem, (int)a.split, stream, a);
 }
 template <int DT, int F>
 int launch_product_df(const MxProductArgs& a, cudaStream_t stream) {
   if (a.m <= 16) return launch_product_t<DT, F, 16>(a, stream);
   if (a.m <= 32) return launch_product_t<DT, F, 32>(a, stream);
   if (a.m <= 64) return launch_product_t<DT, F, 64>(a, stream);
-  return launch_product_t<DT, F, 128>(a, stream);
+  if (a.m <= 128) return launch_product_t<DT, F, 128>(a, stream);
+  return launch_product_pair<DT, F>(a, stream);
 }
 
 }  // namespace
 
-int launch_mx_product(const MxProductArgs& a0, int dtype, int format, cudaStream_t stream) {
-  MxProductArgs a = a0;
-  const int sms = sm_count();
-  if (sms < 1) return FH_ERR_CUDA;
-  const uint64_t steps = ((uint64_t)a.k + 255) / 256;
-  const uint64_t pm = ((uint64_t)a.m + 255) / 256, pn = ((uint64_t)a.n + 255) / 256, tm = ((uint64_t)a.m + 127) / 128, tn = ((uint64_t)a.n + 127) / 128;
-  if (tm * tn > 0x7FFFFFFFull / 8) return FH_ERR_UNSUPPORTED;
-  if (a.m > 128) {
-    const uint64_t split = std::max<uint64_t>(1, std::min<uint64_t>({4, (uint64_t)sms / 2 / (pm * pn), steps / 2}));
-    a.tiles_m = (uint32_t)pm;
-    a.tiles_n = (uint32_t)pn;
-    a.split = (uint32_t)split;
-    const uint32_t clusters = (uint32_t)(split > 1 ? pm * pn : std::min<uint64_t>(pm * pn, (uint64_t)sms / 2));
-    if (dtype == kF32)
-      return format == kMxB32 ? launch_product_pair<kF32, kMxB32>(a, clusters, stream) : launch_product_pair<kF32, kMxB16>(a, clusters, stream);
-    return format == kMxB32 ? launch_product_pair<kBF16, kMxB32>(a, clusters, stream) : launch_product_pair<kBF16, kMxB16>(a, clusters, stream);
-  }
-  // parts of the common axis while that leaves room (two CTAs fit an SM while a tile has few rows of A), each of at least two stages
-  const uint64_t split = std::max<uint64_t>(1, std::min<uint64_t>({8, (uint64_t)sms * (a.m <= 32 ? 2 : 1) / (tm * tn), steps / 2}));
-  a.tiles_m = (uint32_t)tm;
-  a.tiles_n = (uint32_t)tn;
-  a.split = (uint32_t)split;
+int launch_mx_product(const MxProductArgs& a, int dtype, int format, cudaStream_t stream) {
+  if (((uint64_t)a.m + 127) / 128 * (((uint64_t)a.n + 127) / 128) > 0x7FFFFFFFull / 8) return FH_ERR_UNSUPPORTED;
   if (dtype == kF32)
     return format == kMxB32 ? launch_product_df<kF32, kMxB32>(a, stream) : launch_product_df<kF32, kMxB16>(a, stream);
   return format == kMxB32 ? launch_product_df<kBF16, kMxB32>(a, stream) : launch_product_df<kBF16, kMxB16>(a, stream);
