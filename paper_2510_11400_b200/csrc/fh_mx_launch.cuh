@@ -64,13 +64,13 @@ constexpr size_t kMxSmemLimit = 226 * 1024;  // dynamic shared memory a CTA may 
 void count_launch(int kernels = 1);
 
 // Launch of `grid` CTAs, in clusters of `cluster`, that may become resident as the previous kernel on the stream drains (its order
-// is kept by dep_wait()).  A kernel's limit of dynamic shared memory is raised once for each device.
+// is kept by dep_wait()).  A kernel that needs more than the usual 48 KB, with the little that it declares, gets it raised once for each device.
 template <auto Kernel, typename A>
 int launch_plain(uint32_t grid, int threads, size_t smem, int cluster, cudaStream_t stream, const A& a) {
   static std::atomic<uint64_t> raised{0};  // bit per device
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return FH_ERR_CUDA;
-  if (smem > 48 * 1024 && (dev > 63 || !(raised.load() >> dev & 1u))) {
+  if (smem > 40 * 1024 && (dev > 63 || !(raised.load() >> dev & 1u))) {
     if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMxSmemLimit) != cudaSuccess) {
       cudaGetLastError();
       return FH_ERR_CUDA;

@@ -60,7 +60,7 @@ __device__ __forceinline__ void store_vec(uint8_t* row, uint32_t i, uint32_t t, 
   }
 }
 // The same into the thread's own 16 bytes of shared memory, later: what a thread has asked for so it alone reads, so that no barrier
-// stands between.  `ok`: there is such a row.  (An element of bf16 is too small for such a copy: off the grid it is loaded when it is used.)
+// stands between.  (An element of bf16 is too small for such a copy: off the grid it is loaded when it is used.)
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
@@ -72,19 +72,18 @@ template <int N>
 __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+// (of a vector that begins ahead of the last column)
 template <int DT, int TEAM, bool VEC, bool LINES>
-__device__ __forceinline__ void copy_vec(uint32_t dst, const uint8_t* row, uint32_t i, uint32_t t, uint32_t cols, bool ok) {
+__device__ __forceinline__ void copy_vec(uint32_t dst, const uint8_t* row, uint32_t i, uint32_t t, uint32_t cols) {
   constexpr int E = NormVec<DT>::kE;
   const uint32_t col = column<E, TEAM, LINES>(i, t, 0);
   if (VEC) {
-    const uint32_t n = ok && col < cols ? min((uint32_t)E, cols - col) : 0u;
-    copy16(dst, row + (n ? (uint64_t)col * (16 / E) : 0u), n * (16 / E));
+    copy16(dst, row + (uint64_t)col * (16 / E), min((uint32_t)E, cols - col) * (16 / E));
   } else if (DT == kF32) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const uint32_t c = column<E, TEAM, LINES>(i, t, e);
-      const bool there = ok && c < cols;
-      copy4(dst + 4 * e, row + (there ? (uint64_t)c * 4u : 0u), there);
+      copy4(dst + 4 * e, row + (c < cols ? (uint64_t)c * 4u : 0u), c < cols);
     }
   }
 }
@@ -118,6 +117,37 @@ __device__ __forceinline__ uint4 pack(const float (&f)[E]) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// The same as pairs for the two-wide instructions.
+template <int DT, int H>
+__device__ __forceinline__ void unpack(const uint4& v, f32x2 (&f)[H]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+    f[h] = DT == kF32 ? pack2(bits_f(w[2 * h % 4]), bits_f(w[(2 * h + 1) % 4])) : pack2(bits_f(w[h % 4] << 16), bits_f(w[h % 4] & 0xFFFF0000u));
+}
+template <int DT, int H>
+__device__ __forceinline__ uint4 pack(const f32x2 (&f)[H]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    float a, b;
+    unpack2(f[h], a, b);
+    if (DT == kF32) {
+      w[2 * h % 4] = __float_as_uint(a);
+      w[(2 * h + 1) % 4] = __float_as_uint(b);
+    } else {
+      w[h % 4] = f32x2_to_bf16x2(a, b);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ f32x2 both(float v) { return pack2(v, v); }
+__device__ __forceinline__ float halves(f32x2 v) {
+  float a, b;
+  unpack2(v, a, b);
+  return a + b;
+}
+
 // The weights of vector i in fp32; `none` where there are none.
 template <int E, int TEAM, bool LINES>
 __device__ __forceinline__ void load_weights(const uint8_t* p, int wdt, uint32_t i, uint32_t t, uint32_t cols, float none, float (&f)[E]) {
@@ -222,120 +252,187 @@ __device__ __forceinline__ void store_codes(const NormArgs& a, const MxLayout& l
     store_codes_f<DT, kMxB16, E>(a, l, row, col, v, unscale);
 }
 
-// Forward.  y = (x - mean) * rstd * gamma + beta, mean and variance from the row as it is held on the chip (the squares of the
-// distances from the mean, not of the values), sums in fp32.  TEAM threads to a row, V vectors to a thread, each team with the weights
-// of its columns in registers and the next rows on their way into shared memory; V = 0: any number of vectors, each sweep reads the row
-// and the weights again.  What bounds it is memory, once enough rows are on their way: with weights read again for every row, element by
-// element, and nothing asked for ahead, 16384 x 4096 bf16 took 153 us.
+// Forward.  y = (x - mean) * rstd * gamma + beta, mean and variance from the row as it is held in registers (the squares of the
+// distances from the mean, not of the values), sums in fp32.  TEAM threads to a row, V vectors to a thread; a team takes rows in order, with
+// the weights of its columns in registers and the next rows on their way into shared memory.  What bounds it is memory; arithmetic is two
+// elements to an instruction for that (16384 x 4096 bf16: one element to an instruction 66 us, with the weights read again for every row 153).
 constexpr int kAhead = 4;  // rows of a team in shared memory
 
-template <int DT, int TEAM, int V, bool VEC>
+__device__ __forceinline__ void write_header(const NormArgs& a, const MxLayout& l) {
+  if (!a.packed || blockIdx.x != 0 || threadIdx.x >= 8) return;
+  uint4 v = make_uint4(0u, 0u, 0u, 0u);
+  if (threadIdx.x == 0) v = make_uint4(kMxMagic, 1u | l.format << 16, l.rows, l.cols);
+  if (threadIdx.x == 1) v = make_uint4((uint32_t)a.exponent, 0u, (uint32_t)l.total, (uint32_t)(l.total >> 32));
+  if (threadIdx.x == 2) v = make_uint4((uint32_t)a.tensor_id, (uint32_t)(a.tensor_id >> 32), 0u, 0u);
+  reinterpret_cast<uint4*>(a.packed)[threadIdx.x] = v;
+}
+
+// Codes of a vector of y as it is in its type, so that they are those that compressing y gives.
+template <int DT, int E>
+__device__ __forceinline__ void store_codes_of(const NormArgs& a, const MxLayout& l, uint32_t row, uint32_t col, const uint4& out, float unscale) {
+  float f[E];
+  unpack<DT, E>(out, f);
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (col + e >= a.cols) f[e] = 0.0f;
+  store_codes<DT, E>(a, l, row, col, f, unscale);
+}
+
+template <int DT, int TEAM, int V, bool VEC, bool LINES>
 __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormArgs a) {
-  constexpr int E = NormVec<DT>::kE, N = V ? V : 1;
-  constexpr bool kCopies = V && (VEC || DT == kF32);
+  constexpr int E = NormVec<DT>::kE, H = E / 2;
+  constexpr bool kCopies = VEC || DT == kF32;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float2 slots[kNormThreads / TEAM][4][TEAM / 32];
   const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
                  teams = gridDim.x * (kNormThreads / TEAM);
   const MxLayout l(a.rows, a.cols, a.format);
   const uint32_t rows = a.packed ? (a.rows + 127u) / 128u * 128u : a.rows;  // (the padding of a container belongs to it)
-  const uint32_t sweeps = V ? V : (a.cols + TEAM * E - 1u) / (TEAM * E);
+  const uint32_t begin = (uint32_t)((uint64_t)rows * team / teams), end = (uint32_t)((uint64_t)rows * (team + 1u) / teams);
   const float inv = __frcp_rn((float)a.cols), unscale = a.format == kMxB32 ? 1.0f : pow2_f(-a.exponent);
   const uint32_t ring = smem_u32(smem) + threadIdx.x * 16u;
   auto row_of = [&](uint32_t row) { return a.x + (uint64_t)row * a.ldx * (16 / E); };
+  auto column_of = [&](int i, int e) { return column<E, TEAM, LINES>(i, t, e); };
   dep_trigger();
   dep_wait();
-  if (a.packed && blockIdx.x == 0 && threadIdx.x < 8) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (threadIdx.x == 0) v = make_uint4(kMxMagic, 1u | l.format << 16, l.rows, l.cols);
-    if (threadIdx.x == 1) v = make_uint4((uint32_t)a.exponent, 0u, (uint32_t)l.total, (uint32_t)(l.total >> 32));
-    if (threadIdx.x == 2) v = make_uint4((uint32_t)a.tensor_id, (uint32_t)(a.tensor_id >> 32), 0u, 0u);
-    reinterpret_cast<uint4*>(a.packed)[threadIdx.x] = v;
-  }
-  auto ask = [&](uint64_t row, uint32_t slot) {
+  write_header(a, l);
+  auto ask = [&](uint32_t row, uint32_t slot) {
     if (kCopies) {
-      const bool ok = row < a.rows;
+      if (row < end && row < a.rows) {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        copy_vec<DT, TEAM, VEC, false>(ring + (slot * N + i) * (kNormThreads * 16u), ok ? row_of((uint32_t)row) : a.x, i, t, a.cols, ok);
+        for (int i = 0; i < V; ++i)
+          if (column_of(i, 0) < a.cols) copy_vec<DT, TEAM, VEC, LINES>(ring + (slot * V + i) * (kNormThreads * 16u), row_of(row), i, t, a.cols);
+      }
       copy_commit();
     }
   };
 #pragma unroll
-  for (int k = 0; k < kAhead - 1; ++k) ask((uint64_t)team + (uint64_t)k * teams, k);
-  float gamma[N][E], beta[N][E];
-  if (V) {
+  for (int k = 0; k < kAhead - 1; ++k) ask(begin + k, k);
+  f32x2 gamma[V][H], beta[V][H];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      load_weights<E, TEAM, false>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, gamma[i]);
-      load_weights<E, TEAM, false>(a.beta, a.wdtype, i, t, a.cols, 0.0f, beta[i]);
+  for (int i = 0; i < V; ++i) {
+    float g[E], b[E];
+    load_weights<E, TEAM, LINES>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, g);
+    load_weights<E, TEAM, LINES>(a.beta, a.wdtype, i, t, a.cols, 0.0f, b);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      gamma[i][h] = pack2(g[2 * h], g[2 * h + 1]);
+      beta[i][h] = pack2(b[2 * h], b[2 * h + 1]);
     }
   }
   uint32_t turn = 0, slot = 0;
-  for (uint32_t row = team; row < rows; row += teams, turn ^= 2u, slot = slot + 1u == kAhead ? 0u : slot + 1u) {
-    ask((uint64_t)row + (uint64_t)(kAhead - 1) * teams, slot ? slot - 1u : kAhead - 1u);
+  for (uint32_t row = begin; row < end; ++row, turn ^= 2u, slot = slot + 1u == kAhead ? 0u : slot + 1u) {
+    ask(row + kAhead - 1u, slot ? slot - 1u : kAhead - 1u);
     if (row >= a.rows) {
       const float zero[E] = {};
-      for (uint32_t i = 0; i < sweeps; ++i) store_codes<DT, E>(a, l, row, (i * TEAM + t) * E, zero, unscale);
+      for (uint32_t i = 0; i < (uint32_t)V; ++i) store_codes<DT, E>(a, l, row, (i * TEAM + t) * E, zero, unscale);
       continue;
     }
-    const uint8_t* x = row_of(row);
-    uint4 raw[N];
     if (kCopies) copy_wait<kAhead - 1>();
+    f32x2 x[V][H], sum = both(0.0f);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (V) raw[i] = kCopies ? ld_shared16(ring + (slot * N + i) * (kNormThreads * 16u)) : load_vec<DT, TEAM, VEC, false>(x, i, t, a.cols);
-    auto vec = [&](uint32_t i) { return V ? raw[i % N] : load_vec<DT, TEAM, VEC, false>(x, i, t, a.cols); };
-    float sum = 0.0f;
+    for (int i = 0; i < V; ++i) {
+      uint4 raw = make_uint4(0u, 0u, 0u, 0u);
+      if (column_of(i, 0) < a.cols)
+        raw = kCopies ? ld_shared16(ring + (slot * V + i) * (kNormThreads * 16u)) : load_vec<DT, TEAM, VEC, LINES>(row_of(row), i, t, a.cols);
+      unpack<DT, H>(raw, x[i]);
 #pragma unroll
-    for (uint32_t i = 0; i < sweeps; ++i) {
-      float f[E];
-      unpack<DT, E>(vec(i), f);
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum += f[e];
+      for (int h = 0; h < H; ++h) sum = add2(sum, x[i][h]);
     }
-    const float mean = team_sum<TEAM>(sum, 0.0f, slots[in_cta][turn]).x * inv;
-    float sq = 0.0f;
+    const float mean = team_sum<TEAM>(halves(sum), 0.0f, slots[in_cta][turn]).x * inv;
+    f32x2 sq = both(0.0f);
+    float rest = 0.0f;
 #pragma unroll
-    for (uint32_t i = 0; i < sweeps; ++i) {
-      float f[E];
-      unpack<DT, E>(vec(i), f);
+    for (int i = 0; i < V; ++i) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float d = (i * TEAM + t) * E + e < a.cols ? f[e] - mean : 0.0f;
-        sq = __fmaf_rn(d, d, sq);
+      for (int h = 0; h < H; ++h) x[i][h] = add2(x[i][h], both(-mean));
+      if (column_of(i, E - 1) < a.cols) {
+#pragma unroll
+        for (int h = 0; h < H; ++h) sq = fma2(x[i][h], x[i][h], sq);
+      } else if (column_of(i, 0) < a.cols) {  // part of the vector is behind the last column
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          float p, q;
+          unpack2(x[i][h], p, q);
+          if (column_of(i, 2 * h) < a.cols) rest = __fmaf_rn(p, p, rest);
+          if (column_of(i, 2 * h + 1) < a.cols) rest = __fmaf_rn(q, q, rest);
+        }
       }
     }
-    const float rstd = __frsqrt_rn(team_sum<TEAM>(sq, 0.0f, slots[in_cta][turn + 1]).x * inv + a.eps);
+    const float rstd = __frsqrt_rn(team_sum<TEAM>(halves(sq) + rest, 0.0f, slots[in_cta][turn + 1]).x * inv + a.eps);
     if (t == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
     uint8_t* y = a.y ? a.y + (uint64_t)row * a.ldy * (16 / E) : nullptr;
 #pragma unroll
-    for (uint32_t i = 0; i < sweeps; ++i) {
-      const uint32_t col = (i * TEAM + t) * E;
-      float f[E], g[E], b[E];
-      unpack<DT, E>(vec(i), f);
-      if (!V) {
-        load_weights<E, TEAM, false>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, g);
-        load_weights<E, TEAM, false>(a.beta, a.wdtype, i, t, a.cols, 0.0f, b);
-      }
+    for (int i = 0; i < V; ++i) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) f[e] = __fmaf_rn((f[e] - mean) * rstd, V ? gamma[i % N][e] : g[e], V ? beta[i % N][e] : b[e]);
-      const uint4 out = pack<DT, E>(f);
-      if (y && col < a.cols) store_vec<DT, TEAM, VEC, false>(y, i, t, a.cols, out);
-      if (a.packed) {
-        // codes of what y is in its type, so that they are those that compressing y gives
-        unpack<DT, E>(out, f);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (col + e >= a.cols) f[e] = 0.0f;
-        store_codes<DT, E>(a, l, row, col, f, unscale);
-      }
+      for (int h = 0; h < H; ++h) x[i][h] = fma2(mul2(x[i][h], both(rstd)), gamma[i][h], beta[i][h]);
+      const uint4 out = pack<DT, H>(x[i]);
+      if (y && column_of(i, 0) < a.cols) store_vec<DT, TEAM, VEC, LINES>(y, i, t, a.cols, out);
+      if (!LINES && a.packed) store_codes_of<DT, E>(a, l, row, (i * TEAM + t) * E, out, unscale);
     }
   }
   if (kCopies) copy_wait<0>();
+}
+
+// Rows of more vectors than that: each of the three sweeps reads the row again.
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kNormThreads) norm_forward_wide_kernel(const NormArgs a) {
+  constexpr int E = NormVec<DT>::kE, TEAM = kNormThreads;
+  __shared__ float2 slots[4][TEAM / 32];
+  const uint32_t t = threadIdx.x;
+  const MxLayout l(a.rows, a.cols, a.format);
+  const uint32_t rows = a.packed ? (a.rows + 127u) / 128u * 128u : a.rows, sweeps = (a.cols + TEAM * E - 1u) / (TEAM * E);
+  const float inv = __frcp_rn((float)a.cols), unscale = a.format == kMxB32 ? 1.0f : pow2_f(-a.exponent);
+  dep_trigger();
+  dep_wait();
+  write_header(a, l);
+  uint32_t turn = 0;
+  for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 2u) {
+    if (row >= a.rows) {
+      const float zero[E] = {};
+      for (uint32_t i = 0; i < sweeps; ++i) store_codes<DT, E>(a, l, row, (i * TEAM + t) * E, zero, unscale);
+      continue;
+    }
+    const uint8_t* x = a.x + (uint64_t)row * a.ldx * (16 / E);
+    float sum = 0.0f, sq = 0.0f;
+    for (uint32_t i = 0; i < sweeps; ++i) {
+      float f[E];
+      unpack<DT, E>(load_vec<DT, TEAM, VEC, false>(x, i, t, a.cols), f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum += f[e];
+    }
+    const float mean = team_sum<TEAM>(sum, 0.0f, slots[turn]).x * inv;
+    for (uint32_t i = 0; i < sweeps; ++i) {
+      float f[E];
+      unpack<DT, E>(load_vec<DT, TEAM, VEC, false>(x, i, t, a.cols), f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float d = (i * TEAM + t) * E + e < a.cols ? f[e] - mean : 0.0f;
+        sq = __fmaf_rn(d, d, sq);
+      }
+    }
+    const float rstd = __frsqrt_rn(team_sum<TEAM>(sq, 0.0f, slots[turn + 1]).x * inv + a.eps);
+    if (t == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+    uint8_t* y = a.y ? a.y + (uint64_t)row * a.ldy * (16 / E) : nullptr;
+    for (uint32_t i = 0; i < sweeps; ++i) {
+      const uint32_t col = (i * TEAM + t) * E;
+      float f[E], g[E], b[E];
+      unpack<DT, E>(load_vec<DT, TEAM, VEC, false>(x, i, t, a.cols), f);
+      load_weights<E, TEAM, false>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, g);
+      load_weights<E, TEAM, false>(a.beta, a.wdtype, i, t, a.cols, 0.0f, b);
+#pragma unroll
+      for (int e = 0; e < E; ++e) f[e] = __fmaf_rn((f[e] - mean) * rstd, g[e], b[e]);
+      const uint4 out = pack<DT, E>(f);
+      if (y && col < a.cols) store_vec<DT, TEAM, VEC, false>(y, i, t, a.cols, out);
+      if (a.packed) store_codes_of<DT, E>(a, l, row, col, out, unscale);
+    }
+  }
 }
 
 // ---- backward -----------------------------------------------------------------------------------------
@@ -371,114 +468,219 @@ __device__ __forceinline__ void unpack_x(const uint4& v, uint32_t col, float sca
 #pragma unroll
   for (int e = 0; e < E; ++e) f[e] *= s;
 }
+// The kernels' starts and ends in common: the header of a container (false: another one), and the CTA's sums to the workspace.
+template <int X>
+__device__ __forceinline__ bool backward_begin(const NormArgs& a, const MxLayout& l, float* scale) {
+  int32_t exponent = 0;
+  const bool ok = X == 0 || mx_header_ok(a.x, a.x_bytes, l, &exponent);
+  if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = ok ? 0ull : status_word(kErrCorrupt);
+  *scale = ok && X == 1 + kMxB16 ? pow2_f(exponent) : 1.0f;
+  return ok;
+}
+__device__ __forceinline__ void sums_to_work(const NormArgs& a, const float* acc, uint32_t wide) {
+  float* out = a.work + (uint64_t)blockIdx.x * 2u * a.cols;
+  for (uint32_t c = threadIdx.x; c < a.cols; c += kNormThreads) {
+    out[c] = acc[c];
+    out[a.cols + c] = acc[wide + c];
+  }
+}
 
 template <int V, int X>
-struct BackRing {  // bytes of a slot: dy, x, and the row's mean and rstd
-  static constexpr uint32_t kX = kNormThreads * 16 * V, kStat = kX + kNormThreads * (X ? 8 : 16) * V, kSlot = kStat + kNormThreads * 8;
+struct BackRing {  // bytes of a slot: dy and x
+  static constexpr uint32_t kX = kNormThreads * 16 * V, kSlot = kX + kNormThreads * (X ? 8 : 16) * V;
   static constexpr int kRows = V < 4 ? 4 : 3;
 };
 
+// Rows of up to V vectors a thread.  Arithmetic is two elements to an instruction and nothing is computed twice; rows come through a ring in
+// shared memory, of which each thread asks for what it alone reads, and a team's rows follow one another, so that a container's 128-byte
+// pieces (eight rows) are found in L1 (16384 x 4096 bf16 from 4 bits: 146 us without the one and the other).
 template <int DT, int TEAM, int V, bool VEC, int X>
 __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_kernel(const NormArgs a) {
-  constexpr int E = NormVec<DT>::kE, N = V ? V : 1;
+  constexpr int E = NormVec<DT>::kE, H = E / 2;
   constexpr bool kLines = !VEC && X == 0;
-  constexpr bool kCopies = V && (VEC || DT == kF32);
-  using R = BackRing<N, X>;
+  constexpr bool kCopies = VEC || DT == kF32;
+  using R = BackRing<V, X>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float2 slots[kNormThreads / TEAM][2][TEAM / 32];
-  float* acc = reinterpret_cast<float*>(smem);  // V = 0: dgamma and dbeta of the CTA; otherwise room for the other teams' sums
   const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
                  teams = gridDim.x * (kNormThreads / TEAM);
+  const uint32_t begin = (uint32_t)((uint64_t)a.rows * team / teams), end = (uint32_t)((uint64_t)a.rows * (team + 1u) / teams);
   const MxLayout l(a.rows, a.cols, a.format);
-  const uint32_t sweeps = V ? V : (a.cols + TEAM * E - 1u) / (TEAM * E), wide = sweeps * TEAM * E;
   const float inv = __frcp_rn((float)a.cols);
   const uint32_t ring = smem_u32(smem);
+  auto column_of = [&](int i, int e) { return column<E, TEAM, kLines>(i, t, e); };
   dep_trigger();
   dep_wait();
-  int32_t exponent = 0;
-  if (X) {
-    const bool ok = mx_header_ok(a.x, a.x_bytes, l, &exponent);
-    if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = ok ? 0ull : status_word(kErrCorrupt);
-    if (!ok) return;
-  } else if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) {
-    *a.status = 0ull;
-  }
-  auto ask = [&](uint64_t r, uint32_t slot) {
+  float scale;
+  if (!backward_begin<X>(a, l, &scale)) return;
+  auto ask = [&](uint32_t row, uint32_t slot) {
     if (kCopies) {
-      const bool ok = r < a.rows;
-      const uint32_t row = ok ? (uint32_t)r : 0u, at = ring + slot * R::kSlot;
+      if (row < end) {
+        const uint32_t at = ring + slot * R::kSlot, block = row / 128u, rb16 = X ? l.block_rows(block) * 16u : 0u;
+        const uint8_t* dyr = a.dy + (uint64_t)row * a.ldy * (16 / E);
+        const uint8_t* xr = X ? a.x + l.code_at(row, 0) : a.x + (uint64_t)row * a.ldx * (16 / E);
+        const uint8_t* sr = X ? a.x + l.atom_at(block, 0) + MxLayout::scale_in_atom(row) : nullptr;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        copy_vec<DT, TEAM, VEC, kLines>(at + (i * kNormThreads + threadIdx.x) * 16u, a.dy + (uint64_t)row * a.ldy * (16 / E), i, t, a.cols, ok);
-        if (X == 0) {
-          copy_vec<DT, TEAM, VEC, kLines>(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u, a.x + (uint64_t)row * a.ldx * (16 / E), i, t, a.cols, ok);
-        } else {
-          const uint32_t col = column<E, TEAM, kLines>(i, t, 0), to = at + R::kX + (i * kNormThreads + threadIdx.x) * 8u;
-          const bool there = ok && col < a.cols;
-          copy4(to, there ? a.x + l.code_at(row, col / 32u) + col % 32u / 8u * 4u : a.x, there);
-          copy4(to + 4u, there ? a.x + l.atom_at(row / 128u, col / (X > 1 ? 64u : 128u)) + MxLayout::scale_in_atom(row) : a.x, there);
+        for (int i = 0; i < V; ++i) {
+          const uint32_t col = column_of(i, 0);
+          if (col < a.cols) {
+            copy_vec<DT, TEAM, VEC, kLines>(at + (i * kNormThreads + threadIdx.x) * 16u, dyr, i, t, a.cols);
+            if (X == 0) {
+              copy_vec<DT, TEAM, VEC, kLines>(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u, xr, i, t, a.cols);
+            } else {
+              const uint32_t to = at + R::kX + (i * kNormThreads + threadIdx.x) * 8u;
+              copy4(to, xr + (uint64_t)(col / 32u) * rb16 + col % 32u / 8u * 4u, true);
+              copy4(to + 4u, sr + (uint64_t)(col / (X > 1 ? 64u : 128u)) * 512u, true);
+            }
+          }
         }
       }
-      copy4(at + R::kStat + threadIdx.x * 8u, a.mean + row, ok);
-      copy4(at + R::kStat + threadIdx.x * 8u + 4u, a.rstd + row, ok);
       copy_commit();
     }
   };
 #pragma unroll
-  for (int k = 0; k < R::kRows - 1; ++k) ask((uint64_t)team + (uint64_t)k * teams, k);
-  const float scale = X == 1 + kMxB16 ? pow2_f(exponent) : 1.0f;
-  float dg[N][E] = {}, db[N][E] = {}, gamma[N][E];
-  if (V) {
+  for (int k = 0; k < R::kRows - 1; ++k) ask(begin + k, k);
+  f32x2 dg[V][H], db[V][H], gamma[V][H];
 #pragma unroll
-    for (int i = 0; i < N; ++i) load_weights<E, TEAM, kLines>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, gamma[i]);
-  } else {
-    for (uint32_t i = threadIdx.x; i < 2u * wide; i += kNormThreads) acc[i] = 0.0f;
-    __syncthreads();
-  }
-  uint32_t turn = 0, slot = 0;
-  for (uint32_t row = team; row < a.rows; row += teams, turn ^= 1u, slot = slot + 1u == R::kRows ? 0u : slot + 1u) {
-    ask((uint64_t)row + (uint64_t)(R::kRows - 1) * teams, slot ? slot - 1u : R::kRows - 1u);
-    const uint8_t* dyr = a.dy + (uint64_t)row * a.ldy * (16 / E);
-    const uint32_t at = ring + slot * R::kSlot;
-    float mean, rstd;
-    uint4 rx[N], ry[N];
-    if (kCopies) {
-      copy_wait<R::kRows - 1>();
-      const uint2 st = ld_shared8(at + R::kStat + threadIdx.x * 8u);
-      mean = bits_f(st.x);
-      rstd = bits_f(st.y);
-    } else {
-      mean = a.mean[row];
-      rstd = a.rstd[row];
+  for (int i = 0; i < V; ++i) {
+    float g[E];
+    load_weights<E, TEAM, kLines>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, g);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      gamma[i][h] = pack2(g[2 * h], g[2 * h + 1]);
+      dg[i][h] = db[i][h] = both(0.0f);
     }
+  }
+  float next_mean = begin < end ? a.mean[begin] : 0.0f, next_rstd = begin < end ? a.rstd[begin] : 0.0f;
+  uint32_t turn = 0, slot = 0;
+  for (uint32_t row = begin; row < end; ++row, turn ^= 1u, slot = slot + 1u == R::kRows ? 0u : slot + 1u) {
+    ask(row + R::kRows - 1u, slot ? slot - 1u : R::kRows - 1u);
+    const float mean = next_mean, rstd = next_rstd;
+    if (row + 1u < end) {
+      next_mean = a.mean[row + 1u];
+      next_rstd = a.rstd[row + 1u];
+    }
+    const uint32_t at = ring + slot * R::kSlot;
+    if (kCopies) copy_wait<R::kRows - 1>();
+    // xhat and g = dy * gamma; columns behind the last have dy = 0 and add nothing
+    f32x2 xh[V][H], g[V][H], s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (V && kCopies) {
-        ry[i] = ld_shared16(at + (i * kNormThreads + threadIdx.x) * 16u);
-        if (X == 0) {
-          rx[i] = ld_shared16(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u);
+    for (int i = 0; i < V; ++i) {
+      if (column_of(i, 0) < a.cols) {
+        uint4 ry, rx;
+        if (kCopies) {
+          ry = ld_shared16(at + (i * kNormThreads + threadIdx.x) * 16u);
+          if (X == 0) {
+            rx = ld_shared16(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u);
+          } else {
+            const uint2 w = ld_shared8(at + R::kX + (i * kNormThreads + threadIdx.x) * 8u);
+            rx = make_uint4(w.x, w.y, 0u, 0u);
+          }
         } else {
-          const uint2 w = ld_shared8(at + R::kX + (i * kNormThreads + threadIdx.x) * 8u);
-          rx[i] = make_uint4(w.x, w.y, 0u, 0u);
+          ry = load_vec<DT, TEAM, VEC, kLines>(a.dy + (uint64_t)row * a.ldy * (16 / E), i, t, a.cols);
+          rx = load_x<DT, TEAM, VEC, kLines, X>(a, l, row, i, t);
         }
-      } else if (V) {
-        ry[i] = load_vec<DT, TEAM, VEC, kLines>(dyr, i, t, a.cols);
-        rx[i] = load_x<DT, TEAM, VEC, kLines, X>(a, l, row, i, t);
+        f32x2 dy[H];
+        unpack<DT, H>(ry, dy);
+        if (X == 0) {
+          unpack<DT, H>(rx, xh[i]);
+        } else {
+          float f[E];
+          unpack_x<DT, X, E>(rx, column_of(i, 0), scale, f);
+#pragma unroll
+          for (int h = 0; h < H; ++h) xh[i][h] = pack2(f[2 * h], f[2 * h + 1]);
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          xh[i][h] = mul2(add2(xh[i][h], both(-mean)), both(rstd));
+          g[i][h] = mul2(dy[h], gamma[i][h]);
+          s1 = add2(s1, g[i][h]);
+          s2 = fma2(g[i][h], xh[i][h], s2);
+          dg[i][h] = fma2(dy[h], xh[i][h], dg[i][h]);
+          db[i][h] = add2(db[i][h], dy[h]);
+        }
       }
-    // xhat, dy and g = dy * gamma of vector i (zeros behind the last column, as dy is zero there)
+    }
+    if (!a.dx) continue;
+    const float2 m = team_sum<TEAM>(halves(s1), halves(s2), slots[in_cta][turn]);
+    const f32x2 m1 = both(-(m.x * inv)), m2 = both(-(m.y * inv));
+    uint8_t* dxr = a.dx + (uint64_t)row * a.ldx * (16 / E);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (column_of(i, 0) < a.cols) {
+#pragma unroll
+        for (int h = 0; h < H; ++h) g[i][h] = mul2(fma2(xh[i][h], m2, add2(g[i][h], m1)), both(rstd));
+        store_vec<DT, TEAM, VEC, kLines>(dxr, i, t, a.cols, pack<DT, H>(g[i]));
+      }
+    }
+  }
+  if (kCopies) copy_wait<0>();
+  if (!a.work) return;
+  float* acc = reinterpret_cast<float*>(smem);
+  float* out = a.work + (uint64_t)blockIdx.x * 2u * a.cols;
+  constexpr uint32_t wide = V * TEAM * E;
+  for (uint32_t w = 0; w < (uint32_t)(kNormThreads / TEAM); ++w) {  // the CTA's teams one after the other
+    if (TEAM < kNormThreads) __syncthreads();                       // (the first one: nobody reads its rows any more)
+    if (in_cta == w) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          float p[2], q[2];
+          unpack2(dg[i][h], p[0], p[1]);
+          unpack2(db[i][h], q[0], q[1]);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t c = column_of(i, 2 * h + k);
+            if (TEAM < kNormThreads) {
+              acc[c] = w ? acc[c] + p[k] : p[k];
+              acc[wide + c] = w ? acc[wide + c] + q[k] : q[k];
+            } else if (c < a.cols) {
+              out[c] = p[k];
+              out[a.cols + c] = q[k];
+            }
+          }
+        }
+    }
+  }
+  if (TEAM < kNormThreads) {
+    __syncthreads();
+    sums_to_work(a, acc, wide);
+  }
+}
+
+// Rows of more vectors than that: read twice, the sums of the columns in shared memory.
+template <int DT, bool VEC, int X>
+__global__ void __launch_bounds__(kNormThreads) norm_backward_wide_kernel(const NormArgs a) {
+  constexpr int E = NormVec<DT>::kE, TEAM = kNormThreads;
+  constexpr bool kLines = !VEC && X == 0;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float2 slots[2][TEAM / 32];
+  float* acc = reinterpret_cast<float*>(smem);
+  const uint32_t t = threadIdx.x, sweeps = (a.cols + TEAM * E - 1u) / (TEAM * E), wide = sweeps * TEAM * E;
+  const MxLayout l(a.rows, a.cols, a.format);
+  const float inv = __frcp_rn((float)a.cols);
+  dep_trigger();
+  dep_wait();
+  float scale;
+  if (!backward_begin<X>(a, l, &scale)) return;
+  for (uint32_t i = t; i < 2u * wide; i += kNormThreads) acc[i] = 0.0f;
+  __syncthreads();
+  uint32_t turn = 0;
+  for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1u) {
+    const uint8_t* dyr = a.dy + (uint64_t)row * a.ldy * (16 / E);
+    const float mean = a.mean[row], rstd = a.rstd[row];
     auto vec = [&](uint32_t i, float(&xh)[E], float(&dy)[E], float(&g)[E]) {
-      unpack<DT, E>(V ? ry[i % N] : load_vec<DT, TEAM, VEC, kLines>(dyr, i, t, a.cols), dy);
-      unpack_x<DT, X, E>(V ? rx[i % N] : load_x<DT, TEAM, VEC, kLines, X>(a, l, row, i, t), column<E, TEAM, kLines>(i, t, 0), scale, xh);
-      if (!V) load_weights<E, TEAM, kLines>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, g);
+      unpack<DT, E>(load_vec<DT, TEAM, VEC, kLines>(dyr, i, t, a.cols), dy);
+      unpack_x<DT, X, E>(load_x<DT, TEAM, VEC, kLines, X>(a, l, row, i, t), column<E, TEAM, kLines>(i, t, 0), scale, xh);
+      load_weights<E, TEAM, kLines>(a.gamma, a.wdtype, i, t, a.cols, 1.0f, g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         xh[e] = (xh[e] - mean) * rstd;
-        g[e] = dy[e] * (V ? gamma[i % N][e] : g[e]);
-        if (column<E, TEAM, kLines>(i, t, e) >= a.cols) xh[e] = 0.0f;  // (a NaN mean or rstd must not come back through 0 * NaN)
+        g[e] = dy[e] * g[e];
       }
     };
     float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
     for (uint32_t i = 0; i < sweeps; ++i) {
       float xh[E], dy[E], g[E];
       vec(i, xh, dy, g);
@@ -486,21 +688,15 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
       for (int e = 0; e < E; ++e) {
         s1 += g[e];
         s2 = __fmaf_rn(g[e], xh[e], s2);
-        if (V) {
-          dg[i % N][e] = __fmaf_rn(dy[e], xh[e], dg[i % N][e]);
-          db[i % N][e] += dy[e];
-        } else {  // (a team is the CTA; thread t alone has these columns)
-          const uint32_t c = column<E, TEAM, kLines>(i, t, e);
-          acc[c] = __fmaf_rn(dy[e], xh[e], acc[c]);
-          acc[wide + c] += dy[e];
-        }
+        const uint32_t c = column<E, TEAM, kLines>(i, t, e);  // (thread t alone has these columns)
+        acc[c] = __fmaf_rn(dy[e], xh[e], acc[c]);
+        acc[wide + c] += dy[e];
       }
     }
     if (!a.dx) continue;
-    const float2 m = team_sum<TEAM>(s1, s2, slots[in_cta][turn]);
+    const float2 m = team_sum<TEAM>(s1, s2, slots[turn]);
     const float m1 = m.x * inv, m2 = m.y * inv;
     uint8_t* dxr = a.dx + (uint64_t)row * a.ldx * (16 / E);
-#pragma unroll
     for (uint32_t i = 0; i < sweeps; ++i) {
       float xh[E], dy[E], g[E];
       vec(i, xh, dy, g);
@@ -509,42 +705,9 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
       if (column<E, TEAM, kLines>(i, t, 0) < a.cols) store_vec<DT, TEAM, VEC, kLines>(dxr, i, t, a.cols, pack<DT, E>(g));
     }
   }
-  if (kCopies) copy_wait<0>();
   if (!a.work) return;
-  float* out = a.work + (uint64_t)blockIdx.x * 2u * a.cols;
-  if (V && TEAM < kNormThreads) {  // the CTA's teams one after the other
-    for (uint32_t w = 0; w < (uint32_t)(kNormThreads / TEAM); ++w) {
-      __syncthreads();  // (the first one: nobody reads its rows any more)
-      if (in_cta == w) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const uint32_t c = column<E, TEAM, kLines>(i, t, e);
-            acc[c] = w ? acc[c] + dg[i][e] : dg[i][e];
-            acc[wide + c] = w ? acc[wide + c] + db[i][e] : db[i][e];
-          }
-      }
-    }
-  }
-  if (V && TEAM == kNormThreads) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const uint32_t c = column<E, TEAM, kLines>(i, t, e);
-        if (c < a.cols) {
-          out[c] = dg[i][e];
-          out[a.cols + c] = db[i][e];
-        }
-      }
-  } else {
-    __syncthreads();
-    for (uint32_t c = threadIdx.x; c < a.cols; c += kNormThreads) {
-      out[c] = acc[c];
-      out[a.cols + c] = acc[wide + c];
-    }
-  }
+  __syncthreads();
+  sums_to_work(a, acc, wide);
 }
 
 // The CTAs' sums of 32 columns: eight warps take every eighth CTA, then the eight are added up.
@@ -556,8 +719,24 @@ __global__ void __launch_bounds__(kNormThreads) norm_columns_kernel(const NormAr
   int32_t exponent;
   if (a.x_bytes && !mx_header_ok(a.x, a.x_bytes, MxLayout(a.rows, a.cols, a.format), &exponent)) return;
   float s = 0.0f;
-  if (c < 2u * a.cols)
-    for (uint32_t i = warp; i < a.parts; i += kNormWarps) s += a.work[(uint64_t)i * 2u * a.cols + c];
+  if (c < 2u * a.cols) {
+    const float* p = a.work + c;
+    const uint64_t step = (uint64_t)kNormWarps * 2u * a.cols;
+    uint32_t i = warp;
+    p += (uint64_t)warp * 2u * a.cols;
+    for (; i + 7u * kNormWarps < a.parts; i += 8u * kNormWarps) {  // (eight asked for at once: one at a time took 15 us for 296 CTAs)
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k, p += step) v[k] = *p;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[k];
+    }
+    float v[7];
+#pragma unroll
+    for (int k = 0; k < 7; ++k, p += step) v[k] = i + k * kNormWarps < a.parts ? *p : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 7; ++k) s += v[k];
+  }
   part[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && c < 2u * a.cols) {
@@ -575,30 +754,29 @@ __global__ void __launch_bounds__(kNormThreads) norm_columns_kernel(const NormAr
   }
 }
 
-template <int DT, int TEAM, int V, bool VEC>
+template <int DT, int TEAM, int V, bool VEC, bool LINES>
 int launch_forward_t(const NormArgs& a, cudaStream_t stream) {
   const uint64_t rows = a.packed ? ((uint64_t)a.rows + 127) / 128 * 128 : a.rows;
   const uint32_t grid = (uint32_t)std::min<uint64_t>((rows * TEAM + kNormThreads - 1) / kNormThreads, (uint64_t)sm_count() * 4);
-  const size_t smem = V && (VEC || DT == kF32) ? (size_t)kAhead * V * kNormThreads * 16 : 0;
-  return launch_plain<norm_forward_kernel<DT, TEAM, V, VEC>>(grid, kNormThreads, smem, 1, stream, a);
+  constexpr size_t smem = VEC || DT == kF32 ? (size_t)kAhead * V * kNormThreads * 16 : 0;
+  return launch_plain<norm_forward_kernel<DT, TEAM, V, VEC, LINES>>(grid, kNormThreads, smem, 1, stream, a);
 }
-template <int DT, bool VEC>
+template <int DT, bool VEC, bool LINES>
 int launch_forward_dv(const NormArgs& a, cudaStream_t stream) {
   const uint32_t vecs = (a.cols + NormVec<DT>::kE - 1) / NormVec<DT>::kE;
-  if (vecs <= 32) return launch_forward_t<DT, 32, 1, VEC>(a, stream);
-  if (vecs <= 128) return launch_forward_t<DT, 128, 1, VEC>(a, stream);
-  if (vecs <= 256) return launch_forward_t<DT, 256, 1, VEC>(a, stream);
-  if (vecs <= 512) return launch_forward_t<DT, 256, 2, VEC>(a, stream);
-  if (vecs <= 1024) return launch_forward_t<DT, 256, 4, VEC>(a, stream);
-  return launch_forward_t<DT, 256, 0, VEC>(a, stream);
+  if (vecs <= 32) return launch_forward_t<DT, 32, 1, VEC, LINES>(a, stream);
+  if (vecs <= 128) return launch_forward_t<DT, 128, 1, VEC, LINES>(a, stream);
+  if (vecs <= 256) return launch_forward_t<DT, 256, 1, VEC, LINES>(a, stream);
+  if (vecs <= 512) return launch_forward_t<DT, 256, 2, VEC, LINES>(a, stream);
+  if (vecs <= 1024) return launch_forward_t<DT, 256, 4, VEC, LINES>(a, stream);
+  const uint64_t rows = a.packed ? ((uint64_t)a.rows + 127) / 128 * 128 : a.rows;
+  return launch_plain<norm_forward_wide_kernel<DT, VEC>>((uint32_t)std::min<uint64_t>(rows, (uint64_t)sm_count() * 8), kNormThreads, 0, 1, stream, a);
 }
 
 template <int DT, int TEAM, int V, bool VEC, int X>
 int launch_backward_t(const NormArgs& a, cudaStream_t stream) {
-  constexpr uint32_t E = NormVec<DT>::kE;
-  const uint32_t sweeps = V ? V : (a.cols + TEAM * E - 1u) / (TEAM * E);
-  constexpr size_t ring = V && (VEC || DT == kF32) ? (size_t)BackRing<V ? V : 1, X>::kRows * BackRing<V ? V : 1, X>::kSlot : 0;
-  const size_t sums = V == 0 || TEAM < kNormThreads ? (size_t)8 * sweeps * TEAM * E : 0;
+  using R = BackRing<V, X>;
+  constexpr size_t ring = VEC || DT == kF32 ? (size_t)R::kRows * R::kSlot : 0, sums = TEAM < kNormThreads ? (size_t)8 * V * TEAM * NormVec<DT>::kE : 0;
   return launch_plain<norm_backward_kernel<DT, TEAM, V, VEC, X>>(a.parts, kNormThreads, std::max(ring, sums), 1, stream, a);
 }
 template <int DT, bool VEC, int X>
@@ -609,7 +787,8 @@ int launch_backward_dx(const NormArgs& a, cudaStream_t stream) {
   if (vecs <= 256) return launch_backward_t<DT, 256, 1, VEC, X>(a, stream);
   if (vecs <= 512) return launch_backward_t<DT, 256, 2, VEC, X>(a, stream);
   if (vecs <= 1024) return launch_backward_t<DT, 256, 4, VEC, X>(a, stream);
-  return launch_backward_t<DT, 256, 0, VEC, X>(a, stream);
+  return launch_plain<norm_backward_wide_kernel<DT, VEC, X>>(a.parts, kNormThreads, (size_t)8 * ((vecs + 255u) / 256u) * 256u * NormVec<DT>::kE, 1, stream,
+                                                            a);
 }
 template <int DT>
 int launch_backward_d(const NormArgs& a, bool vec, cudaStream_t stream) {
@@ -633,8 +812,12 @@ int launch_norm_forward(const NormArgs& a, int dtype, cudaStream_t stream) {
   if (sm_count() < 1) return FH_ERR_CUDA;
   const uint64_t es = dtype == kF32 ? 4 : 2;
   const bool vec = aligned16(a.x) && aligned16(a.y) && a.ldx * es % 16 == 0 && (!a.y || a.ldy * es % 16 == 0);
-  if (dtype == kF32) return vec ? launch_forward_dv<kF32, true>(a, stream) : launch_forward_dv<kF32, false>(a, stream);
-  return vec ? launch_forward_dv<kBF16, true>(a, stream) : launch_forward_dv<kBF16, false>(a, stream);
+  const bool lines = !vec && !a.packed;  // (codes are made of neighbours)
+  if (dtype == kF32)
+    return vec ? launch_forward_dv<kF32, true, false>(a, stream)
+               : (lines ? launch_forward_dv<kF32, false, true>(a, stream) : launch_forward_dv<kF32, false, false>(a, stream));
+  return vec ? launch_forward_dv<kBF16, true, false>(a, stream)
+             : (lines ? launch_forward_dv<kBF16, false, true>(a, stream) : launch_forward_dv<kBF16, false, false>(a, stream));
 }
 
 int launch_norm_backward(const NormArgs& a0, int dtype, cudaStream_t stream) {
