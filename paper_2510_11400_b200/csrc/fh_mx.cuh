@@ -126,14 +126,17 @@ __device__ __forceinline__ float mx_quotient(float x, const MxScale& s) {
 
 // Random rounding: x between two neighbouring magnitudes L and L + step (times the scale) goes up when what it is beyond L is
 // more than (r + 1/2) / 2^16 of the step, r a uniform 16-bit integer; exact, as the left side is an fp32 number and the right
-// side has at most 17 + 4 bits.  Returns the magnitude with x's sign.
+// side has at most 17 + 4 bits.  Returns the magnitude with x's sign.  `draw`: bits of 1 + r / 2^16.
+// (The step comes from the exponent, L from an addition that rounds down at 2^23 steps: no conversions, which take a scheduler four
+// times as long.)
 template <int F>
-__device__ __forceinline__ float mx_random(float x, const MxScale& s, float unscale, uint32_t r) {
+__device__ __forceinline__ float mx_random(float x, const MxScale& s, float unscale, uint32_t draw) {
   const float u = fabsf(mx_quotient<F>(x, s));
-  const float step = u < 2.0f ? 0.5f : (u < 4.0f ? 1.0f : 2.0f), inv = u < 2.0f ? 2.0f : (u < 4.0f ? 1.0f : 0.5f);
-  const float low = floorf(u * inv) * step, part = ((float)r + 0.5f) * 1.52587890625e-5f * step;
+  const uint32_t step_bits = (max(__float_as_uint(u), 0x3F800000u) & 0x7F800000u) - 0x00800000u;
+  const float step = bits_f(step_bits), at = bits_f(step_bits + (23u << 23));
+  const float low = __fadd_rd(u, at) - at, part = (bits_f(draw) - 0.99999237060546875f) * step;
   const bool up = F == kMxB32 ? u - low > part : __fmaf_rn(-low, s.s, fabsf(x) * unscale) > part * s.s;
-  return copysignf(low + (up ? step : 0.0f), x);
+  return copysignf(up ? low + step : low, x);
 }
 
 // Eight values to codes, the first in the lowest bits: round to nearest, ties to even, beyond 6 is 6.
@@ -184,7 +187,7 @@ template <int F>
 __device__ __forceinline__ float mx_factor(uint32_t byte, float scale) {
   if (F == kMxB32) {
     // 2^(byte - 127): byte 0 is half the smallest normal number, byte 255 a NaN
-    return byte == 255u ? bits_f(0x7FC00000u) : (byte == 0u ? bits_f(0x00400000u) : bits_f(byte << 23));
+    return bits_f(byte == 255u ? 0x7FC00000u : max(byte << 23, 0x00400000u));
   }
   const float v = byte < 8u ? (float)byte * 0.001953125f : bits_f((byte + (120u << 3)) << 20);
   return (byte & 127u) == 127u ? bits_f(0x7FC00000u) : v * scale;

@@ -24,34 +24,49 @@ struct Elem<kBF16> {
 template <int DT>
 constexpr int kPitch = kTile * Elem<DT>::kBytes + 16;
 
-// Loads the tile at (r0, c0), zeros outside the matrix.  VEC: rows start on 16-byte boundaries.
+// Loads the tile at (r0, c0), zeros outside the matrix, and waits for it.  VEC: rows start on 16-byte boundaries.  Copies go straight to shared
+// memory, all of them under way at once; an element of bf16 is too small for one, so rows off the 16-byte grid come by way of registers.
 template <int DT, bool VEC>
 __device__ __forceinline__ void load_tile(uint8_t* tile, const uint8_t* src, uint64_t ld, uint32_t rows, uint32_t cols, uint32_t r0,
                                           uint32_t c0) {
   constexpr int ES = Elem<DT>::kBytes, VE = Elem<DT>::kVec, V = kTile / VE;  // V vectors a row
+  const uint32_t base = smem_u32(tile);
+  if (VEC) {
 #pragma unroll
-  for (int i = 0; i < kTile * V / kSaveThreads; ++i) {
-    const uint32_t at = threadIdx.x + i * kSaveThreads, r = at / V, c = at % V * VE;
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (r0 + r < rows) {
-      const uint8_t* p = src + ((uint64_t)(r0 + r) * ld + c0 + c) * ES;
-      if (VEC && c0 + c + VE <= cols) {
-        v = *reinterpret_cast<const uint4*>(p);
-      } else if (c0 + c < cols) {
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
+    for (int i = 0; i < kTile * V / kSaveThreads; ++i) {
+      const uint32_t at = threadIdx.x + i * kSaveThreads, r = at / V, c = at % V * VE;
+      const uint32_t n = r0 + r < rows && c0 + c < cols ? min((uint32_t)VE, cols - (c0 + c)) : 0u;
+      const uint8_t* p = src + (n ? ((uint64_t)(r0 + r) * ld + c0 + c) * ES : 0u);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(base + r * kPitch<DT> + c * ES), "l"(p), "r"(n * ES) : "memory");
+    }
+  } else if (DT == kF32) {
+#pragma unroll 8
+    for (int i = 0; i < kTile * kTile / kSaveThreads; ++i) {
+      const uint32_t at = threadIdx.x + i * kSaveThreads, r = at / kTile, c = at % kTile;
+      const bool there = r0 + r < rows && c0 + c < cols;
+      const uint8_t* p = src + (there ? ((uint64_t)(r0 + r) * ld + c0 + c) * ES : 0u);
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(base + r * kPitch<DT> + c * ES), "l"(p), "r"(there ? 4u : 0u) : "memory");
+    }
+  } else {
+    const uint16_t* s16 = reinterpret_cast<const uint16_t*>(src);
+#pragma unroll 1
+    for (int i = 0; i < kTile * kTile / 2 / kSaveThreads; i += 8) {
+      uint32_t w[8];
 #pragma unroll
-        for (int e = 0; e < VE; ++e)
-          if (c0 + c + e < cols) {
-            if (DT == kF32)
-              w[e] = *(reinterpret_cast<const uint32_t*>(p) + e);
-            else
-              w[e / 2] |= (uint32_t)*(reinterpret_cast<const uint16_t*>(p) + e) << (e % 2 * 16);
-          }
-        v = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t at = threadIdx.x + (i + k) * kSaveThreads, r = at / (kTile / 2), c = at % (kTile / 2) * 2;
+        const uint16_t* p = s16 + (uint64_t)(r0 + r) * ld + c0 + c;
+        const uint32_t lo = r0 + r < rows && c0 + c < cols ? p[0] : 0u, hi = r0 + r < rows && c0 + c + 1u < cols ? p[1] : 0u;
+        w[k] = lo | hi << 16;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t at = threadIdx.x + (i + k) * kSaveThreads, r = at / (kTile / 2), c = at % (kTile / 2) * 2;
+        *reinterpret_cast<uint32_t*>(tile + r * kPitch<DT> + c * ES) = w[k];
       }
     }
-    *reinterpret_cast<uint4*>(tile + r * kPitch<DT> + c * ES) = v;
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 struct MxKey {
@@ -70,7 +85,7 @@ __device__ __forceinline__ uint32_t encode_block(G get, uint32_t top, float unsc
       uint32_t w[4];
       philox4x32_10(col / 8u + i, row, key.id_lo, key.id_hi, key.seed_lo, key.seed_hi, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = mx_random<F>(get(8 * i + e), s, unscale, e % 2 ? w[e / 2] >> 16 : w[e / 2] & 0xFFFFu);
+      for (int e = 0; e < 8; ++e) v[e] = mx_random<F>(get(8 * i + e), s, unscale, 0x3F800000u | (e % 2 ? w[e / 2] >> 9 & 0x007FFF80u : w[e / 2] << 7 & 0x007FFF80u));
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = mx_quotient<F>(get(8 * i + e), s);

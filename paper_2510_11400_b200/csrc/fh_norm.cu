@@ -191,26 +191,43 @@ __device__ __forceinline__ void team_barrier() {
     asm volatile("bar.sync %0, %1;" ::"r"(1u + threadIdx.x / TEAM), "n"(TEAM) : "memory");
 }
 
-// Sums over the TEAM threads that share a row, in a fixed order, the same in every thread.  `slot`: TEAM / 32 pairs that the team uses for
+// Sum over the TEAM threads that share a row, in a fixed order, the same in every thread.  `slot`: TEAM / 32 values that the team uses for
 // nothing else until another of its barriers has passed.
 template <int TEAM>
-__device__ __forceinline__ float2 team_sum(float a, float b, float2* slot) {
+__device__ __forceinline__ float team_sum(float a, float* slot) {
 #pragma unroll
-  for (int d = 16; d; d /= 2) {
-    a += __shfl_xor_sync(0xFFFFFFFFu, a, d);
-    b += __shfl_xor_sync(0xFFFFFFFFu, b, d);
-  }
-  if (TEAM == 32) return make_float2(a, b);
-  if (threadIdx.x % 32 == 0) slot[threadIdx.x % TEAM / 32] = make_float2(a, b);
+  for (int d = 16; d; d /= 2) a += __shfl_xor_sync(0xFFFFFFFFu, a, d);
+  if (TEAM == 32) return a;
+  if (threadIdx.x % 32 == 0) slot[threadIdx.x % TEAM / 32] = a;
   team_barrier<TEAM>();
-  a = b = 0.0f;
+  a = 0.0f;
 #pragma unroll
-  for (int w = 0; w < TEAM / 32; ++w) {
-    const float2 v = slot[w];
-    a += v.x;
-    b += v.y;
+  for (int w = 0; w < TEAM / 32; w += 4) {
+    const float4 v = *reinterpret_cast<const float4*>(slot + w);
+    a += (v.x + v.y) + (v.z + v.w);
   }
-  return make_float2(a, b);
+  return a;
+}
+// Two sums at once: in the first step each half of the warp keeps one of the two and hands over the other, so that four more steps add up
+// both.  `slot`: two rows of TEAM / 32 values.
+template <int TEAM>
+__device__ __forceinline__ float2 team_sum2(float a, float b, float (*slot)[TEAM / 32]) {
+  const uint32_t lane = threadIdx.x % 32;
+  const float give = lane < 16u ? b : a;
+  float keep = (lane < 16u ? a : b) + __shfl_xor_sync(0xFFFFFFFFu, give, 16);
+#pragma unroll
+  for (int d = 8; d; d /= 2) keep += __shfl_xor_sync(0xFFFFFFFFu, keep, d);
+  if (TEAM == 32) return make_float2(__shfl_sync(0xFFFFFFFFu, keep, 0), __shfl_sync(0xFFFFFFFFu, keep, 16));
+  if (lane % 16u == 0u) slot[lane / 16u][threadIdx.x % TEAM / 32] = keep;
+  team_barrier<TEAM>();
+  float2 r = make_float2(0.0f, 0.0f);
+#pragma unroll
+  for (int w = 0; w < TEAM / 32; w += 4) {
+    const float4 u = *reinterpret_cast<const float4*>(&slot[0][w]), v = *reinterpret_cast<const float4*>(&slot[1][w]);
+    r.x += (u.x + u.y) + (u.z + u.w);
+    r.y += (v.x + v.y) + (v.z + v.w);
+  }
+  return r;
 }
 
 // ---- codes of a row of the output, E of its columns from `col` on in each lane (neighbouring lanes hold neighbouring columns)
@@ -283,7 +300,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
   constexpr int E = NormVec<DT>::kE, H = E / 2;
   constexpr bool kCopies = VEC || DT == kF32;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float2 slots[kNormThreads / TEAM][4][TEAM / 32];
+  __shared__ __align__(16) float slots[kNormThreads / TEAM][4][TEAM / 32];
   const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
                  teams = gridDim.x * (kNormThreads / TEAM);
   const MxLayout l(a.rows, a.cols, a.format);
@@ -339,7 +356,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
 #pragma unroll
       for (int h = 0; h < H; ++h) sum = add2(sum, x[i][h]);
     }
-    const float mean = team_sum<TEAM>(halves(sum), 0.0f, slots[in_cta][turn]).x * inv;
+    const float mean = team_sum<TEAM>(halves(sum), slots[in_cta][turn]) * inv;
     f32x2 sq = both(0.0f);
     float rest = 0.0f;
 #pragma unroll
@@ -359,7 +376,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
         }
       }
     }
-    const float rstd = __frsqrt_rn(team_sum<TEAM>(halves(sq) + rest, 0.0f, slots[in_cta][turn + 1]).x * inv + a.eps);
+    const float rstd = __frsqrt_rn(team_sum<TEAM>(halves(sq) + rest, slots[in_cta][turn + 1]) * inv + a.eps);
     if (t == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
@@ -381,7 +398,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kNormThreads) norm_forward_wide_kernel(const NormArgs a) {
   constexpr int E = NormVec<DT>::kE, TEAM = kNormThreads;
-  __shared__ float2 slots[4][TEAM / 32];
+  __shared__ __align__(16) float slots[4][TEAM / 32];
   const uint32_t t = threadIdx.x;
   const MxLayout l(a.rows, a.cols, a.format);
   const uint32_t rows = a.packed ? (a.rows + 127u) / 128u * 128u : a.rows, sweeps = (a.cols + TEAM * E - 1u) / (TEAM * E);
@@ -404,7 +421,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_wide_kernel(const N
 #pragma unroll
       for (int e = 0; e < E; ++e) sum += f[e];
     }
-    const float mean = team_sum<TEAM>(sum, 0.0f, slots[turn]).x * inv;
+    const float mean = team_sum<TEAM>(sum, slots[turn]) * inv;
     for (uint32_t i = 0; i < sweeps; ++i) {
       float f[E];
       unpack<DT, E>(load_vec<DT, TEAM, VEC, false>(x, i, t, a.cols), f);
@@ -414,7 +431,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_wide_kernel(const N
         sq = __fmaf_rn(d, d, sq);
       }
     }
-    const float rstd = __frsqrt_rn(team_sum<TEAM>(sq, 0.0f, slots[turn + 1]).x * inv + a.eps);
+    const float rstd = __frsqrt_rn(team_sum<TEAM>(sq, slots[turn + 1]) * inv + a.eps);
     if (t == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
@@ -468,6 +485,18 @@ __device__ __forceinline__ void unpack_x(const uint4& v, uint32_t col, float sca
 #pragma unroll
   for (int e = 0; e < E; ++e) f[e] *= s;
 }
+// The same as pairs; `shift`: where the vector's scale is in its word (fixed for a thread).
+template <int X, int H>
+__device__ __forceinline__ void unpack_x2(uint32_t codes, uint32_t word, uint32_t shift, uint32_t col, float scale, f32x2 (&f)[H]) {
+  float v[2 * H];
+  if constexpr (H == 4)
+    mx_values8(codes, v);
+  else
+    mx_values4(codes >> (col % 8u * 4u), v);
+  const f32x2 s = both(mx_factor<(X > 1 ? kMxB16 : kMxB32)>(word >> shift & 255u, scale));
+#pragma unroll
+  for (int h = 0; h < H; ++h) f[h] = mul2(pack2(v[2 * h], v[2 * h + 1]), s);
+}
 // The kernels' starts and ends in common: the header of a container (false: another one), and the CTA's sums to the workspace.
 template <int X>
 __device__ __forceinline__ bool backward_begin(const NormArgs& a, const MxLayout& l, float* scale) {
@@ -501,7 +530,7 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
   constexpr bool kCopies = VEC || DT == kF32;
   using R = BackRing<V, X>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float2 slots[kNormThreads / TEAM][2][TEAM / 32];
+  __shared__ __align__(16) float slots[kNormThreads / TEAM][2][2][TEAM / 32];
   const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
                  teams = gridDim.x * (kNormThreads / TEAM);
   const uint32_t begin = (uint32_t)((uint64_t)a.rows * team / teams), end = (uint32_t)((uint64_t)a.rows * (team + 1u) / teams);
@@ -585,10 +614,8 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
         if (X == 0) {
           unpack<DT, H>(rx, xh[i]);
         } else {
-          float f[E];
-          unpack_x<DT, X, E>(rx, column_of(i, 0), scale, f);
-#pragma unroll
-          for (int h = 0; h < H; ++h) xh[i][h] = pack2(f[2 * h], f[2 * h + 1]);
+          const uint32_t col = column_of(i, 0);
+          unpack_x2<X, H>(rx.x, rx.y, col / (X > 1 ? 16u : 32u) % 4u * 8u, col, scale, xh[i]);
         }
 #pragma unroll
         for (int h = 0; h < H; ++h) {
@@ -602,7 +629,7 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
       }
     }
     if (!a.dx) continue;
-    const float2 m = team_sum<TEAM>(halves(s1), halves(s2), slots[in_cta][turn]);
+    const float2 m = team_sum2<TEAM>(halves(s1), halves(s2), slots[in_cta][turn]);
     const f32x2 m1 = both(-(m.x * inv)), m2 = both(-(m.y * inv));
     uint8_t* dxr = a.dx + (uint64_t)row * a.ldx * (16 / E);
 #pragma unroll
@@ -655,7 +682,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward_wide_kernel(const 
   constexpr int E = NormVec<DT>::kE, TEAM = kNormThreads;
   constexpr bool kLines = !VEC && X == 0;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float2 slots[2][TEAM / 32];
+  __shared__ __align__(16) float slots[2][2][TEAM / 32];
   float* acc = reinterpret_cast<float*>(smem);
   const uint32_t t = threadIdx.x, sweeps = (a.cols + TEAM * E - 1u) / (TEAM * E), wide = sweeps * TEAM * E;
   const MxLayout l(a.rows, a.cols, a.format);
@@ -694,7 +721,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward_wide_kernel(const 
       }
     }
     if (!a.dx) continue;
-    const float2 m = team_sum<TEAM>(s1, s2, slots[turn]);
+    const float2 m = team_sum2<TEAM>(s1, s2, slots[turn]);
     const float m1 = m.x * inv, m2 = m.y * inv;
     uint8_t* dxr = a.dx + (uint64_t)row * a.ldx * (16 / E);
     for (uint32_t i = 0; i < sweeps; ++i) {
@@ -764,10 +791,12 @@ int launch_forward_t(const NormArgs& a, cudaStream_t stream) {
 template <int DT, bool VEC, bool LINES>
 int launch_forward_dv(const NormArgs& a, cudaStream_t stream) {
   const uint32_t vecs = (a.cols + NormVec<DT>::kE - 1) / NormVec<DT>::kE;
+  // a row's two reductions cost a thread some 30 instructions each, so few threads to a row, as long as registers hold their columns' weights
   if (vecs <= 32) return launch_forward_t<DT, 32, 1, VEC, LINES>(a, stream);
-  if (vecs <= 128) return launch_forward_t<DT, 128, 1, VEC, LINES>(a, stream);
-  if (vecs <= 256) return launch_forward_t<DT, 256, 1, VEC, LINES>(a, stream);
-  if (vecs <= 512) return launch_forward_t<DT, 256, 2, VEC, LINES>(a, stream);
+  if (vecs <= 64) return launch_forward_t<DT, 32, 2, VEC, LINES>(a, stream);
+  if (vecs <= 128) return launch_forward_t<DT, 32, 4, VEC, LINES>(a, stream);
+  if (vecs <= 256) return launch_forward_t<DT, 128, 2, VEC, LINES>(a, stream);
+  if (vecs <= 512) return launch_forward_t<DT, 128, 4, VEC, LINES>(a, stream);
   if (vecs <= 1024) return launch_forward_t<DT, 256, 4, VEC, LINES>(a, stream);
   const uint64_t rows = a.packed ? ((uint64_t)a.rows + 127) / 128 * 128 : a.rows;
   return launch_plain<norm_forward_wide_kernel<DT, VEC>>((uint32_t)std::min<uint64_t>(rows, (uint64_t)sm_count() * 8), kNormThreads, 0, 1, stream, a);
