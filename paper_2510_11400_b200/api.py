@@ -321,17 +321,34 @@ def mx_bytes(rows: int, cols: int, format: int) -> int:
     return int(lib().fh_mx_bytes(rows, cols, format))
 
 
-def _ptr(t, elements: int = 0, esize: int = 1) -> Optional[int]:
-    """A tensor's address, once it is known to hold `elements` of `esize` bytes on the current device (the library takes
-    addresses and cannot see what they belong to)."""
+_torch = None
+
+
+def _device() -> int:
+    """The current device.  (Asked for without a lookup of the module: these calls are as short as what they enqueue.)"""
+    global _torch
+    if _torch is None:
+        import torch
+        torch.cuda.current_device()    # (initialises)
+        _torch = torch
+    return _torch._C._cuda_getDevice()
+
+
+def _ptr(t, dev: int, elements: int = 0, esize: int = 1) -> Optional[int]:
+    """A tensor's address, once it is known to hold `elements` of `esize` bytes on the device `dev` (the library takes addresses
+    and cannot see what they belong to)."""
     if t is None:
         return None
-    import torch
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"a tensor on {t.device}, where cuda:{torch.cuda.current_device()} is the current device")
-    if elements and (t.element_size() != esize or t.untyped_storage().nbytes() < (t.storage_offset() + elements) * esize):
+    if t.get_device() != dev:
+        raise ValueError(f"a tensor on {t.device}, where cuda:{dev} is the current device")
+    if elements and (t.element_size() != esize or not (t.numel() >= elements and t.is_contiguous()) and
+                     t.untyped_storage().nbytes() < (t.storage_offset() + elements) * esize):
         raise ValueError(f"a tensor of {t.dtype} and shape {tuple(t.shape)}, where {elements} elements of {esize} bytes are wanted")
     return t.data_ptr()
+
+
+def _on(stream, dev: int) -> int:
+    return _torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
 
 
 def _extent(m) -> int:
@@ -346,14 +363,16 @@ def _esize(dtype: int) -> int:
 def fh_mx_compress(m: fh_matrix, p: fh_mx_params, src, rows=None, cols=None, stream=None) -> int:
     """Enqueue compression of the matrix `src` (a CUDA tensor that `m` describes) into the uint8 CUDA tensors `rows` (blocks
     along its rows) and `cols` (the transpose, blocks along the columns); either may be None."""
-    return lib().fh_mx_compress(C.byref(m), C.byref(p), _ptr(src, _extent(m), _esize(m.dtype)), _ptr(rows), 0 if rows is None else rows.nbytes,
-                                _ptr(cols), 0 if cols is None else cols.nbytes, _stream_ptr(stream))
+    dev = _device()
+    return lib().fh_mx_compress(m, p, _ptr(src, dev, _extent(m), _esize(m.dtype)), _ptr(rows, dev), 0 if rows is None else rows.nbytes,
+                                _ptr(cols, dev), 0 if cols is None else cols.nbytes, _on(stream, dev))
 
 
 def fh_mx_decompress(src, m: fh_matrix, format: int, dst, status=None, stream=None) -> int:
     """Enqueue restoring the container `src` (uint8) into `dst`, which `m` describes."""
-    return lib().fh_mx_decompress(_ptr(src), src.nbytes, C.byref(m), format, _ptr(dst, _extent(m), _esize(m.dtype)),
-                                  _ptr(status), _stream_ptr(stream))
+    dev = _device()
+    return lib().fh_mx_decompress(_ptr(src, dev), src.nbytes, m, format, _ptr(dst, dev, _extent(m), _esize(m.dtype)), _ptr(status, dev),
+                                  _on(stream, dev))
 
 
 def mx_product_desc(m: int, n: int, k: int, format: int = FH_MX_B32, dtype: int = FH_F32, ldc: Optional[int] = None, alpha: float = 1.0,
@@ -363,8 +382,9 @@ def mx_product_desc(m: int, n: int, k: int, format: int = FH_MX_B32, dtype: int 
 
 def fh_mx_product(d: fh_mx_product_desc, a, b, c, status=None, stream=None) -> int:
     """Enqueue the product of the containers `a` (m x k) and `b` (n x k), uint8 CUDA tensors, into the matrix `c` (m x n)."""
-    return lib().fh_mx_product(C.byref(d), _ptr(a), a.nbytes, _ptr(b), b.nbytes,
-                               _ptr(c, max(0, (d.m - 1) * d.ldc + d.n), _esize(d.dtype)), _ptr(status), _stream_ptr(stream))
+    dev = _device()
+    return lib().fh_mx_product(d, _ptr(a, dev), a.nbytes, _ptr(b, dev), b.nbytes, _ptr(c, dev, max(0, (d.m - 1) * d.ldc + d.n), _esize(d.dtype)),
+                               _ptr(status, dev), _on(stream, dev))
 
 
 def norm_desc(rows: int, cols: int, dtype: int = FH_F32, wdtype: int = FH_F32, eps: float = 1e-5, ldx: Optional[int] = None,
@@ -382,9 +402,10 @@ def fh_layer_norm(d: fh_norm_desc, x, gamma, beta, y, mean=None, rstd=None, pack
     """Enqueue the layer norm of `x` into `y` (may be None) and, in 4 bits as `params` says, into the uint8 tensor `packed`; gamma, beta, mean
     and rstd may be None."""
     nx, ny, es, ws = _spans(d)
-    return lib().fh_layer_norm(C.byref(d), _ptr(x, nx, es), _ptr(gamma, d.cols, ws), _ptr(beta, d.cols, ws), _ptr(y, ny, es),
-                               _ptr(mean, d.rows, 4), _ptr(rstd, d.rows, 4), None if params is None else C.byref(params), _ptr(packed),
-                               0 if packed is None else packed.nbytes, _stream_ptr(stream))
+    dev = _device()
+    return lib().fh_layer_norm(d, _ptr(x, dev, nx, es), _ptr(gamma, dev, d.cols, ws), _ptr(beta, dev, d.cols, ws), _ptr(y, dev, ny, es),
+                               _ptr(mean, dev, d.rows, 4), _ptr(rstd, dev, d.rows, 4), params, _ptr(packed, dev),
+                               0 if packed is None else packed.nbytes, _on(stream, dev))
 
 
 def norm_work_bytes(d: fh_norm_desc) -> int:
@@ -396,11 +417,12 @@ def fh_layer_norm_backward(d: fh_norm_desc, dy, x, gamma, mean, rstd, dx, dgamma
     """Enqueue the layer norm's backward pass; `x` is dense, or with `packed` a container (uint8) of that format.  `work`: uint8, at
     least norm_work_bytes, where dgamma or dbeta is wanted."""
     nx, ny, es, ws = _spans(d)
-    return lib().fh_layer_norm_backward(C.byref(d), _ptr(dy, ny, es), _ptr(x, *((nx, es) if packed is None else ())),
-                                        0 if packed is None else x.nbytes, 0 if packed is None else packed, _ptr(gamma, d.cols, ws),
-                                        _ptr(mean, d.rows, 4), _ptr(rstd, d.rows, 4), _ptr(dx, nx, es), _ptr(dgamma, d.cols, ws),
-                                        _ptr(dbeta, d.cols, ws), _ptr(work), 0 if work is None else work.nbytes, _ptr(status),
-                                        _stream_ptr(stream))
+    dev = _device()
+    return lib().fh_layer_norm_backward(d, _ptr(dy, dev, ny, es), _ptr(x, dev, *((nx, es) if packed is None else ())),
+                                        0 if packed is None else x.nbytes, 0 if packed is None else packed, _ptr(gamma, dev, d.cols, ws),
+                                        _ptr(mean, dev, d.rows, 4), _ptr(rstd, dev, d.rows, 4), _ptr(dx, dev, nx, es), _ptr(dgamma, dev, d.cols, ws),
+                                        _ptr(dbeta, dev, d.cols, ws), _ptr(work, dev), 0 if work is None else work.nbytes, _ptr(status, dev),
+                                        _on(stream, dev))
 
 
 def debug_set(what: int, value: int) -> int:
