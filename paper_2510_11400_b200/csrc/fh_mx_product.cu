@@ -94,17 +94,26 @@ struct ProductScale {
   __device__ __forceinline__ float operator()(float v) const { return one ? v * alpha : v * f1 * f2 * alpha; }
 };
 
-// Sums a row of partial sums over the parts of a cluster (CTAs `stride` apart, from `first` on), NR rows at a time, in the order of the parts.
+// Sums rows of partial sums over the parts of a cluster (CTAs `stride` apart, from `first` on), NR rows at a time, in the order of the parts; four
+// parts are asked for at once.
 template <int NR>
 __device__ __forceinline__ void sum_parts(uint32_t at, uint32_t row_bytes, uint32_t first, uint32_t stride, uint32_t parts, float (&v)[NR]) {
 #pragma unroll
   for (int x = 0; x < NR; ++x) v[x] = 0.0f;
-  for (uint32_t r = 0; r < parts; ++r) {
-    float w[NR];
+  for (uint32_t r0 = 0; r0 < parts; r0 += 4u) {
+    float w[4][NR];
 #pragma unroll
-    for (int x = 0; x < NR; ++x) w[x] = ld_cluster(at + x * row_bytes, first + r * stride);
+    for (uint32_t r = 0; r < 4u; ++r)
+      if (r0 + r < parts) {
 #pragma unroll
-    for (int x = 0; x < NR; ++x) v[x] += w[x];
+        for (int x = 0; x < NR; ++x) w[r][x] = ld_cluster(at + x * row_bytes, first + (r0 + r) * stride);
+      }
+#pragma unroll
+    for (uint32_t r = 0; r < 4u; ++r)
+      if (r0 + r < parts) {
+#pragma unroll
+        for (int x = 0; x < NR; ++x) v[x] += w[r][x];
+      }
   }
 }
 
@@ -268,7 +277,10 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
 // A tile of 128 x 128 moves 34 KB from L2 to an SM for 256 cycles of matrix instructions; this one 36 KB for 512.  Pairs take
 // tiles one after the other; the eight warps for the result take the accumulator into registers at once, so that the next tile's matrix
 // instructions start while they write.  With a split, a cluster's pairs share one tile.
-constexpr int kPairThreads = 320;  // eight warps for the result, one for copies, one for matrix instructions
+//
+// Scales are copied to tensor memory by a thread of its own.  In the one that issues the matrix instructions the copies (55 cycles each, 6 a
+// stage in B32, 12 in B16) stood in line with those, which take 512: 4096 x 4096 x 16384 138 and 182 us, now 107 and 143.
+constexpr int kPairThreads = 352;  // eight warps for the result, then one each for loads, matrix instructions and scales
 
 template <int F>
 struct PairShape {
@@ -314,7 +326,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
   uint8_t* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);  // even CTA: both CTAs' stages have arrived
   uint64_t* empty = full + S::kStages;
-  uint64_t* sums = empty + S::kStages;  // the accumulator is complete
+  uint64_t* ready = empty + S::kStages;  // even CTA: its scales are in both CTAs' tensor memory
+  uint64_t* sums = ready + S::kStages;  // the accumulator is complete
   uint64_t* taken = sums + 1;           // even CTA: both CTAs' warps have taken it
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(taken + 1);
   volatile uint32_t* abort = tmem_at + 1;
@@ -326,6 +339,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(full + i, 1);
       mbar_init(empty + i, 1);
+      mbar_init(ready + i, 1);
     }
     mbar_init(sums, 1);
     mbar_init(taken, 16);
@@ -396,24 +410,16 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
         tc_fence_after();
         for (uint32_t it = first; it < last; ++it, turn.next()) {
           const uint32_t s = turn.stage, ph = turn.round;
-          if (!mbar_poll<true>(full + s, ph, kWaitPolls, abort)) {
+          if (!mbar_poll<true>(ready + s, ph, kWaitPolls, abort)) {
             *abort = 1u;
             good = false;
             break;
           }
           tc_fence_after();
           const uint32_t nc = min((uint32_t)kStepChunks, chunks - it * kStepChunks);
-          const uint32_t na = min((uint32_t)S::kAtoms, lp.atoms - it * S::kAtoms);
           const uint32_t st = smem_u32(smem) + s * S::kStage;
           const uint32_t sa = tmem + 256u + s * S::kScaleCols, sb = sa + S::kAtoms * 4u;
-          const uint64_t da = smem_desc(st, 2048u, 128u), db = smem_desc(st + S::kOp, 2048u, 128u), ds = smem_desc(st + 2u * S::kOp, 128u, 128u);
-#pragma unroll
-          for (uint32_t x = 0; x < (uint32_t)S::kAtoms; ++x)
-            if (x < na) {
-              tc_copy_scales_pair(sa + 4u * x, ds + 32u * x);
-              tc_copy_scales_pair(sb + 8u * x, ds + S::kS / 16u + 32u * x);
-              tc_copy_scales_pair(sb + 8u * x + 4u, ds + 2u * S::kS / 16u + 32u * x);
-            }
+          const uint64_t da = smem_desc(st, 2048u, 128u), db = smem_desc(st + S::kOp, 2048u, 128u);
 #pragma unroll
           for (uint32_t x = 0; x < kStepChunks / 2u; ++x)
             if (2u * x < nc) {
@@ -425,6 +431,32 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
         }
         tc_commit_pair(sums, both);
       }
+    }
+  } else if (warp == 10) {
+    if (lane == 0 && half == 0u) {
+      Turn<S::kStages> turn;
+      for (uint32_t tile = pair; tile < tiles && good; tile += pairs)
+        for (uint32_t it = first; it < last; ++it, turn.next()) {
+          const uint32_t s = turn.stage;
+          if (!mbar_poll<true>(full + s, turn.round, kWaitPolls, abort)) {
+            *abort = 1u;
+            good = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t na = min((uint32_t)S::kAtoms, lp.atoms - it * S::kAtoms);
+          const uint32_t st = smem_u32(smem) + s * S::kStage;
+          const uint32_t sa = tmem + 256u + s * S::kScaleCols, sb = sa + S::kAtoms * 4u;
+          const uint64_t ds = smem_desc(st + 2u * S::kOp, 128u, 128u);
+#pragma unroll
+          for (uint32_t x = 0; x < (uint32_t)S::kAtoms; ++x)
+            if (x < na) {
+              tc_copy_scales_pair(sa + 4u * x, ds + 32u * x);
+              tc_copy_scales_pair(sb + 8u * x, ds + S::kS / 16u + 32u * x);
+              tc_copy_scales_pair(sb + 8u * x + 4u, ds + 2u * S::kS / 16u + 32u * x);
+            }
+          tc_commit_pair(ready + s, (uint16_t)(1u << even));
+        }
     }
   } else {
     const ProductScale scaled(ea, eb, g.alpha);
