@@ -75,7 +75,10 @@ int fh_mx_compress(const fh_matrix* matrix, const fh_mx_params* params, const vo
   a.cols = (uint32_t)matrix->cols;
   a.ld = (uint64_t)matrix->ld;
   a.exponent = params->exponent;
-  a.seed = params->seed;
+  for (uint32_t r = 0; r < 10; ++r) {
+    a.round_keys[2 * r] = (uint32_t)params->seed + r * 0x9E3779B9u;
+    a.round_keys[2 * r + 1] = (uint32_t)(params->seed >> 32) + r * 0xBB67AE85u;
+  }
   a.tensor_id = params->tensor_id;
   return fh::launch_mx_save(a, matrix->dtype, params->format, true, params->rounding == 1, (cudaStream_t)stream);
 }

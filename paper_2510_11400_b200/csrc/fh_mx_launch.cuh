@@ -19,7 +19,8 @@ struct MxSaveArgs {
   uint32_t rows, cols;
   uint64_t ld;
   int32_t exponent;
-  uint64_t seed, tensor_id;
+  uint64_t tensor_id;
+  uint32_t round_keys[20];         // compress, random rounding: the keys of Philox's ten rounds
 };
 // (Enqueues on `stream`; returns an fh_status.)
 int launch_mx_save(const MxSaveArgs& a, int dtype, int format, bool compress, bool random, cudaStream_t stream);

@@ -51,31 +51,30 @@ struct ProductShape {
   static_assert(kStages * kStage >= (QT + 8) * 512, "partial sums, and rows read behind them");
 };
 
-// NR rows of a column of C from row `row` on, those below `end`.  What is added to is asked for all at once.  (Addresses step from row
-// to row: a product with ldc for each of them made a tile of 128 x 256 take 4 us.)
+// NR rows of a column of C from row `row` on, those below `end`.  (Addresses step from row to row: a product with ldc for each of them
+// made a tile of 128 x 256 take 4 us.)
+template <int DT>
+using CType = typename std::conditional<DT == kF32, float, __nv_bfloat16>::type;
 template <int DT, int NR>
-__device__ __forceinline__ void store_c(uint8_t* c, uint64_t ldc, uint32_t row, uint32_t end, uint32_t col, const float (&v)[NR], bool add) {
-  using T = typename std::conditional<DT == kF32, float, __nv_bfloat16>::type;
-  T* const p0 = reinterpret_cast<T*>(c) + (uint64_t)row * ldc + col;
-  if (!add && row + NR <= end) {
-    T* p = p0;
+__device__ __forceinline__ void load_c(const uint8_t* c, uint64_t ldc, uint32_t row, uint32_t end, uint32_t col, float (&v)[NR]) {
+  const CType<DT>* p = reinterpret_cast<const CType<DT>*>(c) + (uint64_t)row * ldc + col;
 #pragma unroll
-    for (int x = 0; x < NR; ++x, p += ldc) *p = (T)v[x];
+  for (int x = 0; x < NR; ++x, p += ldc) {
+    v[x] = 0.0f;
+    if (row + x < end) v[x] = (float)*p;
+  }
+}
+template <int DT, int NR>
+__device__ __forceinline__ void store_c(uint8_t* c, uint64_t ldc, uint32_t row, uint32_t end, uint32_t col, const float (&v)[NR]) {
+  CType<DT>* p = reinterpret_cast<CType<DT>*>(c) + (uint64_t)row * ldc + col;
+  if (row + NR <= end) {
+#pragma unroll
+    for (int x = 0; x < NR; ++x, p += ldc) *p = (CType<DT>)v[x];
     return;
   }
-  float old[NR];
-  if (add) {
-    const T* p = p0;
-#pragma unroll
-    for (int x = 0; x < NR; ++x, p += ldc) {
-      old[x] = 0.0f;
-      if (row + x < end) old[x] = (float)*p;
-    }
-  }
-  T* p = p0;
 #pragma unroll
   for (int x = 0; x < NR; ++x, p += ldc)
-    if (row + x < end) *p = (T)(add ? old[x] + v[x] : v[x]);
+    if (row + x < end) *p = (CType<DT>)v[x];
 }
 
 // What the sums are multiplied by: 2^(ea + eb) and alpha, as one factor where that is exact and no product of it leaves the range of normal
@@ -236,7 +235,15 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
         tc_load_wait();
 #pragma unroll
         for (uint32_t x = 0; x < 16u; ++x) f[x] = scaled(bits_f(v[x]));
-        if (col < g.n) store_c<DT, 16>(g.c, g.ldc, tq * 128u + q0, g.m, col, f, g.accumulate);
+        if (col < g.n) {
+          if (g.accumulate) {
+            float old[16];
+            load_c<DT, 16>(g.c, g.ldc, tq * 128u + q0, g.m, col, old);
+#pragma unroll
+            for (uint32_t x = 0; x < 16u; ++x) f[x] += old[x];
+          }
+          store_c<DT, 16>(g.c, g.ldc, tq * 128u + q0, g.m, col, f);
+        }
       }
     }
   } else {
@@ -258,11 +265,12 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
       const uint32_t rows = min((uint32_t)QT, g.m - tq * 128u), end = rows * (rank + 1u) / g.split;
       constexpr int NR = QT < 32 ? 2 : 8;
       for (uint32_t q = rows * rank / g.split; q < end; q += NR) {
-        float f[NR];
+        float f[NR], old[NR] = {};
+        if (g.accumulate) load_c<DT, NR>(g.c, g.ldc, tq * 128u + q, tq * 128u + end, col, old);
         sum_parts<NR>(smem_u32(part + q * 128u + tid), 512u, 0u, 1u, g.split, f);  // (rows behind the last: stage bytes)
 #pragma unroll
-        for (int x = 0; x < NR; ++x) f[x] = scaled(f[x]);
-        store_c<DT, NR>(g.c, g.ldc, tq * 128u + q, tq * 128u + end, col, f, g.accumulate);
+        for (int x = 0; x < NR; ++x) f[x] = g.accumulate ? old[x] + scaled(f[x]) : scaled(f[x]);
+        store_c<DT, NR>(g.c, g.ldc, tq * 128u + q, tq * 128u + end, col, f);
       }
     }
     cluster_sync();
@@ -481,7 +489,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
           float f[16];
 #pragma unroll
           for (uint32_t y = 0; y < 16u; ++y) f[y] = scaled(bits_f(v[x][y]));
-          if (col < g.n) store_c<DT, 16>(g.c, g.ldc, row + 16u * x, g.m, col, f, g.accumulate);
+          if (col < g.n) {
+            if (g.accumulate) {
+              float old[16];
+              load_c<DT, 16>(g.c, g.ldc, row + 16u * x, g.m, col, old);
+#pragma unroll
+              for (uint32_t y = 0; y < 16u; ++y) f[y] += old[y];
+            }
+            store_c<DT, 16>(g.c, g.ldc, row + 16u * x, g.m, col, f);
+          }
         }
       } else {  // (one tile only: all copies into shared memory have been used)
         float* part = reinterpret_cast<float*>(smem) + side * 128u + warp % 4u * 32u + lane;
@@ -504,11 +520,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
       const uint32_t stop = warp < 4u ? mid : end;
       if (col < g.n)
         for (uint32_t q = warp < 4u ? from : mid; q < stop; q += 8u) {
-          float f[8];
+          float f[8], old[8] = {};
+          if (g.accumulate) load_c<DT, 8>(g.c, g.ldc, row + q, row + stop, col, old);
           sum_parts<8>(smem_u32(reinterpret_cast<float*>(smem) + q * 128u + p), 512u, half, 2u, g.split, f);
 #pragma unroll
-          for (int x = 0; x < 8; ++x) f[x] = scaled(f[x]);
-          store_c<DT, 8>(g.c, g.ldc, row + q, row + stop, col, f, g.accumulate);
+          for (int x = 0; x < 8; ++x) f[x] = g.accumulate ? old[x] + scaled(f[x]) : scaled(f[x]);
+          store_c<DT, 8>(g.c, g.ldc, row + q, row + stop, col, f);
         }
     }
   }

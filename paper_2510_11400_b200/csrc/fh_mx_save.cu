@@ -69,23 +69,46 @@ __device__ __forceinline__ void load_tile(uint8_t* tile, const uint8_t* src, uin
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
+// Philox-4x32-10 with the ten rounds' keys made on the host (see philox4x32_10).
 struct MxKey {
-  uint32_t seed_lo, seed_hi, id_lo, id_hi;
+  const uint32_t* rounds;
+  uint32_t id_lo, id_hi;
+  __device__ __forceinline__ void draw(uint32_t c0, uint32_t c1, uint32_t (&out)[4]) const {
+    uint32_t c2 = id_lo, c3 = id_hi;
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+      const uint32_t h0 = __umulhi(0xD2511F53u, c0), l0 = 0xD2511F53u * c0, h1 = __umulhi(0xCD9E8D57u, c2), l1 = 0xCD9E8D57u * c2;
+      c0 = h1 ^ c1 ^ rounds[2 * r];
+      c1 = l1;
+      c2 = h0 ^ c3 ^ rounds[2 * r + 1];
+      c3 = l0;
+    }
+    out[0] = c0;
+    out[1] = c1;
+    out[2] = c2;
+    out[3] = c3;
+  }
 };
 
 // The block of NB elements get(0) ... get(NB - 1) of a matrix's row, from column `col` on, to NB / 8 words of codes; its scale byte.
+// `scale`: 2^exponent, `unscale` its inverse.
 template <int F, bool RANDOM, int NB, typename G>
-__device__ __forceinline__ uint32_t encode_block(G get, uint32_t top, float unscale, uint32_t row, uint32_t col, const MxKey& key,
+__device__ __forceinline__ uint32_t encode_block(G get, uint32_t top, float scale, float unscale, uint32_t row, uint32_t col, const MxKey& key,
                                                  uint32_t* codes) {
   const MxScale s = mx_scale<F>(top, unscale);
+  const float s_full = s.s * scale;
 #pragma unroll
   for (int i = 0; i < NB / 8; ++i) {
     float v[8];
     if (RANDOM) {
       uint32_t w[4];
-      philox4x32_10(col / 8u + i, row, key.id_lo, key.id_hi, key.seed_lo, key.seed_hi, w);
+      key.draw(col / 8u + i, row, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = mx_random<F>(get(8 * i + e), s, unscale, 0x3F800000u | (e % 2 ? w[e / 2] >> 9 & 0x007FFF80u : w[e / 2] << 7 & 0x007FFF80u));
+      for (int e = 0; e < 4; ++e) {
+        v[2 * e] = get(8 * i + 2 * e);
+        v[2 * e + 1] = get(8 * i + 2 * e + 1);
+        mx_random2<F>(v[2 * e], v[2 * e + 1], s, s_full, 0x3F800000u | (w[e] << 7 & 0x007FFF80u), 0x3F800000u | (w[e] >> 9 & 0x007FFF80u));
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = mx_quotient<F>(get(8 * i + e), s);
@@ -102,7 +125,7 @@ __device__ __forceinline__ float bf_hi(uint32_t w) { return bits_f(w & 0xFFFF000
 // row) and blocks along columns (a thread for 32 rows of a column, in bf16 of two columns), each written as 16 bytes next to its
 // neighbours'.
 template <int DT, int F, bool RANDOM, bool VEC>
-__global__ void __launch_bounds__(kSaveThreads) mx_compress_kernel(const MxSaveArgs a) {
+__global__ void __launch_bounds__(kSaveThreads) mx_compress_kernel(const __grid_constant__ MxSaveArgs a) {
   constexpr int ES = Elem<DT>::kBytes, NB = F == kMxB32 ? 32 : 16, NS = 32 / NB;  // NS scales to 32 elements
   extern __shared__ __align__(16) uint8_t smem[];
   uint8_t* tile = smem;
@@ -112,7 +135,8 @@ __global__ void __launch_bounds__(kSaveThreads) mx_compress_kernel(const MxSaveA
   const uint32_t tiles_c = (a.cols + kTile - 1u) / kTile, tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
   const uint32_t r0 = tr * kTile, c0 = tc * kTile;
   const float unscale = F == kMxB32 ? 1.0f : pow2_f(-a.exponent);
-  const MxKey key = {(uint32_t)a.seed, (uint32_t)(a.seed >> 32), (uint32_t)a.tensor_id, (uint32_t)(a.tensor_id >> 32)};
+  const float scale = F == kMxB32 ? 1.0f : pow2_f(a.exponent);
+  const MxKey key = {a.round_keys, (uint32_t)a.tensor_id, (uint32_t)(a.tensor_id >> 32)};
   dep_trigger();
   for (uint32_t i = tid; i < 128; i += kSaveThreads) reinterpret_cast<uint4*>(scales)[i] = make_uint4(0u, 0u, 0u, 0u);
   dep_wait();
@@ -150,12 +174,12 @@ __global__ void __launch_bounds__(kSaveThreads) mx_compress_kernel(const MxSaveA
         if (DT == kF32) {
 #pragma unroll
           for (int i = 0; i < W; ++i) top = max(top, w[i] & 0x7FFFFFFFu);
-          byte = encode_block<F, RANDOM, NB>([&](int i) { return bits_f(w[i]); }, top, unscale, row, col + h * NB, key, codes + h * (NB / 8));
+          byte = encode_block<F, RANDOM, NB>([&](int i) { return bits_f(w[i]); }, top, scale, unscale, row, col + h * NB, key, codes + h * (NB / 8));
         } else {
 #pragma unroll
           for (int i = 0; i < W; ++i) top = __vmaxu2(top, w[i] & 0x7FFF7FFFu);
           top = max(top << 16, top & 0xFFFF0000u);
-          byte = encode_block<F, RANDOM, NB>([&](int i) { return i % 2 ? bf_hi(w[i / 2]) : bf_lo(w[i / 2]); }, top, unscale, row,
+          byte = encode_block<F, RANDOM, NB>([&](int i) { return i % 2 ? bf_hi(w[i / 2]) : bf_lo(w[i / 2]); }, top, scale, unscale, row,
                                              col + h * NB, key, codes + h * (NB / 8));
         }
         if (row < a.rows && col + h * NB < a.cols)
@@ -183,10 +207,10 @@ __global__ void __launch_bounds__(kSaveThreads) mx_compress_kernel(const MxSaveA
         for (int q = 0; q < CW; ++q) {
           uint32_t byte;
           if (DT == kF32)
-            byte = encode_block<F, RANDOM, NB>([&](int i) { return bits_f(w[i]); }, top, unscale, row, col + h * NB, key, codes[q] + h * (NB / 8));
+            byte = encode_block<F, RANDOM, NB>([&](int i) { return bits_f(w[i]); }, top, scale, unscale, row, col + h * NB, key, codes[q] + h * (NB / 8));
           else
             byte = encode_block<F, RANDOM, NB>([&](int i) { return q ? bf_hi(w[i]) : bf_lo(w[i]); }, q ? top & 0xFFFF0000u : top << 16,
-                                               unscale, row + q, col + h * NB, key, codes[q] + h * (NB / 8));
+                                               scale, unscale, row + q, col + h * NB, key, codes[q] + h * (NB / 8));
           if (row + q < a.cols && col + h * NB < a.rows)
             scales[1024 + (j * NS + h) / 4 * 512 + MxLayout::scale_in_atom(c + q) + (j * NS + h) % 4] = (uint8_t)byte;
         }
