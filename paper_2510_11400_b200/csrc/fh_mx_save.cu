@@ -144,10 +144,10 @@ __global__ void __launch_bounds__(kSaveThreads) mx_compress_kernel(const __grid_
   if (blockIdx.x == 0 && tid < 16) {
     const bool col = tid >= 8;
     uint8_t* dst = col ? a.by_cols : a.by_rows;
-    const MxLayout& l = col ? lc : lr;
+    const uint64_t total = col ? lc.total : lr.total;
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (tid % 8 == 0) v = make_uint4(kMxMagic, 1u | (uint32_t)F << 16 | (uint32_t)RANDOM << 24, l.rows, l.cols);
-    if (tid % 8 == 1) v = make_uint4((uint32_t)a.exponent, 0u, (uint32_t)l.total, (uint32_t)(l.total >> 32));
+    if (tid % 8 == 0) v = make_uint4(kMxMagic, 1u | (uint32_t)F << 16 | (uint32_t)RANDOM << 24, col ? a.cols : a.rows, col ? a.rows : a.cols);
+    if (tid % 8 == 1) v = make_uint4((uint32_t)a.exponent, 0u, (uint32_t)total, (uint32_t)(total >> 32));
     if (tid % 8 == 2) v = make_uint4(key.id_lo, key.id_hi, 0u, 0u);
     if (dst) reinterpret_cast<uint4*>(dst)[tid % 8] = v;
   }
@@ -225,10 +225,9 @@ __global__ void __launch_bounds__(kSaveThreads) mx_compress_kernel(const __grid_
     constexpr uint32_t A = F == kMxB32 ? 1 : 2;  // groups of scales to a tile
     const bool col = tid >= 64;
     const uint32_t atom = tid % 64 / 32, at = col ? tr * A + atom : tc * A + atom;
-    const MxLayout& l = col ? lc : lr;
     uint8_t* dst = col ? a.by_cols : a.by_rows;
-    if (dst && atom < A && at < l.atoms)
-      *reinterpret_cast<uint4*>(dst + l.atom_at(col ? tc : tr, at) + tid % 32 * 16) = reinterpret_cast<const uint4*>(scales)[tid];
+    if (dst && atom < A && at < (col ? lc.atoms : lr.atoms))
+      *reinterpret_cast<uint4*>(dst + (col ? lc.atom_at(tc, at) : lr.atom_at(tr, at)) + tid % 32 * 16) = reinterpret_cast<const uint4*>(scales)[tid];
   }
 }
 

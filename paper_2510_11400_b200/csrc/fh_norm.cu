@@ -92,9 +92,9 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t at) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ uint2 ld_shared8(uint32_t at) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+__device__ __forceinline__ uint32_t ld_shared4(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
   return v;
 }
 template <int DT, int E>
@@ -208,26 +208,42 @@ __device__ __forceinline__ float team_sum(float a, float* slot) {
   }
   return a;
 }
-// Two sums at once: in the first step each half of the warp keeps one of the two and hands over the other, so that four more steps add up
-// both.  `slot`: two rows of TEAM / 32 values.
-template <int TEAM>
-__device__ __forceinline__ float2 team_sum2(float a, float b, float (*slot)[TEAM / 32]) {
+// NV sums at once (2, 4 or 8): in each of the first steps a lane keeps half of the values it has and hands over the others, so that NV sums
+// take NV - 1 exchanges and the steps that are left.  `slot`: NV rows of TEAM / 32 values.
+template <int TEAM, int NV>
+__device__ __forceinline__ void team_sums(float (&v)[NV], float (*slot)[TEAM / 32]) {
   const uint32_t lane = threadIdx.x % 32;
-  const float give = lane < 16u ? b : a;
-  float keep = (lane < 16u ? a : b) + __shfl_xor_sync(0xFFFFFFFFu, give, 16);
+  uint32_t which = 0;
+  int d = 16;
 #pragma unroll
-  for (int d = 8; d; d /= 2) keep += __shfl_xor_sync(0xFFFFFFFFu, keep, d);
-  if (TEAM == 32) return make_float2(__shfl_sync(0xFFFFFFFFu, keep, 0), __shfl_sync(0xFFFFFFFFu, keep, 16));
-  if (lane % 16u == 0u) slot[lane / 16u][threadIdx.x % TEAM / 32] = keep;
-  team_barrier<TEAM>();
-  float2 r = make_float2(0.0f, 0.0f);
+  for (int n = NV / 2; n; n /= 2, d /= 2) {
+    const bool upper = lane & d;
+    which += upper ? n : 0;
 #pragma unroll
-  for (int w = 0; w < TEAM / 32; w += 4) {
-    const float4 u = *reinterpret_cast<const float4*>(&slot[0][w]), v = *reinterpret_cast<const float4*>(&slot[1][w]);
-    r.x += (u.x + u.y) + (u.z + u.w);
-    r.y += (v.x + v.y) + (v.z + v.w);
+    for (int j = 0; j < n; ++j) {
+      const float give = upper ? v[j] : v[j + n];
+      v[j] = (upper ? v[j + n] : v[j]) + __shfl_xor_sync(0xFFFFFFFFu, give, d);
+    }
   }
-  return r;
+#pragma unroll
+  for (; d; d /= 2) v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], d);
+  if (TEAM == 32) {
+    const float mine = v[0];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) v[j] = __shfl_sync(0xFFFFFFFFu, mine, j * (32 / NV));
+    return;
+  }
+  if (lane % (32u / NV) == 0u) slot[which][threadIdx.x % TEAM / 32] = v[0];
+  team_barrier<TEAM>();
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    v[j] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < TEAM / 32; w += 4) {
+      const float4 u = *reinterpret_cast<const float4*>(&slot[j][w]);
+      v[j] += (u.x + u.y) + (u.z + u.w);
+    }
+  }
 }
 
 // ---- codes of a row of the output, E of its columns from `col` on in each lane (neighbouring lanes hold neighbouring columns)
@@ -515,14 +531,20 @@ __device__ __forceinline__ void sums_to_work(const NormArgs& a, const float* acc
 }
 
 template <int V, int X>
-struct BackRing {  // bytes of a slot: dy and x
-  static constexpr uint32_t kX = kNormThreads * 16 * V, kSlot = kX + kNormThreads * (X ? 8 : 16) * V;
-  static constexpr int kRows = V < 4 ? 4 : 3;
+struct BackRing {
+  static constexpr int kGroup = X ? 4 : (V < 4 ? 2 : 1);         // rows worked on together ...
+  static constexpr int kRows = X || V < 4 ? 2 * kGroup : 3;      // ... and in shared memory
+  static constexpr uint32_t kX = kNormThreads * 16 * V, kSlot = X ? kX : 2 * kX;   // bytes of a slot: dy, and a dense x
+  static constexpr uint32_t kWarpX = 512 + 64;                   // of a vector of a warp, four rows: codes, scales
+  static constexpr uint32_t kPacked = kRows * kSlot, kGroupX = V * kNormWarps * kWarpX;
+  static constexpr size_t kBytes = kPacked + (X ? 2 * kGroupX : 0);
 };
 
-// Rows of up to V vectors a thread.  Arithmetic is two elements to an instruction and nothing is computed twice; rows come through a ring in
-// shared memory, of which each thread asks for what it alone reads, and a team's rows follow one another, so that a container's 128-byte
-// pieces (eight rows) are found in L1 (16384 x 4096 bf16 from 4 bits: 146 us without the one and the other).
+// Rows of up to V vectors a thread, a group of them at a time: their sums first, with one reduction and one barrier for all, then, from shared
+// memory again, dx.  Rows come through a ring there, of which each thread asks for what it alone reads; a team's rows follow one another,
+// so that a container's 128-byte pieces (eight rows) are found in L1.  Of a container a warp asks for 16 bytes a lane, four rows of eight
+// chunks, and each lane reads its words of them.  Arithmetic is two elements to an instruction.
+// (16384 x 4096 bf16 from 4 bits: each lane asking for its own words 105 us; element by element 138.)
 template <int DT, int TEAM, int V, bool VEC, int X>
 __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_kernel(const NormArgs a) {
   constexpr int E = NormVec<DT>::kE, H = E / 2;
@@ -530,7 +552,7 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
   constexpr bool kCopies = VEC || DT == kF32;
   using R = BackRing<V, X>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ __align__(16) float slots[kNormThreads / TEAM][2][2][TEAM / 32];
+  __shared__ __align__(16) float slots[kNormThreads / TEAM][2][2 * R::kGroup][TEAM / 32];
   const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
                  teams = gridDim.x * (kNormThreads / TEAM);
   const uint32_t begin = (uint32_t)((uint64_t)a.rows * team / teams), end = (uint32_t)((uint64_t)a.rows * (team + 1u) / teams);
@@ -545,30 +567,41 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
   auto ask = [&](uint32_t row, uint32_t slot) {
     if (kCopies) {
       if (row < end) {
-        const uint32_t at = ring + slot * R::kSlot, block = row / 128u, rb16 = X ? l.block_rows(block) * 16u : 0u;
+        const uint32_t at = ring + slot * R::kSlot;
         const uint8_t* dyr = a.dy + (uint64_t)row * a.ldy * (16 / E);
-        const uint8_t* xr = X ? a.x + l.code_at(row, 0) : a.x + (uint64_t)row * a.ldx * (16 / E);
-        const uint8_t* sr = X ? a.x + l.atom_at(block, 0) + MxLayout::scale_in_atom(row) : nullptr;
+        const uint8_t* xr = a.x + (uint64_t)row * a.ldx * (16 / E);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const uint32_t col = column_of(i, 0);
           if (col < a.cols) {
             copy_vec<DT, TEAM, VEC, kLines>(at + (i * kNormThreads + threadIdx.x) * 16u, dyr, i, t, a.cols);
-            if (X == 0) {
-              copy_vec<DT, TEAM, VEC, kLines>(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u, xr, i, t, a.cols);
-            } else {
-              const uint32_t to = at + R::kX + (i * kNormThreads + threadIdx.x) * 8u;
-              copy4(to, xr + (uint64_t)(col / 32u) * rb16 + col % 32u / 8u * 4u, true);
-              copy4(to + 4u, sr + (uint64_t)(col / (X > 1 ? 64u : 128u)) * 512u, true);
-            }
+            if (X == 0) copy_vec<DT, TEAM, VEC, kLines>(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u, xr, i, t, a.cols);
           }
         }
       }
       copy_commit();
     }
   };
+  constexpr int G = R::kGroup, kAsked = R::kRows - G;  // rows asked for ahead of a group
+  // four rows of a container, vector i of the warp: lane 4 c + k asks for chunk c of row k
+  constexpr uint32_t kAtomCols = X > 1 ? 64u : 128u, kWords = 32u * E / kAtomCols;  // columns to a word of scales, words to a warp's vector
+  const uint32_t lane = threadIdx.x % 32u, warp_x = ring + R::kPacked + threadIdx.x / 32u * R::kWarpX;
+  auto x_at = [&](int i, uint32_t half) { return warp_x + half * R::kGroupX + i * (kNormWarps * R::kWarpX); };
+  auto ask_x = [&](uint32_t row, uint32_t half) {
+    if (X && kCopies) {
 #pragma unroll
-  for (int k = 0; k < R::kRows - 1; ++k) ask(begin + k, k);
+      for (int i = 0; i < V; ++i) {
+        const uint32_t col0 = (i * TEAM + (t - lane)) * E, k = lane % 4u, c = lane / 4u, chunk = col0 / 32u + c;
+        if (c < (uint32_t)E && row + k < end && chunk * 32u < a.cols) copy16(x_at(i, half) + k * (16u * E) + c * 16u, a.x + l.code_at(row + k, chunk), 16u);
+        const uint32_t ks = lane / kWords, word = lane % kWords, atom = col0 / kAtomCols + word;
+        if (ks < 4u && row + ks < end && atom < l.atoms)
+          copy4(x_at(i, half) + 512u + (4u * ks + word) * 4u, a.x + l.atom_at((row + ks) / 128u, atom) + MxLayout::scale_in_atom(row + ks), true);
+      }
+    }
+  };
+  ask_x(begin, 0u);
+#pragma unroll
+  for (int k = 0; k < kAsked; ++k) ask(begin + k, k);
   f32x2 dg[V][H], db[V][H], gamma[V][H];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -580,66 +613,107 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
       dg[i][h] = db[i][h] = both(0.0f);
     }
   }
-  float next_mean = begin < end ? a.mean[begin] : 0.0f, next_rstd = begin < end ? a.rstd[begin] : 0.0f;
+  float next_mean[G], next_rstd[G];
+  auto ask_stats = [&](uint32_t row) {
+#pragma unroll
+    for (int k = 0; k < G; ++k)
+      if (row + k < end) {
+        next_mean[k] = a.mean[row + k];
+        next_rstd[k] = a.rstd[row + k];
+      }
+  };
+  ask_stats(begin);
+  // dy, xhat and g = dy * gamma of vector i of a row (one that begins ahead of the last column; columns behind it have dy = 0 and add nothing)
+  auto vec = [&](int i, uint32_t row, uint32_t slot, uint32_t k, uint32_t half, float mean, float rstd, f32x2(&dy)[H], f32x2(&xh)[H], f32x2(&g)[H]) {
+    const uint32_t at = ring + slot * R::kSlot, col = column_of(i, 0);
+    uint4 ry, rx;
+    if (kCopies) {
+      ry = ld_shared16(at + (i * kNormThreads + threadIdx.x) * 16u);
+      if (X == 0) {
+        rx = ld_shared16(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u);
+      } else {
+        rx.x = ld_shared4(x_at(i, half) + k * (16u * E) + lane * E / 8u * 4u);
+        rx.y = ld_shared4(x_at(i, half) + 512u + (4u * k + lane * E / kAtomCols) * 4u);
+      }
+    } else {
+      ry = load_vec<DT, TEAM, VEC, kLines>(a.dy + (uint64_t)row * a.ldy * (16 / E), i, t, a.cols);
+      rx = load_x<DT, TEAM, VEC, kLines, X>(a, l, row, i, t);
+    }
+    unpack<DT, H>(ry, dy);
+    if (X == 0)
+      unpack<DT, H>(rx, xh);
+    else
+      unpack_x2<X, H>(rx.x, rx.y, col / (X > 1 ? 16u : 32u) % 4u * 8u, col, scale, xh);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      xh[h] = mul2(add2(xh[h], both(-mean)), both(rstd));
+      g[h] = mul2(dy[h], gamma[i][h]);
+    }
+  };
   uint32_t turn = 0, slot = 0;
-  for (uint32_t row = begin; row < end; ++row, turn ^= 1u, slot = slot + 1u == R::kRows ? 0u : slot + 1u) {
-    ask(row + R::kRows - 1u, slot ? slot - 1u : R::kRows - 1u);
-    const float mean = next_mean, rstd = next_rstd;
-    if (row + 1u < end) {
-      next_mean = a.mean[row + 1u];
-      next_rstd = a.rstd[row + 1u];
+  for (uint32_t row = begin; row < end; row += G, turn ^= 1u) {
+    uint32_t ahead = slot + kAsked;
+    if (X) {
+      __syncwarp();  // (nobody of the warp reads the group before any more)
+      ask_x(row + G, turn ^ 1u);
     }
-    const uint32_t at = ring + slot * R::kSlot;
-    if (kCopies) copy_wait<R::kRows - 1>();
-    // xhat and g = dy * gamma; columns behind the last have dy = 0 and add nothing
-    f32x2 xh[V][H], g[V][H], s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (column_of(i, 0) < a.cols) {
-        uint4 ry, rx;
-        if (kCopies) {
-          ry = ld_shared16(at + (i * kNormThreads + threadIdx.x) * 16u);
-          if (X == 0) {
-            rx = ld_shared16(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u);
-          } else {
-            const uint2 w = ld_shared8(at + R::kX + (i * kNormThreads + threadIdx.x) * 8u);
-            rx = make_uint4(w.x, w.y, 0u, 0u);
+    for (int k = 0; k < G; ++k) {
+      if (ahead >= (uint32_t)R::kRows) ahead -= R::kRows;
+      ask(row + kAsked + k, ahead++);
+    }
+    float mean[G], rstd[G], s[2 * G];
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+      mean[k] = next_mean[k];
+      rstd[k] = next_rstd[k];
+    }
+    ask_stats(row + G);
+    if (kCopies) copy_wait<kAsked>();
+    if (X) __syncwarp();  // (what the other lanes have asked for)
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+      f32x2 s1 = both(0.0f), s2 = both(0.0f);
+      if (row + k < end) {
+        const uint32_t here = slot + k < (uint32_t)R::kRows ? slot + k : slot + k - R::kRows;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (column_of(i, 0) < a.cols) {
+            f32x2 dy[H], xh[H], g[H];
+            vec(i, row + k, here, (uint32_t)k, turn, mean[k], rstd[k], dy, xh, g);
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+              s1 = add2(s1, g[h]);
+              s2 = fma2(g[h], xh[h], s2);
+              dg[i][h] = fma2(dy[h], xh[h], dg[i][h]);
+              db[i][h] = add2(db[i][h], dy[h]);
+            }
           }
-        } else {
-          ry = load_vec<DT, TEAM, VEC, kLines>(a.dy + (uint64_t)row * a.ldy * (16 / E), i, t, a.cols);
-          rx = load_x<DT, TEAM, VEC, kLines, X>(a, l, row, i, t);
-        }
-        f32x2 dy[H];
-        unpack<DT, H>(ry, dy);
-        if (X == 0) {
-          unpack<DT, H>(rx, xh[i]);
-        } else {
-          const uint32_t col = column_of(i, 0);
-          unpack_x2<X, H>(rx.x, rx.y, col / (X > 1 ? 16u : 32u) % 4u * 8u, col, scale, xh[i]);
-        }
-#pragma unroll
-        for (int h = 0; h < H; ++h) {
-          xh[i][h] = mul2(add2(xh[i][h], both(-mean)), both(rstd));
-          g[i][h] = mul2(dy[h], gamma[i][h]);
-          s1 = add2(s1, g[i][h]);
-          s2 = fma2(g[i][h], xh[i][h], s2);
-          dg[i][h] = fma2(dy[h], xh[i][h], dg[i][h]);
-          db[i][h] = add2(db[i][h], dy[h]);
-        }
       }
+      s[2 * k] = halves(s1);
+      s[2 * k + 1] = halves(s2);
     }
-    if (!a.dx) continue;
-    const float2 m = team_sum2<TEAM>(halves(s1), halves(s2), slots[in_cta][turn]);
-    const f32x2 m1 = both(-(m.x * inv)), m2 = both(-(m.y * inv));
-    uint8_t* dxr = a.dx + (uint64_t)row * a.ldx * (16 / E);
+    if (a.dx) {
+      team_sums<TEAM, 2 * G>(s, slots[in_cta][turn]);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (column_of(i, 0) < a.cols) {
+      for (int k = 0; k < G; ++k)
+        if (row + k < end) {
+          const uint32_t here = slot + k < (uint32_t)R::kRows ? slot + k : slot + k - R::kRows;
+          const f32x2 m1 = both(-(s[2 * k] * inv)), m2 = both(-(s[2 * k + 1] * inv));
+          uint8_t* dxr = a.dx + (uint64_t)(row + k) * a.ldx * (16 / E);
 #pragma unroll
-        for (int h = 0; h < H; ++h) g[i][h] = mul2(fma2(xh[i][h], m2, add2(g[i][h], m1)), both(rstd));
-        store_vec<DT, TEAM, VEC, kLines>(dxr, i, t, a.cols, pack<DT, H>(g[i]));
-      }
+          for (int i = 0; i < V; ++i)
+            if (column_of(i, 0) < a.cols) {
+              f32x2 dy[H], xh[H], g[H];
+              vec(i, row + k, here, (uint32_t)k, turn, mean[k], rstd[k], dy, xh, g);
+#pragma unroll
+              for (int h = 0; h < H; ++h) g[h] = mul2(fma2(xh[h], m2, add2(g[h], m1)), both(rstd[k]));
+              store_vec<DT, TEAM, VEC, kLines>(dxr, i, t, a.cols, pack<DT, H>(g));
+            }
+        }
     }
+    slot += G;
+    if (slot >= (uint32_t)R::kRows) slot -= R::kRows;
   }
   if (kCopies) copy_wait<0>();
   if (!a.work) return;
@@ -721,8 +795,9 @@ __global__ void __launch_bounds__(kNormThreads) norm_backward_wide_kernel(const 
       }
     }
     if (!a.dx) continue;
-    const float2 m = team_sum2<TEAM>(s1, s2, slots[turn]);
-    const float m1 = m.x * inv, m2 = m.y * inv;
+    float m[2] = {s1, s2};
+    team_sums<TEAM, 2>(m, slots[turn]);
+    const float m1 = m[0] * inv, m2 = m[1] * inv;
     uint8_t* dxr = a.dx + (uint64_t)row * a.ldx * (16 / E);
     for (uint32_t i = 0; i < sweeps; ++i) {
       float xh[E], dy[E], g[E];
@@ -804,8 +879,7 @@ int launch_forward_dv(const NormArgs& a, cudaStream_t stream) {
 
 template <int DT, int TEAM, int V, bool VEC, int X>
 int launch_backward_t(const NormArgs& a, cudaStream_t stream) {
-  using R = BackRing<V, X>;
-  constexpr size_t ring = VEC || DT == kF32 ? (size_t)R::kRows * R::kSlot : 0, sums = TEAM < kNormThreads ? (size_t)8 * V * TEAM * NormVec<DT>::kE : 0;
+  constexpr size_t ring = VEC || DT == kF32 ? BackRing<V, X>::kBytes : 0, sums = TEAM < kNormThreads ? (size_t)8 * V * TEAM * NormVec<DT>::kE : 0;
   return launch_plain<norm_backward_kernel<DT, TEAM, V, VEC, X>>(a.parts, kNormThreads, std::max(ring, sums), 1, stream, a);
 }
 template <int DT, bool VEC, int X>
