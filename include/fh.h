@@ -392,7 +392,7 @@ size_t fh_mx_bytes(int32_t rows, int32_t cols, int32_t format);
  *   d_cols   container of its transpose (blocks along its columns), cols_capacity bytes; may be NULL, but not both.  It is the container
  *            that compressing the transposed matrix gives, draws included.
  * A matrix product needs its operands' blocks along the axis it sums over; forward and backward pass sum over different ones.
- * FH_ERR_CAPACITY when a container has less than fh_mx_bytes.  Input and containers must not overlap.
+ * FH_ERR_CAPACITY when a container has less than fh_mx_bytes, FH_ERR_ARG when input and containers overlap.
  */
 int fh_mx_compress(const fh_matrix* matrix, const fh_mx_params* params, const void* d_src, void* d_rows, size_t rows_capacity,
                    void* d_cols, size_t cols_capacity, void* stream);
@@ -412,7 +412,7 @@ int fh_mx_decompress(const void* d_src, size_t src_bytes, const fh_matrix* expec
  * A = x by rows, B = W by rows; the input's gradient A = dy by rows, B = W by columns; the weight's gradient A = dy by columns, B = x by
  * columns.  Where the blocks along k of a row of A or B hold a NaN scale, that row (column) of C is NaN.
  *   d_a, d_b    containers of an m x k and an n x k matrix; another header is FH_ERR_CORRUPT (through d_status; C is not written then)
- *   d_c         element (i, j) at i * ldc + j; must not overlap the containers
+ *   d_c         element (i, j) at i * ldc + j; FH_ERR_ARG when it overlaps a container
  *   d_status    optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
  * Results do not depend on the call's place among others: equal inputs give equal bits.
  */

@@ -341,6 +341,8 @@ def _ptr(t, dev: int, elements: int = 0, esize: int = 1) -> Optional[int]:
         return None
     if t.get_device() != dev:
         raise ValueError(f"a tensor on {t.device}, where cuda:{dev} is the current device")
+    if not elements and not t.is_contiguous():
+        raise ValueError("a buffer that is not contiguous")
     if elements and (t.element_size() != esize or not (t.numel() >= elements and t.is_contiguous()) and
                      t.untyped_storage().nbytes() < (t.storage_offset() + elements) * esize):
         raise ValueError(f"a tensor of {t.dtype} and shape {tuple(t.shape)}, where {elements} elements of {esize} bytes are wanted")

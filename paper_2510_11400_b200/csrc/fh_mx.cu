@@ -22,6 +22,14 @@ int check_matrix(const fh_matrix* m) {
   return FH_OK;
 }
 
+// Whether two pieces of memory have a byte in common (a null pointer has none).
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && x < y + b_bytes && y < x + a_bytes;
+}
+// Bytes from the first to the last of a matrix.
+size_t extent(int64_t rows, int64_t cols, int64_t ld, int dtype) { return ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * esize_of(dtype); }
+
 int check_mx(const fh_mx_params* p) {
   if (!p || !is_format(p->format) || p->reserved != 0) return FH_ERR_ARG;
   if (p->rounding != 0 && p->rounding != 1) return FH_ERR_UNSUPPORTED;
@@ -67,6 +75,9 @@ int fh_mx_compress(const fh_matrix* matrix, const fh_mx_params* params, const vo
     return FH_ERR_ARG;
   if (d_rows && rows_capacity < fh_mx_bytes(matrix->rows, matrix->cols, params->format)) return FH_ERR_CAPACITY;
   if (d_cols && cols_capacity < fh_mx_bytes(matrix->cols, matrix->rows, params->format)) return FH_ERR_CAPACITY;
+  const size_t in = extent(matrix->rows, matrix->cols, matrix->ld, matrix->dtype), by_rows = fh_mx_bytes(matrix->rows, matrix->cols, params->format),
+               by_cols = fh_mx_bytes(matrix->cols, matrix->rows, params->format);
+  if (overlap(d_rows, by_rows, d_cols, by_cols) || overlap(d_src, in, d_rows, by_rows) || overlap(d_src, in, d_cols, by_cols)) return FH_ERR_ARG;
   fh::MxSaveArgs a = {};
   a.src = (const uint8_t*)d_src;
   a.by_rows = (uint8_t*)d_rows;
@@ -89,6 +100,8 @@ int fh_mx_decompress(const void* d_src, size_t src_bytes, const fh_matrix* expec
   if (rc != FH_OK) return rc;
   if (!is_format(format) || !d_src || !d_dst || misaligned(d_src, 16) || misaligned(d_dst, esize_of(expect->dtype)) || misaligned(d_status, 8))
     return FH_ERR_ARG;
+  if (overlap(d_src, fh_mx_bytes(expect->rows, expect->cols, format), d_dst, extent(expect->rows, expect->cols, expect->ld, expect->dtype)))
+    return FH_ERR_ARG;
   fh::MxSaveArgs a = {};
   a.src = (const uint8_t*)d_src;
   a.src_bytes = src_bytes;
@@ -108,6 +121,9 @@ int fh_mx_product(const fh_mx_product_desc* desc, const void* d_a, size_t a_byte
     return FH_ERR_ARG;
   if (!(desc->alpha >= -3.4028235e38f && desc->alpha <= 3.4028235e38f)) return FH_ERR_ARG;
   if (!d_a || !d_b || !d_c || misaligned(d_a, 16) || misaligned(d_b, 16) || misaligned(d_c, esize_of(desc->dtype)) || misaligned(d_status, 8))
+    return FH_ERR_ARG;
+  const size_t out = extent(desc->m, desc->n, desc->ldc, desc->dtype);
+  if (overlap(d_c, out, d_a, fh_mx_bytes(desc->m, desc->k, desc->format)) || overlap(d_c, out, d_b, fh_mx_bytes(desc->n, desc->k, desc->format)))
     return FH_ERR_ARG;
   fh::MxProductArgs a = {};
   a.a = (const uint8_t*)d_a;
@@ -138,7 +154,11 @@ int fh_layer_norm(const fh_norm_desc* desc, const void* d_x, const void* d_gamma
     rc = check_mx(params);
     if (rc != FH_OK) return rc;
     if (params->rounding != 0) return FH_ERR_UNSUPPORTED;
-    if (packed_capacity < fh_mx_bytes(desc->rows, desc->cols, params->format)) return FH_ERR_CAPACITY;
+    const size_t n = fh_mx_bytes(desc->rows, desc->cols, params->format);
+    if (packed_capacity < n) return FH_ERR_CAPACITY;
+    if (overlap(d_packed, n, d_x, extent(desc->rows, desc->cols, desc->ldx, desc->dtype)) ||
+        overlap(d_packed, n, d_y, extent(desc->rows, desc->cols, desc->ldy, desc->dtype)))
+      return FH_ERR_ARG;
     a.packed = (uint8_t*)d_packed;
     a.format = (uint32_t)params->format;
     a.exponent = params->exponent;
@@ -169,6 +189,8 @@ int fh_layer_norm_backward(const fh_norm_desc* desc, const void* d_dy, const voi
       misaligned(d_dx, es) || misaligned(d_dgamma, ws) || misaligned(d_dbeta, ws) || misaligned(d_work, 16) || misaligned(d_status, 8))
     return FH_ERR_ARG;
   fh::NormArgs a = norm_args(desc);
+  const size_t dx = extent(desc->rows, desc->cols, desc->ldx, desc->dtype), weights = (size_t)desc->cols * ws;
+  if ((x_bytes && overlap(d_dx, dx, d_x, fh_mx_bytes(desc->rows, desc->cols, x_format))) || overlap(d_dgamma, weights, d_dbeta, weights)) return FH_ERR_ARG;
   if (d_dgamma || d_dbeta) {
     if (!d_work) return FH_ERR_ARG;
     if (work_bytes < fh_layer_norm_work_bytes(desc)) return FH_ERR_CAPACITY;

@@ -78,19 +78,35 @@ __device__ __forceinline__ void store_c(uint8_t* c, uint64_t ldc, uint32_t row, 
 }
 
 // What the sums are multiplied by: 2^(ea + eb) and alpha, as one factor where that is exact and no product of it leaves the range of normal
-// numbers that the result is in; otherwise one after the other, the power in two steps.
+// numbers that the result is in; otherwise alpha's mantissa and then its power of two with the other in three steps of one direction, so
+// that nothing over- or underflows on the way that does not in the end.
 struct ProductScale {
-  float f1, f2, alpha;
+  float f[4];
   bool one;
-  __device__ __forceinline__ ProductScale(int ea, int eb, float alpha_) : alpha(alpha_) {
-    const int e = ea + eb, e1 = e / 2;
-    f1 = pow2_f(e1);
-    f2 = pow2_f(e - e1);
-    const float m = fabsf(alpha_);
-    one = (e >= -32 && e <= 32 && m >= 0x1p-60f && m <= 0x1p60f) || e == 0;
-    if (one) alpha = alpha_ * f1 * f2;
+  __device__ __forceinline__ ProductScale(int ea, int eb, float alpha) {
+    const int e = ea + eb;
+    const float m = fabsf(alpha);
+    one = e == 0 || (e >= -32 && e <= 32 && m >= 0x1p-60f && m <= 0x1p60f);
+    if (one) {
+      f[0] = alpha * pow2_f(e);
+      return;
+    }
+    int own = 0;
+    f[0] = frexpf(alpha, &own);
+    const int t = m > 0.0f ? e + own : 0, t1 = t / 3, t2 = (t - t1) / 2;
+    f[1] = pow2_f(t1);
+    f[2] = pow2_f(t2);
+    f[3] = pow2_f(t - t1 - t2);
   }
-  __device__ __forceinline__ float operator()(float v) const { return one ? v * alpha : v * f1 * f2 * alpha; }
+  template <int NR>
+  __device__ __forceinline__ void apply(float (&v)[NR]) const {
+#pragma unroll
+    for (int x = 0; x < NR; ++x) v[x] *= f[0];
+    if (!one) {
+#pragma unroll
+      for (int x = 0; x < NR; ++x) v[x] = v[x] * f[1] * f[2] * f[3];
+    }
+  }
 };
 
 // Sums rows of partial sums over the parts of a cluster (CTAs `stride` apart, from `first` on), NR rows at a time, in the order of the parts; four
@@ -234,7 +250,8 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
         tc_load16(tmem + (warp * 32u << 16) + q0, v);
         tc_load_wait();
 #pragma unroll
-        for (uint32_t x = 0; x < 16u; ++x) f[x] = scaled(bits_f(v[x]));
+        for (uint32_t x = 0; x < 16u; ++x) f[x] = bits_f(v[x]);
+        scaled.apply(f);
         if (col < g.n) {
           if (g.accumulate) {
             float old[16];
@@ -268,8 +285,11 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
         float f[NR], old[NR] = {};
         if (g.accumulate) load_c<DT, NR>(g.c, g.ldc, tq * 128u + q, tq * 128u + end, col, old);
         sum_parts<NR>(smem_u32(part + q * 128u + tid), 512u, 0u, 1u, g.split, f);  // (rows behind the last: stage bytes)
+        scaled.apply(f);
+        if (g.accumulate) {
 #pragma unroll
-        for (int x = 0; x < NR; ++x) f[x] = g.accumulate ? old[x] + scaled(f[x]) : scaled(f[x]);
+          for (int x = 0; x < NR; ++x) f[x] += old[x];
+        }
         store_c<DT, NR>(g.c, g.ldc, tq * 128u + q, tq * 128u + end, col, f);
       }
     }
@@ -488,7 +508,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
         for (uint32_t x = 0; x < 8u; ++x) {
           float f[16];
 #pragma unroll
-          for (uint32_t y = 0; y < 16u; ++y) f[y] = scaled(bits_f(v[x][y]));
+          for (uint32_t y = 0; y < 16u; ++y) f[y] = bits_f(v[x][y]);
+          scaled.apply(f);
           if (col < g.n) {
             if (g.accumulate) {
               float old[16];
@@ -523,8 +544,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
           float f[8], old[8] = {};
           if (g.accumulate) load_c<DT, 8>(g.c, g.ldc, row + q, row + stop, col, old);
           sum_parts<8>(smem_u32(reinterpret_cast<float*>(smem) + q * 128u + p), 512u, half, 2u, g.split, f);
+          scaled.apply(f);
+          if (g.accumulate) {
 #pragma unroll
-          for (int x = 0; x < 8; ++x) f[x] = g.accumulate ? old[x] + scaled(f[x]) : scaled(f[x]);
+            for (int x = 0; x < 8; ++x) f[x] += old[x];
+          }
           store_c<DT, 8>(g.c, g.ldc, row + q, row + stop, col, f);
         }
     }

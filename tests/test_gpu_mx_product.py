@@ -48,7 +48,7 @@ def agree(got, want, size, k, dtype):
 
 
 SHAPES = [(1, 1, 1), (1, 8, 32), (1, 128, 64), (3, 40, 100), (8, 200, 256), (16, 128, 512), (17, 129, 300), (33, 500, 1000), (64, 96, 2048), (65, 256, 320),
-          (128, 128, 128), (129, 127, 96), (200, 300, 777), (256, 512, 1024), (300, 260, 4096), (1, 4096, 4096), (5, 1000, 8192)]
+          (128, 128, 128), (129, 127, 96), (200, 300, 777), (256, 512, 1024), (300, 260, 4096), (200, 8, 64), (257, 5, 40), (130, 1000, 256), (1, 4096, 4096), (5, 1000, 8192)]
 
 
 @pytest.mark.parametrize("dtype", [api.FH_F32, api.FH_BF16])
@@ -97,6 +97,55 @@ def test_alpha_strides_and_adding(m, n, k, ldc, dtype):
             agree(got, want, size, k, dtype)
 
 
+@pytest.mark.parametrize("fmt", [mx.B32, mx.B16])
+@pytest.mark.parametrize("dtype,add", [(api.FH_F32, False), (api.FH_F32, True), (api.FH_BF16, False)])
+def test_more_tiles_than_the_device_holds_at_once(dtype, add, fmt):
+    """10 x 11 tiles of 256 x 256, in a band of eight rows of tiles and one of two, the last row and column of tiles in part."""
+    m, n, k = 2500, 2700, 700
+    (a, x), (b, y) = operand(m, k, fmt, 0, 13), operand(n, k, fmt, 0, 14)
+    c0 = torch.from_numpy(np.random.default_rng(15).standard_normal((m, n)).astype(np.float32)).cuda() if add else None
+    st, got = product(api.mx_product_desc(m, n, k, fmt, dtype, n + 3, 0.75, add), a, b, c0)
+    want, size = 0.75 * (x @ y.T), 0.75 * (np.abs(x) @ np.abs(y).T)
+    if add:
+        want, size = want + c0.double().cpu().numpy(), size + c0.double().abs().cpu().numpy()
+    assert st == api.FH_OK
+    agree(got, want, size, k, dtype)
+
+
+def test_two_host_threads_at_once():
+    """Calls from two threads, a stream each: large and small products, layer norms and containers in turn."""
+    import threading
+    found = []
+
+    def work(seed):
+        try:
+            (a, x), (b, y) = operand(260, 900, mx.B16, 0, seed), operand(300, 900, mx.B16, 0, seed + 50)
+            rows = np.random.default_rng(seed).standard_normal((40, 900)).astype(np.float32)
+            want = mx.compress(rows, mx.B32)
+            with torch.cuda.stream(torch.cuda.Stream()):
+                t, c, c1 = torch.from_numpy(rows).cuda(), torch.empty(260, 300, device="cuda"), torch.empty(1, 300, device="cuda")
+                one = mx.compress(x[:1], mx.B16)
+                first, x1 = torch.from_numpy(one).cuda(), mx.restore(one, 1, 900, mx.B16)
+                for _ in range(20):
+                    buf = torch.zeros(api.mx_bytes(40, 900, mx.B32), dtype=torch.uint8, device="cuda")
+                    assert api.fh_mx_product(api.mx_product_desc(260, 300, 900, mx.B16), a, b, c) == api.FH_OK
+                    assert api.fh_mx_compress(api.matrix(40, 900), api.mx_params(), t, buf) == api.FH_OK
+                    assert api.fh_mx_product(api.mx_product_desc(1, 300, 900, mx.B16), first, b, c1) == api.FH_OK
+                    torch.cuda.current_stream().synchronize()
+                    assert np.array_equal(buf.cpu().numpy(), want)
+                    agree(c.cpu().numpy(), x @ y.T, np.abs(x) @ np.abs(y).T, 900, api.FH_F32)
+                    agree(c1.cpu().numpy(), x1 @ y.T, np.abs(x1) @ np.abs(y).T, 900, api.FH_F32)
+            found.append("ok")
+        except BaseException as e:    # noqa: BLE001 (told to the test)
+            found.append(repr(e))
+    threads = [threading.Thread(target=work, args=(s,)) for s in (100, 200)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert found == ["ok", "ok"]
+
+
 def test_equal_inputs_give_equal_bits():
     (a, _), (b, _) = operand(40, 8192, mx.B16, 0, 5), operand(200, 8192, mx.B16, 0, 6)
     d = api.mx_product_desc(40, 200, 8192, mx.B16)
@@ -129,6 +178,10 @@ def test_far_exponents():
         # (numbers below 2^-126 have a step of 2^-149)
         off = np.abs(np.where(beyond, 0, got - want))
         assert (off <= 72 * 2.0 ** -23 * (np.abs(x) @ np.abs(y).T) + 2.0 ** -149).all()
+        # with a factor that brings them back, or that is zero
+        for alpha in (2.0 ** -(ea + eb) * 1.25, 0.0, -(2.0 ** -149) if ea + eb == 124 else 2.0 ** 100):
+            st, got = product(api.mx_product_desc(4, 8, 64, mx.B16, alpha=alpha), a, b)
+            assert st == api.FH_OK and (np.abs(got - alpha * want) <= 72 * 2.0 ** -23 * abs(alpha) * (np.abs(x) @ np.abs(y).T) + 2.0 ** -149).all()
 
 
 @pytest.mark.parametrize("which", ["a", "b"])
