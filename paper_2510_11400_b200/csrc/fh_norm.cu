@@ -48,6 +48,20 @@ __device__ __forceinline__ void store_vec(uint8_t* row, uint32_t i, uint32_t t, 
     return;
   }
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  if (DT == kBF16 && !VEC && !LINES && col + E <= cols) {  // words, wherever the row begins
+    uint16_t* p = reinterpret_cast<uint16_t*>(row) + col;
+    uint32_t* q = reinterpret_cast<uint32_t*>((uintptr_t)p + 2u & ~(uintptr_t)3u);
+    if ((uintptr_t)p & 2u) {
+      p[0] = (uint16_t)w[0];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) q[k] = __funnelshift_r(w[k], w[k + 1], 16);
+      p[7] = (uint16_t)(w[3] >> 16);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) q[k] = w[k];
+    }
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const uint32_t c = column<E, TEAM, LINES>(i, t, e);
@@ -59,8 +73,8 @@ __device__ __forceinline__ void store_vec(uint8_t* row, uint32_t i, uint32_t t, 
     }
   }
 }
-// The same into the thread's own 16 bytes of shared memory, later: what a thread has asked for so it alone reads, so that no barrier
-// stands between.  (An element of bf16 is too small for such a copy: off the grid it is loaded when it is used.)
+// The same into the thread's own bytes of shared memory, later: what a thread has asked for so it alone reads, so that no barrier
+// stands between.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
@@ -72,21 +86,40 @@ template <int N>
 __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// (of a vector that begins ahead of the last column)
-template <int DT, int TEAM, bool VEC, bool LINES>
-__device__ __forceinline__ void copy_vec(uint32_t dst, const uint8_t* row, uint32_t i, uint32_t t, uint32_t cols) {
-  constexpr int E = NormVec<DT>::kE;
-  const uint32_t col = column<E, TEAM, LINES>(i, t, 0);
-  if (VEC) {
-    copy16(dst, row + (uint64_t)col * (16 / E), min((uint32_t)E, cols - col) * (16 / E));
-  } else if (DT == kF32) {
+// Where a thread's vectors of a row lie: 16 bytes each, and off the 16-byte grid in bf16 a fifth word.  An element of bf16 is too small for
+// such a copy, so the words that hold the vector are copied, and the vector is shifted out of them: where rows begin in the middle of a word, the
+// first word's other half is the end of the row before, which is why the first row's first vector and the last row's last ones are loaded
+// when they are used (by_hand).  With LINES nothing is copied, and elements of bf16 are loaded when they are used.
+template <int DT, int TEAM, int V, bool VEC, bool LINES>
+struct RowRing {
+  static constexpr bool kWords = DT == kBF16 && !VEC && !LINES, kNone = DT == kBF16 && !VEC && LINES;
+  static constexpr uint32_t kFifth = V * kNormThreads * 16, kBytes = kNone ? 0 : kFifth + (kWords ? V * kNormThreads * 4 : 0);
+  static __device__ __forceinline__ bool by_hand(uint32_t row, uint32_t rows, uint32_t col, uint32_t cols) {
+    return kWords && ((row == 0u && col == 0u) || (row + 1u == rows && col + 9u >= cols));
+  }
+  // Vector i, one that begins ahead of the last column.
+  static __device__ __forceinline__ void copy(uint32_t at, const uint8_t* p, uint32_t row, uint32_t rows, uint32_t i, uint32_t t, uint32_t cols) {
+    constexpr int E = NormVec<DT>::kE;
+    const uint32_t col = column<E, TEAM, LINES>(i, t, 0), to = at + (i * kNormThreads + threadIdx.x) * 16u;
+    if (VEC) {
+      copy16(to, p + (uint64_t)col * (16 / E), min((uint32_t)E, cols - col) * (16 / E));
+    } else if (DT == kF32) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const uint32_t c = column<E, TEAM, LINES>(i, t, e);
-      copy4(dst + 4 * e, row + (c < cols ? (uint64_t)c * 4u : 0u), c < cols);
+      for (int e = 0; e < E; ++e) {
+        const uint32_t c = column<E, TEAM, LINES>(i, t, e);
+        copy4(to + 4 * e, p + (c < cols ? (uint64_t)c * 4u : 0u), c < cols);
+      }
+    } else if (kWords && !by_hand(row, rows, col, cols)) {
+      const uint32_t shift = (uint32_t)((uintptr_t)p >> 1) & 1u;
+      const uint8_t* q = p + ((int64_t)col - shift) * 2;
+#pragma unroll
+      for (uint32_t k = 0; k < 4u; ++k)
+        if (col + 2u * k < cols + shift) copy4(to + 4u * k, q + 4u * k, true);
+      if (shift && col + 8u < cols + shift) copy4(at + kFifth + (i * kNormThreads + threadIdx.x) * 4u, q + 16, true);
     }
   }
-}
+  static __device__ __forceinline__ uint4 get(uint32_t at, const uint8_t* p, uint32_t row, uint32_t rows, uint32_t i, uint32_t t, uint32_t cols);
+};
 __device__ __forceinline__ uint4 ld_shared16(uint32_t at) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
@@ -95,6 +128,28 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t at) {
 __device__ __forceinline__ uint32_t ld_shared4(uint32_t at) {
   uint32_t v;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+template <int DT, int TEAM, int V, bool VEC, bool LINES>
+__device__ __forceinline__ uint4 RowRing<DT, TEAM, V, VEC, LINES>::get(uint32_t at, const uint8_t* p, uint32_t row, uint32_t rows, uint32_t i,
+                                                                       uint32_t t, uint32_t cols) {
+  constexpr int E = NormVec<DT>::kE;
+  if (kNone) return load_vec<DT, TEAM, VEC, LINES>(p, i, t, cols);
+  const uint32_t to = at + (i * kNormThreads + threadIdx.x) * 16u;
+  if (!kWords) return ld_shared16(to);
+  const uint32_t col = column<E, TEAM, LINES>(i, t, 0);
+  if (by_hand(row, rows, col, cols)) return load_vec<DT, TEAM, VEC, LINES>(p, i, t, cols);
+  uint4 v = ld_shared16(to);
+  if ((uintptr_t)p & 2u) {
+    const uint32_t fifth = ld_shared4(at + kFifth + (i * kNormThreads + threadIdx.x) * 4u);
+    v = make_uint4(__funnelshift_r(v.x, v.y, 16), __funnelshift_r(v.y, v.z, 16), __funnelshift_r(v.z, v.w, 16), __funnelshift_r(v.w, fifth, 16));
+  }
+  if (col + 8u > cols) {  // (nothing was copied behind the last column's word)
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (uint32_t k = 0; k < 4u; ++k) w[k] = col + 2u * k + 1u < cols ? w[k] : (col + 2u * k < cols ? w[k] & 0xFFFFu : 0u);
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
   return v;
 }
 template <int DT, int E>
@@ -314,7 +369,7 @@ __device__ __forceinline__ void store_codes_of(const NormArgs& a, const MxLayout
 template <int DT, int TEAM, int V, bool VEC, bool LINES>
 __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormArgs a) {
   constexpr int E = NormVec<DT>::kE, H = E / 2;
-  constexpr bool kCopies = VEC || DT == kF32;
+  using Row = RowRing<DT, TEAM, V, VEC, LINES>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(16) float slots[kNormThreads / TEAM][4][TEAM / 32];
   const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
@@ -323,21 +378,20 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
   const uint32_t rows = a.packed ? (a.rows + 127u) / 128u * 128u : a.rows;  // (the padding of a container belongs to it)
   const uint32_t begin = (uint32_t)((uint64_t)rows * team / teams), end = (uint32_t)((uint64_t)rows * (team + 1u) / teams);
   const float inv = __frcp_rn((float)a.cols), unscale = a.format == kMxB32 ? 1.0f : pow2_f(-a.exponent);
-  const uint32_t ring = smem_u32(smem) + threadIdx.x * 16u;
+  const uint32_t ring = smem_u32(smem);
   auto row_of = [&](uint32_t row) { return a.x + (uint64_t)row * a.ldx * (16 / E); };
   auto column_of = [&](int i, int e) { return column<E, TEAM, LINES>(i, t, e); };
   dep_trigger();
   dep_wait();
   write_header(a, l);
   auto ask = [&](uint32_t row, uint32_t slot) {
-    if (kCopies) {
-      if (row < end && row < a.rows) {
+    if (row < end && row < a.rows) {
+      const uint8_t* p = row_of(row);
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (column_of(i, 0) < a.cols) copy_vec<DT, TEAM, VEC, LINES>(ring + (slot * V + i) * (kNormThreads * 16u), row_of(row), i, t, a.cols);
-      }
-      copy_commit();
+      for (int i = 0; i < V; ++i)
+        if (column_of(i, 0) < a.cols) Row::copy(ring + slot * Row::kBytes, p, row, a.rows, i, t, a.cols);
     }
+    copy_commit();
   };
 #pragma unroll
   for (int k = 0; k < kAhead - 1; ++k) ask(begin + k, k);
@@ -361,13 +415,12 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
       for (uint32_t i = 0; i < (uint32_t)V; ++i) store_codes<DT, E>(a, l, row, (i * TEAM + t) * E, zero, unscale);
       continue;
     }
-    if (kCopies) copy_wait<kAhead - 1>();
+    copy_wait<kAhead - 1>();
     f32x2 x[V][H], sum = both(0.0f);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-      if (column_of(i, 0) < a.cols)
-        raw = kCopies ? ld_shared16(ring + (slot * V + i) * (kNormThreads * 16u)) : load_vec<DT, TEAM, VEC, LINES>(row_of(row), i, t, a.cols);
+      if (column_of(i, 0) < a.cols) raw = Row::get(ring + slot * Row::kBytes, row_of(row), row, a.rows, i, t, a.cols);
       unpack<DT, H>(raw, x[i]);
 #pragma unroll
       for (int h = 0; h < H; ++h) sum = add2(sum, x[i][h]);
@@ -407,7 +460,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
       if (!LINES && a.packed) store_codes_of<DT, E>(a, l, row, (i * TEAM + t) * E, out, unscale);
     }
   }
-  if (kCopies) copy_wait<0>();
+  copy_wait<0>();
 }
 
 // Rows of more vectors than that: each of the three sweeps reads the row again.
@@ -530,12 +583,14 @@ __device__ __forceinline__ void sums_to_work(const NormArgs& a, const float* acc
   }
 }
 
-template <int V, int X>
+template <int DT, int TEAM, int V, bool VEC, int X>
 struct BackRing {
-  static constexpr int kGroup = X ? 4 : (V < 4 ? 2 : 1);         // rows worked on together ...
-  static constexpr int kRows = X || V < 4 ? 2 * kGroup : 3;      // ... and in shared memory
-  static constexpr uint32_t kX = kNormThreads * 16 * V, kSlot = X ? kX : 2 * kX;   // bytes of a slot: dy, and a dense x
-  static constexpr uint32_t kWarpX = 512 + 64;                   // of a vector of a warp, four rows: codes, scales
+  static constexpr bool kLines = !VEC && X == 0;  // (bf16: 16384 x 4095 157 us, by words 173)
+  using Row = RowRing<DT, TEAM, V, VEC, kLines>;
+  static constexpr int kGroup = X ? 4 : (V < 4 ? 2 : 1);      // rows worked on together ...
+  static constexpr int kRows = X || V < 4 ? 2 * kGroup : 3;   // ... and in shared memory
+  static constexpr uint32_t kX = Row::kBytes, kSlot = X ? kX : 2 * kX;  // bytes of a slot: dy, and a dense x
+  static constexpr uint32_t kWarpX = 512 + 64;                // of a vector of a warp, four rows: codes, scales
   static constexpr uint32_t kPacked = kRows * kSlot, kGroupX = V * kNormWarps * kWarpX;
   static constexpr size_t kBytes = kPacked + (X ? 2 * kGroupX : 0);
 };
@@ -548,9 +603,9 @@ struct BackRing {
 template <int DT, int TEAM, int V, bool VEC, int X>
 __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_kernel(const NormArgs a) {
   constexpr int E = NormVec<DT>::kE, H = E / 2;
-  constexpr bool kLines = !VEC && X == 0;
-  constexpr bool kCopies = VEC || DT == kF32;
-  using R = BackRing<V, X>;
+  using R = BackRing<DT, TEAM, V, VEC, X>;
+  using Row = typename R::Row;
+  constexpr bool kLines = R::kLines;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(16) float slots[kNormThreads / TEAM][2][2 * R::kGroup][TEAM / 32];
   const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
@@ -565,22 +620,18 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
   float scale;
   if (!backward_begin<X>(a, l, &scale)) return;
   auto ask = [&](uint32_t row, uint32_t slot) {
-    if (kCopies) {
-      if (row < end) {
-        const uint32_t at = ring + slot * R::kSlot;
-        const uint8_t* dyr = a.dy + (uint64_t)row * a.ldy * (16 / E);
-        const uint8_t* xr = a.x + (uint64_t)row * a.ldx * (16 / E);
+    if (row < end) {
+      const uint32_t at = ring + slot * R::kSlot;
+      const uint8_t* dyr = a.dy + (uint64_t)row * a.ldy * (16 / E);
+      const uint8_t* xr = a.x + (uint64_t)row * a.ldx * (16 / E);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const uint32_t col = column_of(i, 0);
-          if (col < a.cols) {
-            copy_vec<DT, TEAM, VEC, kLines>(at + (i * kNormThreads + threadIdx.x) * 16u, dyr, i, t, a.cols);
-            if (X == 0) copy_vec<DT, TEAM, VEC, kLines>(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u, xr, i, t, a.cols);
-          }
+      for (int i = 0; i < V; ++i)
+        if (column_of(i, 0) < a.cols) {
+          Row::copy(at, dyr, row, a.rows, i, t, a.cols);
+          if (X == 0) Row::copy(at + R::kX, xr, row, a.rows, i, t, a.cols);
         }
-      }
-      copy_commit();
     }
+    copy_commit();
   };
   constexpr int G = R::kGroup, kAsked = R::kRows - G;  // rows asked for ahead of a group
   // four rows of a container, vector i of the warp: lane 4 c + k asks for chunk c of row k
@@ -588,7 +639,7 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
   const uint32_t lane = threadIdx.x % 32u, warp_x = ring + R::kPacked + threadIdx.x / 32u * R::kWarpX;
   auto x_at = [&](int i, uint32_t half) { return warp_x + half * R::kGroupX + i * (kNormWarps * R::kWarpX); };
   auto ask_x = [&](uint32_t row, uint32_t half) {
-    if (X && kCopies) {
+    if (X) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const uint32_t col0 = (i * TEAM + (t - lane)) * E, k = lane % 4u, c = lane / 4u, chunk = col0 / 32u + c;
@@ -626,18 +677,13 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
   // dy, xhat and g = dy * gamma of vector i of a row (one that begins ahead of the last column; columns behind it have dy = 0 and add nothing)
   auto vec = [&](int i, uint32_t row, uint32_t slot, uint32_t k, uint32_t half, float mean, float rstd, f32x2(&dy)[H], f32x2(&xh)[H], f32x2(&g)[H]) {
     const uint32_t at = ring + slot * R::kSlot, col = column_of(i, 0);
-    uint4 ry, rx;
-    if (kCopies) {
-      ry = ld_shared16(at + (i * kNormThreads + threadIdx.x) * 16u);
-      if (X == 0) {
-        rx = ld_shared16(at + R::kX + (i * kNormThreads + threadIdx.x) * 16u);
-      } else {
-        rx.x = ld_shared4(x_at(i, half) + k * (16u * E) + lane * E / 8u * 4u);
-        rx.y = ld_shared4(x_at(i, half) + 512u + (4u * k + lane * E / kAtomCols) * 4u);
-      }
+    uint4 rx = make_uint4(0u, 0u, 0u, 0u);
+    const uint4 ry = Row::get(at, a.dy + (uint64_t)row * a.ldy * (16 / E), row, a.rows, i, t, a.cols);
+    if (X == 0) {
+      rx = Row::get(at + R::kX, a.x + (uint64_t)row * a.ldx * (16 / E), row, a.rows, i, t, a.cols);
     } else {
-      ry = load_vec<DT, TEAM, VEC, kLines>(a.dy + (uint64_t)row * a.ldy * (16 / E), i, t, a.cols);
-      rx = load_x<DT, TEAM, VEC, kLines, X>(a, l, row, i, t);
+      rx.x = ld_shared4(x_at(i, half) + k * (16u * E) + lane * E / 8u * 4u);
+      rx.y = ld_shared4(x_at(i, half) + 512u + (4u * k + lane * E / kAtomCols) * 4u);
     }
     unpack<DT, H>(ry, dy);
     if (X == 0)
@@ -669,7 +715,7 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
       rstd[k] = next_rstd[k];
     }
     ask_stats(row + G);
-    if (kCopies) copy_wait<kAsked>();
+    copy_wait<kAsked>();
     if (X) __syncwarp();  // (what the other lanes have asked for)
 #pragma unroll
     for (int k = 0; k < G; ++k) {
@@ -715,7 +761,7 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
     slot += G;
     if (slot >= (uint32_t)R::kRows) slot -= R::kRows;
   }
-  if (kCopies) copy_wait<0>();
+  copy_wait<0>();
   if (!a.work) return;
   float* acc = reinterpret_cast<float*>(smem);
   float* out = a.work + (uint64_t)blockIdx.x * 2u * a.cols;
@@ -860,7 +906,7 @@ template <int DT, int TEAM, int V, bool VEC, bool LINES>
 int launch_forward_t(const NormArgs& a, cudaStream_t stream) {
   const uint64_t rows = a.packed ? ((uint64_t)a.rows + 127) / 128 * 128 : a.rows;
   const uint32_t grid = (uint32_t)std::min<uint64_t>((rows * TEAM + kNormThreads - 1) / kNormThreads, (uint64_t)sm_count() * 4);
-  constexpr size_t smem = VEC || DT == kF32 ? (size_t)kAhead * V * kNormThreads * 16 : 0;
+  constexpr size_t smem = (size_t)kAhead * RowRing<DT, TEAM, V, VEC, LINES>::kBytes;
   return launch_plain<norm_forward_kernel<DT, TEAM, V, VEC, LINES>>(grid, kNormThreads, smem, 1, stream, a);
 }
 template <int DT, bool VEC, bool LINES>
@@ -879,7 +925,7 @@ int launch_forward_dv(const NormArgs& a, cudaStream_t stream) {
 
 template <int DT, int TEAM, int V, bool VEC, int X>
 int launch_backward_t(const NormArgs& a, cudaStream_t stream) {
-  constexpr size_t ring = VEC || DT == kF32 ? BackRing<V, X>::kBytes : 0, sums = TEAM < kNormThreads ? (size_t)8 * V * TEAM * NormVec<DT>::kE : 0;
+  constexpr size_t ring = BackRing<DT, TEAM, V, VEC, X>::kBytes, sums = TEAM < kNormThreads ? (size_t)8 * V * TEAM * NormVec<DT>::kE : 0;
   return launch_plain<norm_backward_kernel<DT, TEAM, V, VEC, X>>(a.parts, kNormThreads, std::max(ring, sums), 1, stream, a);
 }
 template <int DT, bool VEC, int X>
@@ -915,7 +961,9 @@ int launch_norm_forward(const NormArgs& a, int dtype, cudaStream_t stream) {
   if (sm_count() < 1) return FH_ERR_CUDA;
   const uint64_t es = dtype == kF32 ? 4 : 2;
   const bool vec = aligned16(a.x) && aligned16(a.y) && a.ldx * es % 16 == 0 && (!a.y || a.ldy * es % 16 == 0);
-  const bool lines = !vec && !a.packed;  // (codes are made of neighbours)
+  // Codes are made of neighbours.  Off the grid, bf16 comes by words for long rows and element by element for short ones: 16384 x 4095 147 and
+  // 257 us, 16384 x 1001 47 and 40.
+  const bool lines = !vec && !a.packed && (dtype == kF32 || a.cols <= 1024);
   if (dtype == kF32)
     return vec ? launch_forward_dv<kF32, true, false>(a, stream)
                : (lines ? launch_forward_dv<kF32, false, true>(a, stream) : launch_forward_dv<kF32, false, false>(a, stream));
