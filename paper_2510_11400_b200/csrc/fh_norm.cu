@@ -302,42 +302,75 @@ __device__ __forceinline__ void team_sums(float (&v)[NV], float (*slot)[TEAM / 3
 }
 
 // ---- codes of a row of the output, E of its columns from `col` on in each lane (neighbouring lanes hold neighbouring columns)
-// Every lane of the warp takes part; rows behind the last and columns behind the last give zeros.
-template <int DT, int F, int E>
-__device__ __forceinline__ void store_codes_f(const NormArgs& a, const MxLayout& l, uint32_t row, uint32_t col, const float (&v)[E], float unscale) {
-  constexpr int kLanes = (F == kMxB32 ? 32 : 16) / E;  // lanes to a block
+// A lane's codes and, in the lane that has the first of four blocks, their scales.  Every lane of the warp takes part; rows behind the last
+// and columns behind the last give zeros.
+template <int E>
+__device__ __forceinline__ uint32_t top_of(const float (&v)[E]) {
   uint32_t top = 0u;
 #pragma unroll
   for (int e = 0; e < E; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+  return top;
+}
+// (`top`: the largest magnitude of v, as bits)
+template <int F, int E>
+__device__ __forceinline__ uint2 codes_of_f(const NormArgs& a, uint32_t row, uint32_t col, const float (&v)[E], uint32_t top, float unscale) {
+  constexpr int kLanes = (F == kMxB32 ? 32 : 16) / E;  // lanes to a block
 #pragma unroll
   for (int d = 1; d < kLanes; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
   const MxScale s = mx_scale<F>(top, unscale);
   float q[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) q[e] = e < E ? mx_quotient<F>(v[e % E], s) : 0.0f;
-  const uint32_t codes = s.bad ? 0u : mx_codes8(q);
-  // (col is a multiple of E, and kp of 64)
-  if (row < l.r8 && col < l.kp) {
-    uint8_t* p = a.packed + l.code_at(row, col / 32u) + col % 32u / 2u;
-    if (E == 8)
-      *reinterpret_cast<uint32_t*>(p) = codes;
-    else
-      *reinterpret_cast<uint16_t*>(p) = (uint16_t)codes;
-  }
-  // four blocks' scales to the lane that has the first of them
   uint32_t word = row < a.rows && col < a.cols ? s.byte : 0u;
   word |= __shfl_down_sync(0xFFFFFFFFu, word, kLanes) << 8;
   word |= __shfl_down_sync(0xFFFFFFFFu, word, 2 * kLanes) << 16;
-  const uint32_t atom = col / (F == kMxB32 ? 128u : 64u);
-  if (col % (F == kMxB32 ? 128u : 64u) == 0u && atom < l.atoms)
-    *reinterpret_cast<uint32_t*>(a.packed + l.atom_at(row / 128u, atom) + MxLayout::scale_in_atom(row)) = word;
+  return make_uint2(s.bad ? 0u : mx_codes8(q), word);
 }
-template <int DT, int E>
+template <int E>
+__device__ __forceinline__ uint2 codes_of(const NormArgs& a, uint32_t format, uint32_t row, uint32_t col, const float (&v)[E], float unscale) {
+  return format == kMxB32 ? codes_of_f<kMxB32, E>(a, row, col, v, top_of<E>(v), unscale) : codes_of_f<kMxB16, E>(a, row, col, v, top_of<E>(v), unscale);
+}
+// ... straight to the container, for rows that are worked on one at a time.  (col is a multiple of E, and kp of 64.)
+template <int E>
 __device__ __forceinline__ void store_codes(const NormArgs& a, const MxLayout& l, uint32_t row, uint32_t col, const float (&v)[E], float unscale) {
-  if (l.format == kMxB32)
-    store_codes_f<DT, kMxB32, E>(a, l, row, col, v, unscale);
+  const uint2 c = codes_of<E>(a, l.format, row, col, v, unscale);
+  if (row < l.r8 && col < l.kp) {
+    uint8_t* p = a.packed + l.code_at(row, col / 32u) + col % 32u / 2u;
+    if (E == 8)
+      *reinterpret_cast<uint32_t*>(p) = c.x;
+    else
+      *reinterpret_cast<uint16_t*>(p) = (uint16_t)c.x;
+  }
+  const uint32_t cols = l.format == kMxB32 ? 128u : 64u, atom = col / cols;
+  if (col % cols == 0u && atom < l.atoms)
+    *reinterpret_cast<uint32_t*>(a.packed + l.atom_at(row / 128u, atom) + MxLayout::scale_in_atom(row)) = c.y;
+}
+// ... or by way of shared memory, four rows of a vector of a warp at `at`, so that a lane writes 16 bytes and four lanes 64 in a row (with 4 bytes a
+// lane 16384 x 4096 took 91 us, 29 more than y alone and longer than compressing y).
+constexpr uint32_t kStageX = 512 + 64;
+template <int F, int E>
+__device__ __forceinline__ void stage_codes(const NormArgs& a, uint8_t* at, uint32_t row, uint32_t col, uint32_t k, const float (&v)[E], uint32_t top,
+                                            float unscale) {
+  constexpr uint32_t cols = F == kMxB32 ? 128u : 64u;
+  const uint32_t lane = threadIdx.x % 32u;
+  const uint2 c = codes_of_f<F, E>(a, row, col, v, top, unscale);
+  if (E == 8)
+    reinterpret_cast<uint32_t*>(at)[k * 32u + lane] = c.x;
   else
-    store_codes_f<DT, kMxB16, E>(a, l, row, col, v, unscale);
+    reinterpret_cast<uint16_t*>(at)[k * 32u + lane] = (uint16_t)c.x;
+  if (col % cols == 0u) reinterpret_cast<uint32_t*>(at + 512)[4u * k + lane * E / cols] = c.y;
+}
+// Rows row ... row + n - 1 of the vector that begins in column col0.
+template <int F, int E>
+__device__ __forceinline__ void flush_codes(const NormArgs& a, const MxLayout& l, const uint8_t* at, uint32_t row, uint32_t n, uint32_t col0) {
+  const uint32_t lane = threadIdx.x % 32u, k = lane % 4u, c = lane / 4u, chunk = col0 / 32u + c;
+  if (c < (uint32_t)E && k < n && row + k < l.r8 && chunk * 32u < l.kp)
+    *reinterpret_cast<uint4*>(a.packed + l.code_at(row + k, chunk)) = *reinterpret_cast<const uint4*>(at + k * (16u * E) + c * 16u);
+  constexpr uint32_t cols = F == kMxB32 ? 128u : 64u, words = 32u * E / cols;
+  const uint32_t ks = lane / words, word = lane % words, atom = col0 / cols + word;
+  if (ks < n && atom < l.atoms)
+    *reinterpret_cast<uint32_t*>(a.packed + l.atom_at((row + ks) / 128u, atom) + MxLayout::scale_in_atom(row + ks)) =
+        reinterpret_cast<const uint32_t*>(at + 512)[4u * ks + word];
 }
 
 // Forward.  y = (x - mean) * rstd * gamma + beta, mean and variance from the row as it is held in registers (the squares of the
@@ -355,37 +388,42 @@ __device__ __forceinline__ void write_header(const NormArgs& a, const MxLayout& 
   reinterpret_cast<uint4*>(a.packed)[threadIdx.x] = v;
 }
 
-// Codes of a vector of y as it is in its type, so that they are those that compressing y gives.
+// A vector of y as it is in its type, so that its codes are those that compressing y gives; its largest magnitude, as bits.
 template <int DT, int E>
-__device__ __forceinline__ void store_codes_of(const NormArgs& a, const MxLayout& l, uint32_t row, uint32_t col, const uint4& out, float unscale) {
-  float f[E];
+__device__ __forceinline__ uint32_t as_stored(const NormArgs& a, uint32_t col, const uint4& out, float (&f)[E]) {
   unpack<DT, E>(out, f);
+  if (DT == kBF16 && col + E <= a.cols) {  // two elements at a time
+    const uint32_t m = __vmaxu2(__vmaxu2(out.x & 0x7FFF7FFFu, out.y & 0x7FFF7FFFu), __vmaxu2(out.z & 0x7FFF7FFFu, out.w & 0x7FFF7FFFu));
+    return max(m << 16, m & 0xFFFF0000u);
+  }
 #pragma unroll
   for (int e = 0; e < E; ++e)
     if (col + e >= a.cols) f[e] = 0.0f;
-  store_codes<DT, E>(a, l, row, col, f, unscale);
+  return top_of<E>(f);
 }
 
-template <int DT, int TEAM, int V, bool VEC, bool LINES>
-__global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormArgs a) {
+// P: no container, or 1 + its format.
+template <int DT, int TEAM, int V, bool VEC, bool LINES, int P>
+__global__ void __launch_bounds__(kNormThreads, 2) norm_forward_kernel(const NormArgs a) {
   constexpr int E = NormVec<DT>::kE, H = E / 2;
   using Row = RowRing<DT, TEAM, V, VEC, LINES>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(16) float slots[kNormThreads / TEAM][4][TEAM / 32];
   const uint32_t t = threadIdx.x % TEAM, in_cta = threadIdx.x / TEAM, team = blockIdx.x * (kNormThreads / TEAM) + in_cta,
                  teams = gridDim.x * (kNormThreads / TEAM);
-  const MxLayout l(a.rows, a.cols, a.format);
-  const uint32_t rows = a.packed ? (a.rows + 127u) / 128u * 128u : a.rows;  // (the padding of a container belongs to it)
+  constexpr int F = P > 1 ? kMxB16 : kMxB32;
+  const MxLayout l(a.rows, a.cols, F);
+  const uint32_t rows = P ? (a.rows + 127u) / 128u * 128u : a.rows;  // (the padding of a container belongs to it)
   const uint32_t begin = (uint32_t)((uint64_t)rows * team / teams), end = (uint32_t)((uint64_t)rows * (team + 1u) / teams);
-  const float inv = __frcp_rn((float)a.cols), unscale = a.format == kMxB32 ? 1.0f : pow2_f(-a.exponent);
+  const float inv = __frcp_rn((float)a.cols), unscale = F == kMxB32 ? 1.0f : pow2_f(-a.exponent);
   const uint32_t ring = smem_u32(smem);
   auto row_of = [&](uint32_t row) { return a.x + (uint64_t)row * a.ldx * (16 / E); };
   auto column_of = [&](int i, int e) { return column<E, TEAM, LINES>(i, t, e); };
   dep_trigger();
   dep_wait();
-  write_header(a, l);
+  if (P) write_header(a, l);
   auto ask = [&](uint32_t row, uint32_t slot) {
-    if (row < end && row < a.rows) {
+    if (row < end && (!P || row < a.rows)) {
       const uint8_t* p = row_of(row);
 #pragma unroll
       for (int i = 0; i < V; ++i)
@@ -407,12 +445,28 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
       beta[i][h] = pack2(b[2 * h], b[2 * h + 1]);
     }
   }
+  // codes of the team's rows, four of them at a time
+  uint8_t* stage = smem + kAhead * Row::kBytes + threadIdx.x / 32u * kStageX;
+  auto put_codes = [&](int i, uint32_t row, const float(&f)[E], uint32_t top) {
+    stage_codes<F, E>(a, stage + i * (kNormWarps * kStageX), row, (i * TEAM + t) * E, (row - begin) % 4u, f, top, unscale);
+  };
+  auto flush = [&](uint32_t row) {
+    const uint32_t k = (row - begin) % 4u;
+    if (k != 3u && row + 1u != end) return;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      flush_codes<F, E>(a, l, stage + i * (kNormWarps * kStageX), row - k, k + 1u, (i * TEAM + (t - threadIdx.x % 32u)) * E);
+    __syncwarp();
+  };
   uint32_t turn = 0, slot = 0;
   for (uint32_t row = begin; row < end; ++row, turn ^= 2u, slot = slot + 1u == kAhead ? 0u : slot + 1u) {
     ask(row + kAhead - 1u, slot ? slot - 1u : kAhead - 1u);
-    if (row >= a.rows) {
+    if (P && row >= a.rows) {
       const float zero[E] = {};
-      for (uint32_t i = 0; i < (uint32_t)V; ++i) store_codes<DT, E>(a, l, row, (i * TEAM + t) * E, zero, unscale);
+#pragma unroll
+      for (int i = 0; i < V; ++i) put_codes(i, row, zero, 0u);
+      flush(row);
       continue;
     }
     copy_wait<kAhead - 1>();
@@ -457,8 +511,13 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
       for (int h = 0; h < H; ++h) x[i][h] = fma2(mul2(x[i][h], both(rstd)), gamma[i][h], beta[i][h]);
       const uint4 out = pack<DT, H>(x[i]);
       if (y && column_of(i, 0) < a.cols) store_vec<DT, TEAM, VEC, LINES>(y, i, t, a.cols, out);
-      if (!LINES && a.packed) store_codes_of<DT, E>(a, l, row, (i * TEAM + t) * E, out, unscale);
+      if (P) {
+        float f[E];
+        const uint32_t top = as_stored<DT, E>(a, (i * TEAM + t) * E, out, f);
+        put_codes(i, row, f, top);
+      }
     }
+    if (P) flush(row);
   }
   copy_wait<0>();
 }
@@ -479,7 +538,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_wide_kernel(const N
   for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 2u) {
     if (row >= a.rows) {
       const float zero[E] = {};
-      for (uint32_t i = 0; i < sweeps; ++i) store_codes<DT, E>(a, l, row, (i * TEAM + t) * E, zero, unscale);
+      for (uint32_t i = 0; i < sweeps; ++i) store_codes<E>(a, l, row, (i * TEAM + t) * E, zero, unscale);
       continue;
     }
     const uint8_t* x = a.x + (uint64_t)row * a.ldx * (16 / E);
@@ -516,7 +575,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_wide_kernel(const N
       for (int e = 0; e < E; ++e) f[e] = __fmaf_rn((f[e] - mean) * rstd, g[e], b[e]);
       const uint4 out = pack<DT, E>(f);
       if (y && col < a.cols) store_vec<DT, TEAM, VEC, false>(y, i, t, a.cols, out);
-      if (a.packed) store_codes_of<DT, E>(a, l, row, col, out, unscale);
+      if (a.packed) {
+        as_stored<DT, E>(a, col, out, f);
+        store_codes<E>(a, l, row, col, f, unscale);
+      }
     }
   }
 }
@@ -902,25 +964,39 @@ __global__ void __launch_bounds__(kNormThreads) norm_columns_kernel(const NormAr
   }
 }
 
-template <int DT, int TEAM, int V, bool VEC, bool LINES>
+template <int DT, int TEAM, int V, bool VEC, bool LINES, int P>
 int launch_forward_t(const NormArgs& a, cudaStream_t stream) {
-  const uint64_t rows = a.packed ? ((uint64_t)a.rows + 127) / 128 * 128 : a.rows;
+  const uint64_t rows = P ? ((uint64_t)a.rows + 127) / 128 * 128 : a.rows;
   const uint32_t grid = (uint32_t)std::min<uint64_t>((rows * TEAM + kNormThreads - 1) / kNormThreads, (uint64_t)sm_count() * 4);
-  constexpr size_t smem = (size_t)kAhead * RowRing<DT, TEAM, V, VEC, LINES>::kBytes;
-  return launch_plain<norm_forward_kernel<DT, TEAM, V, VEC, LINES>>(grid, kNormThreads, smem, 1, stream, a);
+  constexpr size_t smem = (size_t)kAhead * RowRing<DT, TEAM, V, VEC, LINES>::kBytes + (P ? (size_t)V * kNormWarps * kStageX : 0);
+  return launch_plain<norm_forward_kernel<DT, TEAM, V, VEC, LINES, P>>(grid, kNormThreads, smem, 1, stream, a);
 }
-template <int DT, bool VEC, bool LINES>
+template <int DT, bool VEC, bool LINES, int P>
 int launch_forward_dv(const NormArgs& a, cudaStream_t stream) {
   const uint32_t vecs = (a.cols + NormVec<DT>::kE - 1) / NormVec<DT>::kE;
   // a row's two reductions cost a thread some 30 instructions each, so few threads to a row, as long as registers hold their columns' weights
-  if (vecs <= 32) return launch_forward_t<DT, 32, 1, VEC, LINES>(a, stream);
-  if (vecs <= 64) return launch_forward_t<DT, 32, 2, VEC, LINES>(a, stream);
-  if (vecs <= 128) return launch_forward_t<DT, 32, 4, VEC, LINES>(a, stream);
-  if (vecs <= 256) return launch_forward_t<DT, 128, 2, VEC, LINES>(a, stream);
-  if (vecs <= 512) return launch_forward_t<DT, 128, 4, VEC, LINES>(a, stream);
-  if (vecs <= 1024) return launch_forward_t<DT, 256, 4, VEC, LINES>(a, stream);
+  if (vecs <= 32) return launch_forward_t<DT, 32, 1, VEC, LINES, P>(a, stream);
+  if (vecs <= 64) return launch_forward_t<DT, 32, 2, VEC, LINES, P>(a, stream);
+  if (vecs <= 128) return launch_forward_t<DT, 32, 4, VEC, LINES, P>(a, stream);
+  if (vecs <= 256) return launch_forward_t<DT, 128, 2, VEC, LINES, P>(a, stream);
+  if (vecs <= 512) return launch_forward_t<DT, P ? 256 : 128, P ? 2 : 4, VEC, LINES, P>(a, stream);
+  if (vecs <= 1024) return launch_forward_t<DT, 256, 4, VEC, LINES, P>(a, stream);
   const uint64_t rows = a.packed ? ((uint64_t)a.rows + 127) / 128 * 128 : a.rows;
   return launch_plain<norm_forward_wide_kernel<DT, VEC>>((uint32_t)std::min<uint64_t>(rows, (uint64_t)sm_count() * 8), kNormThreads, 0, 1, stream, a);
+}
+template <int DT>
+int launch_forward_d(const NormArgs& a, bool vec, cudaStream_t stream) {
+  if (a.packed) {
+    if (a.format == kMxB32) return vec ? launch_forward_dv<DT, true, false, 1>(a, stream) : launch_forward_dv<DT, false, false, 1>(a, stream);
+    return vec ? launch_forward_dv<DT, true, false, 2>(a, stream) : launch_forward_dv<DT, false, false, 2>(a, stream);
+  }
+  if (vec) return launch_forward_dv<DT, true, false, 0>(a, stream);
+  // Off the grid, bf16 comes by words for long rows and element by element for short ones: 16384 x 4095 147 and 257 us, 16384 x 1001 47 and
+  // 40.
+  if constexpr (DT == kBF16) {
+    if (a.cols > 1024) return launch_forward_dv<DT, false, false, 0>(a, stream);
+  }
+  return launch_forward_dv<DT, false, true, 0>(a, stream);
 }
 
 template <int DT, int TEAM, int V, bool VEC, int X>
@@ -961,14 +1037,7 @@ int launch_norm_forward(const NormArgs& a, int dtype, cudaStream_t stream) {
   if (sm_count() < 1) return FH_ERR_CUDA;
   const uint64_t es = dtype == kF32 ? 4 : 2;
   const bool vec = aligned16(a.x) && aligned16(a.y) && a.ldx * es % 16 == 0 && (!a.y || a.ldy * es % 16 == 0);
-  // Codes are made of neighbours.  Off the grid, bf16 comes by words for long rows and element by element for short ones: 16384 x 4095 147 and
-  // 257 us, 16384 x 1001 47 and 40.
-  const bool lines = !vec && !a.packed && (dtype == kF32 || a.cols <= 1024);
-  if (dtype == kF32)
-    return vec ? launch_forward_dv<kF32, true, false>(a, stream)
-               : (lines ? launch_forward_dv<kF32, false, true>(a, stream) : launch_forward_dv<kF32, false, false>(a, stream));
-  return vec ? launch_forward_dv<kBF16, true, false>(a, stream)
-             : (lines ? launch_forward_dv<kBF16, false, true>(a, stream) : launch_forward_dv<kBF16, false, false>(a, stream));
+  return dtype == kF32 ? launch_forward_d<kF32>(a, vec, stream) : launch_forward_d<kBF16>(a, vec, stream);
 }
 
 int launch_norm_backward(const NormArgs& a0, int dtype, cudaStream_t stream) {
