@@ -141,7 +141,8 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
   uint64_t* full = reinterpret_cast<uint64_t*>(tail);
   uint64_t* empty = full + S::kStages;
   uint64_t* done = empty + S::kStages;
-  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(done + 1);
+  uint64_t* idle = done + 1;  // after a wait that ran out: what was issued is complete
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(idle + 1);
   volatile uint32_t* abort = tmem_at + 1;
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const uint32_t rank = g.split > 1 ? cluster_rank() : 0u;
@@ -153,6 +154,7 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
       mbar_init(empty + i, 1);
     }
     mbar_init(done, 1);
+    mbar_init(idle, 1);
     *abort = 0u;
     fence_mbar_init();
   }
@@ -229,6 +231,10 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
         tc_commit(empty + s);
       }
       tc_commit(done);
+      if (*abort) {
+        tc_commit(idle);
+        mbar_wait(idle, 0u, kDrainPolls);
+      }
     }
   }
   __syncwarp();
@@ -307,7 +313,7 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
 // instructions start while they write.  With a split, a cluster's pairs share one tile.
 //
 // Scales are copied to tensor memory by a thread of its own.  In the one that issues the matrix instructions the copies (55 cycles each, 6 a
-// stage in B32, 12 in B16) stood in line with those, which take 512: 4096 x 4096 x 16384 138 and 182 us, now 107 and 143.
+// stage in B32, 12 in B16) stood in line with those, which take 512: 4096 x 4096 x 16384 138 and 182 us, now 103 and 143.
 constexpr int kPairThreads = 352;  // eight warps for the result, then one each for loads, matrix instructions and scales
 
 template <int F>
@@ -357,7 +363,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
   uint64_t* ready = empty + S::kStages;  // even CTA: its scales are in both CTAs' tensor memory
   uint64_t* sums = ready + S::kStages;  // the accumulator is complete
   uint64_t* taken = sums + 1;           // even CTA: both CTAs' warps have taken it
-  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(taken + 1);
+  uint64_t* idle = taken + 1;           // even CTA, after a wait that ran out: what its two threads issued is complete
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(idle + 2);
   volatile uint32_t* abort = tmem_at + 1;
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const uint32_t crank = cluster_rank(), half = crank & 1u, even = crank & ~1u, rank = crank / 2u;
@@ -371,6 +378,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
     }
     mbar_init(sums, 1);
     mbar_init(taken, 16);
+    mbar_init(idle, 1);
+    mbar_init(idle + 1, 1);
     *abort = 0u;
     fence_mbar_init();
   }
@@ -459,6 +468,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
         }
         tc_commit_pair(sums, both);
       }
+      if (*abort) {
+        tc_commit_pair(idle, (uint16_t)(1u << even));
+        mbar_wait(idle, 0u, kDrainPolls);
+      }
     }
   } else if (warp == 10) {
     if (lane == 0 && half == 0u) {
@@ -485,6 +498,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
             }
           tc_commit_pair(ready + s, (uint16_t)(1u << even));
         }
+      if (*abort) {
+        tc_commit_pair(idle + 1, (uint16_t)(1u << even));
+        mbar_wait(idle + 1, 0u, kDrainPolls);
+      }
     }
   } else {
     const ProductScale scaled(ea, eb, g.alpha);
