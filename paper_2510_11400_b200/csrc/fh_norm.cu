@@ -1040,10 +1040,12 @@ bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
 }  // namespace
 
 uint32_t norm_parts(uint32_t rows, uint32_t cols, int dtype) {
-  // rows that make a CTA worth its sums: four to a team of a warp, of half a CTA, of a CTA (see launch_backward_dx)
-  const uint32_t vecs = (cols + (dtype == kF32 ? 3u : 7u)) / (dtype == kF32 ? 4u : 8u), each = vecs <= 32u ? 32u : (vecs <= 128u ? 8u : 4u);
-  const uint32_t n = rows / each + (rows % each ? 1u : 0u);
-  return n < 296u ? n : 296u;
+  // rows that make a CTA worth its sums: four to a team of a warp, of half a CTA, of a CTA (see launch_backward_dx), and one where a row takes
+  // 10 us (106 x 11902 fp32: 39 us with four)
+  const uint32_t vecs = (cols + (dtype == kF32 ? 3u : 7u)) / (dtype == kF32 ? 4u : 8u);
+  const uint32_t each = vecs <= 32u ? 32u : (vecs <= 128u ? 8u : (vecs <= 1024u ? 4u : 1u));
+  const uint32_t n = rows / each + (rows % each ? 1u : 0u), most = cols <= 14336u ? 296u : 148u;  // (beyond, the sums leave an SM room for one CTA: 4096 x 16000 bf16 215 us and 233)
+  return n < most ? n : most;
 }
 
 int launch_norm_forward(const NormArgs& a, int dtype, cudaStream_t stream) {
