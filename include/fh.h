@@ -447,7 +447,7 @@ typedef struct {
 } fh_norm_desc;
 
 /*
- * Forward pass: one kernel, x is read once (rows of more than 2048 16-byte vectors: three times).
+ * Forward pass: one kernel, x is read once (rows of more than 1024 16-byte vectors: three times).
  *   d_gamma, d_beta   cols weights, either may be NULL (1, 0)
  *   d_y               dense output, may be NULL if d_packed is not; may be d_x when ldx = ldy
  *   d_mean, d_rstd    rows floats for the backward pass, either may be NULL
@@ -467,7 +467,8 @@ int fh_layer_norm(const fh_norm_desc* desc, const void* d_x, const void* d_gamma
  *   d_work            caller-owned workspace, 16-byte aligned, at least fh_layer_norm_work_bytes(desc) bytes, needed when d_dgamma or
  *                     d_dbeta is given; calls that may run at the same time need one each
  *   d_status          optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
- * One kernel, and a second, small one for dgamma and dbeta.  Sums are fp32 in a fixed order: equal inputs give equal bits.
+ * One kernel, and a second, small one for dgamma and dbeta.  Sums are fp32 in a fixed order: equal inputs, strides and alignments give
+ * equal bits.
  */
 size_t fh_layer_norm_work_bytes(const fh_norm_desc* desc);
 int fh_layer_norm_backward(const fh_norm_desc* desc, const void* d_dy, const void* d_x, size_t x_bytes, int32_t x_format, const void* d_gamma,
