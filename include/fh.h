@@ -413,7 +413,8 @@ int fh_mx_decompress(const void* d_src, size_t src_bytes, const fh_matrix* expec
  * columns.  Where the blocks along k of a row of A or B hold a NaN scale, that row (column) of C is NaN.
  *   d_a, d_b    containers of an m x k and an n x k matrix; another header is FH_ERR_CORRUPT (through d_status; C is not written then)
  *   d_c         element (i, j) at i * ldc + j; FH_ERR_ARG when it overlaps a container
- *   d_status    optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
+ *   d_status    optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status.  FH_ERR_TIMEOUT: a wait inside the
+ *               kernel ran out (C is undefined then, the library stays usable)
  * Results do not depend on the call's place among others: equal inputs give equal bits.
  */
 typedef struct {
@@ -483,6 +484,8 @@ int fh_layer_norm_backward(const fh_norm_desc* desc, const void* d_dy, const voi
  *   FH_DEBUG_WAIT_POLLS   limit of those waits in polls of about 0.1 us (default 2^22)
  *   FH_DEBUG_SILENT_TILE  index of a tile that never publishes its size, so that every later tile with
  *                         an outlier-rich plane runs into the limit; UINT64_MAX: none (default)
+ * The waits inside a product (fh_mx_product) have the same limit, and the silent tile is there the stage (256 elements of the common
+ * axis, counted in each CTA) from which on a CTA, of a pair the second one, loads nothing.
  * Both apply to calls enqueued afterwards, process-wide.  Returns FH_OK or FH_ERR_ARG.
  */
 enum { FH_DEBUG_WAIT_POLLS = 0, FH_DEBUG_SILENT_TILE = 1 };

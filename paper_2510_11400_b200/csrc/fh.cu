@@ -336,10 +336,10 @@ inline size_t scan_words(size_t tile_cap) { return tile_cap + 3 * (tile_cap / 32
 std::mutex g_mu;
 std::map<std::pair<int, cudaStream_t>, StreamScratch> g_scratch;
 
-// Fault injection for the time-out test (see fh_debug_set in the header): limit of the device-side waits
-// of the placement scan, and a tile that never publishes.
-uint32_t g_scan_polls = 1u << 22;
-uint32_t g_skip_tile = 0xFFFFFFFFu;
+// Fault injection for the time-out tests (see fh_debug_set in the header): limit of the device-side waits
+// of the placement scan (of a product: 16 of its shorter polls for each), and a tile that never publishes (a product: a stage that is not loaded).
+std::atomic<uint32_t> g_scan_polls{1u << 22};
+std::atomic<uint32_t> g_skip_tile{0xFFFFFFFFu};
 
 // `tiles`: tiles of the compress call that is about to be enqueued (0: none, e.g. for decompress).
 int get_scratch(cudaStream_t stream, size_t tiles, StreamScratch** out) {
@@ -534,6 +534,10 @@ bool misaligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0;
 
 namespace fh {
 void count_launch(int kernels) { g_launches.fetch_add((uint64_t)kernels); }
+void debug_waits(uint32_t* polls, uint32_t* silent) {
+  *polls = (uint32_t)std::min<uint64_t>((uint64_t)g_scan_polls.load() * 16u, 0xFFFFFFFFu);
+  *silent = g_skip_tile.load();
+}
 }  // namespace fh
 
 extern "C" {

@@ -138,6 +138,7 @@ int fh_mx_product(const fh_mx_product_desc* desc, const void* d_a, size_t a_byte
   a.ldc = (uint64_t)desc->ldc;
   a.alpha = desc->alpha;
   a.accumulate = desc->accumulate == 1;
+  fh::debug_waits(&a.polls, &a.silent);
   return fh::launch_mx_product(a, desc->dtype, desc->format, (cudaStream_t)stream);
 }
 

@@ -34,6 +34,7 @@ struct MxProductArgs {
   uint64_t ldc;
   float alpha;
   bool accumulate;
+  uint32_t polls, silent;          // limit of the kernels' waits, and a stage that is not loaded (fh_debug_set)
   uint32_t tiles_m, tiles_n, split;  // set where the kernel is launched
 };
 int launch_mx_product(const MxProductArgs& a, int dtype, int format, cudaStream_t stream);
@@ -60,6 +61,9 @@ int launch_norm_forward(const NormArgs& a, int dtype, cudaStream_t stream);
 int launch_norm_backward(const NormArgs& a, int dtype, cudaStream_t stream);
 
 constexpr size_t kMxSmemLimit = 226 * 1024;  // dynamic shared memory a CTA may have, next to a little that a kernel declares
+
+// What fh_debug_set has set, for the product's waits.
+void debug_waits(uint32_t* polls, uint32_t* silent);
 
 // Counts a kernel for fh_kernel_launches().
 void count_launch(int kernels = 1);

@@ -22,8 +22,24 @@ namespace {
 // rows that come of it are not looked at: a code is always finite, and a NaN scale stays in its row.
 constexpr int kProductThreads = 192;  // four warps for the result, one for copies, one for matrix instructions
 constexpr int kStepChunks = 8;        // 8 x 32 elements to a stage
-constexpr uint32_t kWaitPolls = 1u << 26;   // some seconds
 constexpr uint32_t kDrainPolls = 1u << 20;  // waits of up to 2 us each, for copies under way
+
+// Waits.  Every wait of a role (loads, matrix instructions, scales, result) has a limit, `polls` (2^26, some seconds); the first one that runs
+// out sets a flag, the CTA's or in a pair that of the whole cluster, which ends the others.  What is still under way then is waited for at the
+// end, when no role runs any more and the flag no longer changes: nothing may be in flight, in this CTA's memory or the other one's, when a
+// CTA ends.  Where no wait has run out, everything has been waited for on the way: copies by the thread that reads them (matrix instructions
+// or scales), the instructions by the result's warps, and the word that a stage is free, given only where the stage is used again, by
+// the loading thread.  The status is first written by CTA 0, one of the first to run, as it begins; a CTA that has given up writes
+// FH_ERR_TIMEOUT as it ends, a wait and a drain later.
+
+// An aligned place for a CTA's stages.  `zero` hides from the compiler that it has this address already: what only the end of the pair
+// kernel needs would take registers from its result warps (168 instead of 165; 4096 x 4096 x 4096 42.4 us and 48, 8192 x 16384 x 8192 400 and 428).
+__device__ __forceinline__ uint8_t* stages_at(uint8_t* raw, uint32_t zero = 0u) { return raw + ((128u - (smem_u32(raw) & 127u)) & 127u) + zero; }
+__device__ __forceinline__ uint32_t hidden_zero() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, 0;" : "=r"(r));
+  return r;
+}
 
 // Stage of a ring and the parity of its round.
 template <int STAGES>
@@ -136,7 +152,7 @@ template <int DT, int F, int QT>
 __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxProductArgs g) {
   using S = ProductShape<F, QT>;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
+  uint8_t* smem = stages_at(smem_raw);
   uint8_t* tail = smem + S::kStages * S::kStage;
   uint64_t* full = reinterpret_cast<uint64_t*>(tail);
   uint64_t* empty = full + S::kStages;
@@ -144,6 +160,7 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
   uint64_t* idle = done + 1;  // after a wait that ran out: what was issued is complete
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(idle + 1);
   volatile uint32_t* abort = tmem_at + 1;
+  uint32_t* loads = tmem_at + 2;  // stages that the loading thread has asked for
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const uint32_t rank = g.split > 1 ? cluster_rank() : 0u;
   const uint32_t cell = blockIdx.x / g.split, tp = cell % g.tiles_n, tq = cell / g.tiles_n;  // (clusters are along x)
@@ -180,11 +197,11 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
       const uint8_t* q = g.a + lq.code_at(tq * 128u, 0);
       const uint8_t* sp = g.b + lp.atom_at(tp, 0);
       const uint8_t* sq = g.a + lq.atom_at(tq, 0);
-      uint32_t i = 0;
+      uint32_t loaded = 0;
       Turn<S::kStages> at;
-      for (uint32_t it = first; it < last; ++it, ++i, at.next()) {
+      for (uint32_t it = first; it < last && loaded != g.silent; ++it, ++loaded, at.next()) {
         const uint32_t s = at.stage;
-        if (i >= (uint32_t)S::kStages && !mbar_poll<false>(empty + s, at.round ^ 1u, kWaitPolls, abort)) {
+        if (loaded >= (uint32_t)S::kStages && !mbar_poll<false>(empty + s, at.round ^ 1u, g.polls, abort)) {
           *abort = 1u;
           break;
         }
@@ -197,15 +214,14 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
         bulk_g2s(st + S::kP + S::kQ, sp + (uint64_t)it * S::kAtoms * 512u, na * 512u, full + s);
         bulk_g2s(st + S::kP + S::kQ + S::kS, sq + (uint64_t)it * S::kAtoms * 512u, na * 512u, full + s);
       }
-      // nothing may be in flight when the CTA ends
-      for (uint32_t w = i > (uint32_t)S::kStages ? i - S::kStages : 0u; w < i; ++w) mbar_wait(full + w % S::kStages, w / S::kStages & 1u, kDrainPolls);
+      *loads = loaded;
     }
   } else if (ok && warp == 5) {
     if (lane == 0) {
       Turn<S::kStages> at;
       for (uint32_t it = first; it < last; ++it, at.next()) {
         const uint32_t s = at.stage;
-        if (!mbar_poll<false>(full + s, at.round, kWaitPolls, abort)) {
+        if (!mbar_poll<false>(full + s, at.round, g.polls, abort)) {
           *abort = 1u;
           break;
         }
@@ -228,13 +244,9 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
             tc_mma_mx<F == kMxB32>(tmem, da + 2u * x * rp, db + 2u * x * rq, mx_idesc(128u, QT, F == kMxB32, id), sa + 4u * word, sb + 4u * word,
                                    it > first || x > 0u);
           }
-        tc_commit(empty + s);
+        if (it + (uint32_t)S::kStages < last) tc_commit(empty + s);
       }
       tc_commit(done);
-      if (*abort) {
-        tc_commit(idle);
-        mbar_wait(idle, 0u, kDrainPolls);
-      }
     }
   }
   __syncwarp();
@@ -242,7 +254,8 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
   const bool mine = ok && warp < 4;
   bool good = mine;
   if (mine) {
-    good = mbar_poll_warp(done, 0u, kWaitPolls, abort);
+    good = mbar_poll_warp(done, 0u, g.polls, abort);
+    if (!good && lane == 0) *abort = 1u;
     tc_fence_after();
   }
   const uint32_t col = tp * 128u + warp * 32u + lane;
@@ -301,9 +314,18 @@ __global__ void __launch_bounds__(kProductThreads) mx_product_kernel(const MxPro
     }
     cluster_sync();
   }
-  if (mine && !good && tid == 0 && g.status) *g.status = status_word(kErrTimeout);
   tc_fence_before();
   __syncthreads();
+  if (*abort) {  // (see "Waits" above)
+    if (ok && lane == 0 && warp == 4)
+      for (uint32_t n = *loads, w = n > (uint32_t)S::kStages ? n - S::kStages : 0u; w < n; ++w) mbar_wait(full + w % S::kStages, w / S::kStages & 1u, kDrainPolls);
+    if (ok && lane == 0 && warp == 5) {
+      tc_commit(idle);
+      mbar_wait(idle, 0u, kDrainPolls);
+    }
+    if (tid == 0 && g.status) *g.status = status_word(kErrTimeout);
+    __syncthreads();
+  }
   if (warp == 5) tmem_free(tmem, S::kCols);
 }
 
@@ -329,6 +351,20 @@ struct PairShape {
   static_assert(kStages * kStage >= (256 + 8) * 512, "partial sums, and rows read behind them");
 };
 
+// The barriers behind the stages, and the words behind them.
+template <int F>
+struct PairBars {
+  static constexpr int kStages = PairShape<F>::kStages;
+  static constexpr int kFull = 0;                     // even CTA: both CTAs' stages have arrived
+  static constexpr int kEmpty = kStages;              // a stage may be loaded again
+  static constexpr int kReady = 2 * kStages;          // even CTA: its scales are in both CTAs' tensor memory
+  static constexpr int kSums = 3 * kStages;           // the accumulator is complete
+  static constexpr int kTaken = kSums + 1;            // even CTA: both CTAs' warps have taken it
+  static constexpr int kIdle = kTaken + 1;            // even CTA, after a wait that ran out: what its two threads issued is complete
+  static constexpr int kWords = kIdle + 2;
+  static_assert(kWords * 8 + (3 + kStages) * 4 <= 256, "room behind the stages");
+};
+
 // How the codes and scales of an operand are laid out for the copies, which tell the even CTA's barrier of both CTAs' stages: a plain
 // bulk copy cannot reach the other CTA's, and a thread that passed the word on took 0.3 us a stage.
 struct OperandMaps {
@@ -352,20 +388,57 @@ struct PairTile {
   }
 };
 
+// What a CTA loads of a tile.
+template <int F>
+struct PairLoads {
+  using S = PairShape<F>;
+  uint32_t np, nq;      // blocks of 128 rows that there are of B and of A
+  uint32_t bytes, mine; // to a stage, of both CTAs and of this one
+  uint32_t zp, zq;      // where the codes of this CTA's blocks begin in their maps ...
+  uint32_t yp, yq, ya;  // ... and the scales of its block of B, of both of A, and of A's second one after its first
+  bool p_whole, q_whole;
+  __device__ __forceinline__ PairLoads(const MxProductArgs& g, uint32_t tile, uint32_t half) {
+    const MxLayout lp(g.n, g.k, F), lq(g.m, g.k, F);
+    const PairTile where(tile, g.tiles_m, g.tiles_n);
+    const uint32_t chunks = lp.kp / 32u, blocks_p = (g.n + 127u) / 128u, blocks_q = (g.m + 127u) / 128u;
+    const uint32_t bp0 = where.n * 2u, bq0 = where.m * 2u, bp = bp0 + half, bq = bq0 + half;
+    np = min(2u, blocks_p - bp0);
+    nq = min(2u, blocks_q - bq0);
+    p_whole = lp.block_rows(min(bp, blocks_p - 1u)) == 128u;
+    q_whole = lq.block_rows(min(bq, blocks_q - 1u)) == 128u;
+    bytes = (np + nq) * S::kOp + (np + 2u * nq) * S::kS;
+    mine = ((half < np) + (half < nq)) * S::kOp + ((half < np) + nq) * S::kS;
+    zp = p_whole ? bp * chunks : 0u;
+    zq = q_whole ? bq * chunks : 0u;
+    yp = bp * lp.atoms * 4u;
+    yq = bq0 * lq.atoms * 4u;
+    ya = lq.atoms * 4u;
+  }
+  // Stage `it` of the common axis to stage `s` of the ring.
+  __device__ __forceinline__ void load(const PairArgs& pa, uint8_t* smem, uint64_t* full, uint32_t it, uint32_t s, uint32_t half, uint32_t even) const {
+    const uint32_t st = smem_u32(smem) + s * S::kStage, sc = st + 2u * S::kOp, bar = at_rank(full + s, even);
+    if (half == 0u) mbar_expect_tx(full + s, bytes);
+    if (half < np) tma_pair_3d(st, p_whole ? &pa.b.codes : &pa.b.rest, 0u, 0u, zp + it * kStepChunks, bar);
+    if (half < nq) tma_pair_3d(st + S::kOp, q_whole ? &pa.a.codes : &pa.a.rest, 0u, 0u, zq + it * kStepChunks, bar);
+    const uint32_t y = it * S::kAtoms * 4u;
+    if (half < np) tma_pair_2d(sc, &pa.b.scales, 0u, yp + y, bar);
+    tma_pair_2d(sc + S::kS, &pa.a.scales, 0u, yq + y, bar);
+    if (nq > 1u) tma_pair_2d(sc + 2u * S::kS, &pa.a.scales, 0u, yq + ya + y, bar);
+  }
+};
+
 template <int DT, int F>
 __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const __grid_constant__ PairArgs pa) {
   const MxProductArgs& g = pa.g;
   using S = PairShape<F>;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);  // even CTA: both CTAs' stages have arrived
-  uint64_t* empty = full + S::kStages;
-  uint64_t* ready = empty + S::kStages;  // even CTA: its scales are in both CTAs' tensor memory
-  uint64_t* sums = ready + S::kStages;  // the accumulator is complete
-  uint64_t* taken = sums + 1;           // even CTA: both CTAs' warps have taken it
-  uint64_t* idle = taken + 1;           // even CTA, after a wait that ran out: what its two threads issued is complete
-  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(idle + 2);
+  uint8_t* smem = stages_at(smem_raw);
+  using B = PairBars<F>;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);
+  uint64_t *empty = full + B::kEmpty, *ready = full + B::kReady, *sums = full + B::kSums, *taken = full + B::kTaken, *idle = full + B::kIdle;
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(full + B::kWords);
   volatile uint32_t* abort = tmem_at + 1;
+  uint32_t* loads = tmem_at + 2;  // stages that the loading thread has asked for, and of each stage the odd CTA's bytes
   const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const uint32_t crank = cluster_rank(), half = crank & 1u, even = crank & ~1u, rank = crank / 2u;
   const uint32_t pairs = gridDim.x / (2u * g.split), pair = blockIdx.x / (2u * g.split);  // clusters, each on tiles of its own
@@ -399,40 +472,30 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
   if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
   const uint32_t chunks = lp.kp / 32u, steps = (chunks + kStepChunks - 1u) / kStepChunks;
   const uint32_t first = (uint32_t)((uint64_t)steps * rank / g.split), last = (uint32_t)((uint64_t)steps * (rank + 1u) / g.split);
-  const uint32_t blocks_p = (g.n + 127u) / 128u, blocks_q = (g.m + 127u) / 128u;
   const uint32_t tiles = ok ? g.tiles_m * g.tiles_n : 0u;
   bool good = true;
   if (warp == 8) {
     if (lane == 0) {
-      uint32_t i = 0;
+      uint32_t loaded = 0;
+      const uint32_t silent = half ? g.silent : ~0u;
       Turn<S::kStages> turn;
       for (uint32_t tile = pair; tile < tiles && good; tile += pairs) {
-        const PairTile where(tile, g.tiles_m, g.tiles_n);
-        const uint32_t bp0 = where.n * 2u, bq0 = where.m * 2u, bp = bp0 + half, bq = bq0 + half;
-        const uint32_t np = min(2u, blocks_p - bp0), nq = min(2u, blocks_q - bq0);  // blocks that there are
-        const bool p_whole = lp.block_rows(min(bp, blocks_p - 1u)) == 128u, q_whole = lq.block_rows(min(bq, blocks_q - 1u)) == 128u;
-        const uint32_t bytes = (np + nq) * S::kOp + (np + 2u * nq) * S::kS;  // of both CTAs
-        const uint32_t zp = p_whole ? bp * chunks : 0u, zq = q_whole ? bq * chunks : 0u;
-        for (uint32_t it = first; it < last; ++it, ++i, turn.next()) {
-          const uint32_t s = turn.stage;
-          if (i >= (uint32_t)S::kStages && !mbar_poll<true>(empty + s, turn.round ^ 1u, kWaitPolls, abort)) {
-            *abort = 1u;
+        const PairLoads<F> t(g, tile, half);
+        for (uint32_t it = first; it < last; ++it, ++loaded, turn.next()) {
+          if (loaded == silent) {
             good = false;
             break;
           }
-          const uint32_t st = smem_u32(smem) + s * S::kStage, sc = st + 2u * S::kOp, bar = at_rank(full + s, even);
-          if (half == 0u) mbar_expect_tx(full + s, bytes);
-          if (half < np) tma_pair_3d(st, p_whole ? &pa.b.codes : &pa.b.rest, 0u, 0u, zp + it * kStepChunks, bar);
-          if (half < nq) tma_pair_3d(st + S::kOp, q_whole ? &pa.a.codes : &pa.a.rest, 0u, 0u, zq + it * kStepChunks, bar);
-          const uint32_t word = it * S::kAtoms;
-          if (half < np) tma_pair_2d(sc, &pa.b.scales, 0u, (bp * lp.atoms + word) * 4u, bar);
-          tma_pair_2d(sc + S::kS, &pa.a.scales, 0u, (bq0 * lq.atoms + word) * 4u, bar);
-          if (nq > 1u) tma_pair_2d(sc + 2u * S::kS, &pa.a.scales, 0u, ((bq0 + 1u) * lq.atoms + word) * 4u, bar);
+          if (loaded >= (uint32_t)S::kStages && !mbar_poll<true>(empty + turn.stage, turn.round ^ 1u, g.polls, abort)) {
+            raise_cluster(abort, 2u * g.split);
+            good = false;
+            break;
+          }
+          loads[1u + turn.stage] = half ? t.mine : t.bytes - t.mine;
+          t.load(pa, smem, full, it, turn.stage, half, even);
         }
       }
-      // nothing may be in flight when a CTA ends
-      if (half == 0u)
-        for (uint32_t w = i > (uint32_t)S::kStages ? i - S::kStages : 0u; w < i; ++w) mbar_wait(full + w % S::kStages, w / S::kStages & 1u, kDrainPolls);
+      *loads = loaded;
     }
   } else if (warp == 9) {
     if (lane == 0 && half == 0u) {  // (issues for both)
@@ -440,15 +503,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
       uint32_t n = 0;
       Turn<S::kStages> turn;
       for (uint32_t tile = pair; tile < tiles && good; tile += pairs, ++n) {
-        if (n && !mbar_poll<true>(taken, (n - 1u) & 1u, kWaitPolls, abort)) {
-          *abort = 1u;
+        if (n && !mbar_poll<true>(taken, (n - 1u) & 1u, g.polls, abort)) {
+          raise_cluster(abort, 2u * g.split);
           break;
         }
         tc_fence_after();
         for (uint32_t it = first; it < last; ++it, turn.next()) {
           const uint32_t s = turn.stage, ph = turn.round;
-          if (!mbar_poll<true>(ready + s, ph, kWaitPolls, abort)) {
-            *abort = 1u;
+          if (!mbar_poll<true>(ready + s, ph, g.polls, abort)) {
+            raise_cluster(abort, 2u * g.split);
             good = false;
             break;
           }
@@ -464,13 +527,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
               tc_mma_mx_pair<F == kMxB32>(tmem, da + 256u * x, db + 256u * x, mx_idesc(256u, 256u, F == kMxB32, id), sa + 4u * word, sb + 8u * word,
                                           it > first || x > 0u);
             }
-          tc_commit_pair(empty + s, both);
+          if (it + (uint32_t)S::kStages < last || tile + pairs < tiles) tc_commit_pair(empty + s, both);
         }
-        tc_commit_pair(sums, both);
-      }
-      if (*abort) {
-        tc_commit_pair(idle, (uint16_t)(1u << even));
-        mbar_wait(idle, 0u, kDrainPolls);
+        if (good) tc_commit_pair(sums, both);
       }
     }
   } else if (warp == 10) {
@@ -479,8 +538,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
       for (uint32_t tile = pair; tile < tiles && good; tile += pairs)
         for (uint32_t it = first; it < last; ++it, turn.next()) {
           const uint32_t s = turn.stage;
-          if (!mbar_poll<true>(full + s, turn.round, kWaitPolls, abort)) {
-            *abort = 1u;
+          if (!mbar_poll<true>(full + s, turn.round, g.polls, abort)) {
+            raise_cluster(abort, 2u * g.split);
             good = false;
             break;
           }
@@ -498,18 +557,17 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
             }
           tc_commit_pair(ready + s, (uint16_t)(1u << even));
         }
-      if (*abort) {
-        tc_commit_pair(idle + 1, (uint16_t)(1u << even));
-        mbar_wait(idle + 1, 0u, kDrainPolls);
-      }
     }
   } else {
     const ProductScale scaled(ea, eb, g.alpha);
     const uint32_t side = warp / 4u * 128u;  // columns of the accumulator: rows of A
     uint32_t n = 0;
     for (uint32_t tile = pair; tile < tiles && good; tile += pairs, ++n) {
-      good = mbar_poll_warp(sums, n & 1u, kWaitPolls, abort);
-      if (!good) break;
+      good = mbar_poll_warp(sums, n & 1u, g.polls, abort);
+      if (!good) {
+        if (lane == 0) raise_cluster(abort, 2u * g.split);
+        break;
+      }
       tc_fence_after();
       const PairTile where(tile, g.tiles_m, g.tiles_n);
       const uint32_t col = where.n * 256u + half * 128u + warp % 4u * 32u + lane, row = where.m * 256u + side;
@@ -550,7 +608,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
   tc_fence_before();
   if (g.split > 1u) {
     cluster_sync();
-    if (warp < 8u && good && tiles) {
+    if (warp < 8u && tiles && !*abort) {
       const ProductScale scaled(ea, eb, g.alpha);
       const PairTile where(pair, g.tiles_m, g.tiles_n);
       const uint32_t p = warp % 4u * 32u + lane, col = where.n * 256u + half * 128u + p, row = where.m * 256u;
@@ -570,9 +628,36 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx_product_pair_kernel(const 
         }
     }
   }
-  if (*abort && lane == 0 && g.status) *g.status = status_word(kErrTimeout);
   __syncthreads();
   cluster_sync();  // (a pair's memory serves both until both are done)
+  if (*abort) {    // (in all CTAs of the cluster or in none; see "Waits" above)
+    uint64_t* bars = reinterpret_cast<uint64_t*>(stages_at(smem_raw, hidden_zero()) + S::kStages * S::kStage);
+    const uint32_t me = cluster_rank(), who = threadIdx.x;
+    if (me % 2u == 0u && who == 8u * 32u) {
+      // The pair's loading threads may have stopped at different stages, and a barrier counts the bytes of both: those that the odd CTA
+      // has not asked for are taken off, those that it alone has asked for are expected.
+      const uint32_t* count = reinterpret_cast<const uint32_t*>(bars + PairBars<F>::kWords) + 2;
+      const uint32_t mine = count[0], other = ld_cluster_u32(count, me ^ 1u), most = max(mine, other);
+#pragma unroll 1
+      for (uint32_t w = min(mine, other); w < most; ++w) {
+        const uint32_t s = w % S::kStages;
+        if (mine < other)
+          mbar_expect_tx(bars + s, ld_cluster_u32(count + 1 + s, me ^ 1u));
+        else
+          mbar_complete_tx(bars + s, count[1 + s]);
+      }
+#pragma unroll 1
+      for (uint32_t w = most > (uint32_t)S::kStages ? most - S::kStages : 0u; w < most; ++w) mbar_wait(bars + w % S::kStages, w / S::kStages & 1u, kDrainPolls);
+    }
+    if (me % 2u == 0u && (who == 9u * 32u || who == 10u * 32u)) {
+      uint64_t* bar = bars + PairBars<F>::kIdle + (who / 32u - 9u);
+      tc_commit_pair(bar, (uint16_t)(1u << me));
+      mbar_wait(bar, 0u, kDrainPolls);
+    }
+    if (who == 0u && g.status) *g.status = status_word(kErrTimeout);
+    __syncthreads();
+    cluster_sync();
+  }
   if (warp == 9) tmem_free_pair(tmem, S::kCols);
 }
 
