@@ -349,6 +349,13 @@ def _ptr(t, dev: int, elements: int = 0, esize: int = 1) -> Optional[int]:
     return t.data_ptr()
 
 
+def _status_ptr(t, dev: int) -> Optional[int]:
+    """A status word's address: the library writes eight bytes there."""
+    if t is not None and (t.element_size() != 8 or t.is_floating_point() or t.is_complex() or t.numel() < 1):
+        raise ValueError(f"a status of {t.dtype} and shape {tuple(t.shape)}, where an int64 or uint64 is wanted")
+    return _ptr(t, dev)
+
+
 def _on(stream, dev: int) -> int:
     return _torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
 
@@ -373,7 +380,7 @@ def fh_mx_compress(m: fh_matrix, p: fh_mx_params, src, rows=None, cols=None, str
 def fh_mx_decompress(src, m: fh_matrix, format: int, dst, status=None, stream=None) -> int:
     """Enqueue restoring the container `src` (uint8) into `dst`, which `m` describes."""
     dev = _device()
-    return lib().fh_mx_decompress(_ptr(src, dev), src.nbytes, m, format, _ptr(dst, dev, _extent(m), _esize(m.dtype)), _ptr(status, dev),
+    return lib().fh_mx_decompress(_ptr(src, dev), src.nbytes, m, format, _ptr(dst, dev, _extent(m), _esize(m.dtype)), _status_ptr(status, dev),
                                   _on(stream, dev))
 
 
@@ -386,7 +393,7 @@ def fh_mx_product(d: fh_mx_product_desc, a, b, c, status=None, stream=None) -> i
     """Enqueue the product of the containers `a` (m x k) and `b` (n x k), uint8 CUDA tensors, into the matrix `c` (m x n)."""
     dev = _device()
     return lib().fh_mx_product(d, _ptr(a, dev), a.nbytes, _ptr(b, dev), b.nbytes, _ptr(c, dev, max(0, (d.m - 1) * d.ldc + d.n), _esize(d.dtype)),
-                               _ptr(status, dev), _on(stream, dev))
+                               _status_ptr(status, dev), _on(stream, dev))
 
 
 def norm_desc(rows: int, cols: int, dtype: int = FH_F32, wdtype: int = FH_F32, eps: float = 1e-5, ldx: Optional[int] = None,
@@ -423,7 +430,7 @@ def fh_layer_norm_backward(d: fh_norm_desc, dy, x, gamma, mean, rstd, dx, dgamma
     return lib().fh_layer_norm_backward(d, _ptr(dy, dev, ny, es), _ptr(x, dev, *((nx, es) if packed is None else ())),
                                         0 if packed is None else x.nbytes, 0 if packed is None else packed, _ptr(gamma, dev, d.cols, ws),
                                         _ptr(mean, dev, d.rows, 4), _ptr(rstd, dev, d.rows, 4), _ptr(dx, dev, nx, es), _ptr(dgamma, dev, d.cols, ws),
-                                        _ptr(dbeta, dev, d.cols, ws), _ptr(work, dev), 0 if work is None else work.nbytes, _ptr(status, dev),
+                                        _ptr(dbeta, dev, d.cols, ws), _ptr(work, dev), 0 if work is None else work.nbytes, _status_ptr(status, dev),
                                         _on(stream, dev))
 
 
