@@ -334,18 +334,43 @@ def _device() -> int:
     return _torch._C._cuda_getDevice()
 
 
-def _ptr(t, dev: int, elements: int = 0, esize: int = 1) -> Optional[int]:
+def _lies(t, rows: int, cols: int, ld: int) -> bool:
+    """Whether a tensor's elements lie where those of a rows x cols matrix of leading dimension `ld` do."""
+    dims = []    # (size, stride), neighbouring dimensions that are one joined
+    for n, s in zip(t.shape, t.stride()):
+        if n == 1:
+            continue
+        if dims and dims[-1][1] == n * s:
+            dims[-1] = (dims[-1][0] * n, s)
+        else:
+            dims.append((n, s))
+    if rows > 1 and cols > 1 and ld == cols:
+        rows, cols = 1, rows * cols
+    if dims and (cols > 1 or (dims[-1][1] == 1 and len(dims) > 1)):
+        n, s = dims.pop()
+        if s != 1 or n < cols:
+            return False
+    elif cols > 1:
+        return False
+    return rows == 1 or (bool(dims) and dims[-1][0] >= rows and dims[-1][1] == ld)
+
+
+def _ptr(t, dev: int, elements: int = 0, esize: int = 1, shape: Optional[Tuple[int, int, int]] = None) -> Optional[int]:
     """A tensor's address, once it is known to hold `elements` of `esize` bytes on the device `dev` (the library takes addresses
-    and cannot see what they belong to)."""
+    and cannot see what they belong to), a view those of `shape` (rows, cols, ld) in their places."""
     if t is None:
         return None
     if t.get_device() != dev:
         raise ValueError(f"a tensor on {t.device}, where cuda:{dev} is the current device")
-    if not elements and not t.is_contiguous():
-        raise ValueError("a buffer that is not contiguous")
-    if elements and (t.element_size() != esize or not (t.numel() >= elements and t.is_contiguous()) and
-                     t.untyped_storage().nbytes() < (t.storage_offset() + elements) * esize):
+    whole = t.is_contiguous()
+    if not elements:
+        if not whole:
+            raise ValueError("a buffer that is not contiguous")
+    elif t.element_size() != esize or not (whole and t.numel() >= elements) and \
+            t.untyped_storage().nbytes() < (t.storage_offset() + elements) * esize:
         raise ValueError(f"a tensor of {t.dtype} and shape {tuple(t.shape)}, where {elements} elements of {esize} bytes are wanted")
+    elif shape and not whole and t.stride() != (shape[2], 1) and not _lies(t, *shape):
+        raise ValueError(f"a tensor of shape {tuple(t.shape)} and strides {t.stride()}, where {shape[0]} rows of {shape[1]} elements, {shape[2]} apart, are wanted")
     return t.data_ptr()
 
 
@@ -360,9 +385,9 @@ def _on(stream, dev: int) -> int:
     return _torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
 
 
-def _extent(m) -> int:
-    """Elements from a matrix's first to its last, 0 where the library will refuse it."""
-    return max(0, (m.rows - 1) * m.ld + m.cols)
+def _dense(t, dev: int, rows: int, cols: int, ld: int, esize: int) -> Optional[int]:
+    """The address of a matrix (what the library will refuse is its own affair)."""
+    return _ptr(t, dev, max(0, (rows - 1) * ld + cols), esize, (rows, cols, ld))
 
 
 def _esize(dtype: int) -> int:
@@ -373,14 +398,14 @@ def fh_mx_compress(m: fh_matrix, p: fh_mx_params, src, rows=None, cols=None, str
     """Enqueue compression of the matrix `src` (a CUDA tensor that `m` describes) into the uint8 CUDA tensors `rows` (blocks
     along its rows) and `cols` (the transpose, blocks along the columns); either may be None."""
     dev = _device()
-    return lib().fh_mx_compress(m, p, _ptr(src, dev, _extent(m), _esize(m.dtype)), _ptr(rows, dev), 0 if rows is None else rows.nbytes,
+    return lib().fh_mx_compress(m, p, _dense(src, dev, m.rows, m.cols, m.ld, _esize(m.dtype)), _ptr(rows, dev), 0 if rows is None else rows.nbytes,
                                 _ptr(cols, dev), 0 if cols is None else cols.nbytes, _on(stream, dev))
 
 
 def fh_mx_decompress(src, m: fh_matrix, format: int, dst, status=None, stream=None) -> int:
     """Enqueue restoring the container `src` (uint8) into `dst`, which `m` describes."""
     dev = _device()
-    return lib().fh_mx_decompress(_ptr(src, dev), src.nbytes, m, format, _ptr(dst, dev, _extent(m), _esize(m.dtype)), _status_ptr(status, dev),
+    return lib().fh_mx_decompress(_ptr(src, dev), src.nbytes, m, format, _dense(dst, dev, m.rows, m.cols, m.ld, _esize(m.dtype)), _status_ptr(status, dev),
                                   _on(stream, dev))
 
 
@@ -392,7 +417,7 @@ def mx_product_desc(m: int, n: int, k: int, format: int = FH_MX_B32, dtype: int 
 def fh_mx_product(d: fh_mx_product_desc, a, b, c, status=None, stream=None) -> int:
     """Enqueue the product of the containers `a` (m x k) and `b` (n x k), uint8 CUDA tensors, into the matrix `c` (m x n)."""
     dev = _device()
-    return lib().fh_mx_product(d, _ptr(a, dev), a.nbytes, _ptr(b, dev), b.nbytes, _ptr(c, dev, max(0, (d.m - 1) * d.ldc + d.n), _esize(d.dtype)),
+    return lib().fh_mx_product(d, _ptr(a, dev), a.nbytes, _ptr(b, dev), b.nbytes, _dense(c, dev, d.m, d.n, d.ldc, _esize(d.dtype)),
                                _status_ptr(status, dev), _on(stream, dev))
 
 
@@ -401,20 +426,16 @@ def norm_desc(rows: int, cols: int, dtype: int = FH_F32, wdtype: int = FH_F32, e
     return fh_norm_desc(dtype, wdtype, rows, cols, eps, 0, cols if ldx is None else ldx, cols if ldy is None else ldy)
 
 
-def _spans(d: fh_norm_desc) -> Tuple[int, int, int, int]:
-    """Elements of x and of y from the first to the last, their size and that of a weight."""
-    return max(0, (d.rows - 1) * d.ldx + d.cols), max(0, (d.rows - 1) * d.ldy + d.cols), _esize(d.dtype), _esize(d.wdtype)
-
-
 def fh_layer_norm(d: fh_norm_desc, x, gamma, beta, y, mean=None, rstd=None, packed=None, params: Optional[fh_mx_params] = None,
                   stream=None) -> int:
     """Enqueue the layer norm of `x` into `y` (may be None) and, in 4 bits as `params` says, into the uint8 tensor `packed`; gamma, beta, mean
     and rstd may be None."""
-    nx, ny, es, ws = _spans(d)
+    rows, cols, es, ws = d.rows, d.cols, _esize(d.dtype), _esize(d.wdtype)
+    weight, stat = (1, cols, cols), (1, rows, rows)
     dev = _device()
-    return lib().fh_layer_norm(d, _ptr(x, dev, nx, es), _ptr(gamma, dev, d.cols, ws), _ptr(beta, dev, d.cols, ws), _ptr(y, dev, ny, es),
-                               _ptr(mean, dev, d.rows, 4), _ptr(rstd, dev, d.rows, 4), params, _ptr(packed, dev),
-                               0 if packed is None else packed.nbytes, _on(stream, dev))
+    return lib().fh_layer_norm(d, _dense(x, dev, rows, cols, d.ldx, es), _ptr(gamma, dev, cols, ws, weight), _ptr(beta, dev, cols, ws, weight),
+                               _dense(y, dev, rows, cols, d.ldy, es), _ptr(mean, dev, rows, 4, stat), _ptr(rstd, dev, rows, 4, stat), params,
+                               _ptr(packed, dev), 0 if packed is None else packed.nbytes, _on(stream, dev))
 
 
 def norm_work_bytes(d: fh_norm_desc) -> int:
@@ -425,13 +446,15 @@ def fh_layer_norm_backward(d: fh_norm_desc, dy, x, gamma, mean, rstd, dx, dgamma
                            status=None, stream=None) -> int:
     """Enqueue the layer norm's backward pass; `x` is dense, or with `packed` a container (uint8) of that format.  `work`: uint8, at
     least norm_work_bytes, where dgamma or dbeta is wanted."""
-    nx, ny, es, ws = _spans(d)
+    rows, cols, es, ws = d.rows, d.cols, _esize(d.dtype), _esize(d.wdtype)
+    weight, stat = (1, cols, cols), (1, rows, rows)
     dev = _device()
-    return lib().fh_layer_norm_backward(d, _ptr(dy, dev, ny, es), _ptr(x, dev, *((nx, es) if packed is None else ())),
-                                        0 if packed is None else x.nbytes, 0 if packed is None else packed, _ptr(gamma, dev, d.cols, ws),
-                                        _ptr(mean, dev, d.rows, 4), _ptr(rstd, dev, d.rows, 4), _ptr(dx, dev, nx, es), _ptr(dgamma, dev, d.cols, ws),
-                                        _ptr(dbeta, dev, d.cols, ws), _ptr(work, dev), 0 if work is None else work.nbytes, _status_ptr(status, dev),
-                                        _on(stream, dev))
+    return lib().fh_layer_norm_backward(d, _dense(dy, dev, rows, cols, d.ldy, es),
+                                        _dense(x, dev, rows, cols, d.ldx, es) if packed is None else _ptr(x, dev), 0 if packed is None else x.nbytes,
+                                        0 if packed is None else packed, _ptr(gamma, dev, cols, ws, weight), _ptr(mean, dev, rows, 4, stat),
+                                        _ptr(rstd, dev, rows, 4, stat), _dense(dx, dev, rows, cols, d.ldx, es), _ptr(dgamma, dev, cols, ws, weight),
+                                        _ptr(dbeta, dev, cols, ws, weight), _ptr(work, dev), 0 if work is None else work.nbytes,
+                                        _status_ptr(status, dev), _on(stream, dev))
 
 
 def debug_set(what: int, value: int) -> int:

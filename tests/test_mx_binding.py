@@ -58,3 +58,54 @@ def test_a_status_is_64_bits(calls):
                 torch.zeros(4, dtype=torch.int64)[::2]):
         for call in with_status(bad):
             refused(calls, call)
+
+
+def with_matrix(x, rows, cols, ld):
+    """Every call that has a dense matrix, with `x` in each place that `rows`, `cols` and `ld` describe."""
+    buf, m, d = torch.zeros(1 << 16, dtype=U8), api.matrix(rows, cols, api.FH_F32, ld), api.norm_desc(rows, cols, ldx=ld, ldy=ld)
+    other, one = torch.zeros(rows * ld), torch.zeros(rows)
+    return [lambda: api.fh_mx_compress(m, api.mx_params(), x, buf, None, STREAM),
+            lambda: api.fh_mx_decompress(buf, m, api.FH_MX_B32, x, None, STREAM),
+            lambda: api.fh_mx_product(api.mx_product_desc(rows, cols, 32, ldc=ld), buf, buf, x, None, STREAM),
+            lambda: api.fh_layer_norm(d, x, None, None, other, stream=STREAM),
+            lambda: api.fh_layer_norm(d, other, None, None, x, stream=STREAM),
+            lambda: api.fh_layer_norm_backward(d, x, other, None, one, one, other, stream=STREAM),
+            lambda: api.fh_layer_norm_backward(d, other, x, None, one, one, other, stream=STREAM),
+            lambda: api.fh_layer_norm_backward(d, other, other, None, one, one, x, stream=STREAM)]
+
+
+def test_a_matrix_lies_as_it_is_described(calls):
+    wide, deep = torch.zeros(64, 96), torch.zeros(4, 16, 96)
+    for x, rows, cols, ld in ((torch.zeros(8, 40), 8, 40, 40), (torch.zeros(320), 8, 40, 40), (torch.zeros(2, 4, 40), 8, 40, 40), (torch.zeros(4, 80), 8, 40, 40),
+                              (wide[:, :40], 64, 40, 96), (wide[8:, 5:45], 56, 40, 96), (wide[:, :40], 10, 30, 96), (wide[::2, :40], 32, 40, 192),
+                              (deep[:, :, 30:70], 64, 40, 96), (wide[3:4, :40], 1, 40, 96), (wide[3:4, :40], 1, 40, 40), (wide[:, 7], 64, 1, 96),
+                              (wide[:, 7:8], 64, 1, 96), (wide[:, 7:9], 64, 1, 96), (wide[0, :40], 1, 40, 40)):
+        for call in with_matrix(x, rows, cols, ld):
+            taken(calls, call)
+    for x, rows, cols, ld in ((wide[:, :40], 32, 40, 40),                  # rows 96 apart, described as 40 apart
+                              (wide[:, :40], 32, 40, 41), (torch.zeros(40, 8).t(), 8, 40, 40),
+                              (wide[:, :80:2], 20, 40, 96), (wide[:, :80:2], 20, 40, 192), (torch.zeros(2000)[::2], 8, 40, 40),
+                              (torch.zeros(4000)[:40].expand(8, 40), 8, 40, 40), (deep[:, :10, :40], 40, 40, 96),
+                              (wide[:, 7], 32, 1, 1), (wide[0, ::2], 1, 40, 40), (wide[:, :40].t(), 40, 64, 96)):
+        for call in with_matrix(x, rows, cols, ld):
+            refused(calls, call)
+
+
+def test_vectors_have_their_elements_side_by_side(calls):
+    x, y, d = torch.zeros(8, 40), torch.zeros(8, 40), api.norm_desc(8, 40)
+    work = torch.zeros(api.norm_work_bytes(d), dtype=U8)
+
+    def each(v, r):
+        return [lambda: api.fh_layer_norm(d, x, v, None, y, stream=STREAM), lambda: api.fh_layer_norm(d, x, None, v, y, stream=STREAM),
+                lambda: api.fh_layer_norm(d, x, None, None, y, r, None, stream=STREAM), lambda: api.fh_layer_norm(d, x, None, None, y, None, r, stream=STREAM),
+                lambda: api.fh_layer_norm_backward(d, x, y, v, r, r, None, v, v, work, stream=STREAM)]
+
+    for v, r in ((torch.zeros(40), torch.zeros(8)), (torch.zeros(1, 40), torch.zeros(8, 1)), (torch.zeros(100)[7:47], torch.zeros(4, 8)[1]),
+                 (torch.zeros(3, 100)[1:2, 5:45], torch.zeros(1, 8, 1))):
+        for call in each(v, r):
+            taken(calls, call)
+    fine_v, fine_r = torch.zeros(40), torch.zeros(8)
+    for v, r in ((torch.zeros(200)[::2], torch.zeros(64)[::2]), (torch.zeros(40, 40)[:, 3], torch.zeros(8, 8)[:, 3]),
+                 (torch.zeros(4000)[:1].expand(40), torch.zeros(4000)[:1].expand(8))):
+        for call in each(v, fine_r)[:2] + each(fine_v, r)[2:]:
+            refused(calls, call)
