@@ -334,6 +334,18 @@ def _device() -> int:
     return _torch._C._cuda_getDevice()
 
 
+_half = None
+
+
+def _is_half(t) -> bool:
+    """fp16, which has the size of bf16."""
+    global _half
+    if _half is None:
+        import torch
+        _half = torch.float16
+    return t.dtype is _half
+
+
 def _lies(t, rows: int, cols: int, ld: int) -> bool:
     """Whether a tensor's elements lie where those of a rows x cols matrix of leading dimension `ld` do."""
     dims = []    # (size, stride), neighbouring dimensions that are one joined
@@ -366,7 +378,7 @@ def _ptr(t, dev: int, elements: int = 0, esize: int = 1, shape: Optional[Tuple[i
     if not elements:
         if not whole:
             raise ValueError("a buffer that is not contiguous")
-    elif t.element_size() != esize or not (whole and t.numel() >= elements) and \
+    elif t.element_size() != esize or (esize == 2 and _is_half(t)) or not (whole and t.numel() >= elements) and \
             t.untyped_storage().nbytes() < (t.storage_offset() + elements) * esize:
         raise ValueError(f"a tensor of {t.dtype} and shape {tuple(t.shape)}, where {elements} elements of {esize} bytes are wanted")
     elif shape and not whole and t.stride() != (shape[2], 1) and not _lies(t, *shape):

@@ -109,3 +109,23 @@ def test_vectors_have_their_elements_side_by_side(calls):
                  (torch.zeros(4000)[:1].expand(40), torch.zeros(4000)[:1].expand(8))):
         for call in each(v, fine_r)[:2] + each(fine_v, r)[2:]:
             refused(calls, call)
+
+
+def test_fp16_is_not_taken_for_bf16(calls):
+    """Both have two bytes."""
+    buf, work = torch.zeros(1 << 16, dtype=U8), torch.zeros(1 << 16, dtype=U8)
+    m, d = api.matrix(8, 40, api.FH_BF16), api.norm_desc(8, 40, api.FH_BF16, api.FH_BF16)
+    r = torch.zeros(8)
+
+    def each(x, w):
+        return [lambda: api.fh_mx_compress(m, api.mx_params(), x, buf, None, STREAM), lambda: api.fh_mx_decompress(buf, m, api.FH_MX_B32, x, None, STREAM),
+                lambda: api.fh_mx_product(api.mx_product_desc(8, 40, 32, dtype=api.FH_BF16), buf, buf, x, None, STREAM),
+                lambda: api.fh_layer_norm(d, x, w, w, x, r, r, stream=STREAM),
+                lambda: api.fh_layer_norm_backward(d, x, x, w, r, r, x, w, w, work, stream=STREAM)]
+
+    bf = dict(dtype=torch.bfloat16)
+    for t in (torch.bfloat16, torch.uint16, torch.int16):    # (bits, as the plane codec's callers hold them)
+        for call in each(torch.zeros(8, 40, dtype=t), torch.zeros(40, dtype=t)):
+            taken(calls, call)
+    for call in each(torch.zeros(8, 40, dtype=torch.float16), torch.zeros(40, **bf)) + each(torch.zeros(8, 40, **bf), torch.zeros(40, dtype=torch.float16))[3:]:
+        refused(calls, call)
