@@ -412,7 +412,7 @@ int fh_mx_decompress(const void* d_src, size_t src_bytes, const fh_matrix* expec
  * A = x by rows, B = W by rows; the input's gradient A = dy by rows, B = W by columns; the weight's gradient A = dy by columns, B = x by
  * columns.  Where the blocks along k of a row of A or B hold a NaN scale, that row (column) of C is NaN.
  *   d_a, d_b    containers of an m x k and an n x k matrix; another header is FH_ERR_CORRUPT (through d_status; C is not written then)
- *   d_c         element (i, j) at i * ldc + j; FH_ERR_ARG when it overlaps a container
+ *   d_c         element (i, j) at i * ldc + j; FH_ERR_ARG when it overlaps a container (or d_status any of the three)
  *   d_status    optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status.  FH_ERR_TIMEOUT: a wait inside the
  *               kernel ran out (C is undefined then, the library stays usable)
  * Results do not depend on the call's place among others: equal inputs give equal bits.
@@ -454,6 +454,8 @@ typedef struct {
  *   d_mean, d_rstd    rows floats for the backward pass, either may be NULL
  *   params, d_packed  container of y (blocks along its rows, rounding to nearest), packed_capacity bytes; byte for byte what
  *                     fh_mx_compress makes of the dense y in its type; may be NULL
+ * FH_ERR_ARG when an output has a byte in common with an input or another output, other than d_y = d_x as above (rows of x and y that lie
+ * between one another's, as in slices of a wider matrix, have none).
  */
 int fh_layer_norm(const fh_norm_desc* desc, const void* d_x, const void* d_gamma, const void* d_beta, void* d_y, float* d_mean,
                   float* d_rstd, const fh_mx_params* params, void* d_packed, size_t packed_capacity, void* stream);
@@ -468,6 +470,8 @@ int fh_layer_norm(const fh_norm_desc* desc, const void* d_x, const void* d_gamma
  *   d_work            caller-owned workspace, 16-byte aligned, at least fh_layer_norm_work_bytes(desc) bytes, needed when d_dgamma or
  *                     d_dbeta is given; calls that may run at the same time need one each
  *   d_status          optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
+ * FH_ERR_ARG when an output, the workspace or the status has a byte in common with an input or another of them, other than d_dx as above and
+ * d_dgamma or d_dbeta over dense inputs, which have been read by then.
  * One kernel, and a second, small one for dgamma and dbeta.  Sums are fp32 in a fixed order: equal inputs, strides and alignments give
  * equal bits.
  */

@@ -4,6 +4,8 @@
 
 #include <cuda_runtime.h>
 
+#include <algorithm>
+
 #include "fh_launch.cuh"
 #include "fh_mx.cuh"
 #include "fh_mx_launch.cuh"
@@ -29,6 +31,38 @@ bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
 }
 // Bytes from the first to the last of a matrix.
 size_t extent(int64_t rows, int64_t cols, int64_t ld, int dtype) { return ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * esize_of(dtype); }
+
+// Rows of `width` bytes, `step` apart (a vector, a container: one).
+struct Rows {
+  uintptr_t at;
+  uint64_t rows, step, width;  // width <= step
+  Rows(const void* p, uint64_t bytes) : at((uintptr_t)p), rows(1), step(bytes), width(bytes) {}
+  Rows(const void* p, int64_t r, int64_t cols, int64_t ld, int dtype) : at((uintptr_t)p), rows(r), step((uint64_t)ld * esize_of(dtype)), width((uint64_t)cols * esize_of(dtype)) {}
+  uint64_t end() const { return at + (rows - 1) * step + width; }
+};
+// Whether they have a byte in common; rows that lie between one another's have none.
+bool meet(const Rows& a, const Rows& b) {
+  if (!a.at || !b.at || a.at >= b.end() || b.at >= a.end()) return false;
+  if (a.rows > b.rows) return meet(b, a);
+  if (a.rows > 1 && a.step == b.step) {
+    // row j of b begins d + (j - i) * step behind row i of a: only the two distances next to zero, `near` and `near - step`, can be too small
+    const int64_t step = (int64_t)a.step, d = (int64_t)(b.at - a.at), less = d >= 0 ? d / step : -((-d + step - 1) / step);
+    const uint64_t near = (uint64_t)(d - less * step);
+    auto there = [&](int64_t rows) { return rows > -(int64_t)a.rows && rows < (int64_t)b.rows; };  // j - i
+    return (near < a.width && there(-less)) || (a.step - near < b.width && there(-less - 1));
+  }
+  for (uint64_t i = 0; i < a.rows; ++i) {
+    const uint64_t x = a.at + i * a.step, j = x > b.at ? std::min<uint64_t>((x - b.at) / b.step, b.rows - 1) : 0, y = b.at + j * b.step;
+    if (x < y + b.width && y < x + a.width) return true;
+    if (j + 1 < b.rows && y + b.step < x + a.width) return true;
+  }
+  return false;
+}
+// Whether the first of them meets one of the others.
+template <typename... T>
+bool meets(const Rows& a, const T&... others) {
+  return (meet(a, others) || ...);
+}
 
 int check_mx(const fh_mx_params* p) {
   if (!p || !is_format(p->format) || p->reserved != 0) return FH_ERR_ARG;
@@ -102,6 +136,8 @@ int fh_mx_decompress(const void* d_src, size_t src_bytes, const fh_matrix* expec
     return FH_ERR_ARG;
   if (overlap(d_src, fh_mx_bytes(expect->rows, expect->cols, format), d_dst, extent(expect->rows, expect->cols, expect->ld, expect->dtype)))
     return FH_ERR_ARG;
+  if (meets(Rows(d_status, 8), Rows(d_src, fh_mx_bytes(expect->rows, expect->cols, format)), Rows(d_dst, expect->rows, expect->cols, expect->ld, expect->dtype)))
+    return FH_ERR_ARG;
   fh::MxSaveArgs a = {};
   a.src = (const uint8_t*)d_src;
   a.src_bytes = src_bytes;
@@ -124,6 +160,9 @@ int fh_mx_product(const fh_mx_product_desc* desc, const void* d_a, size_t a_byte
     return FH_ERR_ARG;
   const size_t out = extent(desc->m, desc->n, desc->ldc, desc->dtype);
   if (overlap(d_c, out, d_a, fh_mx_bytes(desc->m, desc->k, desc->format)) || overlap(d_c, out, d_b, fh_mx_bytes(desc->n, desc->k, desc->format)))
+    return FH_ERR_ARG;
+  if (meets(Rows(d_status, 8), Rows(d_a, fh_mx_bytes(desc->m, desc->k, desc->format)), Rows(d_b, fh_mx_bytes(desc->n, desc->k, desc->format)),
+            Rows(d_c, desc->m, desc->n, desc->ldc, desc->dtype)))
     return FH_ERR_ARG;
   fh::MxProductArgs a = {};
   a.a = (const uint8_t*)d_a;
@@ -165,6 +204,13 @@ int fh_layer_norm(const fh_norm_desc* desc, const void* d_x, const void* d_gamma
     a.exponent = params->exponent;
     a.tensor_id = params->tensor_id;
   }
+  const Rows x(d_x, desc->rows, desc->cols, desc->ldx, desc->dtype), y(d_y, desc->rows, desc->cols, desc->ldy, desc->dtype);
+  const Rows gamma(d_gamma, desc->cols * ws), beta(d_beta, desc->cols * ws), mean(d_mean, desc->rows * sizeof(float)), rstd(d_rstd, desc->rows * sizeof(float));
+  const Rows packed(d_packed, d_packed ? fh_mx_bytes(desc->rows, desc->cols, params->format) : 1);
+  const bool in_place = d_y == d_x && (desc->ldx == desc->ldy || desc->rows == 1);
+  if ((!in_place && meet(y, x)) || meets(y, gamma, beta) || meets(mean, x, gamma, beta, y) || meets(rstd, x, gamma, beta, y, mean) ||
+      meets(packed, gamma, beta, mean, rstd))
+    return FH_ERR_ARG;
   a.x = (const uint8_t*)d_x;
   a.gamma = (const uint8_t*)d_gamma;
   a.beta = (const uint8_t*)d_beta;
@@ -196,6 +242,17 @@ int fh_layer_norm_backward(const fh_norm_desc* desc, const void* d_dy, const voi
     if (!d_work) return FH_ERR_ARG;
     if (work_bytes < fh_layer_norm_work_bytes(desc)) return FH_ERR_CAPACITY;
     a.work = (float*)d_work;
+  }
+  {
+    const Rows dy(d_dy, desc->rows, desc->cols, desc->ldy, desc->dtype), dx(d_dx, desc->rows, desc->cols, desc->ldx, desc->dtype);
+    const Rows x = x_bytes ? Rows(d_x, fh_mx_bytes(desc->rows, desc->cols, x_format)) : Rows(d_x, desc->rows, desc->cols, desc->ldx, desc->dtype);
+    const Rows gamma(d_gamma, weights), dgamma(d_dgamma, weights), dbeta(d_dbeta, weights), work(a.work, a.work ? fh_layer_norm_work_bytes(desc) : 1);
+    const Rows mean(d_mean, desc->rows * sizeof(float)), rstd(d_rstd, desc->rows * sizeof(float)), status(d_status, 8);
+    const bool over_dy = d_dx == d_dy && (desc->ldx == desc->ldy || desc->rows == 1), over_x = d_dx == d_x && !x_bytes;
+    if ((!over_dy && meet(dx, dy)) || (!over_x && meet(dx, x)) || meets(dx, gamma, mean, rstd, dgamma, dbeta)) return FH_ERR_ARG;
+    if (meets(work, dy, x, gamma, mean, rstd, dx, dgamma, dbeta) || meets(status, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, work)) return FH_ERR_ARG;
+    // (the weights' gradients may lie over dense inputs: the second kernel writes them; a container's header it reads)
+    if (x_bytes && (meet(x, dgamma) || meet(x, dbeta))) return FH_ERR_ARG;
   }
   a.dy = (const uint8_t*)d_dy;
   a.x = (const uint8_t*)d_x;
