@@ -433,9 +433,9 @@ int fh_mx_product(const fh_mx_product_desc* desc, const void* d_a, size_t a_byte
 /*
  * Layer norm with its output, and its saved input, in 4 bits.
  *
- * y = (x - mean) * rstd * gamma + beta over each row, mean and variance (divisor cols) of the row, rstd = 1 / sqrt(variance + eps).  A
- * linear layer behind it reads y from the container that the same kernel writes; the backward pass reads x from a container, so that
- * neither has to be kept dense.
+ * y = (x - mean) * rstd * gamma + beta over each row, mean (the fp32 sum divided by cols, rounded once) and variance (divisor cols) of
+ * the row, rstd = 1 / sqrt(variance + eps).  A linear layer behind it reads y from the container that the same kernel writes; the
+ * backward pass reads x from a container, so that neither has to be kept dense.
  */
 typedef struct {
   int32_t dtype;    /* fh_dtype of x, y, dy, dx                                                */
