@@ -124,7 +124,7 @@ __device__ __forceinline__ float mx_quotient(float x, const MxScale& s) {
   return F == kMxB32 ? x * s.hi : __fmaf_rn(x, s.hi, x * s.lo);
 }
 
-// Random rounding: x between two neighbouring magnitudes L and L + step (times the scale) goes up when what it is beyond L is
+// Random rounding (of finite x with quotients below 2^105): x between two neighbouring magnitudes L and L + step (times the scale) goes up when what it is beyond L is
 // more than (r + 1/2) / 2^16 of the step, r a uniform 16-bit integer; exact, as the left side is an fp32 number and the right
 // side has at most 17 + 4 bits.  Leaves the magnitude with x's sign.  `draw`: bits of 1 + r / 2^16; `s_full`: the
 // scale with 2^exponent (B16; exact, as x is then compared as it is).

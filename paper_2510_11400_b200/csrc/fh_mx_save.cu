@@ -137,6 +137,19 @@ __device__ __forceinline__ uint32_t encode_block(G get, uint32_t top, float scal
   return s.byte;
 }
 
+// Random rounding, blocks of 16: magnitudes beyond eight times the largest scale become that, which is stored as 6 all the same; mx_random2's
+// arithmetic holds for quotients up to 2^105 only.  (Blocks that have such a value are rare, and the others pay one comparison.)
+// `top`: bits of the block's largest magnitude, in bf16 of both columns' that a word holds.
+template <int F, bool RANDOM, int DT, int W>
+__device__ __forceinline__ void clip_far(uint32_t (&w)[W], uint32_t top, int32_t exponent) {
+  if (F != kMxB16 || !RANDOM) return;
+  const uint32_t far = (uint32_t)(138 + exponent) << 23 | 0x00600000u;  // 8 * 448 * 2^exponent = 1.75 * 2^(11 + exponent)
+  if (top <= far) return;
+#pragma unroll
+  for (int i = 0; i < W; ++i)
+    w[i] = DT == kF32 ? (w[i] & 0x80000000u) | min(w[i] & 0x7FFFFFFFu, far) : (w[i] & 0x80008000u) | __vminu2(w[i] & 0x7FFF7FFFu, far >> 16 | far);
+}
+
 __device__ __forceinline__ float bf_lo(uint32_t w) { return bits_f(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return bits_f(w & 0xFFFF0000u); }
 
@@ -193,11 +206,13 @@ __global__ void __launch_bounds__(kSaveThreads) mx_compress_kernel(const __grid_
         if (DT == kF32) {
 #pragma unroll
           for (int i = 0; i < W; ++i) top = max(top, w[i] & 0x7FFFFFFFu);
+          clip_far<F, RANDOM, DT>(w, top, a.exponent);
           byte = encode_block<F, RANDOM, NB>([&](int i) { return bits_f(w[i]); }, top, scale, unscale, row, col + h * NB, key, codes + h * (NB / 8));
         } else {
 #pragma unroll
           for (int i = 0; i < W; ++i) top = __vmaxu2(top, w[i] & 0x7FFF7FFFu);
           top = max(top << 16, top & 0xFFFF0000u);
+          clip_far<F, RANDOM, DT>(w, top, a.exponent);
           byte = encode_block<F, RANDOM, NB>([&](int i) { return i % 2 ? bf_hi(w[i / 2]) : bf_lo(w[i / 2]); }, top, scale, unscale, row,
                                              col + h * NB, key, codes + h * (NB / 8));
         }
@@ -222,6 +237,7 @@ __global__ void __launch_bounds__(kSaveThreads) mx_compress_kernel(const __grid_
         for (int i = 0; i < NB; ++i) w[i] = *reinterpret_cast<const uint32_t*>(p + (h * NB + i) * kPitch<DT>);
 #pragma unroll
         for (int i = 0; i < NB; ++i) top = DT == kF32 ? max(top, w[i] & 0x7FFFFFFFu) : __vmaxu2(top, w[i] & 0x7FFF7FFFu);
+        clip_far<F, RANDOM, DT>(w, DT == kF32 ? top : max(top << 16, top & 0xFFFF0000u), a.exponent);
 #pragma unroll
         for (int q = 0; q < CW; ++q) {
           uint32_t byte;
