@@ -61,11 +61,11 @@ static_assert(sizeof(MxHeader) == kMxHeadBytes, "MxHeader layout");
 
 // Whether a container is the one expected, and its exponent.  (Rounding and tensor id do not matter to a reader.)
 __device__ __forceinline__ bool mx_header_ok(const uint8_t* src, uint64_t src_bytes, const MxLayout& l, int32_t* exponent) {
-  if (src_bytes < l.total) return false;  // (the host has refused src_bytes < 128)
+  if (src_bytes < l.total) return false;  // (so that the header is there to be read)
   const uint4 a = *reinterpret_cast<const uint4*>(src), b = *reinterpret_cast<const uint4*>(src + 16);
   *exponent = (int32_t)b.x;
   return a.x == kMxMagic && (a.y & 0x00FFFFFFu) == (1u | l.format << 16) && a.z == l.rows && a.w == l.cols && b.y == 0u &&
-         ((uint64_t)b.w << 32 | b.z) == l.total && *exponent >= -64 && *exponent <= 64;
+         ((uint64_t)b.w << 32 | b.z) == l.total && (l.format == kMxB32 ? *exponent == 0 : *exponent >= -64 && *exponent <= 64);
 }
 
 __device__ __forceinline__ float bits_f(uint32_t u) { return __uint_as_float(u); }
