@@ -872,6 +872,8 @@ __global__ void __launch_bounds__(kNormThreads, V < 4 ? 2 : 1) norm_backward_ker
 // (i E + e) * TEAM + t, so that a warp's accesses are neighbours.  (4096 x 16000 bf16: half the threads, and sums in the order of the columns,
 // 422 us.)
 constexpr int kWideThreads = 512;
+// Vectors of a row whose sums the kernel holds.
+constexpr uint32_t wide_vecs(uint32_t vecs) { return (vecs + kWideThreads - 1u) / kWideThreads * kWideThreads; }
 template <int DT, bool VEC, int X>
 __global__ void __launch_bounds__(kWideThreads) norm_backward_wide_kernel(const NormArgs a) {
   constexpr int E = NormVec<DT>::kE, TEAM = kWideThreads;
@@ -1035,8 +1037,7 @@ int launch_backward_dx(const NormArgs& a, cudaStream_t stream) {
   if (vecs <= 256) return launch_backward_t<DT, 256, 1, VEC, X>(a, stream);
   if (vecs <= 512) return launch_backward_t<DT, 256, 2, VEC, X>(a, stream);
   if (vecs <= 1024) return launch_backward_t<DT, 256, 4, VEC, X>(a, stream);
-  const uint32_t wide = (vecs + kWideThreads - 1u) / kWideThreads * kWideThreads;
-  return launch_plain<norm_backward_wide_kernel<DT, VEC, X>>(a.parts, kWideThreads, (size_t)8 * wide * NormVec<DT>::kE, 1, stream, a);
+  return launch_plain<norm_backward_wide_kernel<DT, VEC, X>>(a.parts, kWideThreads, (size_t)8 * wide_vecs(vecs) * NormVec<DT>::kE, 1, stream, a);
 }
 template <int DT>
 int launch_backward_d(const NormArgs& a, bool vec, cudaStream_t stream) {
@@ -1051,10 +1052,13 @@ bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
 
 uint32_t norm_parts(uint32_t rows, uint32_t cols, int dtype) {
   // rows that make a CTA worth its sums: four to a team of a warp, of half a CTA, of a CTA (see launch_backward_dx), and one where a row takes
-  // 10 us (106 x 11902 fp32: 39 us with four)
-  const uint32_t vecs = (cols + (dtype == kF32 ? 3u : 7u)) / (dtype == kF32 ? 4u : 8u);
+  // 10 us (106 x 11902 fp32: 13 us, 37 with four)
+  const uint32_t e = dtype == kF32 ? 4u : 8u, vecs = (cols + e - 1u) / e;
   const uint32_t each = vecs <= 32u ? 32u : (vecs <= 128u ? 8u : (vecs <= 1024u ? 4u : 1u));
-  const uint32_t n = rows / each + (rows % each ? 1u : 0u), most = cols <= 14336u ? 296u : 148u;  // (beyond, the sums leave an SM room for one CTA: 4096 x 16000 bf16 215 us and 233)
+  // Two CTAs to an SM; one where rows keep their sums in shared memory and those of two do not fit (4096 x 16000 bf16 215 us and 236,
+  // 4096 x 13000, whose columns are rounded up to as many, 211 and 229).
+  const uint32_t wide = vecs > 1024u ? wide_vecs(vecs) * e : 0u;
+  const uint32_t n = rows / each + (rows % each ? 1u : 0u), most = wide <= 14336u ? 296u : 148u;
   return n < most ? n : most;
 }
 
