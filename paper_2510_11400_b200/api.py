@@ -322,6 +322,7 @@ def mx_bytes(rows: int, cols: int, format: int) -> int:
 
 
 _torch = None
+_types = {}    # fh_dtype: torch's type, once a call has been made
 
 
 def _device() -> int:
@@ -330,6 +331,7 @@ def _device() -> int:
     if _torch is None:
         import torch
         torch.cuda.current_device()    # (initialises)
+        _types.update({FH_F32: torch.float32, FH_BF16: torch.bfloat16})
         _torch = torch
     return _torch._C._cuda_getDevice()
 
@@ -388,7 +390,9 @@ def _ptr(t, dev: int, elements: int = 0, esize: int = 1, shape: Optional[Tuple[i
 
 def _status_ptr(t, dev: int) -> Optional[int]:
     """A status word's address: the library writes eight bytes there."""
-    if t is not None and (t.element_size() != 8 or t.is_floating_point() or t.is_complex() or t.numel() < 1):
+    if t is None:
+        return None
+    if t.element_size() != 8 or t.is_floating_point() or t.is_complex() or t.numel() < 1:
         raise ValueError(f"a status of {t.dtype} and shape {tuple(t.shape)}, where an int64 or uint64 is wanted")
     return _ptr(t, dev)
 
@@ -397,9 +401,15 @@ def _on(stream, dev: int) -> int:
     return _torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream.cuda_stream)
 
 
-def _dense(t, dev: int, rows: int, cols: int, ld: int, esize: int) -> Optional[int]:
-    """The address of a matrix (what the library will refuse is its own affair)."""
-    return _ptr(t, dev, max(0, (rows - 1) * ld + cols), esize, (rows, cols, ld))
+def _dense(t, dev: int, rows: int, cols: int, ld: int, dtype: int) -> Optional[int]:
+    """The address of a matrix (what the library will refuse is its own affair).  What is plainly right is told at once."""
+    if t is not None and t.dtype is _types.get(dtype) and t.get_device() == dev:
+        if t.is_contiguous():
+            if t.numel() >= (rows - 1) * ld + cols:
+                return t.data_ptr()
+        elif t.stride() == (ld, 1) and t.size(0) >= rows and t.size(1) >= cols:
+            return t.data_ptr()
+    return _ptr(t, dev, max(0, (rows - 1) * ld + cols), _esize(dtype), (rows, cols, ld))
 
 
 def _esize(dtype: int) -> int:
@@ -410,14 +420,14 @@ def fh_mx_compress(m: fh_matrix, p: fh_mx_params, src, rows=None, cols=None, str
     """Enqueue compression of the matrix `src` (a CUDA tensor that `m` describes) into the uint8 CUDA tensors `rows` (blocks
     along its rows) and `cols` (the transpose, blocks along the columns); either may be None."""
     dev = _device()
-    return lib().fh_mx_compress(m, p, _dense(src, dev, m.rows, m.cols, m.ld, _esize(m.dtype)), _ptr(rows, dev), 0 if rows is None else rows.nbytes,
+    return lib().fh_mx_compress(m, p, _dense(src, dev, m.rows, m.cols, m.ld, m.dtype), _ptr(rows, dev), 0 if rows is None else rows.nbytes,
                                 _ptr(cols, dev), 0 if cols is None else cols.nbytes, _on(stream, dev))
 
 
 def fh_mx_decompress(src, m: fh_matrix, format: int, dst, status=None, stream=None) -> int:
     """Enqueue restoring the container `src` (uint8) into `dst`, which `m` describes."""
     dev = _device()
-    return lib().fh_mx_decompress(_ptr(src, dev), src.nbytes, m, format, _dense(dst, dev, m.rows, m.cols, m.ld, _esize(m.dtype)), _status_ptr(status, dev),
+    return lib().fh_mx_decompress(_ptr(src, dev), src.nbytes, m, format, _dense(dst, dev, m.rows, m.cols, m.ld, m.dtype), _status_ptr(status, dev),
                                   _on(stream, dev))
 
 
@@ -429,7 +439,7 @@ def mx_product_desc(m: int, n: int, k: int, format: int = FH_MX_B32, dtype: int 
 def fh_mx_product(d: fh_mx_product_desc, a, b, c, status=None, stream=None) -> int:
     """Enqueue the product of the containers `a` (m x k) and `b` (n x k), uint8 CUDA tensors, into the matrix `c` (m x n)."""
     dev = _device()
-    return lib().fh_mx_product(d, _ptr(a, dev), a.nbytes, _ptr(b, dev), b.nbytes, _dense(c, dev, d.m, d.n, d.ldc, _esize(d.dtype)),
+    return lib().fh_mx_product(d, _ptr(a, dev), a.nbytes, _ptr(b, dev), b.nbytes, _dense(c, dev, d.m, d.n, d.ldc, d.dtype),
                                _status_ptr(status, dev), _on(stream, dev))
 
 
@@ -442,12 +452,11 @@ def fh_layer_norm(d: fh_norm_desc, x, gamma, beta, y, mean=None, rstd=None, pack
                   stream=None) -> int:
     """Enqueue the layer norm of `x` into `y` (may be None) and, in 4 bits as `params` says, into the uint8 tensor `packed`; gamma, beta, mean
     and rstd may be None."""
-    rows, cols, es, ws = d.rows, d.cols, _esize(d.dtype), _esize(d.wdtype)
-    weight, stat = (1, cols, cols), (1, rows, rows)
+    rows, cols, t, w = d.rows, d.cols, d.dtype, d.wdtype
     dev = _device()
-    return lib().fh_layer_norm(d, _dense(x, dev, rows, cols, d.ldx, es), _ptr(gamma, dev, cols, ws, weight), _ptr(beta, dev, cols, ws, weight),
-                               _dense(y, dev, rows, cols, d.ldy, es), _ptr(mean, dev, rows, 4, stat), _ptr(rstd, dev, rows, 4, stat), params,
-                               _ptr(packed, dev), 0 if packed is None else packed.nbytes, _on(stream, dev))
+    return lib().fh_layer_norm(d, _dense(x, dev, rows, cols, d.ldx, t), _dense(gamma, dev, 1, cols, cols, w), _dense(beta, dev, 1, cols, cols, w),
+                               _dense(y, dev, rows, cols, d.ldy, t), _dense(mean, dev, 1, rows, rows, FH_F32),
+                               _dense(rstd, dev, 1, rows, rows, FH_F32), params, _ptr(packed, dev), 0 if packed is None else packed.nbytes, _on(stream, dev))
 
 
 def norm_work_bytes(d: fh_norm_desc) -> int:
@@ -458,14 +467,13 @@ def fh_layer_norm_backward(d: fh_norm_desc, dy, x, gamma, mean, rstd, dx, dgamma
                            status=None, stream=None) -> int:
     """Enqueue the layer norm's backward pass; `x` is dense, or with `packed` a container (uint8) of that format.  `work`: uint8, at
     least norm_work_bytes, where dgamma or dbeta is wanted."""
-    rows, cols, es, ws = d.rows, d.cols, _esize(d.dtype), _esize(d.wdtype)
-    weight, stat = (1, cols, cols), (1, rows, rows)
+    rows, cols, t, w = d.rows, d.cols, d.dtype, d.wdtype
     dev = _device()
-    return lib().fh_layer_norm_backward(d, _dense(dy, dev, rows, cols, d.ldy, es),
-                                        _dense(x, dev, rows, cols, d.ldx, es) if packed is None else _ptr(x, dev), 0 if packed is None else x.nbytes,
-                                        0 if packed is None else packed, _ptr(gamma, dev, cols, ws, weight), _ptr(mean, dev, rows, 4, stat),
-                                        _ptr(rstd, dev, rows, 4, stat), _dense(dx, dev, rows, cols, d.ldx, es), _ptr(dgamma, dev, cols, ws, weight),
-                                        _ptr(dbeta, dev, cols, ws, weight), _ptr(work, dev), 0 if work is None else work.nbytes,
+    return lib().fh_layer_norm_backward(d, _dense(dy, dev, rows, cols, d.ldy, t),
+                                        _dense(x, dev, rows, cols, d.ldx, t) if packed is None else _ptr(x, dev), 0 if packed is None else x.nbytes,
+                                        0 if packed is None else packed, _dense(gamma, dev, 1, cols, cols, w), _dense(mean, dev, 1, rows, rows, FH_F32),
+                                        _dense(rstd, dev, 1, rows, rows, FH_F32), _dense(dx, dev, rows, cols, d.ldx, t),
+                                        _dense(dgamma, dev, 1, cols, cols, w), _dense(dbeta, dev, 1, cols, cols, w), _ptr(work, dev), 0 if work is None else work.nbytes,
                                         _status_ptr(status, dev), _on(stream, dev))
 
 

@@ -11,8 +11,10 @@ STREAM = types.SimpleNamespace(cuda_stream=0)
 U8 = torch.uint8
 
 
-@pytest.fixture
-def calls(monkeypatch):
+@pytest.fixture(params=[False, True], ids=["first call", "later"])
+def calls(monkeypatch, request):
+    """The library's calls; torch's types are known to the binding from its first call on."""
+    monkeypatch.setattr(api, "_types", {api.FH_F32: torch.float32, api.FH_BF16: torch.bfloat16} if request.param else {})
     build.build()
     real, made = api.lib(), []
 
