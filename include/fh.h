@@ -376,7 +376,8 @@ typedef struct {
 typedef struct {
   int32_t format;   /* fh_mx_format                                                            */
   int32_t exponent; /* B16: the matrix's exponent, its largest magnitude is held when it is
-                       at most 2688 * 2^exponent; B32: 0                                         */
+                       at most 2688 * 2^exponent (what is larger becomes that, and nothing
+                       says so); B32: 0                                                          */
   int32_t rounding; /* 0 = to nearest, 1 = random                                              */
   int32_t reserved; /* 0                                                                       */
   uint64_t seed;    /* key of the random draws                                                 */
@@ -441,7 +442,7 @@ typedef struct {
   int32_t dtype;    /* fh_dtype of x, y, dy, dx                                                */
   int32_t wdtype;   /* fh_dtype of gamma, beta and their gradients                             */
   int32_t rows, cols; /* cols <= 28672 (FH_ERR_UNSUPPORTED beyond)                              */
-  float eps;        /* >= 0                                                                    */
+  float eps;        /* >= 0; with 0 a row without spread is NaN                                */
   int32_t reserved; /* 0                                                                       */
   int64_t ldx;      /* elements from one row of x (and of dx) to the next, >= cols            */
   int64_t ldy;      /* ... of y (and of dy)                                                    */

@@ -190,7 +190,8 @@ __device__ __forceinline__ void mx_values8(uint32_t codes, float (&v)[8]) {
 }
 
 // Four codes (the low 16 bits) to values: the upper two bytes of an fp32 number picked from tables of the eight magnitudes, and the
-// sign.  (The conversion instruction, asked for two bytes out of four, was compiled into one that took the upper two.)
+// sign.  (With the conversion instruction on the lower two of a word's four bytes and the upper two unused, the upper two's values came
+// out; why was not found.)
 __device__ __forceinline__ void mx_values4(uint32_t codes, float (&v)[4]) {
   const uint32_t m = codes & 0x7777u;
   const uint32_t hi = __byte_perm(0x3F3F3F00u, 0x40404040u, m), lo = __byte_perm(0xC0800000u, 0xC0804000u, m);

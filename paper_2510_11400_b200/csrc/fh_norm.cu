@@ -657,7 +657,7 @@ __device__ __forceinline__ void sums_to_work(const NormArgs& a, const float* acc
 
 template <int DT, int TEAM, int V, bool VEC, int X>
 struct BackRing {
-  static constexpr bool kLines = !VEC && X == 0;  // (bf16: 16384 x 4095 157 us, by words 173)
+  static constexpr bool kLines = !VEC && X == 0;  // (bf16: 16384 x 4095 154 us, by words 171)
   using Row = RowRing<DT, TEAM, V, VEC, kLines>;
   static constexpr int kGroup = X ? 4 : (V < 4 ? 2 : 1);      // rows worked on together ...
   static constexpr int kRows = X || V < 4 ? 2 * kGroup : 3;   // ... and in shared memory
@@ -1016,8 +1016,8 @@ int launch_forward_d(const NormArgs& a, bool vec, cudaStream_t stream) {
     return vec ? launch_forward_dv<DT, true, false, 2>(a, stream) : launch_forward_dv<DT, false, false, 2>(a, stream);
   }
   if (vec) return launch_forward_dv<DT, true, false, 0>(a, stream);
-  // Off the grid, bf16 comes by words for long rows and element by element for short ones: 16384 x 4095 147 and 257 us, 16384 x 1001 47 and
-  // 40.
+  // Off the grid, bf16 comes by words for long rows and element by element for short ones: 16384 x 4095 105 and 256 us, x 1501 49 and 50, x 1001
+  // 28.5 and 26.8.
   if constexpr (DT == kBF16) {
     if (a.cols > 1024) return launch_forward_dv<DT, false, false, 0>(a, stream);
   }
