@@ -482,6 +482,163 @@ int fh_layer_norm_backward(const fh_norm_desc* desc, const void* d_dy, const voi
                            size_t work_bytes, uint64_t* d_status, void* stream);
 
 /*
+ * Matrices in 8-bit integers, where 4 bits are too coarse: a scale for each row.
+ *
+ * A matrix's row is whole numbers q from -127 to 127 times its scale s, which follows from the row's largest magnitude a:
+ * s = a times 1 / 127 in fp32 (both rounded), at least 2^-126, and 0 where a is 0.  q is the element divided by s, rounded to nearest, ties to even; the
+ * quotient is rounded once, so that containers are pure functions of the input.  A row with a NaN or an infinity has the magnitude NaN and codes 0, and is restored
+ * as NaN.  Restored values are q * s, rounded to fp32 (at most its largest finite number) and then to the result's type.
+ *
+ * Container of a rows x cols matrix (little-endian): 128 bytes of header: u32 magic "FHI8" | u32 version (1) | i32 rows | i32 cols | u64 0 | u64 total
+ * bytes | zeros.  Then the codes, rows padded to a multiple of 8 and columns to one of 32 with zeros: for each 128 rows (the last ones: as many as there
+ * are), for each 16 columns, 16 bytes a row.  Then the magnitudes, an fp32 number a row, zeros behind the last.
+ */
+size_t fh_i8_bytes(int32_t rows, int32_t cols); /* 0 for invalid arguments.  Host-only, no CUDA call. */
+
+/*
+ * Compress a matrix: one kernel for each container.
+ *   d_rows   container of the matrix (a scale for each row: for tokens), 16-byte aligned, rows_capacity bytes; may be NULL
+ *   d_cols   container of its transpose (a scale for each column: for channels), cols_capacity bytes; may be NULL, but not both
+ * Elements are read twice where a row (column) does not fit the registers of the CTAs that work on it.
+ * FH_ERR_CAPACITY when a container has less than fh_i8_bytes, FH_ERR_ARG when input and containers overlap.
+ */
+int fh_i8_compress(const fh_matrix* matrix, const void* d_src, void* d_rows, size_t rows_capacity, void* d_cols, size_t cols_capacity, void* stream);
+
+/*
+ * Restore a matrix from its container: one kernel.
+ *   expect     what the caller expects; another header is FH_ERR_CORRUPT (through d_status; nothing is written then)
+ *   d_dst      the matrix; elements between cols and ld are left alone
+ *   d_status   optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
+ */
+int fh_i8_decompress(const void* d_src, size_t src_bytes, const fh_matrix* expect, void* d_dst, uint64_t* d_status, void* stream);
+
+/*
+ * C = alpha * A B^T, or C + alpha * A B^T, of matrices held in 8 bits: A m x k, B n x k, C m x n, dense.  One kernel.  Sums of the codes' products are
+ * exact (32-bit integers, hence k <= FH_I8_MAX_K, FH_ERR_UNSUPPORTED beyond); the scales and alpha are multiplied in fp32, or in 64 bits where a
+ * factor is so large or small that the way there could leave fp32's range; C is rounded once.  A linear layer's forward and backward pass take the
+ * containers that fh_mx_product's description names.  A row of A or B that is NaN makes its row (column) of C NaN.
+ *   d_a, d_b    containers of an m x k and an n x k matrix; another header is FH_ERR_CORRUPT (through d_status; C is not written then)
+ *   d_c         element (i, j) at i * ldc + j; FH_ERR_ARG when it overlaps a container (or d_status any of the three)
+ *   d_status    optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status.  FH_ERR_TIMEOUT: a wait inside the
+ *               kernel ran out (C is undefined then, the library stays usable)
+ * Equal inputs give equal bits.
+ */
+#define FH_I8_MAX_K 133120
+typedef struct {
+  int32_t m, n, k;
+  int32_t dtype;      /* fh_dtype of C                            */
+  int32_t accumulate; /* 1: C is added to                         */
+  float alpha;        /* finite                                   */
+  int64_t ldc;        /* >= n                                     */
+} fh_i8_product_desc;
+
+int fh_i8_product(const fh_i8_product_desc* desc, const void* d_a, size_t a_bytes, const void* d_b, size_t b_bytes, void* d_c, uint64_t* d_status,
+                  void* stream);
+
+/*
+ * The gated feed-forward block: both projections, the activation and the product in one kernel.
+ *
+ *   g = x Wg^T, u = x Wu^T, h = act(g) * u
+ * with x (rows x k), Wg and Wu (width x k) held in 8 bits.  The projection behind it is fh_i8_product of h, compressed.
+ */
+typedef enum { FH_SILU = 0, FH_GELU = 1, FH_GELU_TANH = 2, FH_RELU = 3 } fh_activation;
+typedef struct {
+  int32_t rows, width;
+  int32_t k;          /* of x and the weights, <= FH_I8_MAX_K (fh_gated_backward does not look at it) */
+  int32_t activation; /* fh_activation                                                                */
+  int32_t dtype;      /* fh_dtype of h, pre and their gradients                                       */
+  int32_t reserved;   /* 0                                                                            */
+  int64_t ldh;        /* elements from one row of h (of dh) to the next, >= width                     */
+  int64_t ldp;        /* ... of pre (of dpre), >= 2 * width                                           */
+} fh_gated_desc;
+
+/*
+ *   d_x, d_gate, d_up   containers; another header is FH_ERR_CORRUPT (through d_status; nothing is written then)
+ *   d_h                 rows x width, may be NULL if d_pre is not.  act(g) * u is made of g and u before they are rounded
+ *   d_pre               rows x 2 width, g and behind it u in each row, what the backward pass reads; may be NULL.  (Who keeps x's container
+ *                       instead calls again with d_h = NULL.)
+ *   d_status            as in fh_i8_product
+ * FH_ERR_ARG when an output has a byte in common with a container or the other one.
+ */
+int fh_i8_gated(const fh_gated_desc* desc, const void* d_x, size_t x_bytes, const void* d_gate, size_t gate_bytes, const void* d_up, size_t up_bytes,
+                void* d_h, void* d_pre, uint64_t* d_status, void* stream);
+
+/*
+ * Its backward pass up to the products: dg = dh * u * act'(g), du = dh * act(g) from what the forward pass kept.  (relu's derivative at 0 is 0.)
+ *   d_dh      rows x width (ldh);  d_pre  rows x 2 width (ldp)
+ *   d_dpre    rows x 2 width (ldp), dg and behind it du in each row, may be NULL; may be d_pre
+ *   d_packed  8-bit container of that, a scale for each row, byte for byte what fh_i8_compress makes of the dense dpre in its type; may be NULL, but
+ *             not both.  With W the 2 width x k matrix of Wg above Wu: dx = dpre W is fh_i8_product of d_packed and the container of W's columns, and
+ *             dW = dpre^T x that of the containers of dpre's columns (fh_i8_compress of d_dpre) and of x's
+ * One kernel.  FH_ERR_CAPACITY when packed_capacity is less than fh_i8_bytes(rows, 2 width), FH_ERR_ARG when an output has a byte in common with an
+ * input or the other one, other than d_dpre = d_pre.
+ */
+int fh_gated_backward(const fh_gated_desc* desc, const void* d_dh, const void* d_pre, void* d_dpre, void* d_packed, size_t packed_capacity, void* stream);
+
+/*
+ * Norms of queries and keys for each head, with the rotation by position in the same pass.
+ *
+ * For each token and head, x of `dim` elements:  xhat = x * rstd, rstd = 1 / sqrt(mean(x^2) + eps)  (FH_HEADS_RMS), or xhat = (x - mean) * rstd with
+ * the variance instead (FH_HEADS_LAYER);  z = xhat * gamma;  and of the first `rotary` elements the pairs (a, b) become
+ * (a c - b n, b c + a n), c and n the cosine and sine that the table has for the token's position and the pair.
+ */
+typedef enum { FH_HEADS_RMS = 0, FH_HEADS_LAYER = 1 } fh_heads_kind;
+typedef enum { FH_PAIRS_HALVES = 0,     /* elements i and i + rotary / 2 are pair i */
+               FH_PAIRS_NEIGHBOURS = 1  /* elements 2 i and 2 i + 1                  */
+} fh_heads_pairs;
+typedef struct {
+  int32_t dtype;            /* fh_dtype of queries and keys and their gradients                        */
+  int32_t wdtype;           /* fh_dtype of gamma and its gradients                                     */
+  int32_t kind, pairs;      /* fh_heads_kind, fh_heads_pairs                                           */
+  int32_t tokens, dim;      /* dim <= 8192 (FH_ERR_UNSUPPORTED beyond)                                 */
+  int32_t rotary;           /* elements of a head that are rotated, even, 0 ... dim                    */
+  int32_t positions;        /* rows of the table                                                       */
+  int32_t q_heads, k_heads; /* either may be 0, but not both                                           */
+  float eps;                /* >= 0; with 0 a row without spread is NaN                                */
+  int32_t reserved;         /* 0                                                                       */
+  /* elements from one token, or one head, to the next: of q and k (and of dq and dk), and of the outputs (and their gradients).  Rows of `dim`
+     elements must not overlap: tokens in the heads' strides or the other way round. */
+  int64_t q_token, q_head, k_token, k_head;
+  int64_t q_out_token, q_out_head, k_out_token, k_out_head;
+} fh_heads_desc;
+
+/*
+ * d_table[p][i] = (cos, sin) of p * base^(-2 i / rotary) * scale for `positions` rows of rotary / 2 pairs, fp32, the angles in 64 bits.
+ * base > 0, scale finite, rotary even and >= 2.  One kernel.
+ */
+int fh_rotation_table(int32_t positions, int32_t rotary, double base, double scale, float* d_table, void* stream);
+
+/*
+ * Forward pass: one kernel for queries and keys.
+ *   d_q, d_k             dtype, either may be NULL when it has no heads
+ *   d_gamma_q, d_gamma_k dim weights, either may be NULL (1)
+ *   d_table              positions x rotary / 2 pairs (cos, sin), 8-byte aligned; may be NULL when rotary is 0
+ *   d_positions          a position for each token; NULL: 0, 1, 2 ...  A token whose position is negative or not in the table is left out: nothing of
+ *                        it is written, and the status is FH_ERR_CORRUPT
+ *   d_q_out, d_k_out     may be d_q (d_k) where the strides are the same
+ *   d_status             optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
+ * FH_ERR_ARG when an output or the status has a byte in common with an input or another of them, other than in place as above.
+ */
+int fh_head_norm(const fh_heads_desc* desc, const void* d_q, const void* d_k, const void* d_gamma_q, const void* d_gamma_k, const float* d_table,
+                 const int32_t* d_positions, void* d_q_out, void* d_k_out, uint64_t* d_status, void* stream);
+
+/*
+ * Backward pass, from the forward pass's inputs: dz is dy rotated back, g = dz * gamma, dx = rstd * (g - xhat * mean(g * xhat)), less
+ * rstd * mean(g) for FH_HEADS_LAYER; dgamma = sum over tokens and heads of dz * xhat.
+ *   d_dq_out, d_dk_out      gradients of the outputs;  the inputs as in the forward pass
+ *   d_dq, d_dk              any of the four may be NULL, but not all; d_dq may be d_q, or d_dq_out where the strides are the same
+ *   d_dgamma_q, d_dgamma_k  dim weights' gradients
+ *   d_work                  caller-owned workspace, 16-byte aligned, at least fh_head_norm_work_bytes(desc) bytes, needed when d_dgamma_q or d_dgamma_k is
+ *                           given; calls that may run at the same time need one each
+ *   d_status                as in the forward pass; a token that is left out adds nothing to dgamma
+ * One kernel, and a second, small one for dgamma.  Sums are fp32 in a fixed order: equal inputs, strides and alignments give equal bits.
+ */
+size_t fh_head_norm_work_bytes(const fh_heads_desc* desc);
+int fh_head_norm_backward(const fh_heads_desc* desc, const void* d_dq_out, const void* d_dk_out, const void* d_q, const void* d_k, const void* d_gamma_q,
+                          const void* d_gamma_k, const float* d_table, const int32_t* d_positions, void* d_dq, void* d_dk, void* d_dgamma_q,
+                          void* d_dgamma_k, void* d_work, size_t work_bytes, uint64_t* d_status, void* stream);
+
+/*
  * Fault injection on the host side, for tests of the error path of the device-side waits.  (The paper has no
  * counterpart.)  Compressing places the overflow parts of outlier-rich planes in plane order: a tile of
  * planes waits, with a limit, until every earlier tile has published its size; a wait that runs out ends the
@@ -489,8 +646,8 @@ int fh_layer_norm_backward(const fh_norm_desc* desc, const void* d_dy, const voi
  *   FH_DEBUG_WAIT_POLLS   limit of those waits in polls of about 0.1 us (default 2^22)
  *   FH_DEBUG_SILENT_TILE  index of a tile that never publishes its size, so that every later tile with
  *                         an outlier-rich plane runs into the limit; UINT64_MAX: none (default)
- * The waits inside a product (fh_mx_product) have the same limit, and the silent tile is there the stage (256 elements of the common
- * axis, counted in each CTA) from which on a CTA, of a pair the second one, loads nothing.
+ * The waits inside a product (fh_mx_product, fh_i8_product, fh_i8_gated) have the same limit, and the silent tile is there the stage (256 elements of
+ * the common axis, in 8 bits 128, counted in each CTA) from which on a CTA, of a pair the second one, loads nothing.
  * Both apply to calls enqueued afterwards, process-wide.  Returns FH_OK or FH_ERR_ARG.
  */
 enum { FH_DEBUG_WAIT_POLLS = 0, FH_DEBUG_SILENT_TILE = 1 };

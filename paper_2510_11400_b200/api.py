@@ -20,6 +20,10 @@ FH_F32, FH_BF16 = 0, 1
 FH_SALIENT_AUTO, FH_SALIENT_OFF, FH_SALIENT_ALL, FH_SALIENT_CHANNEL, FH_SALIENT_TENSOR = 0, 1, 2, 3, 4
 FH_KEEP, FH_COMPRESS, FH_EVICT = 0, 1, 2
 FH_MX_B32, FH_MX_B16 = 0, 1
+FH_I8_MAX_K = 133120
+FH_SILU, FH_GELU, FH_GELU_TANH, FH_RELU = 0, 1, 2, 3
+FH_HEADS_RMS, FH_HEADS_LAYER = 0, 1
+FH_PAIRS_HALVES, FH_PAIRS_NEIGHBOURS = 0, 1
 FH_STATIC_MAX_PLANES = 131072
 FH_DEBUG_WAIT_POLLS, FH_DEBUG_SILENT_TILE = 0, 1
 
@@ -28,7 +32,8 @@ EXPORTS = ["fh_default_params", "fh_version", "fh_device_count", "fh_compressed_
            "fh_decompress_host", "fh_compress_static", "fh_plan_generate", "fh_plan_measure", "fh_debug_set",
            "fh_kernel_launches",
            "fh_shutdown", "fh_mx_bytes", "fh_mx_compress", "fh_mx_decompress", "fh_mx_product", "fh_layer_norm",
-           "fh_layer_norm_work_bytes", "fh_layer_norm_backward"]
+           "fh_layer_norm_work_bytes", "fh_layer_norm_backward", "fh_i8_bytes", "fh_i8_compress", "fh_i8_decompress", "fh_i8_product",
+           "fh_i8_gated", "fh_gated_backward", "fh_rotation_table", "fh_head_norm", "fh_head_norm_work_bytes", "fh_head_norm_backward"]
 
 
 class FhError(RuntimeError):
@@ -102,6 +107,24 @@ class fh_norm_desc(C.Structure):
                 ("reserved", C.c_int32), ("ldx", C.c_int64), ("ldy", C.c_int64)]
 
 
+class fh_i8_product_desc(C.Structure):
+    _fields_ = [("m", C.c_int32), ("n", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32), ("accumulate", C.c_int32), ("alpha", C.c_float),
+                ("ldc", C.c_int64)]
+
+
+class fh_gated_desc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("width", C.c_int32), ("k", C.c_int32), ("activation", C.c_int32), ("dtype", C.c_int32),
+                ("reserved", C.c_int32), ("ldh", C.c_int64), ("ldp", C.c_int64)]
+
+
+class fh_heads_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("wdtype", C.c_int32), ("kind", C.c_int32), ("pairs", C.c_int32), ("tokens", C.c_int32),
+                ("dim", C.c_int32), ("rotary", C.c_int32), ("positions", C.c_int32), ("q_heads", C.c_int32), ("k_heads", C.c_int32),
+                ("eps", C.c_float), ("reserved", C.c_int32), ("q_token", C.c_int64), ("q_head", C.c_int64), ("k_token", C.c_int64),
+                ("k_head", C.c_int64), ("q_out_token", C.c_int64), ("q_out_head", C.c_int64), ("k_out_token", C.c_int64),
+                ("k_out_head", C.c_int64)]
+
+
 _lib = None
 
 
@@ -166,6 +189,20 @@ def lib() -> C.CDLL:
         L.fh_layer_norm_work_bytes.restype = C.c_size_t
         L.fh_layer_norm_backward.argtypes = [N, V, V, C.c_size_t, C.c_int32, V, V, V, V, V, V, V, C.c_size_t, V, V]
         L.fh_layer_norm_backward.restype = C.c_int
+        M, Z, I = C.POINTER(fh_matrix), C.c_size_t, C.c_int32
+        G, H = C.POINTER(fh_gated_desc), C.POINTER(fh_heads_desc)
+        for name, args, result in (("fh_i8_bytes", [I, I], Z),
+                                   ("fh_i8_compress", [M, V, V, Z, V, Z, V], C.c_int),
+                                   ("fh_i8_decompress", [V, Z, M, V, V, V], C.c_int),
+                                   ("fh_i8_product", [C.POINTER(fh_i8_product_desc), V, Z, V, Z, V, V, V], C.c_int),
+                                   ("fh_i8_gated", [G, V, Z, V, Z, V, Z, V, V, V, V], C.c_int),
+                                   ("fh_gated_backward", [G, V, V, V, V, Z, V], C.c_int),
+                                   ("fh_rotation_table", [I, I, C.c_double, C.c_double, V, V], C.c_int),
+                                   ("fh_head_norm", [H, V, V, V, V, V, V, V, V, V, V], C.c_int),
+                                   ("fh_head_norm_work_bytes", [H], Z),
+                                   ("fh_head_norm_backward", [H, V, V, V, V, V, V, V, V, V, V, V, V, V, Z, V, V], C.c_int)):
+            f = getattr(L, name)
+            f.argtypes, f.restype = args, result
         _lib = L
     return _lib
 
@@ -475,6 +512,138 @@ def fh_layer_norm_backward(d: fh_norm_desc, dy, x, gamma, mean, rstd, dx, dgamma
                                         _dense(rstd, dev, 1, rows, rows, FH_F32), _dense(dx, dev, rows, cols, d.ldx, t),
                                         _dense(dgamma, dev, 1, cols, cols, w), _dense(dbeta, dev, 1, cols, cols, w), _ptr(work, dev), 0 if work is None else work.nbytes,
                                         _status_ptr(status, dev), _on(stream, dev))
+
+
+# ---- matrices in 8-bit integers, the gated feed-forward block ------------------------------------
+
+def i8_bytes(rows: int, cols: int) -> int:
+    return int(lib().fh_i8_bytes(rows, cols))
+
+
+def fh_i8_compress(m: fh_matrix, src, rows=None, cols=None, stream=None) -> int:
+    """Enqueue compression of the matrix `src` (a CUDA tensor that `m` describes) into the uint8 CUDA tensors `rows` (a scale for each
+    row) and `cols` (the transpose, a scale for each column); either may be None."""
+    dev = _device()
+    return lib().fh_i8_compress(m, _dense(src, dev, m.rows, m.cols, m.ld, m.dtype), _ptr(rows, dev), 0 if rows is None else rows.nbytes,
+                                _ptr(cols, dev), 0 if cols is None else cols.nbytes, _on(stream, dev))
+
+
+def fh_i8_decompress(src, m: fh_matrix, dst, status=None, stream=None) -> int:
+    """Enqueue restoring the container `src` (uint8) into `dst`, which `m` describes."""
+    dev = _device()
+    return lib().fh_i8_decompress(_ptr(src, dev), src.nbytes, m, _dense(dst, dev, m.rows, m.cols, m.ld, m.dtype), _status_ptr(status, dev),
+                                  _on(stream, dev))
+
+
+def i8_product_desc(m: int, n: int, k: int, dtype: int = FH_F32, ldc: Optional[int] = None, alpha: float = 1.0,
+                    accumulate: bool = False) -> fh_i8_product_desc:
+    return fh_i8_product_desc(m, n, k, dtype, int(accumulate), alpha, n if ldc is None else ldc)
+
+
+def fh_i8_product(d: fh_i8_product_desc, a, b, c, status=None, stream=None) -> int:
+    """Enqueue the product of the 8-bit containers `a` (m x k) and `b` (n x k), uint8 CUDA tensors, into the matrix `c` (m x n)."""
+    dev = _device()
+    return lib().fh_i8_product(d, _ptr(a, dev), a.nbytes, _ptr(b, dev), b.nbytes, _dense(c, dev, d.m, d.n, d.ldc, d.dtype),
+                               _status_ptr(status, dev), _on(stream, dev))
+
+
+def gated_desc(rows: int, width: int, k: int, activation: int = FH_SILU, dtype: int = FH_F32, ldh: Optional[int] = None,
+               ldp: Optional[int] = None) -> fh_gated_desc:
+    return fh_gated_desc(rows, width, k, activation, dtype, 0, width if ldh is None else ldh, 2 * width if ldp is None else ldp)
+
+
+def fh_i8_gated(d: fh_gated_desc, x, gate, up, h=None, pre=None, status=None, stream=None) -> int:
+    """Enqueue h = act(x gate^T) * (x up^T) of 8-bit containers; `pre` receives both products side by side.  Either of the two may be None."""
+    dev = _device()
+    return lib().fh_i8_gated(d, _ptr(x, dev), x.nbytes, _ptr(gate, dev), gate.nbytes, _ptr(up, dev), up.nbytes,
+                             _dense(h, dev, d.rows, d.width, d.ldh, d.dtype), _dense(pre, dev, d.rows, 2 * d.width, d.ldp, d.dtype),
+                             _status_ptr(status, dev), _on(stream, dev))
+
+
+def fh_gated_backward(d: fh_gated_desc, dh, pre, dpre=None, packed=None, stream=None) -> int:
+    """Enqueue the gradients of both products, dense into `dpre` and in 8 bits into the uint8 tensor `packed`; either may be None."""
+    dev = _device()
+    return lib().fh_gated_backward(d, _dense(dh, dev, d.rows, d.width, d.ldh, d.dtype), _dense(pre, dev, d.rows, 2 * d.width, d.ldp, d.dtype),
+                                   _dense(dpre, dev, d.rows, 2 * d.width, d.ldp, d.dtype), _ptr(packed, dev), 0 if packed is None else packed.nbytes,
+                                   _on(stream, dev))
+
+
+# ---- norms of queries and keys with the rotation by position -------------------------------------
+
+def heads_desc(tokens: int, q_heads: int, k_heads: int, dim: int, rotary: Optional[int] = None, dtype: int = FH_F32, wdtype: int = FH_F32,
+               kind: int = FH_HEADS_RMS, pairs: int = FH_PAIRS_HALVES, eps: float = 1e-6, positions: int = 0,
+               q_strides: Optional[Sequence[int]] = None, k_strides: Optional[Sequence[int]] = None,
+               q_out_strides: Optional[Sequence[int]] = None, k_out_strides: Optional[Sequence[int]] = None) -> fh_heads_desc:
+    """Strides are (from one token, from one head) to the next, in elements; without them tensors are [tokens, heads, dim].  `positions`: rows of
+    the table."""
+    q, k = (q_heads * dim, dim), (k_heads * dim, dim)
+    return fh_heads_desc(dtype, wdtype, kind, pairs, tokens, dim, dim if rotary is None else rotary, positions, q_heads, k_heads, eps, 0,
+                         *(q_strides or q), *(k_strides or k), *(q_out_strides or q), *(k_out_strides or k))
+
+
+def rotation_table(positions: int, rotary: int, base: float = 10000.0, scale: float = 1.0, out=None, stream=None):
+    """A table of cosines and sines, fp32 [positions, rotary / 2, 2]."""
+    dev = _device()
+    if out is None:
+        out = _torch.empty(positions, rotary // 2, 2, dtype=_torch.float32, device=f"cuda:{dev}")
+    rc = lib().fh_rotation_table(positions, rotary, base, scale, _ptr(out, dev, positions * rotary, 4), _on(stream, dev))
+    if rc != FH_OK:
+        raise FhError(rc, "fh_rotation_table")
+    return out
+
+
+def _heads(t, dev: int, d: fh_heads_desc, heads: int, token: int, head: int) -> Optional[int]:
+    """The address of rows of heads, once they are known to lie as they are described."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise ValueError(f"a tensor on {t.device}, where cuda:{dev} is the current device")
+    if t.element_size() != _esize(d.dtype) or (d.dtype == FH_F32) != (t.element_size() == 4) or _is_half(t):
+        raise ValueError(f"a tensor of {t.dtype}, where elements of {_esize(d.dtype)} bytes are wanted")
+    if t.dim() == 3 and tuple(t.shape) == (d.tokens, heads, d.dim):
+        s = t.stride()
+        if (d.tokens == 1 or s[0] == token) and (heads == 1 or s[1] == head) and (d.dim == 1 or s[2] == 1):
+            return t.data_ptr()
+    elif t.is_contiguous() and t.numel() >= (d.tokens - 1) * token + (heads - 1) * head + d.dim:
+        return t.data_ptr()
+    raise ValueError(f"a tensor of shape {tuple(t.shape)} and strides {t.stride()}, where {d.tokens} tokens, {token} apart, of {heads} heads, {head} apart, "
+                     f"of {d.dim} elements are wanted")
+
+
+def _turn(d: fh_heads_desc, table, at, dev: int):
+    """The addresses of the table and the positions."""
+    if at is not None and (at.dtype.is_floating_point or at.element_size() != 4):
+        raise ValueError(f"positions of {at.dtype}, where int32 is wanted")
+    return _dense(table, dev, 1, d.positions * d.rotary, d.positions * d.rotary, FH_F32), _ptr(at, dev, d.tokens, 4, (1, d.tokens, d.tokens))
+
+
+def fh_head_norm(d: fh_heads_desc, q, k, gamma_q, gamma_k, table, positions, q_out, k_out, status=None, stream=None) -> int:
+    """Enqueue the norms of the heads of `q` and `k` and their rotation into `q_out` and `k_out`; gammas, positions and what has no heads may be
+    None."""
+    dev, w = _device(), d.wdtype
+    t, at = _turn(d, table, positions, dev)
+    return lib().fh_head_norm(d, _heads(q, dev, d, d.q_heads, d.q_token, d.q_head), _heads(k, dev, d, d.k_heads, d.k_token, d.k_head),
+                              _dense(gamma_q, dev, 1, d.dim, d.dim, w), _dense(gamma_k, dev, 1, d.dim, d.dim, w), t, at,
+                              _heads(q_out, dev, d, d.q_heads, d.q_out_token, d.q_out_head),
+                              _heads(k_out, dev, d, d.k_heads, d.k_out_token, d.k_out_head), _status_ptr(status, dev), _on(stream, dev))
+
+
+def heads_work_bytes(d: fh_heads_desc) -> int:
+    return int(lib().fh_head_norm_work_bytes(C.byref(d)))
+
+
+def fh_head_norm_backward(d: fh_heads_desc, dq_out, dk_out, q, k, gamma_q, gamma_k, table, positions, dq=None, dk=None, dgamma_q=None, dgamma_k=None,
+                          work=None, status=None, stream=None) -> int:
+    """Enqueue the backward pass of fh_head_norm.  `work`: uint8, at least heads_work_bytes, where dgamma_q or dgamma_k is wanted."""
+    dev, w = _device(), d.wdtype
+    t, at = _turn(d, table, positions, dev)
+    return lib().fh_head_norm_backward(d, _heads(dq_out, dev, d, d.q_heads, d.q_out_token, d.q_out_head),
+                                       _heads(dk_out, dev, d, d.k_heads, d.k_out_token, d.k_out_head), _heads(q, dev, d, d.q_heads, d.q_token, d.q_head),
+                                       _heads(k, dev, d, d.k_heads, d.k_token, d.k_head), _dense(gamma_q, dev, 1, d.dim, d.dim, w),
+                                       _dense(gamma_k, dev, 1, d.dim, d.dim, w), t, at, _heads(dq, dev, d, d.q_heads, d.q_token, d.q_head),
+                                       _heads(dk, dev, d, d.k_heads, d.k_token, d.k_head), _dense(dgamma_q, dev, 1, d.dim, d.dim, w),
+                                       _dense(dgamma_k, dev, 1, d.dim, d.dim, w), _ptr(work, dev), 0 if work is None else work.nbytes,
+                                       _status_ptr(status, dev), _on(stream, dev))
 
 
 def debug_set(what: int, value: int) -> int:

@@ -13,10 +13,12 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfh_sm100a.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("fh_warp_f32.cu", "fh_warp_bf16.cu", "fh_warp_f32_plain.cu", "fh_warp_bf16_plain.cu",
                                           "fh_warp_f32_random.cu", "fh_warp_bf16_random.cu", "fh_cta_f32.cu", "fh_cta_bf16.cu",
-                                          "fh_generic.cu", "fh_decompress.cu", "fh_mx_save.cu", "fh_mx_product.cu", "fh_norm.cu", "fh_mx.cu", "fh.cu", "fh_plan.cpp")]
+                                          "fh_generic.cu", "fh_decompress.cu", "fh_mx_save.cu", "fh_mx_product.cu", "fh_norm.cu", "fh_mx.cu",
+                                          "fh_i8_save.cu", "fh_i8_product.cu", "fh_gated.cu", "fh_heads.cu", "fh_i8.cu", "fh.cu", "fh_plan.cpp")]
 HEADERS = [os.path.join(CSRC, f) for f in ("fh_device.cuh", "fh_blocks.cuh", "fh_channel.cuh", "fh_compress.cuh",
                                           "fh_decompress.cuh", "fh_launch.cuh", "fh_launch_cta.cuh",
-                                          "fh_launch_warp.cuh", "fh_mx.cuh", "fh_mx_launch.cuh", "fh_tcgen05.cuh")] + \
+                                          "fh_launch_warp.cuh", "fh_mx.cuh", "fh_mx_launch.cuh", "fh_tcgen05.cuh", "fh_product.cuh",
+                                          "fh_checks.cuh", "fh_i8.cuh", "fh_i8_launch.cuh", "fh_act.cuh")] + \
     [os.path.join(os.path.dirname(HERE), "include", "fh.h")]
 DEPS = SOURCES + HEADERS + [os.path.abspath(__file__)]    # (this file: the flags)
 OBJDIR = os.path.join(HERE, "_build")

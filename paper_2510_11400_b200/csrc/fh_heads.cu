@@ -1,0 +1,650 @@
+// Norms of queries and keys for each head with the rotation by position, forward and backward.
+#include <algorithm>
+#include <cmath>
+
+#include "fh_i8_launch.cuh"
+#include "fh_launch.cuh"
+
+namespace fh {
+namespace {
+
+constexpr int kHeadThreads = 128;
+constexpr uint32_t kHeadWarps = kHeadThreads / 32;
+
+template <int DT>
+constexpr uint32_t kEs = DT == kF32 ? 4u : 2u;
+template <int DT>
+constexpr uint32_t kV = 16u / kEs<DT>;  // elements of a 16-byte vector
+
+// Memory bounds both passes: a row of a head is read and written once.  Nothing is kept between them: the backward pass has the row in registers
+// and makes its mean and rstd again, which costs less than reading them.
+//
+// A slot is two vectors of 16 bytes that hold both elements of their pairs: a vector of the first half and its partner of the second, or two neighbouring
+// vectors; where a part of a head is not rotated, it is made of slots too, whose angle is zero.  A team of T lanes has a row, a slot to a lane, so
+// that a row needs no exchange but its sums', and a lane's cosines, sines and weights stay in registers from head to head of a token.
+template <int DT>
+struct Slot {
+  uint32_t a, b;   // first element of its two vectors
+  uint32_t pair;   // its first pair in the table
+  bool there, turned;
+  __device__ __forceinline__ Slot(uint32_t s, uint32_t dim, uint32_t rotary, bool halves) {
+    constexpr uint32_t V = kV<DT>;
+    there = s < dim / (2u * V);
+    turned = s < rotary / (2u * V);
+    pair = s * V;
+    if (!halves) {
+      a = 2u * V * s;
+      b = a + V;
+    } else if (turned) {
+      a = V * s;
+      b = rotary / 2u + a;
+    } else {
+      a = rotary + V * (s - rotary / (2u * V));
+      b = a + (dim - rotary) / 2u;
+    }
+  }
+};
+
+template <int DT>
+__device__ __forceinline__ void load_vec(const uint8_t* p, float* v) {
+  const uint4 w = *reinterpret_cast<const uint4*>(p);
+  if (DT == kF32) {
+    v[0] = __uint_as_float(w.x);
+    v[1] = __uint_as_float(w.y);
+    v[2] = __uint_as_float(w.z);
+    v[3] = __uint_as_float(w.w);
+  } else {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(u[i] << 16);
+      v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store_vec(uint8_t* p, const float* v) {
+  uint4 w;
+  if (DT == kF32)
+    w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+  else
+    w = make_uint4(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4 % kV<DT>], v[5 % kV<DT>]), f32x2_to_bf16x2(v[6 % kV<DT>], v[7 % kV<DT>]));
+  *reinterpret_cast<uint4*>(p) = w;
+}
+__device__ __forceinline__ float weight_at(const uint8_t* gamma, int wdtype, uint32_t i) {
+  if (!gamma) return 1.0f;
+  return wdtype == kF32 ? reinterpret_cast<const float*>(gamma)[i] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(gamma)[i]);
+}
+template <int DT>
+__device__ __forceinline__ float elem_at(const uint8_t* p, uint32_t i) {
+  return DT == kF32 ? reinterpret_cast<const float*>(p)[i] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(p)[i]);
+}
+template <int DT>
+__device__ __forceinline__ void put_elem(uint8_t* p, uint32_t i, float v) {
+  if (DT == kF32)
+    reinterpret_cast<float*>(p)[i] = v;
+  else
+    reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)f32_to_bf16_bits(v);
+}
+
+// Sum over the T lanes of a team (all lanes of the warp take part).
+template <int T>
+__device__ __forceinline__ float team_sum(float v) {
+#pragma unroll
+  for (int s = 1; s < T; s *= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, s);
+  return v;
+}
+
+// The pairs of a slot: `first` and `second` of pair i of its V pairs among its 2 V elements.
+template <bool HALVES, uint32_t V>
+__device__ __forceinline__ constexpr uint32_t first_of(uint32_t i) { return HALVES ? i : 2 * i; }
+template <bool HALVES, uint32_t V>
+__device__ __forceinline__ constexpr uint32_t second_of(uint32_t i) { return HALVES ? V + i : 2 * i + 1; }
+
+// A token's position: -1 for one that is left out.
+__device__ __forceinline__ int64_t position_of(const HeadsArgs& g, uint32_t token) {
+  if (g.rotary == 0u) return 0;
+  if (!g.at) return token;
+  const int32_t p = g.at[token];
+  return p < 0 || (uint32_t)p >= g.positions ? -1 : p;
+}
+// The status, by one CTA that does nothing else (the others' order is not known).
+__device__ __forceinline__ void report_positions(const HeadsArgs& g) {
+  __shared__ uint32_t bad;
+  if (threadIdx.x == 0) bad = 0u;
+  __syncthreads();
+  bool mine = false;
+  if (g.at && g.rotary)
+    for (uint32_t t = threadIdx.x; t < g.tokens; t += blockDim.x) mine = mine || position_of(g, t) < 0;
+  if (mine) bad = 1u;
+  __syncthreads();
+  if (threadIdx.x == 0) *g.status = bad ? status_word(kErrCorrupt) : 0ull;
+}
+
+// Cosines and sines of a slot's pairs at a position.
+template <int DT>
+__device__ __forceinline__ void load_turn(const HeadsArgs& g, const Slot<DT>& s, int64_t at, float (&c)[kV<DT>], float (&n)[kV<DT>]) {
+  if (s.turned) {
+    const float4* p = reinterpret_cast<const float4*>(g.table + (uint64_t)at * (g.rotary / 2u) + s.pair);
+#pragma unroll
+    for (uint32_t i = 0; i < kV<DT> / 2u; ++i) {
+      const float4 v = p[i];
+      c[2 * i] = v.x;
+      n[2 * i] = v.y;
+      c[2 * i + 1] = v.z;
+      n[2 * i + 1] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < kV<DT>; ++i) {
+      c[i] = 1.0f;
+      n[i] = 0.0f;
+    }
+  }
+}
+
+// Whether unit `u` is of queries or keys, of which token, and its first head.  A unit is a warp's work: `span` heads of a token.
+struct HeadUnit {
+  uint32_t side, token, head;
+  __device__ __forceinline__ HeadUnit(uint64_t u, const HeadsArgs& g, uint32_t span) {
+    const uint32_t nq = (g.side[0].heads + span - 1u) / span, nk = (g.side[1].heads + span - 1u) / span;
+    token = (uint32_t)(u / (nq + nk));
+    const uint32_t at = (uint32_t)(u % (nq + nk));
+    side = at >= nq;
+    head = (side ? at - nq : at) * span;
+  }
+};
+
+// T lanes to a row, U rows of a team asked for at once.
+template <int DT, int T, int U, bool HALVES>
+__global__ void __launch_bounds__(kHeadThreads) heads_forward_kernel(const HeadsArgs g) {
+  constexpr uint32_t V = kV<DT>, kTeams = 32 / T, kSpan = kTeams * U;
+  dep_trigger();
+  dep_wait();
+  const uint32_t extra = g.status ? 1u : 0u;
+  if (blockIdx.x < extra) {
+    report_positions(g);
+    return;
+  }
+  const uint32_t lane = threadIdx.x % 32, team = lane / T;
+  const uint64_t units = (uint64_t)g.tokens * ((g.side[0].heads + kSpan - 1u) / kSpan + (g.side[1].heads + kSpan - 1u) / kSpan);
+  const uint64_t u = (uint64_t)(blockIdx.x - extra) * kHeadWarps + threadIdx.x / 32;
+  if (u >= units) return;
+  const HeadUnit unit(u, g, kSpan);
+  const HeadsSide& s = g.side[unit.side];
+  const int64_t at = position_of(g, unit.token);
+  if (at < 0) return;
+  const Slot<DT> slot(lane % T, g.dim, g.rotary, HALVES);
+  float x[U][2 * V];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const uint32_t head = unit.head + i * kTeams + team;
+#pragma unroll
+    for (uint32_t e = 0; e < 2 * V; ++e) x[i][e] = 0.0f;
+    if (slot.there && head < s.heads) {
+      const uint8_t* p = s.x + ((uint64_t)unit.token * s.token + (uint64_t)head * s.head) * kEs<DT>;
+      load_vec<DT>(p + slot.a * kEs<DT>, x[i]);
+      load_vec<DT>(p + slot.b * kEs<DT>, x[i] + V);
+    }
+  }
+  float c[V], n[V], w[2 * V];
+  if (slot.there) {
+    load_turn<DT>(g, slot, at, c, n);
+#pragma unroll
+    for (uint32_t e = 0; e < V; ++e) {
+      w[e] = weight_at(s.gamma, g.wdtype, slot.a + e);
+      w[V + e] = weight_at(s.gamma, g.wdtype, slot.b + e);
+    }
+  }
+  const float size = (float)g.dim;
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const uint32_t head = unit.head + i * kTeams + team;
+    if (g.layer) {
+      float sum = 0.0f;
+#pragma unroll
+      for (uint32_t e = 0; e < 2 * V; ++e) sum += x[i][e];
+      const float mean = __fdiv_rn(team_sum<T>(sum), size);
+#pragma unroll
+      for (uint32_t e = 0; e < 2 * V; ++e) x[i][e] = slot.there ? x[i][e] - mean : 0.0f;
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (uint32_t e = 0; e < 2 * V; ++e) sum = __fmaf_rn(x[i][e], x[i][e], sum);
+    const float rstd = 1.0f / sqrtf(__fdiv_rn(team_sum<T>(sum), size) + g.eps);
+    if (!slot.there || head >= s.heads) continue;
+    float y[2 * V];
+#pragma unroll
+    for (uint32_t p = 0; p < V; ++p) {
+      const uint32_t fi = first_of<HALVES, V>(p), se = second_of<HALVES, V>(p);
+      const float za = x[i][fi] * rstd * w[fi], zb = x[i][se] * rstd * w[se];
+      y[fi] = __fmaf_rn(za, c[p], -(zb * n[p]));
+      y[se] = __fmaf_rn(zb, c[p], za * n[p]);
+    }
+    uint8_t* o = s.out + ((uint64_t)unit.token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
+    store_vec<DT>(o + slot.a * kEs<DT>, y);
+    store_vec<DT>(o + slot.b * kEs<DT>, y + V);
+  }
+}
+
+// Backward.  CTAs are dealt out to queries and keys, and each adds up its rows' part of the weights' gradient: a lane for its slot, then teams, then warps,
+// in a fixed order.
+template <int DT, int T, int U, bool HALVES>
+__global__ void __launch_bounds__(kHeadThreads) heads_backward_kernel(const HeadsArgs g) {
+  constexpr uint32_t V = kV<DT>, kTeams = 32 / T, kSpan = kTeams * U;
+  __shared__ float sums[kHeadWarps][T * 2 * V];
+  dep_trigger();
+  dep_wait();
+  const uint32_t extra = g.status ? 1u : 0u;
+  if (blockIdx.x < extra) {
+    report_positions(g);
+    return;
+  }
+  const uint32_t cta = blockIdx.x - extra, which = cta >= g.side[0].parts, part = which ? cta - g.side[0].parts : cta;
+  const HeadsSide& s = g.side[which];
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, team = lane / T;
+  const Slot<DT> slot(lane % T, g.dim, g.rotary, HALVES);
+  const uint32_t spans = (s.heads + kSpan - 1u) / kSpan;
+  const uint64_t units = (uint64_t)g.tokens * spans;
+  const float size = (float)g.dim;
+  float w[2 * V], acc[2 * V];
+#pragma unroll
+  for (uint32_t e = 0; e < 2 * V; ++e) {
+    w[e] = slot.there ? weight_at(s.gamma, g.wdtype, (e < V ? slot.a : slot.b - V) + e) : 0.0f;
+    acc[e] = 0.0f;
+  }
+  for (uint64_t u = (uint64_t)part * kHeadWarps + warp; u < units; u += (uint64_t)s.parts * kHeadWarps) {
+    const uint32_t token = (uint32_t)(u / spans), head0 = (uint32_t)(u % spans) * kSpan;
+    const int64_t at = position_of(g, token);
+    if (at < 0) continue;
+    float c[V], n[V];
+    float x[U][2 * V], d[U][2 * V];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const uint32_t head = head0 + i * kTeams + team;
+#pragma unroll
+      for (uint32_t e = 0; e < 2 * V; ++e) x[i][e] = d[i][e] = 0.0f;
+      if (slot.there && head < s.heads) {
+        const uint8_t* p = s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
+        const uint8_t* q = s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
+        load_vec<DT>(p + slot.a * kEs<DT>, x[i]);
+        load_vec<DT>(p + slot.b * kEs<DT>, x[i] + V);
+        load_vec<DT>(q + slot.a * kEs<DT>, d[i]);
+        load_vec<DT>(q + slot.b * kEs<DT>, d[i] + V);
+      }
+    }
+    if (slot.there) load_turn<DT>(g, slot, at, c, n);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const uint32_t head = head0 + i * kTeams + team;
+      const bool there = slot.there && head < s.heads;
+      if (g.layer) {
+        float sum = 0.0f;
+#pragma unroll
+        for (uint32_t e = 0; e < 2 * V; ++e) sum += x[i][e];
+        const float mean = __fdiv_rn(team_sum<T>(sum), size);
+#pragma unroll
+        for (uint32_t e = 0; e < 2 * V; ++e) x[i][e] = there ? x[i][e] - mean : 0.0f;
+      }
+      // dz in d, then the sums of x^2, g x and g
+      if (there) {
+#pragma unroll
+        for (uint32_t p = 0; p < V; ++p) {
+          const uint32_t fi = first_of<HALVES, V>(p), se = second_of<HALVES, V>(p);
+          const float ya = d[i][fi], yb = d[i][se];
+          d[i][fi] = __fmaf_rn(ya, c[p], yb * n[p]);
+          d[i][se] = __fmaf_rn(yb, c[p], -(ya * n[p]));
+        }
+      }
+      float xx = 0.0f, gx = 0.0f, gs = 0.0f;
+#pragma unroll
+      for (uint32_t e = 0; e < 2 * V; ++e) {
+        const float gg = d[i][e] * w[e];
+        xx = __fmaf_rn(x[i][e], x[i][e], xx);
+        gx = __fmaf_rn(gg, x[i][e], gx);
+        gs += gg;
+      }
+      xx = team_sum<T>(xx);
+      gx = team_sum<T>(gx);
+      if (g.layer) gs = team_sum<T>(gs);
+      const float rstd = 1.0f / sqrtf(__fdiv_rn(xx, size) + g.eps);
+      const float along = gx * rstd / size, level = g.layer ? gs / size : 0.0f;  // mean(g xhat), mean(g)
+      if (!there) continue;
+      float dx[2 * V];
+#pragma unroll
+      for (uint32_t e = 0; e < 2 * V; ++e) {
+        const float xhat = x[i][e] * rstd;
+        acc[e] = __fmaf_rn(d[i][e], xhat, acc[e]);
+        dx[e] = rstd * (__fmaf_rn(-xhat, along, d[i][e] * w[e]) - level);
+      }
+      if (s.dx) {
+        uint8_t* o = s.dx + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
+        store_vec<DT>(o + slot.a * kEs<DT>, dx);
+        store_vec<DT>(o + slot.b * kEs<DT>, dx + V);
+      }
+    }
+  }
+  if (!s.dgamma) return;
+#pragma unroll
+  for (uint32_t e = 0; e < 2 * V; ++e) {
+#pragma unroll
+    for (int o = T; o < 32; o *= 2) acc[e] += __shfl_xor_sync(0xFFFFFFFFu, acc[e], o);
+    if (team == 0) sums[warp][(lane % T) * 2 * V + e] = acc[e];
+  }
+  __syncthreads();
+  float* out = g.work + (uint64_t)((which ? g.side[0].parts : 0u) + part) * g.dim;
+  for (uint32_t i = threadIdx.x; i < T * 2 * V; i += kHeadThreads) {
+    const Slot<DT> of(i / (2 * V), g.dim, g.rotary, HALVES);
+    const uint32_t e = i % (2 * V);
+    float sum = 0.0f;
+#pragma unroll
+    for (uint32_t x = 0; x < kHeadWarps; ++x) sum += sums[x][i];
+    if (of.there) out[(e < V ? of.a : of.b - V) + e] = sum;
+  }
+}
+
+// ---- any size, stride and alignment: a warp to a row, a lane to pairs 32 apart, the row's elements read again from L1.
+// An element that is not rotated is a pair with nothing.
+struct LoosePairs {
+  uint32_t half, rest;  // pairs, and elements behind them
+  bool halves;
+  __device__ __forceinline__ explicit LoosePairs(const HeadsArgs& g) : half(g.rotary / 2u), rest(g.dim - g.rotary), halves(g.halves) {}
+  __device__ __forceinline__ uint32_t count() const { return half + rest; }
+  __device__ __forceinline__ bool paired(uint32_t i) const { return i < half; }
+  __device__ __forceinline__ uint32_t first(uint32_t i) const { return i < half ? (halves ? i : 2u * i) : half + i; }
+  __device__ __forceinline__ uint32_t second(uint32_t i) const { return halves ? half + i : 2u * i + 1u; }
+};
+
+template <int DT>
+__device__ __forceinline__ float loose_mean(const HeadsArgs& g, const uint8_t* p, uint32_t lane) {
+  if (!g.layer) return 0.0f;
+  float sum = 0.0f;
+  for (uint32_t e = lane; e < g.dim; e += 32u) sum += elem_at<DT>(p, e);
+  return __fdiv_rn(team_sum<32>(sum), (float)g.dim);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kHeadThreads) heads_forward_loose_kernel(const HeadsArgs g) {
+  dep_trigger();
+  dep_wait();
+  const uint32_t extra = g.status ? 1u : 0u;
+  if (blockIdx.x < extra) {
+    report_positions(g);
+    return;
+  }
+  const uint32_t lane = threadIdx.x % 32;
+  const uint64_t units = (uint64_t)g.tokens * (g.side[0].heads + g.side[1].heads);
+  const uint64_t u = (uint64_t)(blockIdx.x - extra) * kHeadWarps + threadIdx.x / 32;
+  if (u >= units) return;
+  const HeadUnit unit(u, g, 1u);
+  const HeadsSide& s = g.side[unit.side];
+  const int64_t at = position_of(g, unit.token);
+  if (at < 0) return;
+  const uint8_t* p = s.x + ((uint64_t)unit.token * s.token + (uint64_t)unit.head * s.head) * kEs<DT>;
+  uint8_t* o = s.out + ((uint64_t)unit.token * s.out_token + (uint64_t)unit.head * s.out_head) * kEs<DT>;
+  const float2* turn = g.table + (uint64_t)at * (g.rotary / 2u);
+  const float mean = loose_mean<DT>(g, p, lane);
+  float sum = 0.0f;
+  for (uint32_t e = lane; e < g.dim; e += 32u) {
+    const float v = elem_at<DT>(p, e) - mean;
+    sum = __fmaf_rn(v, v, sum);
+  }
+  const float rstd = 1.0f / sqrtf(__fdiv_rn(team_sum<32>(sum), (float)g.dim) + g.eps);
+  __syncwarp();  // (in place, the row has been read by all lanes before one of them writes)
+  const LoosePairs pairs(g);
+  for (uint32_t i = lane; i < pairs.count(); i += 32u) {
+    const uint32_t fi = pairs.first(i);
+    const float za = (elem_at<DT>(p, fi) - mean) * rstd * weight_at(s.gamma, g.wdtype, fi);
+    if (!pairs.paired(i)) {
+      put_elem<DT>(o, fi, za);
+      continue;
+    }
+    const uint32_t se = pairs.second(i);
+    const float zb = (elem_at<DT>(p, se) - mean) * rstd * weight_at(s.gamma, g.wdtype, se);
+    const float2 t = turn[i];
+    put_elem<DT>(o, fi, __fmaf_rn(za, t.x, -(zb * t.y)));
+    put_elem<DT>(o, se, __fmaf_rn(zb, t.x, za * t.y));
+  }
+}
+
+// Warps of a CTA each have sums of their own in shared memory, `dim` floats.
+template <int DT>
+__global__ void __launch_bounds__(kHeadThreads) heads_backward_loose_kernel(const HeadsArgs g) {
+  extern __shared__ float loose_sums[];
+  dep_trigger();
+  dep_wait();
+  const uint32_t extra = g.status ? 1u : 0u;
+  if (blockIdx.x < extra) {
+    report_positions(g);
+    return;
+  }
+  const uint32_t cta = blockIdx.x - extra, which = cta >= g.side[0].parts, part = which ? cta - g.side[0].parts : cta;
+  const HeadsSide& s = g.side[which];
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
+  float* acc = loose_sums + (uint64_t)warp * g.dim;
+  if (s.dgamma)
+    for (uint32_t e = lane; e < g.dim; e += 32u) acc[e] = 0.0f;
+  __syncwarp();
+  const LoosePairs pairs(g);
+  const float size = (float)g.dim;
+  const uint64_t units = (uint64_t)g.tokens * s.heads;
+  for (uint64_t u = (uint64_t)part * warps + warp; u < units; u += (uint64_t)s.parts * warps) {
+    const uint32_t token = (uint32_t)(u / s.heads), head = (uint32_t)(u % s.heads);
+    const int64_t at = position_of(g, token);
+    if (at < 0) continue;
+    const uint8_t* p = s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
+    const uint8_t* q = s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
+    const float2* turn = g.table + (uint64_t)at * (g.rotary / 2u);
+    const float mean = loose_mean<DT>(g, p, lane);
+    // dz of pair i
+    auto dz = [&](uint32_t i, uint32_t fi, uint32_t se, float& da, float& db) {
+      const float ya = elem_at<DT>(q, fi);
+      da = ya;
+      db = 0.0f;
+      if (!pairs.paired(i)) return;
+      const float yb = elem_at<DT>(q, se);
+      const float2 t = turn[i];
+      da = __fmaf_rn(ya, t.x, yb * t.y);
+      db = __fmaf_rn(yb, t.x, -(ya * t.y));
+    };
+    float xx = 0.0f, gx = 0.0f, gs = 0.0f;
+    for (uint32_t i = lane; i < pairs.count(); i += 32u) {
+      const uint32_t fi = pairs.first(i), se = pairs.second(i);
+      float da, db;
+      dz(i, fi, se, da, db);
+      const float xa = elem_at<DT>(p, fi) - mean, ga = da * weight_at(s.gamma, g.wdtype, fi);
+      xx = __fmaf_rn(xa, xa, xx);
+      gx = __fmaf_rn(ga, xa, gx);
+      gs += ga;
+      if (pairs.paired(i)) {
+        const float xb = elem_at<DT>(p, se) - mean, gb = db * weight_at(s.gamma, g.wdtype, se);
+        xx = __fmaf_rn(xb, xb, xx);
+        gx = __fmaf_rn(gb, xb, gx);
+        gs += gb;
+      }
+    }
+    xx = team_sum<32>(xx);
+    gx = team_sum<32>(gx);
+    gs = team_sum<32>(gs);
+    const float rstd = 1.0f / sqrtf(__fdiv_rn(xx, size) + g.eps);
+    const float along = gx * rstd / size, level = g.layer ? gs / size : 0.0f;
+    uint8_t* o = s.dx + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
+    for (uint32_t i = lane; i < pairs.count(); i += 32u) {
+      const uint32_t fi = pairs.first(i), se = pairs.second(i);
+      float da, db;
+      dz(i, fi, se, da, db);
+      const float xa = (elem_at<DT>(p, fi) - mean) * rstd, ga = da * weight_at(s.gamma, g.wdtype, fi);
+      const float xb = pairs.paired(i) ? (elem_at<DT>(p, se) - mean) * rstd : 0.0f, gb = pairs.paired(i) ? db * weight_at(s.gamma, g.wdtype, se) : 0.0f;
+      if (s.dgamma) acc[fi] = __fmaf_rn(da, xa, acc[fi]);
+      if (s.dx) put_elem<DT>(o, fi, rstd * (__fmaf_rn(-xa, along, ga) - level));
+      if (pairs.paired(i)) {
+        if (s.dgamma) acc[se] = __fmaf_rn(db, xb, acc[se]);
+        if (s.dx) put_elem<DT>(o, se, rstd * (__fmaf_rn(-xb, along, gb) - level));
+      }
+    }
+  }
+  if (!s.dgamma) return;
+  __syncthreads();
+  float* out = g.work + (uint64_t)((which ? g.side[0].parts : 0u) + part) * g.dim;
+  for (uint32_t e = threadIdx.x; e < g.dim; e += blockDim.x) {
+    float sum = 0.0f;
+    for (uint32_t w = 0; w < warps; ++w) sum += loose_sums[(uint64_t)w * g.dim + e];
+    out[e] = sum;
+  }
+}
+
+// The weights' gradients: a warp's lanes have 32 columns, eight warps share the parts, and are added up in their order.
+__global__ void __launch_bounds__(256) heads_columns_kernel(const HeadsArgs g) {
+  __shared__ float sums[8][32];
+  dep_trigger();
+  dep_wait();
+  const uint32_t groups = (g.dim + 31u) / 32u, which = blockIdx.x / groups, col = blockIdx.x % groups * 32u + threadIdx.x % 32, warp = threadIdx.x / 32;
+  const HeadsSide& s = g.side[which];
+  if (!s.dgamma) return;
+  const float* p = g.work + (which ? (uint64_t)g.side[0].parts * g.dim : 0u) + col;
+  float sum = 0.0f;
+  if (col < g.dim) {
+#pragma unroll 4
+    for (uint32_t x = warp; x < s.parts; x += 8u) sum += p[(uint64_t)x * g.dim];
+  }
+  sums[warp][threadIdx.x % 32] = sum;
+  __syncthreads();
+  if (warp || col >= g.dim) return;
+  sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) sum += sums[w][threadIdx.x];
+  if (g.wdtype == kF32)
+    put_elem<kF32>(s.dgamma, col, sum);
+  else
+    put_elem<kBF16>(s.dgamma, col, sum);
+}
+
+struct TableArgs {
+  float2* table;
+  uint32_t positions, half;
+  double step, scale;  // base^(-2 / rotary)'s logarithm to base 2
+};
+__global__ void __launch_bounds__(256) rotation_table_kernel(const TableArgs g) {
+  dep_trigger();
+  dep_wait();
+  const uint64_t total = (uint64_t)g.positions * g.half;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < total; i += (uint64_t)gridDim.x * 256u) {
+    const double angle = (double)(i / g.half) * exp2((double)(i % g.half) * g.step) * g.scale;
+    double n, c;
+    sincos(angle, &n, &c);
+    g.table[i] = make_float2((float)c, (float)n);
+  }
+}
+
+// Whether rows can be taken in slots: whole slots of what is rotated and of the rest, at most one to a lane, vectors on 16-byte boundaries.
+template <int DT>
+uint32_t heads_slots(const HeadsArgs& a) {
+  const uint32_t two = 2u * kV<DT>;
+  uint64_t all = a.dim % two || a.rotary % two || a.dim / two > 32u ? 1u : 0u;
+  if (a.rotary) all |= (uintptr_t)a.table % 16u;
+  for (const HeadsSide& s : a.side) {
+    if (!s.heads) continue;
+    all |= ((uintptr_t)s.x | (uintptr_t)s.out | (uintptr_t)s.dx | (uintptr_t)s.dy) % 16u;
+    const uint64_t tokens = a.tokens > 1u ? s.token | s.out_token : 0u, heads = s.heads > 1u ? s.head | s.out_head : 0u;
+    all |= ((tokens | heads) * kEs<DT>) % 16u;
+  }
+  return all ? 0u : a.dim / two;
+}
+
+template <int DT, int T, int U, bool HALVES>
+int forward_t(const HeadsArgs& a, cudaStream_t stream) {
+  constexpr uint32_t span = 32 / T * U;
+  const uint64_t units = (uint64_t)a.tokens * ((a.side[0].heads + span - 1u) / span + (a.side[1].heads + span - 1u) / span);
+  const uint64_t grid = (units + kHeadWarps - 1u) / kHeadWarps + (a.status ? 1u : 0u);
+  if (grid > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
+  return launch_plain<heads_forward_kernel<DT, T, U, HALVES>>((uint32_t)grid, kHeadThreads, 0, 1, stream, a);
+}
+template <int DT, int T>
+int forward_n(const HeadsArgs& a, cudaStream_t stream) {
+  // four rows to a team where that leaves every SM four warps
+  const uint64_t rows = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads);
+  const bool many = rows >= (uint64_t)std::max(1, sm_count()) * 4u * (32u / T * 4u);
+  if (a.halves) return many ? forward_t<DT, T, 4, true>(a, stream) : forward_t<DT, T, 1, true>(a, stream);
+  return many ? forward_t<DT, T, 4, false>(a, stream) : forward_t<DT, T, 1, false>(a, stream);
+}
+template <int DT>
+int forward_d(const HeadsArgs& a, cudaStream_t stream) {
+  const uint32_t slots = heads_slots<DT>(a);
+  if (!slots) {
+    const uint64_t units = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads), grid = (units + kHeadWarps - 1u) / kHeadWarps + (a.status ? 1u : 0u);
+    if (grid > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
+    return launch_plain<heads_forward_loose_kernel<DT>>((uint32_t)grid, kHeadThreads, 0, 1, stream, a);
+  }
+  if (slots <= 4u) return forward_n<DT, 4>(a, stream);
+  if (slots <= 8u) return forward_n<DT, 8>(a, stream);
+  if (slots <= 16u) return forward_n<DT, 16>(a, stream);
+  return forward_n<DT, 32>(a, stream);
+}
+
+// CTAs of the backward pass, at most (three to an SM), and for how few rows there is another.  The workspace is sized for kHeadFewest.
+constexpr uint32_t kHeadParts = 148 * 3, kHeadFewest = 4;
+
+uint64_t heads_parts_of(const HeadsArgs& a, uint32_t rows_per_cta) {
+  const uint64_t rows = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads);
+  return std::min<uint64_t>(kHeadParts, std::max<uint64_t>(2, (rows + rows_per_cta - 1) / rows_per_cta));
+}
+// Dealt out to queries and keys by the rows that they have, so that all end together.
+void heads_parts(HeadsArgs* a, uint32_t rows_per_cta) {
+  const uint64_t q = a->side[0].heads, k = a->side[1].heads, all = heads_parts_of(*a, rows_per_cta);
+  a->side[0].parts = !q ? 0u : !k ? (uint32_t)all : (uint32_t)std::min<uint64_t>(all - 1, std::max<uint64_t>(1, all * q / (q + k)));
+  a->side[1].parts = !k ? 0u : (uint32_t)(all - a->side[0].parts);
+}
+
+template <typename L>
+int backward_launch(const HeadsArgs& a, cudaStream_t stream, L rows) {
+  const int rc = rows(a.side[0].parts + a.side[1].parts + (a.status ? 1u : 0u));
+  if (rc != FH_OK || (!a.side[0].dgamma && !a.side[1].dgamma)) return rc;
+  return launch_plain<heads_columns_kernel>((a.dim + 31u) / 32u * 2u, 256, 0, 1, stream, a);
+}
+template <int DT, int T, int U, bool HALVES>
+int backward_t(const HeadsArgs& a0, cudaStream_t stream) {
+  HeadsArgs a = a0;
+  heads_parts(&a, U * kHeadWarps * (32u / T));
+  static_assert(U * kHeadWarps * (32u / T) >= kHeadFewest, "the workspace's size");
+  return backward_launch(a, stream, [&](uint32_t grid) { return launch_plain<heads_backward_kernel<DT, T, U, HALVES>>(grid, kHeadThreads, 0, 1, stream, a); });
+}
+template <int DT, int T>
+int backward_n(const HeadsArgs& a, cudaStream_t stream) {
+  return a.halves ? backward_t<DT, T, 2, true>(a, stream) : backward_t<DT, T, 2, false>(a, stream);
+}
+template <int DT>
+int backward_d(const HeadsArgs& a0, cudaStream_t stream) {
+  const uint32_t slots = heads_slots<DT>(a0);
+  if (!slots) {
+    HeadsArgs a = a0;
+    const uint32_t warps = std::max(1u, std::min(kHeadWarps, 8192u / a.dim));  // (32 KB of sums)
+    heads_parts(&a, kHeadFewest * warps);
+    return backward_launch(a, stream, [&](uint32_t grid) {
+      return launch_plain<heads_backward_loose_kernel<DT>>(grid, (int)warps * 32, (size_t)warps * a.dim * sizeof(float), 1, stream, a);
+    });
+  }
+  if (slots <= 4u) return backward_n<DT, 4>(a0, stream);
+  if (slots <= 8u) return backward_n<DT, 8>(a0, stream);
+  if (slots <= 16u) return backward_n<DT, 16>(a0, stream);
+  return backward_n<DT, 32>(a0, stream);
+}
+
+}  // namespace
+
+size_t heads_work_floats(const HeadsArgs& a) { return (size_t)heads_parts_of(a, kHeadFewest) * a.dim; }
+
+int launch_heads_forward(const HeadsArgs& a, int dtype, cudaStream_t stream) {
+  return dtype == kF32 ? forward_d<kF32>(a, stream) : forward_d<kBF16>(a, stream);
+}
+
+int launch_heads_backward(const HeadsArgs& a, int dtype, cudaStream_t stream) {
+  return dtype == kF32 ? backward_d<kF32>(a, stream) : backward_d<kBF16>(a, stream);
+}
+
+int launch_rotation_table(uint32_t positions, uint32_t rotary, double base, double scale, float2* table, cudaStream_t stream) {
+  TableArgs a = {table, positions, rotary / 2u, -2.0 * std::log2(base) / rotary, scale};
+  const uint64_t ctas = ((uint64_t)positions * a.half + 255u) / 256u;
+  return launch_plain<rotation_table_kernel>((uint32_t)std::min<uint64_t>(ctas, (uint64_t)std::max(1, sm_count()) * 16u), 256, 0, 1, stream, a);
+}
+
+}  // namespace fh

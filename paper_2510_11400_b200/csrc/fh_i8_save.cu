@@ -1,0 +1,284 @@
+// Dense matrices into 8-bit containers and back.
+#include "fh_i8.cuh"
+#include "fh_i8_launch.cuh"
+#include "fh_launch.cuh"
+#include "fh_tcgen05.cuh"
+
+namespace fh {
+namespace {
+
+constexpr int kI8Threads = 256;
+
+template <int DT>
+constexpr uint32_t kEs = DT == kF32 ? 4u : 2u;
+
+// ---- by rows ---------------------------------------------------------------------------------------
+// A CTA takes R rows.  Lanes of a warp lie R rows by 32 / R chunks of 16 columns: R lanes that write the codes of the same chunk write R x 16 bytes
+// side by side (a sector or more from R = 2 on), and lanes of the same row read 32 / R chunks side by side.  A lane's I chunks stay in registers from the
+// row's maximum to its codes; I = 0: the row is too long for that and is read again, from L2.
+template <int DT, int R, int I, bool VEC>
+__global__ void __launch_bounds__(512) i8_rows_kernel(const I8SaveArgs g) {
+  __shared__ uint32_t tops[16][R];
+  constexpr uint32_t kLanes = 32 / R;
+  const I8Layout l(g.rows, g.cols);
+  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = blockDim.x / 32;
+  const uint32_t r = lane % R, row = blockIdx.x * R + r, chunks = l.chunks(), first = warp * kLanes + lane / R, step = warps * kLanes;
+  dep_trigger();
+  dep_wait();
+  if (blockIdx.x == 0 && tid < 32) i8_write_header(g.dst, l, tid);
+  const uint8_t* src = g.src + (uint64_t)row * g.ld * kEs<DT>;
+  const bool there = row < g.rows;
+  auto fetch = [&](Raw16<DT>& x, uint32_t j) {
+    const uint32_t c = j * 16u;
+    x.template load<VEC>(src + (uint64_t)c * kEs<DT>, there && c < g.cols ? (int)min(16u, g.cols - c) : 0);
+  };
+  constexpr int N = I ? I : 1;
+  Raw16<DT> x[N];
+  uint32_t top = 0;
+  if (I) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) fetch(x[i], first + i * step);
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, x[i].top());
+  } else {
+#pragma unroll 2
+    for (uint32_t j = first; j < chunks; j += step) {
+      fetch(x[0], j);
+      top = max(top, x[0].top());
+    }
+  }
+#pragma unroll
+  for (int s = R; s < 32; s *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+  if (lane < R) tops[warp][r] = top;
+  __syncthreads();
+  for (uint32_t w = 0; w < warps; ++w) top = max(top, tops[w][r]);
+  const I8Coder coder(top);
+  uint8_t* dst = g.dst + l.code_at(row, 0);
+  const uint64_t pitch = 16ull * l.block_rows(row / 128u);
+  auto put = [&](const Raw16<DT>& v, uint32_t j) {
+    float f[16];
+    v.values(f);
+    *reinterpret_cast<uint4*>(dst + j * pitch) = i8_codes16(f, coder);
+  };
+  if (row < l.r8) {
+    if (I) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (first + i * step < chunks) put(x[i], first + i * step);
+    } else {
+#pragma unroll 2
+      for (uint32_t j = first; j < chunks; j += step) {
+        fetch(x[0], j);
+        put(x[0], j);
+      }
+    }
+    if (warp == 0 && lane < R) *reinterpret_cast<uint32_t*>(g.dst + l.magnitude_at(row)) = i8_magnitude_bits(top);
+  }
+}
+
+template <int DT, int R, int I, bool VEC>
+int rows_launch(const I8SaveArgs& a, uint32_t warps, cudaStream_t stream) {
+  const uint64_t grid = (I8Layout(a.rows, a.cols).r8 + R - 1ull) / R;
+  if (grid > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
+  return launch_plain<i8_rows_kernel<DT, R, I, VEC>>((uint32_t)grid, (int)warps * 32, 0, 1, stream, a);
+}
+template <int DT, int R, bool VEC>
+int rows_by_length(const I8SaveArgs& a, cudaStream_t stream) {
+  constexpr uint32_t kLanes = 32 / R, kMost = DT == kF32 ? 2 : 4;
+  const uint32_t need = (I8Layout(a.rows, a.cols).chunks() + kLanes - 1u) / kLanes;  // steps of a warp in all
+  if (need <= 16u) return rows_launch<DT, R, 1, VEC>(a, need, stream);
+  if (need <= 32u) return rows_launch<DT, R, 2, VEC>(a, (need + 1u) / 2u, stream);
+  if (kMost >= 4 && need <= 64u) return rows_launch<DT, R, DT == kF32 ? 2 : 4, VEC>(a, (need + 3u) / 4u, stream);
+  return rows_launch<DT, R, 0, VEC>(a, 16u, stream);
+}
+template <int DT, bool VEC>
+int rows_by_group(const I8SaveArgs& a, cudaStream_t stream) {
+  // Rows to a CTA: as few as keep the row in the registers of 16 warps, and as few as give every SM one; with 8, pieces of codes are written whole.
+  const uint32_t chunks = I8Layout(a.rows, a.cols).chunks(), sms = (uint32_t)std::max(1, sm_count()), most = DT == kF32 ? 32u : 64u;
+  uint32_t r = 8u;
+  while (r > 1u && ((chunks + 32u / r - 1u) / (32u / r) > most || (a.rows + r - 1u) / r < sms)) r /= 2u;
+  if (r == 1u) return rows_by_length<DT, 1, VEC>(a, stream);
+  if (r == 2u) return rows_by_length<DT, 2, VEC>(a, stream);
+  if (r == 4u) return rows_by_length<DT, 4, VEC>(a, stream);
+  return rows_by_length<DT, 8, VEC>(a, stream);
+}
+
+// ---- by columns ------------------------------------------------------------------------------------
+// The container of the transpose: its rows are the matrix's columns, its chunks 16 of the matrix's rows.  A lane has C neighbouring columns and 16 rows at
+// a time, whose codes are C times 16 bytes side by side in the container, 32 C columns to a warp: both sides are in whole sectors without a detour through
+// shared memory.  A cluster's CTAs share the rows of a group of columns, put their maxima together and then read their rows again, from L2 as a
+// rule.
+constexpr int kColWarps = 8;
+
+template <int DT, int C, bool VEC>
+struct ColChunk {
+  static constexpr int kWords = C * (int)kEs<DT> / 4 ? C * (int)kEs<DT> / 4 : 1;
+  uint32_t w[16][kWords];
+  // Rows 16 j ... of the columns from `col` on (n of them there), zeros elsewhere.
+  __device__ __forceinline__ void load(const I8SaveArgs& g, uint32_t j, uint32_t col, int n) {
+    const uint8_t* p = g.src + ((uint64_t)j * 16u * g.ld + col) * kEs<DT>;
+    const uint64_t step = g.ld * kEs<DT>;
+#pragma unroll
+    for (int i = 0; i < 16; ++i, p += step) {
+      const bool there = (uint64_t)j * 16u + i < g.rows;
+#pragma unroll
+      for (int x = 0; x < kWords; ++x) w[i][x] = 0u;
+      if (VEC) {
+        if (there && n == C) {
+          if (kWords == 1) w[i][0] = *reinterpret_cast<const uint32_t*>(p);
+          if (kWords == 2) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            w[i][0] = v.x;
+            w[i][kWords - 1] = v.y;
+          }
+          continue;
+        }
+      }
+      if (there) {
+#pragma unroll
+        for (int x = 0; x < C; ++x)
+          if (x < n) {
+            if (DT == kF32)
+              w[i][x] = reinterpret_cast<const uint32_t*>(p)[x];
+            else
+              w[i][x / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[x] << (x % 2 * 16);
+          }
+      }
+    }
+  }
+  __device__ __forceinline__ float at(int row, int col) const {
+    if (DT == kF32) return __uint_as_float(w[row][col]);
+    return __uint_as_float(col % 2 ? w[row][col / 2] & 0xFFFF0000u : w[row][col / 2] << 16);
+  }
+};
+
+template <int DT, int C, bool VEC>
+__global__ void __launch_bounds__(kColWarps * 32) i8_cols_kernel(const I8SaveArgs g) {
+  constexpr uint32_t kCols = 32 * C;
+  __shared__ uint32_t tops[kColWarps][kCols];
+  __shared__ uint32_t mine[kCols];
+  const I8Layout l(g.cols, g.rows);
+  const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const uint32_t rank = g.parts > 1u ? blockIdx.x % g.parts : 0u, c0 = blockIdx.x / g.parts * kCols, col = c0 + lane * C;
+  const uint32_t chunks = l.chunks(), first = (uint32_t)((uint64_t)chunks * rank / g.parts) + warp, last = (uint32_t)((uint64_t)chunks * (rank + 1u) / g.parts);
+  const int n = col < g.cols ? (int)min((uint32_t)C, g.cols - col) : 0;
+  dep_trigger();
+  dep_wait();
+  if (blockIdx.x == 0 && tid < 32) i8_write_header(g.dst, l, tid);
+  ColChunk<DT, C, VEC> x;
+  uint32_t top[C] = {};
+  for (uint32_t j = first; j < last; j += kColWarps) {
+    x.load(g, j, col, n);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int c = 0; c < C; ++c) top[c] = max(top[c], __float_as_uint(x.at(i, c)) & 0x7FFFFFFFu);
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) tops[warp][lane * C + c] = top[c];
+  __syncthreads();
+  if (tid < kCols) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int w = 0; w < kColWarps; ++w) t = max(t, tops[w][tid]);
+    mine[tid] = t;
+  }
+  if (g.parts > 1u) {
+    cluster_sync();
+    if (tid < kCols) {
+      uint32_t t = 0;
+      for (uint32_t p = 0; p < g.parts; ++p) t = max(t, ld_cluster_u32(mine + tid, p));
+      tops[0][tid] = t;
+    }
+    cluster_sync();  // (before any CTA ends: others read its maxima)
+  } else if (tid < kCols) {
+    tops[0][tid] = mine[tid];
+  }
+  __syncthreads();
+  if (rank == 0u && tid < kCols && c0 + tid < l.r8) *reinterpret_cast<uint32_t*>(g.dst + l.magnitude_at(c0 + tid)) = i8_magnitude_bits(tops[0][tid]);
+  if (col >= l.r8) return;
+  const uint64_t pitch = 16ull * l.block_rows(col / 128u);
+  uint8_t* dst = g.dst + l.code_at(col, 0);
+  for (uint32_t j = first; j < last; j += kColWarps) {
+    x.load(g, j, col, n);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const I8Coder coder(tops[0][lane * C + c]);
+      float f[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = x.at(i, c);
+      *reinterpret_cast<uint4*>(dst + j * pitch + c * 16u) = i8_codes16(f, coder);
+    }
+  }
+}
+
+template <int DT, int C, bool VEC>
+int cols_launch(const I8SaveArgs& a0, cudaStream_t stream) {
+  I8SaveArgs a = a0;
+  const uint32_t chunks = I8Layout(a.cols, a.rows).chunks();
+  const uint64_t groups = ((uint64_t)a.cols + 32u * C - 1u) / (32u * C);
+  a.parts = 1u;
+  while (a.parts < 8u && chunks >= 2u * kColWarps * a.parts) a.parts *= 2u;
+  if (groups * a.parts > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
+  return launch_plain<i8_cols_kernel<DT, C, VEC>>((uint32_t)(groups * a.parts), kColWarps * 32, 0, (int)a.parts, stream, a);
+}
+
+// ---- and back --------------------------------------------------------------------------------------
+// A warp's lanes lie 8 rows by 4 chunks, as in the kernel by rows.
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kI8Threads) i8_restore_kernel(const I8SaveArgs g) {
+  const I8Layout l(g.rows, g.cols);
+  const uint32_t tid = threadIdx.x, lane = tid % 32;
+  dep_trigger();
+  dep_wait();
+  const bool ok = i8_header_ok(g.src, g.src_bytes, l);
+  if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
+  if (!ok) return;
+  const uint32_t quads = (l.chunks() + 3u) / 4u;
+  const uint64_t items = (uint64_t)(l.r8 / 8u) * quads, step = (uint64_t)gridDim.x * (kI8Threads / 32);
+  for (uint64_t it = (uint64_t)blockIdx.x * (kI8Threads / 32) + tid / 32; it < items; it += step) {
+    const uint32_t row = (uint32_t)(it / quads) * 8u + lane % 8u, j = (uint32_t)(it % quads) * 4u + lane / 8u, c = j * 16u;
+    if (row >= g.rows || c >= g.cols) continue;
+    const uint4 q = *reinterpret_cast<const uint4*>(g.src + l.code_at(row, j));
+    const float s = i8_scale(*reinterpret_cast<const float*>(g.src + l.magnitude_at(row)));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    float f[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)  // (127 scales of a row that has fp32's largest number may be beyond it)
+      f[i] = max_nan(min_nan((float)((int32_t)(w[i / 4] << (24 - i % 4 * 8)) >> 24) * s, 3.4028235e38f), -3.4028235e38f);
+    Raw16<DT> x;
+    x.take(f);
+    x.template store<VEC>(g.dst + ((uint64_t)row * g.ld + c) * kEs<DT>, (int)min(16u, g.cols - c));
+  }
+}
+
+template <int DT>
+bool on_grid(const void* p, uint64_t ld) { return ((uintptr_t)p | ld * kEs<DT>) % 16u == 0u; }
+
+template <int DT>
+int restore_launch(const I8SaveArgs& a, cudaStream_t stream) {
+  const I8Layout l(a.rows, a.cols);
+  const uint64_t items = (uint64_t)(l.r8 / 8u) * ((l.chunks() + 3u) / 4u), ctas = (items + kI8Threads / 32 - 1) / (kI8Threads / 32);
+  const uint32_t grid = (uint32_t)std::min<uint64_t>(ctas, (uint64_t)std::max(1, sm_count()) * 32u);
+  if (on_grid<DT>(a.dst, a.ld)) return launch_plain<i8_restore_kernel<DT, true>>(grid, kI8Threads, 0, 1, stream, a);
+  return launch_plain<i8_restore_kernel<DT, false>>(grid, kI8Threads, 0, 1, stream, a);
+}
+
+}  // namespace
+
+int launch_i8_rows(const I8SaveArgs& a, int dtype, cudaStream_t stream) {
+  if (dtype == kF32) return on_grid<kF32>(a.src, a.ld) ? rows_by_group<kF32, true>(a, stream) : rows_by_group<kF32, false>(a, stream);
+  return on_grid<kBF16>(a.src, a.ld) ? rows_by_group<kBF16, true>(a, stream) : rows_by_group<kBF16, false>(a, stream);
+}
+
+int launch_i8_cols(const I8SaveArgs& a, int dtype, cudaStream_t stream) {
+  if (dtype == kF32) return cols_launch<kF32, 1, false>(a, stream);
+  const bool words = ((uintptr_t)a.src | a.ld * 2u) % 4u == 0u;
+  return words ? cols_launch<kBF16, 2, true>(a, stream) : cols_launch<kBF16, 1, false>(a, stream);
+}
+
+int launch_i8_decompress(const I8SaveArgs& a, int dtype, cudaStream_t stream) {
+  return dtype == kF32 ? restore_launch<kF32>(a, stream) : restore_launch<kBF16>(a, stream);
+}
+
+}  // namespace fh

@@ -55,6 +55,25 @@ __device__ __forceinline__ void tc_mma_mx(uint32_t d, uint64_t a, uint64_t b, ui
         : "memory");
 }
 
+// Instruction descriptor: both operands signed 8-bit integers, sums in 32 bits, M x N.
+__host__ __device__ constexpr uint32_t i8_idesc(uint32_t m, uint32_t n) { return 2u << 4 | 1u << 7 | 1u << 10 | n / 8u << 17 | m / 16u << 24; }
+// D (+)= A B^T over 32 elements; with PAIR of a pair of CTAs (see below).
+template <bool PAIR>
+__device__ __forceinline__ void tc_mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  if (PAIR)
+    asm volatile(
+        "{ .reg .pred p; setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p; }" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+  else
+    asm volatile(
+        "{ .reg .pred p; setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p; }" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+
 // ---- a pair of CTAs (neighbouring ranks of a cluster) on one accumulator: 256 rows, 128 in each CTA's tensor memory.  The even one issues;
 // an address is that in either CTA's own memory.
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* at, uint32_t cols) {
