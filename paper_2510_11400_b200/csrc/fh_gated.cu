@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(512) gated_backward_kernel(const GatedArgs g) 
   __syncthreads();
   for (uint32_t w = 0; w < warps; ++w) top = max(top, tops[w][r]);
   if (row >= l.r8) return;
-  const I8Coder coder(top);
+  const I8Coder<DT> coder(top);
   uint8_t* dst = g.packed + l.code_at(row, 0);
   const uint64_t pitch = 16ull * l.block_rows(row / 128u);
   // Codes of n elements from column c of dpre on, n < 16 or c off the chunks' boundaries where the width is no multiple of 16.

@@ -45,9 +45,9 @@ struct Slot {
   }
 };
 
+// The values of a 16-byte vector.
 template <int DT>
-__device__ __forceinline__ void load_vec(const uint8_t* p, float* v) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
+__device__ __forceinline__ void vec_values(const uint4& w, float* v) {
   if (DT == kF32) {
     v[0] = __uint_as_float(w.x);
     v[1] = __uint_as_float(w.y);
@@ -62,6 +62,21 @@ __device__ __forceinline__ void load_vec(const uint8_t* p, float* v) {
     }
   }
 }
+// A slot of a row as it is in memory (as values it would take twice the registers in bf16, of which there are several rows at once).
+struct RawSlot {
+  uint4 a, b;
+  __device__ __forceinline__ void zero() { a = b = make_uint4(0u, 0u, 0u, 0u); }
+  template <int DT>
+  __device__ __forceinline__ void load(const uint8_t* p, uint32_t at, uint32_t bt) {
+    a = *reinterpret_cast<const uint4*>(p + at * kEs<DT>);
+    b = *reinterpret_cast<const uint4*>(p + bt * kEs<DT>);
+  }
+  template <int DT>
+  __device__ __forceinline__ void values(float (&v)[2 * kV<DT>]) const {
+    vec_values<DT>(a, v);
+    vec_values<DT>(b, v + kV<DT>);
+  }
+};
 template <int DT>
 __device__ __forceinline__ void store_vec(uint8_t* p, const float* v) {
   uint4 w;
@@ -74,6 +89,21 @@ __device__ __forceinline__ void store_vec(uint8_t* p, const float* v) {
 __device__ __forceinline__ float weight_at(const uint8_t* gamma, int wdtype, uint32_t i) {
   if (!gamma) return 1.0f;
   return wdtype == kF32 ? reinterpret_cast<const float*>(gamma)[i] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(gamma)[i]);
+}
+// The weights of a slot.
+template <int DT>
+__device__ __forceinline__ void load_weights(const uint8_t* gamma, const HeadsArgs& g, uint32_t a, uint32_t b, float (&w)[2 * kV<DT>]) {
+  constexpr uint32_t V = kV<DT>;
+  if (gamma && (uintptr_t)gamma % 16u == 0u && g.wdtype == kF32) {
+#pragma unroll
+    for (uint32_t e = 0; e < 2 * V; e += 4) vec_values<kF32>(*reinterpret_cast<const uint4*>(gamma + ((e < V ? a : b - V) + e) * 4u), w + e);
+  } else if (gamma && (uintptr_t)gamma % 16u == 0u && DT == kBF16) {
+#pragma unroll
+    for (uint32_t e = 0; e < 2 * V; e += 8) vec_values<kBF16>(*reinterpret_cast<const uint4*>(gamma + ((e < V ? a : b - V) + e) * 2u), w + e % (2 * V));
+  } else {
+#pragma unroll
+    for (uint32_t e = 0; e < 2 * V; ++e) w[e] = weight_at(gamma, g.wdtype, (e < V ? a : b - V) + e);
+  }
 }
 template <int DT>
 __device__ __forceinline__ float elem_at(const uint8_t* p, uint32_t i) {
@@ -172,52 +202,43 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_kernel(const Heads
   if (u >= units) return;
   const HeadUnit unit(u, g, kSpan);
   const HeadsSide& s = g.side[unit.side];
-  const int64_t at = position_of(g, unit.token);
-  if (at < 0) return;
   const Slot<DT> slot(lane % T, g.dim, g.rotary, HALVES);
-  float x[U][2 * V];
+  RawSlot raw[U];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     const uint32_t head = unit.head + i * kTeams + team;
-#pragma unroll
-    for (uint32_t e = 0; e < 2 * V; ++e) x[i][e] = 0.0f;
-    if (slot.there && head < s.heads) {
-      const uint8_t* p = s.x + ((uint64_t)unit.token * s.token + (uint64_t)head * s.head) * kEs<DT>;
-      load_vec<DT>(p + slot.a * kEs<DT>, x[i]);
-      load_vec<DT>(p + slot.b * kEs<DT>, x[i] + V);
-    }
+    raw[i].zero();
+    if (slot.there && head < s.heads) raw[i].load<DT>(s.x + ((uint64_t)unit.token * s.token + (uint64_t)head * s.head) * kEs<DT>, slot.a, slot.b);
   }
   float c[V], n[V], w[2 * V];
-  if (slot.there) {
-    load_turn<DT>(g, slot, at, c, n);
-#pragma unroll
-    for (uint32_t e = 0; e < V; ++e) {
-      w[e] = weight_at(s.gamma, g.wdtype, slot.a + e);
-      w[V + e] = weight_at(s.gamma, g.wdtype, slot.b + e);
-    }
-  }
+  if (slot.there) load_weights<DT>(s.gamma, g, slot.a, slot.b, w);
+  const int64_t at = position_of(g, unit.token);
+  if (at < 0) return;
+  if (slot.there) load_turn<DT>(g, slot, at, c, n);
   const float size = (float)g.dim;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     const uint32_t head = unit.head + i * kTeams + team;
+    float x[2 * V];
+    raw[i].values<DT>(x);
     if (g.layer) {
       float sum = 0.0f;
 #pragma unroll
-      for (uint32_t e = 0; e < 2 * V; ++e) sum += x[i][e];
+      for (uint32_t e = 0; e < 2 * V; ++e) sum += x[e];
       const float mean = __fdiv_rn(team_sum<T>(sum), size);
 #pragma unroll
-      for (uint32_t e = 0; e < 2 * V; ++e) x[i][e] = slot.there ? x[i][e] - mean : 0.0f;
+      for (uint32_t e = 0; e < 2 * V; ++e) x[e] = slot.there ? x[e] - mean : 0.0f;
     }
     float sum = 0.0f;
 #pragma unroll
-    for (uint32_t e = 0; e < 2 * V; ++e) sum = __fmaf_rn(x[i][e], x[i][e], sum);
+    for (uint32_t e = 0; e < 2 * V; ++e) sum = __fmaf_rn(x[e], x[e], sum);
     const float rstd = 1.0f / sqrtf(__fdiv_rn(team_sum<T>(sum), size) + g.eps);
     if (!slot.there || head >= s.heads) continue;
     float y[2 * V];
 #pragma unroll
     for (uint32_t p = 0; p < V; ++p) {
       const uint32_t fi = first_of<HALVES, V>(p), se = second_of<HALVES, V>(p);
-      const float za = x[i][fi] * rstd * w[fi], zb = x[i][se] * rstd * w[se];
+      const float za = x[fi] * rstd * w[fi], zb = x[se] * rstd * w[se];
       y[fi] = __fmaf_rn(za, c[p], -(zb * n[p]));
       y[se] = __fmaf_rn(zb, c[p], za * n[p]);
     }
@@ -247,61 +268,56 @@ __global__ void __launch_bounds__(kHeadThreads) heads_backward_kernel(const Head
   const uint32_t spans = (s.heads + kSpan - 1u) / kSpan;
   const uint64_t units = (uint64_t)g.tokens * spans;
   const float size = (float)g.dim;
-  float w[2 * V], acc[2 * V];
-#pragma unroll
-  for (uint32_t e = 0; e < 2 * V; ++e) {
-    w[e] = slot.there ? weight_at(s.gamma, g.wdtype, (e < V ? slot.a : slot.b - V) + e) : 0.0f;
-    acc[e] = 0.0f;
-  }
+  float w[2 * V] = {}, acc[2 * V] = {};
+  if (slot.there) load_weights<DT>(s.gamma, g, slot.a, slot.b, w);
   for (uint64_t u = (uint64_t)part * kHeadWarps + warp; u < units; u += (uint64_t)s.parts * kHeadWarps) {
     const uint32_t token = (uint32_t)(u / spans), head0 = (uint32_t)(u % spans) * kSpan;
-    const int64_t at = position_of(g, token);
-    if (at < 0) continue;
-    float c[V], n[V];
-    float x[U][2 * V], d[U][2 * V];
+    RawSlot xs[U], ds[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const uint32_t head = head0 + i * kTeams + team;
-#pragma unroll
-      for (uint32_t e = 0; e < 2 * V; ++e) x[i][e] = d[i][e] = 0.0f;
+      xs[i].zero();
+      ds[i].zero();
       if (slot.there && head < s.heads) {
-        const uint8_t* p = s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
-        const uint8_t* q = s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
-        load_vec<DT>(p + slot.a * kEs<DT>, x[i]);
-        load_vec<DT>(p + slot.b * kEs<DT>, x[i] + V);
-        load_vec<DT>(q + slot.a * kEs<DT>, d[i]);
-        load_vec<DT>(q + slot.b * kEs<DT>, d[i] + V);
+        xs[i].load<DT>(s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>, slot.a, slot.b);
+        ds[i].load<DT>(s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>, slot.a, slot.b);
       }
     }
+    const int64_t at = position_of(g, token);
+    if (at < 0) continue;
+    float c[V], n[V];
     if (slot.there) load_turn<DT>(g, slot, at, c, n);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const uint32_t head = head0 + i * kTeams + team;
       const bool there = slot.there && head < s.heads;
+      float x[2 * V], d[2 * V];
+      xs[i].values<DT>(x);
+      ds[i].values<DT>(d);
       if (g.layer) {
         float sum = 0.0f;
 #pragma unroll
-        for (uint32_t e = 0; e < 2 * V; ++e) sum += x[i][e];
+        for (uint32_t e = 0; e < 2 * V; ++e) sum += x[e];
         const float mean = __fdiv_rn(team_sum<T>(sum), size);
 #pragma unroll
-        for (uint32_t e = 0; e < 2 * V; ++e) x[i][e] = there ? x[i][e] - mean : 0.0f;
+        for (uint32_t e = 0; e < 2 * V; ++e) x[e] = there ? x[e] - mean : 0.0f;
       }
       // dz in d, then the sums of x^2, g x and g
       if (there) {
 #pragma unroll
         for (uint32_t p = 0; p < V; ++p) {
           const uint32_t fi = first_of<HALVES, V>(p), se = second_of<HALVES, V>(p);
-          const float ya = d[i][fi], yb = d[i][se];
-          d[i][fi] = __fmaf_rn(ya, c[p], yb * n[p]);
-          d[i][se] = __fmaf_rn(yb, c[p], -(ya * n[p]));
+          const float ya = d[fi], yb = d[se];
+          d[fi] = __fmaf_rn(ya, c[p], yb * n[p]);
+          d[se] = __fmaf_rn(yb, c[p], -(ya * n[p]));
         }
       }
       float xx = 0.0f, gx = 0.0f, gs = 0.0f;
 #pragma unroll
       for (uint32_t e = 0; e < 2 * V; ++e) {
-        const float gg = d[i][e] * w[e];
-        xx = __fmaf_rn(x[i][e], x[i][e], xx);
-        gx = __fmaf_rn(gg, x[i][e], gx);
+        const float gg = d[e] * w[e];
+        xx = __fmaf_rn(x[e], x[e], xx);
+        gx = __fmaf_rn(gg, x[e], gx);
         gs += gg;
       }
       xx = team_sum<T>(xx);
@@ -313,9 +329,9 @@ __global__ void __launch_bounds__(kHeadThreads) heads_backward_kernel(const Head
       float dx[2 * V];
 #pragma unroll
       for (uint32_t e = 0; e < 2 * V; ++e) {
-        const float xhat = x[i][e] * rstd;
-        acc[e] = __fmaf_rn(d[i][e], xhat, acc[e]);
-        dx[e] = rstd * (__fmaf_rn(-xhat, along, d[i][e] * w[e]) - level);
+        const float xhat = x[e] * rstd;
+        acc[e] = __fmaf_rn(d[e], xhat, acc[e]);
+        dx[e] = rstd * (__fmaf_rn(-xhat, along, d[e] * w[e]) - level);
       }
       if (s.dx) {
         uint8_t* o = s.dx + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fh_device.cuh"
 
 namespace fh {
@@ -63,33 +65,51 @@ __device__ __forceinline__ float i8_scale(float a) {
   return a == 0.0f ? 0.0f : s < 1.17549435e-38f ? 1.17549435e-38f : s;  // (a NaN stays one)
 }
 
+constexpr float kI8Magic23 = 12582912.0f;  // 1.5 * 2^23
+
 // How the elements of a row become codes: t = x * inv, rounded to a whole number k by adding 1.5 * 2^23, whose last bits then hold it.  inv is 1 / s
 // to within 2^-24, and |x / s| <= 127 (1 + 2^-22), so t is within 2^-16 of x / s: k is right unless x / s lies that near to the middle between two whole
-// numbers, and what is left over, r = x - k s, is exact (a multiple of the last place of x or of s, at most 0.51 s), so that comparing 2 |r| with s
-// settles the others.  Few elements do; `near` says that one of those seen so far does.
+// numbers.
+//
+// fp32: what is left over, r = x - k s, is exact (a multiple of the last place of x or of s, at most 0.51 s), so that comparing 2 |r| with s settles the
+// few elements whose |r| is next to s / 2.
+//
+// bf16: only half of the row's magnitude is that near to a middle (63.5), and elements whose quotient is a middle exactly.  With x = X 2^p and the
+// magnitude M 2^q, X and M of eight bits, 127 x / magnitude is |254 X - (2 k + 1) M 2^(q - p)| / (2 M 2^(q - p)) away from the middle above k: nothing, or at
+// least 1 / (2 M 2^(q - p)), which is fifty times what t may be off by (127 * 255 / (M 2^(q - p)) times 2^-21).  Nothing: 127 divides M, which then
+// is 254, so that s is a power of two and everything is exact; or it divides 2 k + 1, which then is 127: x is half of the magnitude.  So inv is moved
+// by a last place where half the magnitude would come out on the wrong side, and no element is looked at again.  (Half of the magnitude is no rare
+// value: looking again at 16 elements where one of them is near a middle made 8192 x 4096 take 60 us instead of @@.)
+template <int DT>
 struct I8Coder {
   float inv, s, edge;
+  __device__ __forceinline__ I8Coder() {}
   // `bits`: of the row's largest magnitude.  A row with a NaN or an infinity has codes 0, whatever x is.
   __device__ __forceinline__ explicit I8Coder(uint32_t bits) {
     const bool bad = bits >= 0x7F800000u;
     s = bad ? 0.0f : i8_scale(__uint_as_float(bits));
     inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
     edge = s > 0.0f ? s * 0.49997f : __uint_as_float(0x7F800000u);
+    if (DT == kBF16 && s > 1.17549435e-38f) {  // (the smallest scale is a power of two)
+      const float half = 0.5f * __uint_as_float(bits);
+      const bool up = __fmaf_rn(-63.5f, s, half) >= 0.0f, got = __fmaf_rn(half, inv, -63.5f) >= 0.0f;
+      if (up != got) inv = __uint_as_float(__float_as_uint(inv) + (up ? 1u : ~0u));
+    }
   }
 };
-constexpr float kI8Magic23 = 12582912.0f;
 __device__ __forceinline__ uint32_t i8_magnitude_bits(uint32_t top) { return top >= 0x7F800000u ? 0x7FC00000u : top; }
 
 // One element, exactly.
-__device__ __forceinline__ uint32_t i8_code_exact(float x, const I8Coder& c) {
+__device__ __forceinline__ uint32_t i8_code_exact(float x, const I8Coder<kF32>& c) {
   if (!(c.s > 0.0f)) return 0u;
   float k = __fmaf_rn(x, c.inv, kI8Magic23) - kI8Magic23;
   const float r = __fmaf_rn(-k, c.s, x), twice = 2.0f * fabsf(r);
   if (twice > c.s || (twice == c.s && ((int)k & 1))) k += r > 0.0f ? 1.0f : -1.0f;
   return (uint32_t)(int)k & 255u;
 }
-// 16 elements to 16 bytes.
-__device__ __forceinline__ uint4 i8_codes16(const float (&x)[16], const I8Coder& c) {
+// 16 elements, those of a row in bf16 all of that type, to 16 bytes.
+template <int DT>
+__device__ __forceinline__ uint4 i8_codes16(const float (&x)[16], const I8Coder<DT>& c) {
   const f32x2 inv = pack2(c.inv, c.inv), magic = pack2(kI8Magic23, kI8Magic23), less = pack2(-kI8Magic23, -kI8Magic23), ms = pack2(-c.s, -c.s);
   uint32_t t[16];
   float far = 0.0f;
@@ -97,13 +117,17 @@ __device__ __forceinline__ uint4 i8_codes16(const float (&x)[16], const I8Coder&
   for (int i = 0; i < 16; i += 2) {
     const f32x2 v = pack2(x[i], x[i + 1]), w = fma2(v, inv, magic);
     unpack2u(w, t[i], t[i + 1]);
-    float r0, r1;
-    unpack2(fma2(add2(w, less), ms, v), r0, r1);
-    far = fmaxf(fmaxf(far, fabsf(r0)), fabsf(r1));
+    if (DT == kF32) {
+      float r0, r1;
+      unpack2(fma2(add2(w, less), ms, v), r0, r1);
+      far = fmaxf(fmaxf(far, fabsf(r0)), fabsf(r1));
+    }
   }
-  if (!(far <= c.edge)) {
+  if (DT == kF32 && !(far <= c.edge)) {
+    if constexpr (DT == kF32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t[i] = i8_code_exact(x[i], c);
+      for (int i = 0; i < 16; ++i) t[i] = i8_code_exact(x[i], c);
+    }
   } else if (c.s == 0.0f) {
     return make_uint4(0u, 0u, 0u, 0u);
   }
@@ -193,6 +217,41 @@ struct Raw16 {
 #pragma unroll
     for (int i = 1; i < kWords; ++i) m = DT == kF32 ? max(m, w[i] & 0x7FFFFFFFu) : __vmaxu2(m, w[i] & 0x7FFF7FFFu);
     return DT == kF32 ? m : max(m << 16, m & 0x7FFF0000u);
+  }
+};
+
+// Rows off the 16-byte grid: a warp's R rows by 512 / R columns go through shared memory, so that neighbouring lanes touch neighbouring elements of the
+// matrix (element by element where each lane needs its 16, a warp's access met 32 sectors: restoring 8192 x 4095 bf16 203 us).
+template <int DT, int R>
+struct LooseRows {
+  static constexpr uint32_t kEsize = DT == kF32 ? 4u : 2u, kCols = 512u / R, kPitch = kCols * kEsize + 16u, kBytes = R * kPitch;
+  using E = typename std::conditional<DT == kF32, uint32_t, uint16_t>::type;
+  // Columns c0 ... of `rows` rows at p, `ld` elements apart, those below `cols`, zeros elsewhere: each lane gets the 16 of row lane % R, chunk lane / R.
+  static __device__ __forceinline__ void load(Raw16<DT>& x, uint8_t* stage, const uint8_t* p, uint64_t ld, uint32_t rows, uint32_t c0, uint32_t cols, uint32_t lane) {
+    E v[16];
+#pragma unroll
+    for (uint32_t i = 0; i < 16u; ++i) {
+      const uint32_t at = i * 32u + lane, r = at / kCols, c = c0 + at % kCols;
+      v[i] = r < rows && c < cols ? reinterpret_cast<const E*>(p)[r * ld + c] : (E)0;
+    }
+    __syncwarp();  // (what was read of the stage before has been)
+#pragma unroll
+    for (uint32_t i = 0; i < 16u; ++i) {
+      const uint32_t at = i * 32u + lane;
+      reinterpret_cast<E*>(stage + at / kCols * kPitch)[at % kCols] = v[i];
+    }
+    __syncwarp();
+    x.template load<true>(stage + lane % R * kPitch + lane / R * 16u * kEsize, 16);
+  }
+  static __device__ __forceinline__ void store(const Raw16<DT>& x, uint8_t* stage, uint8_t* p, uint64_t ld, uint32_t rows, uint32_t c0, uint32_t cols, uint32_t lane) {
+    __syncwarp();
+    x.template store<true>(stage + lane % R * kPitch + lane / R * 16u * kEsize, 16);
+    __syncwarp();
+#pragma unroll
+    for (uint32_t i = 0; i < 16u; ++i) {
+      const uint32_t at = i * 32u + lane, r = at / kCols, c = c0 + at % kCols;
+      if (r < rows && c < cols) reinterpret_cast<E*>(p)[r * ld + c] = reinterpret_cast<const E*>(stage + r * kPitch)[at % kCols];
+    }
   }
 };
 

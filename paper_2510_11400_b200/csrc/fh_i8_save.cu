@@ -17,7 +17,7 @@ constexpr uint32_t kEs = DT == kF32 ? 4u : 2u;
 // side by side (a sector or more from R = 2 on), and lanes of the same row read 32 / R chunks side by side.  A lane's I chunks stay in registers from the
 // row's maximum to its codes; I = 0: the row is too long for that and is read again, from L2.
 template <int DT, int R, int I, bool VEC>
-__global__ void __launch_bounds__(512) i8_rows_kernel(const I8SaveArgs g) {
+__global__ void __launch_bounds__(512, 2) i8_rows_kernel(const I8SaveArgs g) {
   __shared__ uint32_t tops[16][R];
   constexpr uint32_t kLanes = 32 / R;
   const I8Layout l(g.rows, g.cols);
@@ -26,11 +26,17 @@ __global__ void __launch_bounds__(512) i8_rows_kernel(const I8SaveArgs g) {
   dep_trigger();
   dep_wait();
   if (blockIdx.x == 0 && tid < 32) i8_write_header(g.dst, l, tid);
-  const uint8_t* src = g.src + (uint64_t)row * g.ld * kEs<DT>;
+  using Loose = LooseRows<DT, R>;
+  __shared__ __align__(16) uint8_t stages[VEC ? 16 : 16 * Loose::kBytes];
+  const uint8_t* src = g.src + (uint64_t)(VEC ? row : blockIdx.x * R) * g.ld * kEs<DT>;
   const bool there = row < g.rows;
+  const uint32_t rows = blockIdx.x * R < g.rows ? min((uint32_t)R, g.rows - blockIdx.x * R) : 0u;
   auto fetch = [&](Raw16<DT>& x, uint32_t j) {
     const uint32_t c = j * 16u;
-    x.template load<VEC>(src + (uint64_t)c * kEs<DT>, there && c < g.cols ? (int)min(16u, g.cols - c) : 0);
+    if (VEC)
+      x.template load<true>(src + (uint64_t)c * kEs<DT>, there && c < g.cols ? (int)min(16u, g.cols - c) : 0);
+    else
+      Loose::load(x, stages + warp * Loose::kBytes, src, g.ld, rows, (j - lane / R) * 16u, g.cols, lane);
   };
   constexpr int N = I ? I : 1;
   Raw16<DT> x[N];
@@ -42,7 +48,7 @@ __global__ void __launch_bounds__(512) i8_rows_kernel(const I8SaveArgs g) {
     for (int i = 0; i < N; ++i) top = max(top, x[i].top());
   } else {
 #pragma unroll 2
-    for (uint32_t j = first; j < chunks; j += step) {
+    for (uint32_t j = first; j < chunks + lane / R; j += step) {  // (all lanes of a warp as often)
       fetch(x[0], j);
       top = max(top, x[0].top());
     }
@@ -52,7 +58,7 @@ __global__ void __launch_bounds__(512) i8_rows_kernel(const I8SaveArgs g) {
   if (lane < R) tops[warp][r] = top;
   __syncthreads();
   for (uint32_t w = 0; w < warps; ++w) top = max(top, tops[w][r]);
-  const I8Coder coder(top);
+  const I8Coder<DT> coder(top);
   uint8_t* dst = g.dst + l.code_at(row, 0);
   const uint64_t pitch = 16ull * l.block_rows(row / 128u);
   auto put = [&](const Raw16<DT>& v, uint32_t j) {
@@ -60,20 +66,18 @@ __global__ void __launch_bounds__(512) i8_rows_kernel(const I8SaveArgs g) {
     v.values(f);
     *reinterpret_cast<uint4*>(dst + j * pitch) = i8_codes16(f, coder);
   };
-  if (row < l.r8) {
-    if (I) {
+  if (I) {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (first + i * step < chunks) put(x[i], first + i * step);
-    } else {
+    for (int i = 0; i < N; ++i)
+      if (first + i * step < chunks) put(x[i], first + i * step);
+  } else {
 #pragma unroll 2
-      for (uint32_t j = first; j < chunks; j += step) {
-        fetch(x[0], j);
-        put(x[0], j);
-      }
+    for (uint32_t j = first; j < chunks + lane / R; j += step) {
+      fetch(x[0], j);
+      if (j < chunks) put(x[0], j);
     }
-    if (warp == 0 && lane < R) *reinterpret_cast<uint32_t*>(g.dst + l.magnitude_at(row)) = i8_magnitude_bits(top);
   }
+  if (warp == 0 && lane < R) *reinterpret_cast<uint32_t*>(g.dst + l.magnitude_at(row)) = i8_magnitude_bits(top);
 }
 
 template <int DT, int R, int I, bool VEC>
@@ -199,15 +203,17 @@ __global__ void __launch_bounds__(kColWarps * 32) i8_cols_kernel(const I8SaveArg
   if (col >= l.r8) return;
   const uint64_t pitch = 16ull * l.block_rows(col / 128u);
   uint8_t* dst = g.dst + l.code_at(col, 0);
+  I8Coder<DT> coder[C] = {I8Coder<DT>(tops[0][lane * C])};
+#pragma unroll
+  for (int c = 1; c < C; ++c) coder[c] = I8Coder<DT>(tops[0][lane * C + c]);
   for (uint32_t j = first; j < last; j += kColWarps) {
     x.load(g, j, col, n);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const I8Coder coder(tops[0][lane * C + c]);
       float f[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) f[i] = x.at(i, c);
-      *reinterpret_cast<uint4*>(dst + j * pitch + c * 16u) = i8_codes16(f, coder);
+      *reinterpret_cast<uint4*>(dst + j * pitch + c * 16u) = i8_codes16(f, coder[c]);
     }
   }
 }
@@ -234,13 +240,16 @@ __global__ void __launch_bounds__(kI8Threads) i8_restore_kernel(const I8SaveArgs
   const bool ok = i8_header_ok(g.src, g.src_bytes, l);
   if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
   if (!ok) return;
+  using Loose = LooseRows<DT, 8>;
+  __shared__ __align__(16) uint8_t stages[VEC ? 16 : kI8Threads / 32 * Loose::kBytes];
   const uint32_t quads = (l.chunks() + 3u) / 4u;
   const uint64_t items = (uint64_t)(l.r8 / 8u) * quads, step = (uint64_t)gridDim.x * (kI8Threads / 32);
   for (uint64_t it = (uint64_t)blockIdx.x * (kI8Threads / 32) + tid / 32; it < items; it += step) {
     const uint32_t row = (uint32_t)(it / quads) * 8u + lane % 8u, j = (uint32_t)(it % quads) * 4u + lane / 8u, c = j * 16u;
-    if (row >= g.rows || c >= g.cols) continue;
-    const uint4 q = *reinterpret_cast<const uint4*>(g.src + l.code_at(row, j));
-    const float s = i8_scale(*reinterpret_cast<const float*>(g.src + l.magnitude_at(row)));
+    const bool there = row < g.rows && c < g.cols;
+    if (VEC && !there) continue;
+    const uint4 q = there ? *reinterpret_cast<const uint4*>(g.src + l.code_at(row, j)) : make_uint4(0u, 0u, 0u, 0u);
+    const float s = there ? i8_scale(*reinterpret_cast<const float*>(g.src + l.magnitude_at(row))) : 0.0f;
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
     float f[16];
 #pragma unroll
@@ -248,7 +257,12 @@ __global__ void __launch_bounds__(kI8Threads) i8_restore_kernel(const I8SaveArgs
       f[i] = max_nan(min_nan((float)((int32_t)(w[i / 4] << (24 - i % 4 * 8)) >> 24) * s, 3.4028235e38f), -3.4028235e38f);
     Raw16<DT> x;
     x.take(f);
-    x.template store<VEC>(g.dst + ((uint64_t)row * g.ld + c) * kEs<DT>, (int)min(16u, g.cols - c));
+    if (VEC) {
+      x.template store<true>(g.dst + ((uint64_t)row * g.ld + c) * kEs<DT>, (int)min(16u, g.cols - c));
+    } else {
+      const uint32_t r0 = row - lane % 8u;
+      Loose::store(x, stages + tid / 32 * Loose::kBytes, g.dst + (uint64_t)r0 * g.ld * kEs<DT>, g.ld, g.rows > r0 ? min(8u, g.rows - r0) : 0u, (j - lane / 8u) * 16u, g.cols, lane);
+    }
   }
 }
 
