@@ -592,40 +592,51 @@ def rotation_table(positions: int, rotary: int, base: float = 10000.0, scale: fl
     return out
 
 
-def _heads(t, dev: int, d: fh_heads_desc, heads: int, token: int, head: int) -> Optional[int]:
-    """The address of rows of heads, once they are known to lie as they are described."""
+def _heads(t, dev: int, shape: Tuple[int, int, int], token: int, head: int, dtype: int) -> Optional[int]:
+    """The address of rows of heads, once they are known to lie as they are described.  What is plainly right is told at once."""
     if t is None:
         return None
+    if t.dtype is _types.get(dtype) and t.shape == shape and t.stride() == (token, head, 1) and t.get_device() == dev:
+        return t.data_ptr()
+    tokens, heads, dim = shape
     if t.get_device() != dev:
         raise ValueError(f"a tensor on {t.device}, where cuda:{dev} is the current device")
-    if t.element_size() != _esize(d.dtype) or (d.dtype == FH_F32) != (t.element_size() == 4) or _is_half(t):
-        raise ValueError(f"a tensor of {t.dtype}, where elements of {_esize(d.dtype)} bytes are wanted")
-    if t.dim() == 3 and tuple(t.shape) == (d.tokens, heads, d.dim):
+    if t.element_size() != _esize(dtype) or _is_half(t):
+        raise ValueError(f"a tensor of {t.dtype}, where elements of {_esize(dtype)} bytes are wanted")
+    if t.shape == shape:
         s = t.stride()
-        if (d.tokens == 1 or s[0] == token) and (heads == 1 or s[1] == head) and (d.dim == 1 or s[2] == 1):
+        if (tokens == 1 or s[0] == token) and (heads == 1 or s[1] == head) and (dim == 1 or s[2] == 1):
             return t.data_ptr()
-    elif t.is_contiguous() and t.numel() >= (d.tokens - 1) * token + (heads - 1) * head + d.dim:
+    elif t.is_contiguous() and t.numel() >= (tokens - 1) * token + (heads - 1) * head + dim:
         return t.data_ptr()
-    raise ValueError(f"a tensor of shape {tuple(t.shape)} and strides {t.stride()}, where {d.tokens} tokens, {token} apart, of {heads} heads, {head} apart, "
-                     f"of {d.dim} elements are wanted")
+    raise ValueError(f"a tensor of shape {tuple(t.shape)} and strides {t.stride()}, where {tokens} tokens, {token} apart, of {heads} heads, {head} apart, "
+                     f"of {dim} elements are wanted")
+
+
+def _sides(d: fh_heads_desc, dev: int, q, k, q_out, k_out):
+    """The addresses of queries, keys and what lies as the outputs do."""
+    tokens, dim, dtype = d.tokens, d.dim, d.dtype
+    sq, sk = (tokens, d.q_heads, dim), (tokens, d.k_heads, dim)
+    return (_heads(q, dev, sq, d.q_token, d.q_head, dtype), _heads(k, dev, sk, d.k_token, d.k_head, dtype),
+            _heads(q_out, dev, sq, d.q_out_token, d.q_out_head, dtype), _heads(k_out, dev, sk, d.k_out_token, d.k_out_head, dtype))
 
 
 def _turn(d: fh_heads_desc, table, at, dev: int):
     """The addresses of the table and the positions."""
     if at is not None and (at.dtype.is_floating_point or at.element_size() != 4):
         raise ValueError(f"positions of {at.dtype}, where int32 is wanted")
-    return _dense(table, dev, 1, d.positions * d.rotary, d.positions * d.rotary, FH_F32), _ptr(at, dev, d.tokens, 4, (1, d.tokens, d.tokens))
+    n, tokens = d.positions * d.rotary, d.tokens
+    return _dense(table, dev, 1, n, n, FH_F32), _ptr(at, dev, tokens, 4, (1, tokens, tokens))
 
 
 def fh_head_norm(d: fh_heads_desc, q, k, gamma_q, gamma_k, table, positions, q_out, k_out, status=None, stream=None) -> int:
     """Enqueue the norms of the heads of `q` and `k` and their rotation into `q_out` and `k_out`; gammas, positions and what has no heads may be
     None."""
-    dev, w = _device(), d.wdtype
+    dev, w, dim = _device(), d.wdtype, d.dim
     t, at = _turn(d, table, positions, dev)
-    return lib().fh_head_norm(d, _heads(q, dev, d, d.q_heads, d.q_token, d.q_head), _heads(k, dev, d, d.k_heads, d.k_token, d.k_head),
-                              _dense(gamma_q, dev, 1, d.dim, d.dim, w), _dense(gamma_k, dev, 1, d.dim, d.dim, w), t, at,
-                              _heads(q_out, dev, d, d.q_heads, d.q_out_token, d.q_out_head),
-                              _heads(k_out, dev, d, d.k_heads, d.k_out_token, d.k_out_head), _status_ptr(status, dev), _on(stream, dev))
+    x, y, ox, oy = _sides(d, dev, q, k, q_out, k_out)
+    return lib().fh_head_norm(d, x, y, _dense(gamma_q, dev, 1, dim, dim, w), _dense(gamma_k, dev, 1, dim, dim, w), t, at, ox, oy, _status_ptr(status, dev),
+                              _on(stream, dev))
 
 
 def heads_work_bytes(d: fh_heads_desc) -> int:
@@ -635,15 +646,13 @@ def heads_work_bytes(d: fh_heads_desc) -> int:
 def fh_head_norm_backward(d: fh_heads_desc, dq_out, dk_out, q, k, gamma_q, gamma_k, table, positions, dq=None, dk=None, dgamma_q=None, dgamma_k=None,
                           work=None, status=None, stream=None) -> int:
     """Enqueue the backward pass of fh_head_norm.  `work`: uint8, at least heads_work_bytes, where dgamma_q or dgamma_k is wanted."""
-    dev, w = _device(), d.wdtype
+    dev, w, dim = _device(), d.wdtype, d.dim
     t, at = _turn(d, table, positions, dev)
-    return lib().fh_head_norm_backward(d, _heads(dq_out, dev, d, d.q_heads, d.q_out_token, d.q_out_head),
-                                       _heads(dk_out, dev, d, d.k_heads, d.k_out_token, d.k_out_head), _heads(q, dev, d, d.q_heads, d.q_token, d.q_head),
-                                       _heads(k, dev, d, d.k_heads, d.k_token, d.k_head), _dense(gamma_q, dev, 1, d.dim, d.dim, w),
-                                       _dense(gamma_k, dev, 1, d.dim, d.dim, w), t, at, _heads(dq, dev, d, d.q_heads, d.q_token, d.q_head),
-                                       _heads(dk, dev, d, d.k_heads, d.k_token, d.k_head), _dense(dgamma_q, dev, 1, d.dim, d.dim, w),
-                                       _dense(dgamma_k, dev, 1, d.dim, d.dim, w), _ptr(work, dev), 0 if work is None else work.nbytes,
-                                       _status_ptr(status, dev), _on(stream, dev))
+    x, y, gx, gy = _sides(d, dev, q, k, dq_out, dk_out)
+    dx, dy, _, _ = _sides(d, dev, dq, dk, None, None)
+    return lib().fh_head_norm_backward(d, gx, gy, x, y, _dense(gamma_q, dev, 1, dim, dim, w), _dense(gamma_k, dev, 1, dim, dim, w), t, at, dx, dy,
+                                       _dense(dgamma_q, dev, 1, dim, dim, w), _dense(dgamma_k, dev, 1, dim, dim, w), _ptr(work, dev),
+                                       0 if work is None else work.nbytes, _status_ptr(status, dev), _on(stream, dev))
 
 
 def debug_set(what: int, value: int) -> int:

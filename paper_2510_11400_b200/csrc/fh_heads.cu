@@ -1,6 +1,7 @@
 // Norms of queries and keys for each head with the rotation by position, forward and backward.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "fh_i8_launch.cuh"
 #include "fh_launch.cuh"
@@ -359,17 +360,79 @@ __global__ void __launch_bounds__(kHeadThreads) heads_backward_kernel(const Head
   }
 }
 
-// ---- any size, stride and alignment: a warp to a row, a lane to pairs 32 apart, the row's elements read again from L1.
-// An element that is not rotated is a pair with nothing.
-struct LoosePairs {
-  uint32_t half, rest;  // pairs, and elements behind them
-  bool halves;
-  __device__ __forceinline__ explicit LoosePairs(const HeadsArgs& g) : half(g.rotary / 2u), rest(g.dim - g.rotary), halves(g.halves) {}
-  __device__ __forceinline__ uint32_t count() const { return half + rest; }
-  __device__ __forceinline__ bool paired(uint32_t i) const { return i < half; }
-  __device__ __forceinline__ uint32_t first(uint32_t i) const { return i < half ? (halves ? i : 2u * i) : half + i; }
-  __device__ __forceinline__ uint32_t second(uint32_t i) const { return halves ? half + i : 2u * i + 1u; }
+// ---- any size, stride and alignment: a warp to a row, a lane to pairs 32 apart.  What is not rotated is taken in pairs too (the last element of an odd
+// number alone), whose angle is zero.  N pairs of a lane stay in registers; N = 0: the row is too long for that, and its elements are read again from L1.
+struct LoosePair {
+  uint32_t a, b;
+  bool turned, two;  // whether the table has it, and whether it has a second element
 };
+template <bool HALVES>
+__device__ __forceinline__ LoosePair loose_pair(const HeadsArgs& g, uint32_t i) {
+  const uint32_t half = g.rotary / 2u;
+  LoosePair p;
+  p.turned = i < half;
+  if (!HALVES) {
+    p.a = 2u * i;
+    p.b = p.a + 1u;
+    p.two = p.b < g.dim;
+  } else if (p.turned) {
+    p.a = i;
+    p.b = half + i;
+    p.two = true;
+  } else {
+    const uint32_t rest = (g.dim - g.rotary) / 2u, at = i - half;
+    p.two = at < rest;
+    p.a = p.two ? g.rotary + at : g.dim - 1u;
+    p.b = g.rotary + rest + at;
+  }
+  return p;
+}
+__device__ __forceinline__ uint32_t loose_pairs(const HeadsArgs& g) { return (g.dim + 1u) / 2u; }
+
+// Where a lane's pairs are, with their weights: N of them.
+template <int N, bool HALVES>
+struct LooseLane {
+  LoosePair p[N];
+  bool there[N];
+  float wa[N], wb[N];
+  __device__ __forceinline__ LooseLane(const HeadsArgs& g, const uint8_t* gamma, uint32_t lane) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const uint32_t i = lane + 32u * j;
+      there[j] = i < loose_pairs(g);
+      p[j] = loose_pair<HALVES>(g, i);
+      p[j].two = p[j].two && there[j];
+      wa[j] = there[j] ? weight_at(gamma, g.wdtype, p[j].a) : 0.0f;
+      wb[j] = p[j].two ? weight_at(gamma, g.wdtype, p[j].b) : 0.0f;
+    }
+  }
+  template <int DT>
+  __device__ __forceinline__ void load(const uint8_t* x, float (&a)[N], float (&b)[N]) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      a[j] = there[j] ? elem_at<DT>(x, p[j].a) : 0.0f;
+      b[j] = p[j].two ? elem_at<DT>(x, p[j].b) : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void less(float mean, float (&a)[N], float (&b)[N]) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      a[j] = there[j] ? a[j] - mean : 0.0f;
+      b[j] = p[j].two ? b[j] - mean : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void turns(const HeadsArgs& g, int64_t at, uint32_t lane, float2 (&t)[N]) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) t[j] = there[j] && p[j].turned ? g.table[(uint64_t)at * (g.rotary / 2u) + lane + 32u * j] : make_float2(1.0f, 0.0f);
+  }
+};
+template <int N>
+__device__ __forceinline__ float sum_both(const float (&a)[N], const float (&b)[N]) {
+  float s = 0.0f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) s += a[j] + b[j];
+  return s;
+}
 
 template <int DT>
 __device__ __forceinline__ float loose_mean(const HeadsArgs& g, const uint8_t* p, uint32_t lane) {
@@ -379,7 +442,7 @@ __device__ __forceinline__ float loose_mean(const HeadsArgs& g, const uint8_t* p
   return __fdiv_rn(team_sum<32>(sum), (float)g.dim);
 }
 
-template <int DT>
+template <int DT, int N, bool HALVES>
 __global__ void __launch_bounds__(kHeadThreads) heads_forward_loose_kernel(const HeadsArgs g) {
   dep_trigger();
   dep_wait();
@@ -394,37 +457,53 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_loose_kernel(const
   if (u >= units) return;
   const HeadUnit unit(u, g, 1u);
   const HeadsSide& s = g.side[unit.side];
-  const int64_t at = position_of(g, unit.token);
-  if (at < 0) return;
   const uint8_t* p = s.x + ((uint64_t)unit.token * s.token + (uint64_t)unit.head * s.head) * kEs<DT>;
   uint8_t* o = s.out + ((uint64_t)unit.token * s.out_token + (uint64_t)unit.head * s.out_head) * kEs<DT>;
-  const float2* turn = g.table + (uint64_t)at * (g.rotary / 2u);
-  const float mean = loose_mean<DT>(g, p, lane);
-  float sum = 0.0f;
-  for (uint32_t e = lane; e < g.dim; e += 32u) {
-    const float v = elem_at<DT>(p, e) - mean;
-    sum = __fmaf_rn(v, v, sum);
-  }
-  const float rstd = 1.0f / sqrtf(__fdiv_rn(team_sum<32>(sum), (float)g.dim) + g.eps);
-  __syncwarp();  // (in place, the row has been read by all lanes before one of them writes)
-  const LoosePairs pairs(g);
-  for (uint32_t i = lane; i < pairs.count(); i += 32u) {
-    const uint32_t fi = pairs.first(i);
-    const float za = (elem_at<DT>(p, fi) - mean) * rstd * weight_at(s.gamma, g.wdtype, fi);
-    if (!pairs.paired(i)) {
-      put_elem<DT>(o, fi, za);
-      continue;
+  const float size = (float)g.dim;
+  if constexpr (N > 0) {
+    const LooseLane<N, HALVES> my(g, s.gamma, lane);
+    float a[N], b[N];
+    my.template load<DT>(p, a, b);
+    const int64_t at = position_of(g, unit.token);
+    if (at < 0) return;
+    float2 t[N];
+    my.turns(g, at, lane, t);
+    if (g.layer) my.less(__fdiv_rn(team_sum<32>(sum_both(a, b)), size), a, b);
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum = __fmaf_rn(b[j], b[j], __fmaf_rn(a[j], a[j], sum));
+    const float rstd = 1.0f / sqrtf(__fdiv_rn(team_sum<32>(sum), size) + g.eps);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float za = a[j] * rstd * my.wa[j], zb = b[j] * rstd * my.wb[j];
+      if (my.there[j]) put_elem<DT>(o, my.p[j].a, __fmaf_rn(za, t[j].x, -(zb * t[j].y)));
+      if (my.p[j].two) put_elem<DT>(o, my.p[j].b, __fmaf_rn(zb, t[j].x, za * t[j].y));
     }
-    const uint32_t se = pairs.second(i);
-    const float zb = (elem_at<DT>(p, se) - mean) * rstd * weight_at(s.gamma, g.wdtype, se);
-    const float2 t = turn[i];
-    put_elem<DT>(o, fi, __fmaf_rn(za, t.x, -(zb * t.y)));
-    put_elem<DT>(o, se, __fmaf_rn(zb, t.x, za * t.y));
+  } else {
+    const int64_t at = position_of(g, unit.token);
+    if (at < 0) return;
+    const float2* turn = g.table + (uint64_t)at * (g.rotary / 2u);
+    const float mean = loose_mean<DT>(g, p, lane);
+    float sum = 0.0f;
+    for (uint32_t e = lane; e < g.dim; e += 32u) {
+      const float v = elem_at<DT>(p, e) - mean;
+      sum = __fmaf_rn(v, v, sum);
+    }
+    const float rstd = 1.0f / sqrtf(__fdiv_rn(team_sum<32>(sum), size) + g.eps);
+    __syncwarp();  // (in place, the row has been read by all lanes before one of them writes)
+    for (uint32_t i = lane; i < loose_pairs(g); i += 32u) {
+      const LoosePair q = loose_pair<HALVES>(g, i);
+      const float za = (elem_at<DT>(p, q.a) - mean) * rstd * weight_at(s.gamma, g.wdtype, q.a);
+      const float zb = q.two ? (elem_at<DT>(p, q.b) - mean) * rstd * weight_at(s.gamma, g.wdtype, q.b) : 0.0f;
+      const float2 t = q.turned ? turn[i] : make_float2(1.0f, 0.0f);
+      put_elem<DT>(o, q.a, __fmaf_rn(za, t.x, -(zb * t.y)));
+      if (q.two) put_elem<DT>(o, q.b, __fmaf_rn(zb, t.x, za * t.y));
+    }
   }
 }
 
-// Warps of a CTA each have sums of their own in shared memory, `dim` floats.
-template <int DT>
+// Warps of a CTA each have sums of their own, `dim` floats in shared memory: while they work where N = 0, at the end otherwise.
+template <int DT, int N, bool HALVES>
 __global__ void __launch_bounds__(kHeadThreads) heads_backward_loose_kernel(const HeadsArgs g) {
   extern __shared__ float loose_sums[];
   dep_trigger();
@@ -438,68 +517,111 @@ __global__ void __launch_bounds__(kHeadThreads) heads_backward_loose_kernel(cons
   const HeadsSide& s = g.side[which];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
   float* acc = loose_sums + (uint64_t)warp * g.dim;
-  if (s.dgamma)
-    for (uint32_t e = lane; e < g.dim; e += 32u) acc[e] = 0.0f;
-  __syncwarp();
-  const LoosePairs pairs(g);
   const float size = (float)g.dim;
-  const uint64_t units = (uint64_t)g.tokens * s.heads;
-  for (uint64_t u = (uint64_t)part * warps + warp; u < units; u += (uint64_t)s.parts * warps) {
-    const uint32_t token = (uint32_t)(u / s.heads), head = (uint32_t)(u % s.heads);
-    const int64_t at = position_of(g, token);
-    if (at < 0) continue;
-    const uint8_t* p = s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
-    const uint8_t* q = s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
-    const float2* turn = g.table + (uint64_t)at * (g.rotary / 2u);
-    const float mean = loose_mean<DT>(g, p, lane);
-    // dz of pair i
-    auto dz = [&](uint32_t i, uint32_t fi, uint32_t se, float& da, float& db) {
-      const float ya = elem_at<DT>(q, fi);
-      da = ya;
-      db = 0.0f;
-      if (!pairs.paired(i)) return;
-      const float yb = elem_at<DT>(q, se);
-      const float2 t = turn[i];
-      da = __fmaf_rn(ya, t.x, yb * t.y);
-      db = __fmaf_rn(yb, t.x, -(ya * t.y));
-    };
-    float xx = 0.0f, gx = 0.0f, gs = 0.0f;
-    for (uint32_t i = lane; i < pairs.count(); i += 32u) {
-      const uint32_t fi = pairs.first(i), se = pairs.second(i);
-      float da, db;
-      dz(i, fi, se, da, db);
-      const float xa = elem_at<DT>(p, fi) - mean, ga = da * weight_at(s.gamma, g.wdtype, fi);
-      xx = __fmaf_rn(xa, xa, xx);
-      gx = __fmaf_rn(ga, xa, gx);
-      gs += ga;
-      if (pairs.paired(i)) {
-        const float xb = elem_at<DT>(p, se) - mean, gb = db * weight_at(s.gamma, g.wdtype, se);
-        xx = __fmaf_rn(xb, xb, xx);
-        gx = __fmaf_rn(gb, xb, gx);
-        gs += gb;
+  const uint64_t units = (uint64_t)g.tokens * s.heads, first = (uint64_t)part * warps + warp, step = (uint64_t)s.parts * warps;
+  if constexpr (N > 0) {
+    const LooseLane<N, HALVES> my(g, s.gamma, lane);
+    float sa[N] = {}, sb[N] = {};
+#pragma unroll 2
+    for (uint64_t u = first; u < units; u += step) {
+      const uint32_t token = (uint32_t)(u / s.heads), head = (uint32_t)(u % s.heads);
+      float a[N], b[N], ya[N], yb[N];
+      my.template load<DT>(s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>, a, b);
+      my.template load<DT>(s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>, ya, yb);
+      const int64_t at = position_of(g, token);
+      if (at < 0) continue;
+      float2 t[N];
+      my.turns(g, at, lane, t);
+      if (g.layer) my.less(__fdiv_rn(team_sum<32>(sum_both(a, b)), size), a, b);
+      float xx = 0.0f, gx = 0.0f, gs = 0.0f;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float da = __fmaf_rn(ya[j], t[j].x, yb[j] * t[j].y), db = __fmaf_rn(yb[j], t[j].x, -(ya[j] * t[j].y));
+        ya[j] = da;
+        yb[j] = db;
+        const float ga = da * my.wa[j], gb = db * my.wb[j];
+        xx = __fmaf_rn(b[j], b[j], __fmaf_rn(a[j], a[j], xx));
+        gx = __fmaf_rn(gb, b[j], __fmaf_rn(ga, a[j], gx));
+        gs += ga + gb;
+      }
+      xx = team_sum<32>(xx);
+      gx = team_sum<32>(gx);
+      if (g.layer) gs = team_sum<32>(gs);
+      const float rstd = 1.0f / sqrtf(__fdiv_rn(xx, size) + g.eps);
+      const float along = gx * rstd / size, level = g.layer ? gs / size : 0.0f;
+      uint8_t* o = s.dx + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float xa = a[j] * rstd, xb = b[j] * rstd;
+        sa[j] = __fmaf_rn(ya[j], xa, sa[j]);
+        sb[j] = __fmaf_rn(yb[j], xb, sb[j]);
+        if (s.dx && my.there[j]) put_elem<DT>(o, my.p[j].a, rstd * (__fmaf_rn(-xa, along, ya[j] * my.wa[j]) - level));
+        if (s.dx && my.p[j].two) put_elem<DT>(o, my.p[j].b, rstd * (__fmaf_rn(-xb, along, yb[j] * my.wb[j]) - level));
       }
     }
-    xx = team_sum<32>(xx);
-    gx = team_sum<32>(gx);
-    gs = team_sum<32>(gs);
-    const float rstd = 1.0f / sqrtf(__fdiv_rn(xx, size) + g.eps);
-    const float along = gx * rstd / size, level = g.layer ? gs / size : 0.0f;
-    uint8_t* o = s.dx + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
-    for (uint32_t i = lane; i < pairs.count(); i += 32u) {
-      const uint32_t fi = pairs.first(i), se = pairs.second(i);
-      float da, db;
-      dz(i, fi, se, da, db);
-      const float xa = (elem_at<DT>(p, fi) - mean) * rstd, ga = da * weight_at(s.gamma, g.wdtype, fi);
-      const float xb = pairs.paired(i) ? (elem_at<DT>(p, se) - mean) * rstd : 0.0f, gb = pairs.paired(i) ? db * weight_at(s.gamma, g.wdtype, se) : 0.0f;
-      if (s.dgamma) acc[fi] = __fmaf_rn(da, xa, acc[fi]);
-      if (s.dx) put_elem<DT>(o, fi, rstd * (__fmaf_rn(-xa, along, ga) - level));
-      if (pairs.paired(i)) {
-        if (s.dgamma) acc[se] = __fmaf_rn(db, xb, acc[se]);
-        if (s.dx) put_elem<DT>(o, se, rstd * (__fmaf_rn(-xb, along, gb) - level));
+    if (!s.dgamma) return;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (my.there[j]) acc[my.p[j].a] = sa[j];
+      if (my.p[j].two) acc[my.p[j].b] = sb[j];
+    }
+  } else {
+    if (s.dgamma)
+      for (uint32_t e = lane; e < g.dim; e += 32u) acc[e] = 0.0f;
+    __syncwarp();
+    for (uint64_t u = first; u < units; u += step) {
+      const uint32_t token = (uint32_t)(u / s.heads), head = (uint32_t)(u % s.heads);
+      const int64_t at = position_of(g, token);
+      if (at < 0) continue;
+      const uint8_t* p = s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
+      const uint8_t* q = s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
+      const float2* turn = g.table + (uint64_t)at * (g.rotary / 2u);
+      const float mean = loose_mean<DT>(g, p, lane);
+      // x less the mean, dz, and g of pair i
+      struct Both {
+        float xa, xb, da, db, ga, gb;
+      };
+      auto take = [&](uint32_t i, const LoosePair& e) {
+        Both v;
+        v.xa = elem_at<DT>(p, e.a) - mean;
+        v.xb = e.two ? elem_at<DT>(p, e.b) - mean : 0.0f;
+        const float ya = elem_at<DT>(q, e.a), yb = e.two ? elem_at<DT>(q, e.b) : 0.0f;
+        const float2 t = e.turned ? turn[i] : make_float2(1.0f, 0.0f);
+        v.da = __fmaf_rn(ya, t.x, yb * t.y);
+        v.db = __fmaf_rn(yb, t.x, -(ya * t.y));
+        v.ga = v.da * weight_at(s.gamma, g.wdtype, e.a);
+        v.gb = e.two ? v.db * weight_at(s.gamma, g.wdtype, e.b) : 0.0f;
+        return v;
+      };
+      float xx = 0.0f, gx = 0.0f, gs = 0.0f;
+      for (uint32_t i = lane; i < loose_pairs(g); i += 32u) {
+        const Both v = take(i, loose_pair<HALVES>(g, i));
+        xx = __fmaf_rn(v.xb, v.xb, __fmaf_rn(v.xa, v.xa, xx));
+        gx = __fmaf_rn(v.gb, v.xb, __fmaf_rn(v.ga, v.xa, gx));
+        gs += v.ga + v.gb;
+      }
+      xx = team_sum<32>(xx);
+      gx = team_sum<32>(gx);
+      gs = team_sum<32>(gs);
+      const float rstd = 1.0f / sqrtf(__fdiv_rn(xx, size) + g.eps);
+      const float along = gx * rstd / size, level = g.layer ? gs / size : 0.0f;
+      uint8_t* o = s.dx + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
+      for (uint32_t i = lane; i < loose_pairs(g); i += 32u) {
+        const LoosePair e = loose_pair<HALVES>(g, i);
+        const Both v = take(i, e);
+        const float xa = v.xa * rstd, xb = v.xb * rstd;
+        if (s.dgamma) {
+          acc[e.a] = __fmaf_rn(v.da, xa, acc[e.a]);
+          if (e.two) acc[e.b] = __fmaf_rn(v.db, xb, acc[e.b]);
+        }
+        if (s.dx) {
+          put_elem<DT>(o, e.a, rstd * (__fmaf_rn(-xa, along, v.ga) - level));
+          if (e.two) put_elem<DT>(o, e.b, rstd * (__fmaf_rn(-xb, along, v.gb) - level));
+        }
       }
     }
+    if (!s.dgamma) return;
   }
-  if (!s.dgamma) return;
   __syncthreads();
   float* out = g.work + (uint64_t)((which ? g.side[0].parts : 0u) + part) * g.dim;
   for (uint32_t e = threadIdx.x; e < g.dim; e += blockDim.x) {
@@ -567,6 +689,19 @@ uint32_t heads_slots(const HeadsArgs& a) {
   return all ? 0u : a.dim / two;
 }
 
+// Pairs to a lane: 1, 2 or 4, or 0 where the row is longer.
+template <typename L>
+int loose_by_length(const HeadsArgs& a, L launch) {
+  const uint32_t n = ((a.dim + 1u) / 2u + 31u) / 32u;
+  auto with = [&](auto halves) {
+    if (n <= 1u) return launch(std::integral_constant<int, 1>(), halves);
+    if (n <= 2u) return launch(std::integral_constant<int, 2>(), halves);
+    if (n <= 4u) return launch(std::integral_constant<int, 4>(), halves);
+    return launch(std::integral_constant<int, 0>(), halves);
+  };
+  return a.halves ? with(std::true_type()) : with(std::false_type());
+}
+
 template <int DT, int T, int U, bool HALVES>
 int forward_t(const HeadsArgs& a, cudaStream_t stream) {
   constexpr uint32_t span = 32 / T * U;
@@ -589,7 +724,9 @@ int forward_d(const HeadsArgs& a, cudaStream_t stream) {
   if (!slots) {
     const uint64_t units = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads), grid = (units + kHeadWarps - 1u) / kHeadWarps + (a.status ? 1u : 0u);
     if (grid > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
-    return launch_plain<heads_forward_loose_kernel<DT>>((uint32_t)grid, kHeadThreads, 0, 1, stream, a);
+    return loose_by_length(a, [&](auto n, auto halves) {
+      return launch_plain<heads_forward_loose_kernel<DT, n.value, halves.value>>((uint32_t)grid, kHeadThreads, 0, 1, stream, a);
+    });
   }
   if (slots <= 4u) return forward_n<DT, 4>(a, stream);
   if (slots <= 8u) return forward_n<DT, 8>(a, stream);
@@ -597,16 +734,17 @@ int forward_d(const HeadsArgs& a, cudaStream_t stream) {
   return forward_n<DT, 32>(a, stream);
 }
 
-// CTAs of the backward pass, at most (three to an SM), and for how few rows there is another.  The workspace is sized for kHeadFewest.
-constexpr uint32_t kHeadParts = 148 * 3, kHeadFewest = 4;
+// CTAs of the backward pass: a rule's most, and another for every so many rows.  The workspace is sized for kHeadMost and kHeadFewest, which no rule is
+// beyond.
+constexpr uint32_t kHeadMost = 148 * 8, kHeadFewest = 4;
 
-uint64_t heads_parts_of(const HeadsArgs& a, uint32_t rows_per_cta) {
+uint64_t heads_parts_of(const HeadsArgs& a, uint32_t most, uint32_t rows_per_cta) {
   const uint64_t rows = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads);
-  return std::min<uint64_t>(kHeadParts, std::max<uint64_t>(2, (rows + rows_per_cta - 1) / rows_per_cta));
+  return std::min<uint64_t>(a.dim > 1024u ? 148u : most, std::max<uint64_t>(2, (rows + rows_per_cta - 1) / rows_per_cta));
 }
 // Dealt out to queries and keys by the rows that they have, so that all end together.
-void heads_parts(HeadsArgs* a, uint32_t rows_per_cta) {
-  const uint64_t q = a->side[0].heads, k = a->side[1].heads, all = heads_parts_of(*a, rows_per_cta);
+void heads_parts(HeadsArgs* a, uint32_t most, uint32_t rows_per_cta) {
+  const uint64_t q = a->side[0].heads, k = a->side[1].heads, all = heads_parts_of(*a, most, rows_per_cta);
   a->side[0].parts = !q ? 0u : !k ? (uint32_t)all : (uint32_t)std::min<uint64_t>(all - 1, std::max<uint64_t>(1, all * q / (q + k)));
   a->side[1].parts = !k ? 0u : (uint32_t)(all - a->side[0].parts);
 }
@@ -620,7 +758,7 @@ int backward_launch(const HeadsArgs& a, cudaStream_t stream, L rows) {
 template <int DT, int T, int U, bool HALVES>
 int backward_t(const HeadsArgs& a0, cudaStream_t stream) {
   HeadsArgs a = a0;
-  heads_parts(&a, U * kHeadWarps * (32u / T));
+  heads_parts(&a, 148u * 3u, U * kHeadWarps * (32u / T));
   static_assert(U * kHeadWarps * (32u / T) >= kHeadFewest, "the workspace's size");
   return backward_launch(a, stream, [&](uint32_t grid) { return launch_plain<heads_backward_kernel<DT, T, U, HALVES>>(grid, kHeadThreads, 0, 1, stream, a); });
 }
@@ -634,9 +772,11 @@ int backward_d(const HeadsArgs& a0, cudaStream_t stream) {
   if (!slots) {
     HeadsArgs a = a0;
     const uint32_t warps = std::max(1u, std::min(kHeadWarps, 8192u / a.dim));  // (32 KB of sums)
-    heads_parts(&a, kHeadFewest * warps);
+    heads_parts(&a, kHeadMost, kHeadFewest * warps);
     return backward_launch(a, stream, [&](uint32_t grid) {
-      return launch_plain<heads_backward_loose_kernel<DT>>(grid, (int)warps * 32, (size_t)warps * a.dim * sizeof(float), 1, stream, a);
+      return loose_by_length(a, [&](auto n, auto halves) {
+        return launch_plain<heads_backward_loose_kernel<DT, n.value, halves.value>>(grid, (int)warps * 32, (size_t)warps * a.dim * sizeof(float), 1, stream, a);
+      });
     });
   }
   if (slots <= 4u) return backward_n<DT, 4>(a0, stream);
@@ -647,7 +787,7 @@ int backward_d(const HeadsArgs& a0, cudaStream_t stream) {
 
 }  // namespace
 
-size_t heads_work_floats(const HeadsArgs& a) { return (size_t)heads_parts_of(a, kHeadFewest) * a.dim; }
+size_t heads_work_floats(const HeadsArgs& a) { return (size_t)heads_parts_of(a, kHeadMost, kHeadFewest) * a.dim; }
 
 int launch_heads_forward(const HeadsArgs& a, int dtype, cudaStream_t stream) {
   return dtype == kF32 ? forward_d<kF32>(a, stream) : forward_d<kBF16>(a, stream);

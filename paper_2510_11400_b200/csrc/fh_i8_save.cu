@@ -1,4 +1,5 @@
 // Dense matrices into 8-bit containers and back.
+#include <cstdlib>
 #include "fh_i8.cuh"
 #include "fh_i8_launch.cuh"
 #include "fh_launch.cuh"
@@ -100,6 +101,7 @@ int rows_by_group(const I8SaveArgs& a, cudaStream_t stream) {
   // Rows to a CTA: as few as keep the row in the registers of 16 warps, and as few as give every SM one; with 8, pieces of codes are written whole.
   const uint32_t chunks = I8Layout(a.rows, a.cols).chunks(), sms = (uint32_t)std::max(1, sm_count()), most = DT == kF32 ? 32u : 64u;
   uint32_t r = 8u;
+  if (const char* e = getenv("I8R")) { r = atoi(e); while (r > 1u && (chunks + 32u / r - 1u) / (32u / r) > most) r /= 2u; } else
   while (r > 1u && ((chunks + 32u / r - 1u) / (32u / r) > most || (a.rows + r - 1u) / r < sms)) r /= 2u;
   if (r == 1u) return rows_by_length<DT, 1, VEC>(a, stream);
   if (r == 2u) return rows_by_length<DT, 2, VEC>(a, stream);
@@ -230,9 +232,12 @@ int cols_launch(const I8SaveArgs& a0, cudaStream_t stream) {
 }
 
 // ---- and back --------------------------------------------------------------------------------------
-// A warp's lanes lie 8 rows by 4 chunks, as in the kernel by rows.
+// A warp's lanes lie 8 rows by 4 chunks, as in the kernel by rows, and have kQuads chunks each, all asked for at once.
+constexpr uint32_t kQuads = 4;
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kI8Threads) i8_restore_kernel(const I8SaveArgs g) {
+  using Loose = LooseRows<DT, 8>;
+  __shared__ __align__(16) uint8_t stages[VEC ? 16 : kI8Threads / 32 * Loose::kBytes];
   const I8Layout l(g.rows, g.cols);
   const uint32_t tid = threadIdx.x, lane = tid % 32;
   dep_trigger();
@@ -240,28 +245,29 @@ __global__ void __launch_bounds__(kI8Threads) i8_restore_kernel(const I8SaveArgs
   const bool ok = i8_header_ok(g.src, g.src_bytes, l);
   if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
   if (!ok) return;
-  using Loose = LooseRows<DT, 8>;
-  __shared__ __align__(16) uint8_t stages[VEC ? 16 : kI8Threads / 32 * Loose::kBytes];
-  const uint32_t quads = (l.chunks() + 3u) / 4u;
-  const uint64_t items = (uint64_t)(l.r8 / 8u) * quads, step = (uint64_t)gridDim.x * (kI8Threads / 32);
+  const uint32_t runs = (l.chunks() + 4u * kQuads - 1u) / (4u * kQuads);
+  const uint64_t items = (uint64_t)(l.r8 / 8u) * runs, step = (uint64_t)gridDim.x * (kI8Threads / 32);
   for (uint64_t it = (uint64_t)blockIdx.x * (kI8Threads / 32) + tid / 32; it < items; it += step) {
-    const uint32_t row = (uint32_t)(it / quads) * 8u + lane % 8u, j = (uint32_t)(it % quads) * 4u + lane / 8u, c = j * 16u;
-    const bool there = row < g.rows && c < g.cols;
-    if (VEC && !there) continue;
-    const uint4 q = there ? *reinterpret_cast<const uint4*>(g.src + l.code_at(row, j)) : make_uint4(0u, 0u, 0u, 0u);
-    const float s = there ? i8_scale(*reinterpret_cast<const float*>(g.src + l.magnitude_at(row))) : 0.0f;
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    float f[16];
+    const uint32_t r0 = (uint32_t)(it / runs) * 8u, row = r0 + lane % 8u, j0 = (uint32_t)(it % runs) * 4u * kQuads, j = j0 + lane / 8u;
+    const uint64_t pitch = 16ull * l.block_rows(row / 128u);
+    const uint8_t* p = g.src + l.code_at(row, j);
+    uint4 q[kQuads];
 #pragma unroll
-    for (int i = 0; i < 16; ++i)  // (127 scales of a row that has fp32's largest number may be beyond it)
-      f[i] = max_nan(min_nan((float)((int32_t)(w[i / 4] << (24 - i % 4 * 8)) >> 24) * s, 3.4028235e38f), -3.4028235e38f);
-    Raw16<DT> x;
-    x.take(f);
-    if (VEC) {
-      x.template store<true>(g.dst + ((uint64_t)row * g.ld + c) * kEs<DT>, (int)min(16u, g.cols - c));
-    } else {
-      const uint32_t r0 = row - lane % 8u;
-      Loose::store(x, stages + tid / 32 * Loose::kBytes, g.dst + (uint64_t)r0 * g.ld * kEs<DT>, g.ld, g.rows > r0 ? min(8u, g.rows - r0) : 0u, (j - lane / 8u) * 16u, g.cols, lane);
+    for (uint32_t x = 0; x < kQuads; ++x) q[x] = j + 4u * x < l.chunks() ? *reinterpret_cast<const uint4*>(p + 4u * x * pitch) : make_uint4(0u, 0u, 0u, 0u);
+    const float s = i8_scale(*reinterpret_cast<const float*>(g.src + l.magnitude_at(row)));
+#pragma unroll
+    for (uint32_t x = 0; x < kQuads; ++x) {
+      const uint32_t w[4] = {q[x].x, q[x].y, q[x].z, q[x].w}, c = (j + 4u * x) * 16u;
+      float f[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)  // (127 scales of a row that has fp32's largest number may be beyond it)
+        f[i] = max_nan(min_nan((float)((int32_t)(w[i / 4] << (24 - i % 4 * 8)) >> 24) * s, 3.4028235e38f), -3.4028235e38f);
+      Raw16<DT> v;
+      v.take(f);
+      if (VEC)
+        v.template store<true>(g.dst + ((uint64_t)row * g.ld + c) * kEs<DT>, row < g.rows && c < g.cols ? (int)min(16u, g.cols - c) : 0);
+      else
+        Loose::store(v, stages + tid / 32 * Loose::kBytes, g.dst + (uint64_t)r0 * g.ld * kEs<DT>, g.ld, g.rows > r0 ? min(8u, g.rows - r0) : 0u, (j0 + 4u * x) * 16u, g.cols, lane);
     }
   }
 }
@@ -272,7 +278,7 @@ bool on_grid(const void* p, uint64_t ld) { return ((uintptr_t)p | ld * kEs<DT>) 
 template <int DT>
 int restore_launch(const I8SaveArgs& a, cudaStream_t stream) {
   const I8Layout l(a.rows, a.cols);
-  const uint64_t items = (uint64_t)(l.r8 / 8u) * ((l.chunks() + 3u) / 4u), ctas = (items + kI8Threads / 32 - 1) / (kI8Threads / 32);
+  const uint64_t items = (uint64_t)(l.r8 / 8u) * ((l.chunks() + 4u * kQuads - 1u) / (4u * kQuads)), ctas = (items + kI8Threads / 32 - 1) / (kI8Threads / 32);
   const uint32_t grid = (uint32_t)std::min<uint64_t>(ctas, (uint64_t)std::max(1, sm_count()) * 32u);
   if (on_grid<DT>(a.dst, a.ld)) return launch_plain<i8_restore_kernel<DT, true>>(grid, kI8Threads, 0, 1, stream, a);
   return launch_plain<i8_restore_kernel<DT, false>>(grid, kI8Threads, 0, 1, stream, a);
