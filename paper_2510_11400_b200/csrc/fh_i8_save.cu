@@ -1,5 +1,4 @@
 // Dense matrices into 8-bit containers and back.
-#include <cstdlib>
 #include "fh_i8.cuh"
 #include "fh_i8_launch.cuh"
 #include "fh_launch.cuh"
@@ -15,7 +14,7 @@ constexpr uint32_t kEs = DT == kF32 ? 4u : 2u;
 
 // ---- by rows ---------------------------------------------------------------------------------------
 // A CTA takes R rows.  Lanes of a warp lie R rows by 32 / R chunks of 16 columns: R lanes that write the codes of the same chunk write R x 16 bytes
-// side by side (a sector or more from R = 2 on), and lanes of the same row read 32 / R chunks side by side.  A lane's I chunks stay in registers from the
+// side by side, and lanes of the same row read 32 / R chunks side by side.  A lane's I chunks stay in registers from the
 // row's maximum to its codes; I = 0: the row is too long for that and is read again, from L2.
 template <int DT, int R, int I, bool VEC>
 __global__ void __launch_bounds__(512, 2) i8_rows_kernel(const I8SaveArgs g) {
@@ -88,25 +87,26 @@ int rows_launch(const I8SaveArgs& a, uint32_t warps, cudaStream_t stream) {
   return launch_plain<i8_rows_kernel<DT, R, I, VEC>>((uint32_t)grid, (int)warps * 32, 0, 1, stream, a);
 }
 template <int DT, int R, bool VEC>
-int rows_by_length(const I8SaveArgs& a, cudaStream_t stream) {
+int rows_by_length(const I8SaveArgs& a, bool many, cudaStream_t stream) {
   constexpr uint32_t kLanes = 32 / R, kMost = DT == kF32 ? 2 : 4;
   const uint32_t need = (I8Layout(a.rows, a.cols).chunks() + kLanes - 1u) / kLanes;  // steps of a warp in all
-  if (need <= 16u) return rows_launch<DT, R, 1, VEC>(a, need, stream);
-  if (need <= 32u) return rows_launch<DT, R, 2, VEC>(a, (need + 1u) / 2u, stream);
-  if (kMost >= 4 && need <= 64u) return rows_launch<DT, R, DT == kF32 ? 2 : 4, VEC>(a, (need + 3u) / 4u, stream);
+  // Four warps to a CTA, or as few as hold the row, where there are many rows: CTAs that load run beside CTAs that write (8192 x 4096 bf16 in two rows to a
+  // CTA: 16 warps 26 us, 8 18.5, 4 17.4); as many warps as the row has work for where there are few.
+  const uint32_t most = many ? 4u : 16u;
+  if (need <= most) return rows_launch<DT, R, 1, VEC>(a, need, stream);
+  if (need <= 2u * most || (kMost == 2 && need <= 32u)) return rows_launch<DT, R, 2, VEC>(a, (need + 1u) / 2u, stream);
+  if (kMost == 4 && need <= 64u) return rows_launch<DT, R, kMost, VEC>(a, (need + 3u) / 4u, stream);
   return rows_launch<DT, R, 0, VEC>(a, 16u, stream);
 }
 template <int DT, bool VEC>
 int rows_by_group(const I8SaveArgs& a, cudaStream_t stream) {
-  // Rows to a CTA: as few as keep the row in the registers of 16 warps, and as few as give every SM one; with 8, pieces of codes are written whole.
-  const uint32_t chunks = I8Layout(a.rows, a.cols).chunks(), sms = (uint32_t)std::max(1, sm_count()), most = DT == kF32 ? 32u : 64u;
-  uint32_t r = 8u;
-  if (const char* e = getenv("I8R")) { r = atoi(e); while (r > 1u && (chunks + 32u / r - 1u) / (32u / r) > most) r /= 2u; } else
-  while (r > 1u && ((chunks + 32u / r - 1u) / (32u / r) > most || (a.rows + r - 1u) / r < sms)) r /= 2u;
-  if (r == 1u) return rows_by_length<DT, 1, VEC>(a, stream);
-  if (r == 2u) return rows_by_length<DT, 2, VEC>(a, stream);
-  if (r == 4u) return rows_by_length<DT, 4, VEC>(a, stream);
-  return rows_by_length<DT, 8, VEC>(a, stream);
+  // Two rows to a CTA write whole sectors of codes (one row 16384 x 512 17.8 us, two 9.3, four 6.8; 8192 x 4096 20.8, 17.4 and 18.5); one where there are not
+  // enough rows for every SM, or where two do not fit the registers of 16 warps.
+  const uint32_t chunks = I8Layout(a.rows, a.cols).chunks(), most = DT == kF32 ? 32u : 64u;
+  const bool many = a.rows / 2u >= (uint32_t)std::max(1, sm_count());
+  if (!many || (chunks + 15u) / 16u > most) return rows_by_length<DT, 1, VEC>(a, many, stream);
+  if (chunks > 32u) return rows_by_length<DT, 2, VEC>(a, true, stream);
+  return rows_by_length<DT, 4, VEC>(a, true, stream);
 }
 
 // ---- by columns ------------------------------------------------------------------------------------
@@ -232,8 +232,8 @@ int cols_launch(const I8SaveArgs& a0, cudaStream_t stream) {
 }
 
 // ---- and back --------------------------------------------------------------------------------------
-// A warp's lanes lie 8 rows by 4 chunks, as in the kernel by rows, and have kQuads chunks each, all asked for at once.
-constexpr uint32_t kQuads = 4;
+// A warp's lanes lie 8 rows by 4 chunks, as in the kernel by rows.  (Four chunks to a lane, asked for at once: the same on large matrices, where two
+// thirds of the traffic are writes, and 1 x 8192 2.7 us instead of 1.8.)
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kI8Threads) i8_restore_kernel(const I8SaveArgs g) {
   using Loose = LooseRows<DT, 8>;
@@ -245,30 +245,23 @@ __global__ void __launch_bounds__(kI8Threads) i8_restore_kernel(const I8SaveArgs
   const bool ok = i8_header_ok(g.src, g.src_bytes, l);
   if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
   if (!ok) return;
-  const uint32_t runs = (l.chunks() + 4u * kQuads - 1u) / (4u * kQuads);
-  const uint64_t items = (uint64_t)(l.r8 / 8u) * runs, step = (uint64_t)gridDim.x * (kI8Threads / 32);
+  const uint32_t quads = (l.chunks() + 3u) / 4u;
+  const uint64_t items = (uint64_t)(l.r8 / 8u) * quads, step = (uint64_t)gridDim.x * (kI8Threads / 32);
   for (uint64_t it = (uint64_t)blockIdx.x * (kI8Threads / 32) + tid / 32; it < items; it += step) {
-    const uint32_t r0 = (uint32_t)(it / runs) * 8u, row = r0 + lane % 8u, j0 = (uint32_t)(it % runs) * 4u * kQuads, j = j0 + lane / 8u;
-    const uint64_t pitch = 16ull * l.block_rows(row / 128u);
-    const uint8_t* p = g.src + l.code_at(row, j);
-    uint4 q[kQuads];
-#pragma unroll
-    for (uint32_t x = 0; x < kQuads; ++x) q[x] = j + 4u * x < l.chunks() ? *reinterpret_cast<const uint4*>(p + 4u * x * pitch) : make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t r0 = (uint32_t)(it / quads) * 8u, row = r0 + lane % 8u, j0 = (uint32_t)(it % quads) * 4u, j = j0 + lane / 8u, c = j * 16u;
+    const uint4 q = j < l.chunks() ? *reinterpret_cast<const uint4*>(g.src + l.code_at(row, j)) : make_uint4(0u, 0u, 0u, 0u);
     const float s = i8_scale(*reinterpret_cast<const float*>(g.src + l.magnitude_at(row)));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    float f[16];
 #pragma unroll
-    for (uint32_t x = 0; x < kQuads; ++x) {
-      const uint32_t w[4] = {q[x].x, q[x].y, q[x].z, q[x].w}, c = (j + 4u * x) * 16u;
-      float f[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i)  // (127 scales of a row that has fp32's largest number may be beyond it)
-        f[i] = max_nan(min_nan((float)((int32_t)(w[i / 4] << (24 - i % 4 * 8)) >> 24) * s, 3.4028235e38f), -3.4028235e38f);
-      Raw16<DT> v;
-      v.take(f);
-      if (VEC)
-        v.template store<true>(g.dst + ((uint64_t)row * g.ld + c) * kEs<DT>, row < g.rows && c < g.cols ? (int)min(16u, g.cols - c) : 0);
-      else
-        Loose::store(v, stages + tid / 32 * Loose::kBytes, g.dst + (uint64_t)r0 * g.ld * kEs<DT>, g.ld, g.rows > r0 ? min(8u, g.rows - r0) : 0u, (j0 + 4u * x) * 16u, g.cols, lane);
-    }
+    for (int i = 0; i < 16; ++i)  // (127 scales of a row that has fp32's largest number may be beyond it)
+      f[i] = max_nan(min_nan((float)((int32_t)(w[i / 4] << (24 - i % 4 * 8)) >> 24) * s, 3.4028235e38f), -3.4028235e38f);
+    Raw16<DT> v;
+    v.take(f);
+    if (VEC)
+      v.template store<true>(g.dst + ((uint64_t)row * g.ld + c) * kEs<DT>, row < g.rows && c < g.cols ? (int)min(16u, g.cols - c) : 0);
+    else
+      Loose::store(v, stages + tid / 32 * Loose::kBytes, g.dst + (uint64_t)r0 * g.ld * kEs<DT>, g.ld, g.rows > r0 ? min(8u, g.rows - r0) : 0u, j0 * 16u, g.cols, lane);
   }
 }
 
@@ -278,7 +271,7 @@ bool on_grid(const void* p, uint64_t ld) { return ((uintptr_t)p | ld * kEs<DT>) 
 template <int DT>
 int restore_launch(const I8SaveArgs& a, cudaStream_t stream) {
   const I8Layout l(a.rows, a.cols);
-  const uint64_t items = (uint64_t)(l.r8 / 8u) * ((l.chunks() + 4u * kQuads - 1u) / (4u * kQuads)), ctas = (items + kI8Threads / 32 - 1) / (kI8Threads / 32);
+  const uint64_t items = (uint64_t)(l.r8 / 8u) * ((l.chunks() + 3u) / 4u), ctas = (items + kI8Threads / 32 - 1) / (kI8Threads / 32);
   const uint32_t grid = (uint32_t)std::min<uint64_t>(ctas, (uint64_t)std::max(1, sm_count()) * 32u);
   if (on_grid<DT>(a.dst, a.ld)) return launch_plain<i8_restore_kernel<DT, true>>(grid, kI8Threads, 0, 1, stream, a);
   return launch_plain<i8_restore_kernel<DT, false>>(grid, kI8Threads, 0, 1, stream, a);
