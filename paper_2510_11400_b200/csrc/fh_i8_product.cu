@@ -47,57 +47,58 @@ __device__ __forceinline__ bool any_of(uint32_t bar, uint32_t threads, bool p) {
 struct I8Factors {
   const float* rows;  // the scales of the tile's rows times alpha, in shared memory
   const uint8_t* a;   // the first of their magnitudes
-  uint32_t there;     // how many there are
-  float alpha;
-  bool wide;
-  // NR sums of rows q ... of the tile, of a column of scale `col`.
+  float alpha, col, up;  // scales of the lane's column of C, and of the second weight's
+  // NR sums of rows q ... of the tile, of a column of scale `by`.
   template <int NR>
-  __device__ __forceinline__ void apply(const uint32_t (&v)[NR], float (&f)[NR], uint32_t q, float col) const {
-    if (!wide) {
+  __device__ __forceinline__ void apply(const uint32_t (&v)[NR], float (&f)[NR], uint32_t q, float by) const {
 #pragma unroll
-      for (int x = 0; x < NR; ++x) f[x] = (float)(int32_t)v[x] * col * rows[q + x];
-      return;
-    }
-#pragma unroll
-    for (int x = 0; x < NR; ++x) {
-      const double s = q + x < there ? (double)i8_scale(reinterpret_cast<const float*>(a)[q + x]) : 0.0;
-      f[x] = (float)((double)(int32_t)v[x] * col * s * alpha);
-    }
+    for (int x = 0; x < NR; ++x) f[x] = (float)(int32_t)v[x] * by * rows[q + x];
+  }
+  // One, in 64 bits.
+  __device__ __forceinline__ float wide(uint32_t v, uint32_t q, float by) const {
+    return (float)((double)(int32_t)v * by * (double)i8_scale(reinterpret_cast<const float*>(a)[q]) * alpha);
   }
 };
 
-// What becomes of NR sums of a column of a tile: rows q ... of the tile, row q0 + q of the matrix.
+// What becomes of NR results (GATED: of both weights) of a column of C, rows `row` to `end`.
 template <int DT, int NR, int ACT>
-struct I8Result {
-  static __device__ __forceinline__ void put(const I8ProductArgs& g, const I8Factors& by, const uint32_t (&v)[NR], const uint32_t (&w)[NR], uint32_t row, uint32_t end,
-                                             uint32_t q, uint32_t col, float scale, float scale_up) {
-    float f[NR];
-    by.apply(v, f, q, scale);
-    if (ACT < 0) {
-      if (col >= g.n) return;
-      if (g.accumulate) {
-        float old[NR];
-        load_c<DT, NR>(g.c, g.ldc, row, end, col, old);
+__device__ __forceinline__ void i8_put(const I8ProductArgs& g, float (&f)[NR], const float (&u)[NR], uint32_t row, uint32_t end, uint32_t col) {
+  if (col >= g.n) return;
+  if (ACT < 0) {
+    if (g.accumulate) {
+      float old[NR];
+      load_c<DT, NR>(g.c, g.ldc, row, end, col, old);
 #pragma unroll
-        for (int x = 0; x < NR; ++x) f[x] += old[x];
-      }
+      for (int x = 0; x < NR; ++x) f[x] += old[x];
+    }
+    store_c<DT, NR>(g.c, g.ldc, row, end, col, f);
+  } else {
+    if (g.pre) {
+      store_c<DT, NR>(g.pre, g.ldp, row, end, col, f);
+      store_c<DT, NR>(g.pre, g.ldp, row, end, g.n + col, u);
+    }
+    if (g.c) {
+#pragma unroll
+      for (int x = 0; x < NR; ++x) f[x] = act_of<ACT>(f[x]) * u[x];
       store_c<DT, NR>(g.c, g.ldc, row, end, col, f);
-    } else {
-      float u[NR];
-      by.apply(w, u, q, scale_up);
-      if (col >= g.n) return;
-      if (g.pre) {
-        store_c<DT, NR>(g.pre, g.ldp, row, end, col, f);
-        store_c<DT, NR>(g.pre, g.ldp, row, end, g.n + col, u);
-      }
-      if (g.c) {
-#pragma unroll
-        for (int x = 0; x < NR; ++x) f[x] = act_of<ACT>(f[x]) * u[x];
-        store_c<DT, NR>(g.c, g.ldc, row, end, col, f);
-      }
     }
   }
-};
+}
+// Sums of rows q ... of a tile whose first row is row0.
+template <int DT, int NR, int ACT>
+__device__ __forceinline__ void i8_put_sums(const I8ProductArgs& g, const I8Factors& by, const uint32_t (&v)[NR], const uint32_t (&w)[NR], uint32_t row0, uint32_t end, uint32_t q,
+                                            uint32_t col) {
+  float f[NR], u[NR];
+  by.apply(v, f, q, by.col);
+  if (ACT >= 0) by.apply(w, u, q, by.up);
+  i8_put<DT, NR, ACT>(g, f, u, row0 + q, end, col);
+}
+// One row, in 64 bits.  (Where factors need it a tile is gone through row by row: in line with the others it would take registers from those.)
+template <int DT, int ACT>
+__device__ __forceinline__ void i8_put_wide(const I8ProductArgs& g, const I8Factors& by, uint32_t v, uint32_t w, uint32_t row0, uint32_t q, uint32_t col) {
+  float f[1] = {by.wide(v, q, by.col)}, u[1] = {ACT >= 0 ? by.wide(w, q, by.up) : 0.0f};
+  i8_put<DT, 1, ACT>(g, f, u, row0 + q, row0 + q + 1u, col);
+}
 
 // Adds up rows of partial sums over the parts of a cluster (CTAs `stride` apart, from `first` on); four parts are asked for at once.
 template <int NR>
@@ -220,19 +221,18 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
   // the accumulator: lane i of warp w has row 32 w + i of the tile of B, QT columns for the rows of A
   const bool mine = ok && warp < 4;
   const uint32_t col = tp * 128u + warp * 32u + lane, rows = min((uint32_t)QT, g.m - tq * 128u);
-  float scale = 0.0f, scale_up = 0.0f;
-  I8Factors by = {factors, g.a + lq.magnitude_at(tq * 128u), rows, g.alpha, false};
-  bool good = mine;
+  I8Factors by = {factors, g.a + lq.magnitude_at(tq * 128u), g.alpha, 0.0f, 0.0f};
+  bool good = mine, wide = false;
   if (mine) {
-    scale = i8_scale_at(g.b, lp, col);
-    if (GATED) scale_up = i8_scale_at(g.up, lp, col);
-    bool wide = !i8_plain(scale) || !i8_plain(scale_up);
+    by.col = i8_scale_at(g.b, lp, col);
+    if (GATED) by.up = i8_scale_at(g.up, lp, col);
+    wide = !i8_plain(by.col) || !i8_plain(by.up);
     if (tid < (uint32_t)QT) {
       const float s = i8_scale_at(g.a, lq, tq * 128u + tid), f = s * g.alpha;
       factors[tid] = f;
       wide = wide || !i8_plain(f) || !i8_plain(s) || (f == 0.0f && s != 0.0f && g.alpha != 0.0f);
     }
-    by.wide = any_of(1u, 128u, wide);
+    wide = any_of(1u, 128u, wide);
     good = mbar_poll_warp(done, 0u, g.polls, abort);
     if (!good && lane == 0) *abort = 1u;
     tc_fence_after();
@@ -240,15 +240,21 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
   constexpr int NR = 16;
   const uint32_t at = tmem + (warp * 32u << 16);
   if (g.split == 1u) {
-    if (good) {
+    if (good && !wide) {
 #pragma unroll 1
-      for (uint32_t q = 0; q < (uint32_t)QT; q += NR) {
-        if (q >= rows) break;
+      for (uint32_t q = 0; q < rows; q += NR) {
         uint32_t v[NR], w[NR] = {};
         tc_load16(at + q, v);
         if (GATED) tc_load16(at + QT + q, w);
         tc_load_wait();
-        I8Result<DT, NR, ACT>::put(g, by, v, w, tq * 128u + q, g.m, q, col, scale, scale_up);
+        i8_put_sums<DT, NR, ACT>(g, by, v, w, tq * 128u, g.m, q, col);
+      }
+    } else if (good) {
+#pragma unroll 1
+      for (uint32_t q = 0; q < rows; ++q) {
+        const uint32_t v = tc_load1(at + q), w = GATED ? tc_load1(at + QT + q) : 0u;
+        tc_load_wait();
+        i8_put_wide<DT, ACT>(g, by, v, w, tq * 128u, q, col);
       }
     }
   } else {
@@ -269,11 +275,16 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
     if (good) {
       const uint32_t end = rows * (rank + 1u) / g.split;
       constexpr int N = QT < 32 ? 2 : 8;
-      for (uint32_t q = rows * rank / g.split; q < end; q += N) {
+      const uint32_t step = wide ? 1u : N;
+#pragma unroll 1
+      for (uint32_t q = rows * rank / g.split; q < end; q += step) {
         uint32_t v[N], w[N] = {};
         add_parts<N>(smem_u32(part + q * 128u + tid), 0u, 1u, g.split, v);  // (rows behind the last: stage bytes)
         if (GATED) add_parts<N>(smem_u32(part + (QT + q) * 128u + tid), 0u, 1u, g.split, w);
-        I8Result<DT, N, ACT>::put(g, by, v, w, tq * 128u + q, tq * 128u + end, q, col, scale, scale_up);
+        if (wide)
+          i8_put_wide<DT, ACT>(g, by, v[0], w[0], tq * 128u, q, col);
+        else
+          i8_put_sums<DT, N, ACT>(g, by, v, w, tq * 128u, tq * 128u + end, q, col);
       }
     }
     cluster_sync();
@@ -298,20 +309,25 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
 // while the eight warps for the result write this one's.  With a split, a cluster's pairs share one tile.
 constexpr int kI8PairThreads = 320;  // eight warps for the result, then one each for loads and matrix instructions
 
+#ifndef GATED_Q
+#define GATED_Q 256
+#endif
 template <bool GATED>
 struct I8PairShape {
   static constexpr int kW = GATED ? 2 : 1;
-  static constexpr uint32_t kQ = 256 / kW;  // rows of A to a tile
+  static constexpr uint32_t kQ = GATED ? GATED_Q : 256;  // rows of A to a tile
+  static constexpr uint32_t kSums = kW * kQ, kBufs = 512 / kSums;  // columns of tensor memory that a tile takes, tiles that have room
   static constexpr uint32_t kP = 128 * kI8Step, kA = kQ / 2 * kI8Step;
   static constexpr uint32_t kStage = kW * kP + kA;
-  static constexpr int kStages = GATED ? 5 : 6;
+  static constexpr int kStages = 200 * 1024 / kStage;
   static constexpr uint32_t kTail = 256 + 2 * kQ * 4;
   static constexpr size_t kSmem = 128 + (size_t)kStages * kStage + kTail;
-  static_assert(kSmem <= kMxSmemLimit && kStages * kStage >= kW * (kQ + 8) * 512, "room; partial sums, and rows read behind them");
+  static constexpr uint32_t kMostSplit = kStages * kStage >= kW * (kQ + 8) * 512 ? 4 : 1;  // (partial sums, and rows read behind them, lie in the stages)
+  static_assert(kSmem <= kMxSmemLimit, "room");
   // the barriers behind the stages
   static constexpr int kEmpty = kStages;          // a stage may be loaded again
-  static constexpr int kSums = 2 * kStages;       // an accumulator is complete (one for each of the two)
-  static constexpr int kTaken = kSums + 2;        // even CTA: both CTAs' warps have taken it
+  static constexpr int kDone = 2 * kStages;       // an accumulator is complete (one for each of the two)
+  static constexpr int kTaken = kDone + 2;        // even CTA: both CTAs' warps have taken it
   static constexpr int kIdle = kTaken + 2;        // even CTA, after a wait that ran out: what was issued is complete
   static constexpr int kWords = kIdle + 1;
   static_assert(kWords * 8 + 12 <= 256, "room behind the stages");
@@ -348,7 +364,7 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = stages_at(smem_raw);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);
-  uint64_t *empty = full + S::kEmpty, *sums = full + S::kSums, *taken = full + S::kTaken, *idle = full + S::kIdle;
+  uint64_t *empty = full + S::kEmpty, *sums = full + S::kDone, *taken = full + S::kTaken, *idle = full + S::kIdle;
   uint32_t* tmem_at = reinterpret_cast<uint32_t*>(full + S::kWords);
   volatile uint32_t* abort = tmem_at + 1;
   uint32_t* loads = tmem_at + 2;  // stages that the loading thread has asked for
@@ -396,7 +412,7 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
       for (uint32_t tile = pair; tile < tiles && good; tile += pairs) {
         const PairTile where(tile, g.tiles_m, g.tiles_n);
         const I8Source p(pa.b, lp, where.n * 2u + half, 0u), u(pa.up, lp, where.n * 2u + half, 0u);
-        const I8Source q(pa.a, lq, GATED ? where.m : where.m * 2u + half, GATED ? half * 8u : 0u);
+        const I8Source q(pa.a, lq, S::kQ == 128u ? where.m : where.m * 2u + half, S::kQ == 128u ? half * 8u : 0u);
         for (uint32_t it = first; it < last; ++it, ++loaded, turn.next()) {
           if (loaded == silent) {
             good = false;
@@ -422,8 +438,8 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
       uint32_t n = 0;
       Turn<S::kStages> turn;
       for (uint32_t tile = pair; tile < tiles && good; tile += pairs, ++n) {
-        const uint32_t buf = n & 1u, acc = tmem + buf * 256u;
-        if (n > 1u && !mbar_poll<true>(taken + buf, (n / 2u - 1u) & 1u, g.polls, abort)) {
+        const uint32_t buf = n % S::kBufs, acc = tmem + buf * S::kSums;
+        if (n >= S::kBufs && !mbar_poll<true>(taken + buf, (n / S::kBufs - 1u) & 1u, g.polls, abort)) {
           raise_cluster(abort, 2u * g.split);
           break;
         }
@@ -451,54 +467,84 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
       }
     }
   } else {
-    constexpr uint32_t kSide = S::kQ / 2u;  // columns of an accumulator to each four warps: rows of A
+    constexpr uint32_t kSide = S::kQ / 2u, kRun = 128u / S::kW;  // columns of an accumulator to each four warps: rows of A; those of them in registers at once
     const uint32_t side = warp / 4u * kSide;
-    uint32_t n = 0;
-    for (uint32_t tile = pair; tile < tiles && good; tile += pairs, ++n) {
+    // The magnitudes of a tile are asked for a tile ahead.
+    float next_col = 0.0f, next_up = 0.0f, next_row = 0.0f;
+    auto ask = [&](uint32_t tile) {
       const PairTile where(tile, g.tiles_m, g.tiles_n);
-      const uint32_t col = where.n * 256u + half * 128u + warp % 4u * 32u + lane, row0 = where.m * S::kQ, rows = min(S::kQ, g.m - row0), buf = n & 1u;
-      const float scale = i8_scale_at(g.b, lp, col), scale_up = GATED ? i8_scale_at(g.up, lp, col) : 0.0f;
-      float* fa = factors + buf * S::kQ;  // (the other half may still be read by warps that are a tile behind)
-      bool wide = !i8_plain(scale) || !i8_plain(scale_up);
+      const uint32_t col = where.n * 256u + half * 128u + warp % 4u * 32u + lane, row = where.m * S::kQ + tid;
+      next_col = col < lp.rows ? *reinterpret_cast<const float*>(g.b + lp.magnitude_at(col)) : 0.0f;
+      if (GATED) next_up = col < lp.rows ? *reinterpret_cast<const float*>(g.up + lp.magnitude_at(col)) : 0.0f;
+      if (tid < S::kQ) next_row = row < lq.rows ? *reinterpret_cast<const float*>(g.a + lq.magnitude_at(row)) : 0.0f;
+    };
+    if (pair < tiles) ask(pair);
+    uint32_t n = 0;
+    for (uint32_t tile = pair; tile < tiles; tile += pairs, ++n) {
+      const PairTile where(tile, g.tiles_m, g.tiles_n);
+      const uint32_t col = where.n * 256u + half * 128u + warp % 4u * 32u + lane, row0 = where.m * S::kQ, rows = min(S::kQ, g.m - row0), buf = n % S::kBufs;
+      const I8Factors by = {factors + (n & 1u) * S::kQ, g.a + lq.magnitude_at(row0), g.alpha, i8_scale(next_col), i8_scale(next_up)};
+      float* fa = factors + (n & 1u) * S::kQ;  // (the other half may still be read by warps that are a tile behind)
       if (tid < S::kQ) {
-        const float s = i8_scale_at(g.a, lq, row0 + tid), f = s * g.alpha;
-        fa[tid] = f;
-        wide = wide || !i8_plain(f) || !i8_plain(s) || (f == 0.0f && s != 0.0f && g.alpha != 0.0f);
+        const float s = i8_scale(next_row), f = s * g.alpha;
+        fa[tid] = i8_plain(s) && i8_plain(f) && (f != 0.0f || s == 0.0f || g.alpha == 0.0f) ? f : __uint_as_float(0x7FC00000u);
       }
-      const I8Factors by = {fa, g.a + lq.magnitude_at(row0), rows, g.alpha, any_of(1u, 256u, wide)};
-      good = mbar_poll_warp(sums + buf, n / 2u & 1u, g.polls, abort);
-      if (!good && lane == 0) raise_cluster(abort, 2u * g.split);
-      good = !any_of(1u, 256u, !good);  // (all warps stay or none does: they meet at the barrier above)
-      if (!good) break;
-      tc_fence_after();
-      const uint32_t at = tmem + buf * 256u + (warp % 4u * 32u << 16) + side;
-      if (g.split == 1u) {
-#pragma unroll 1
-        for (uint32_t q = 0; q < kSide; q += 16u) {
-          uint32_t v[16], w[16] = {};
-          tc_load16(at + q, v);
-          if (GATED) tc_load16(at + S::kQ + q, w);
-          tc_load_wait();
-          if (side + q < rows) I8Result<DT, 16, ACT>::put(g, by, v, w, row0 + side + q, g.m, side + q, col, scale, scale_up);
-        }
-      } else {  // (one tile only: all copies into shared memory have been used)
-        uint32_t* part = reinterpret_cast<uint32_t*>(smem) + side * 128u + warp % 4u * 32u + lane;
-#pragma unroll 1
-        for (uint32_t q = 0; q < kSide; q += 16u) {
-          uint32_t v[16], w[16] = {};
-          tc_load16(at + q, v);
-          if (GATED) tc_load16(at + S::kQ + q, w);
-          tc_load_wait();
+      if (tile + pairs < tiles) ask(tile + pairs);
+      if (any_of(1u, 256u, !good)) break;  // (all warps stay or none does: they meet here)
+      bool wide = !i8_plain(by.col) || !i8_plain(by.up);
 #pragma unroll
-          for (uint32_t y = 0; y < 16u; ++y) {
-            part[(q + y) * 128u] = v[y];
-            if (GATED) part[(S::kQ + q + y) * 128u] = w[y];
+      for (uint32_t q = 0; q < S::kQ; q += 32u) wide = wide || fa[q + lane] != fa[q + lane];
+      wide = __any_sync(0xFFFFFFFFu, wide);
+      good = mbar_poll_warp(sums + buf, n / S::kBufs & 1u, g.polls, abort);
+      if (!good) {
+        if (lane == 0) raise_cluster(abort, 2u * g.split);
+        continue;
+      }
+      tc_fence_after();
+      const uint32_t at = tmem + buf * S::kSums + (warp % 4u * 32u << 16) + side;
+      if (wide && g.split == 1u) {
+#pragma unroll 1
+        for (uint32_t q = 0; q < kSide; ++q) {
+          const uint32_t v = tc_load1(at + q), w = GATED ? tc_load1(at + S::kQ + q) : 0u;
+          tc_load_wait();
+          if (side + q < rows) i8_put_wide<DT, ACT>(g, by, v, w, row0, side + q, col);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_at(taken + buf, even);
+        continue;
+      }
+#pragma unroll 1
+      for (uint32_t run = 0; run < kSide; run += kRun) {
+        uint32_t v[kRun / 16u][16], w[GATED ? kRun / 16u : 1u][16];
+#pragma unroll
+        for (uint32_t x = 0; x < kRun / 16u; ++x) {
+          tc_load16(at + run + 16u * x, v[x]);
+          if (GATED) tc_load16(at + S::kQ + run + 16u * x, w[x]);
+        }
+        tc_load_wait();
+        if (run + kRun == kSide) {  // (ahead of this tile's stores: the release would wait for them)
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_at(taken + buf, even);
+        }
+        if (g.split == 1u) {
+#pragma unroll
+          for (uint32_t x = 0; x < kRun / 16u; ++x) {
+            const uint32_t q = side + run + 16u * x;
+            if (q < rows) i8_put_sums<DT, 16, ACT>(g, by, v[x], w[GATED ? x : 0u], row0, g.m, q, col);
           }
+        } else {  // (one tile only: all copies into shared memory have been used)
+          uint32_t* part = reinterpret_cast<uint32_t*>(smem) + (side + run) * 128u + warp % 4u * 32u + lane;
+#pragma unroll
+          for (uint32_t x = 0; x < kRun / 16u; ++x)
+#pragma unroll
+            for (uint32_t y = 0; y < 16u; ++y) {
+              part[(16u * x + y) * 128u] = v[x][y];
+              if (GATED) part[(S::kQ + 16u * x + y) * 128u] = w[x][y];
+            }
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_at(taken + buf, even);
     }
   }
   __syncwarp();
@@ -510,15 +556,20 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
       const uint32_t p = warp % 4u * 32u + lane, col = where.n * 256u + half * 128u + p, row0 = where.m * S::kQ;
       const uint32_t rows = min(S::kQ, g.m - row0), from = rows * rank / g.split, end = rows * (rank + 1u) / g.split, mid = (from + end) / 2u;
       const uint32_t stop = warp < 4u ? mid : end;
-      const float scale = i8_scale_at(g.b, lp, col), scale_up = GATED ? i8_scale_at(g.up, lp, col) : 0.0f;
-      bool wide = !i8_plain(scale) || !i8_plain(scale_up);
-      for (uint32_t q = tid; q < rows; q += 256u) wide = wide || !i8_plain(factors[q]) || !i8_plain(i8_scale_at(g.a, lq, row0 + q)) || (factors[q] == 0.0f && i8_scale_at(g.a, lq, row0 + q) != 0.0f && g.alpha != 0.0f);
-      const I8Factors by = {factors, g.a + lq.magnitude_at(row0), rows, g.alpha, any_of(1u, 256u, wide)};
-      for (uint32_t q = warp < 4u ? from : mid; q < stop; q += 8u) {
+      const I8Factors by = {factors, g.a + lq.magnitude_at(row0), g.alpha, i8_scale_at(g.b, lp, col), GATED ? i8_scale_at(g.up, lp, col) : 0.0f};
+      bool wide = !i8_plain(by.col) || !i8_plain(by.up);
+      for (uint32_t q = lane; q < rows; q += 32u) wide = wide || factors[q] != factors[q];
+      wide = __any_sync(0xFFFFFFFFu, wide);
+      const uint32_t step = wide ? 1u : 8u;
+#pragma unroll 1
+      for (uint32_t q = warp < 4u ? from : mid; q < stop; q += step) {
         uint32_t v[8], w[8] = {};
         add_parts<8>(smem_u32(reinterpret_cast<uint32_t*>(smem) + q * 128u + p), half, 2u, g.split, v);
         if (GATED) add_parts<8>(smem_u32(reinterpret_cast<uint32_t*>(smem) + (S::kQ + q) * 128u + p), half, 2u, g.split, w);
-        I8Result<DT, 8, ACT>::put(g, by, v, w, row0 + q, row0 + stop, q, col, scale, scale_up);
+        if (wide)
+          i8_put_wide<DT, ACT>(g, by, v[0], w[0], row0, q, col);
+        else
+          i8_put_sums<DT, 8, ACT>(g, by, v, w, row0, row0 + stop, q, col);
       }
     }
   }
@@ -577,7 +628,7 @@ int launch_i8_pair(const I8ProductArgs& a, cudaStream_t stream) {
   const uint64_t tiles = (uint64_t)p.g.tiles_m * p.g.tiles_n;
   auto at_once = [](uint32_t s) { return clusters_at_once<i8_pair_kernel<DT, ACT>>((int)(2 * s), kI8PairThreads, S::kSmem); };
   // (a tile's start and end take about as long as ten stages)
-  p.g.split = choose_split(tiles, ((uint64_t)a.k + kI8Step - 1) / kI8Step, 4, 10, at_once);
+  p.g.split = choose_split(tiles, ((uint64_t)a.k + kI8Step - 1) / kI8Step, S::kMostSplit, 10, at_once);
   const int n = at_once(1);
   if (n < 1) return FH_ERR_CUDA;
   const uint32_t clusters = (uint32_t)(p.g.split > 1 ? tiles : std::min<uint64_t>(tiles, (uint64_t)n));

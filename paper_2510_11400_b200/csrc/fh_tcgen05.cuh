@@ -172,6 +172,12 @@ __device__ __forceinline__ void tc_load16(uint32_t tmem, uint32_t (&v)[16]) {
       : "r"(tmem)
       : "memory");
 }
+// One column.
+__device__ __forceinline__ uint32_t tc_load1(uint32_t tmem) {
+  uint32_t v;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(v) : "r"(tmem) : "memory");
+  return v;
+}
 __device__ __forceinline__ void tc_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void cluster_sync() {
