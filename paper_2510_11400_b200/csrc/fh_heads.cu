@@ -133,11 +133,11 @@ template <bool HALVES, uint32_t V>
 __device__ __forceinline__ constexpr uint32_t second_of(uint32_t i) { return HALVES ? V + i : 2 * i + 1; }
 
 // A token's position: -1 for one that is left out.
-__device__ __forceinline__ int64_t position_of(const HeadsArgs& g, uint32_t token) {
+__device__ __forceinline__ int32_t position_of(const HeadsArgs& g, uint32_t token) {
   if (g.rotary == 0u) return 0;
-  if (!g.at) return token;
+  if (!g.at) return (int32_t)token;  // (the host has seen that the table has them all)
   const int32_t p = g.at[token];
-  return p < 0 || (uint32_t)p >= g.positions ? -1 : p;
+  return (uint32_t)p >= g.positions ? -1 : p;
 }
 // The status, by one CTA that does nothing else (the others' order is not known).
 __device__ __forceinline__ void report_positions(const HeadsArgs& g) {
@@ -154,7 +154,7 @@ __device__ __forceinline__ void report_positions(const HeadsArgs& g) {
 
 // Cosines and sines of a slot's pairs at a position.
 template <int DT>
-__device__ __forceinline__ void load_turn(const HeadsArgs& g, const Slot<DT>& s, int64_t at, float (&c)[kV<DT>], float (&n)[kV<DT>]) {
+__device__ __forceinline__ void load_turn(const HeadsArgs& g, const Slot<DT>& s, int32_t at, float (&c)[kV<DT>], float (&n)[kV<DT>]) {
   if (s.turned) {
     const float4* p = reinterpret_cast<const float4*>(g.table + (uint64_t)at * (g.rotary / 2u) + s.pair);
 #pragma unroll
@@ -174,19 +174,54 @@ __device__ __forceinline__ void load_turn(const HeadsArgs& g, const Slot<DT>& s,
   }
 }
 
+// Two elements to an instruction: instructions bound the bf16 kernels as much as memory does.
+__device__ __forceinline__ f32x2 twice(float x) { return pack2(x, x); }
+__device__ __forceinline__ float sum2(f32x2 v) {
+  float a, b;
+  unpack2(v, a, b);
+  return a + b;
+}
+// First and second elements of the V pairs of a slot.
+template <bool HALVES, uint32_t V>
+__device__ __forceinline__ void split(const float (&x)[2 * V], f32x2 (&a)[V / 2], f32x2 (&b)[V / 2]) {
+#pragma unroll
+  for (uint32_t p = 0; p < V; p += 2) {
+    a[p / 2] = pack2(x[first_of<HALVES, V>(p)], x[first_of<HALVES, V>(p + 1)]);
+    b[p / 2] = pack2(x[second_of<HALVES, V>(p)], x[second_of<HALVES, V>(p + 1)]);
+  }
+}
+template <bool HALVES, uint32_t V>
+__device__ __forceinline__ void join(const f32x2 (&a)[V / 2], const f32x2 (&b)[V / 2], float (&x)[2 * V]) {
+#pragma unroll
+  for (uint32_t p = 0; p < V; p += 2) {
+    unpack2(a[p / 2], x[first_of<HALVES, V>(p)], x[first_of<HALVES, V>(p + 1)]);
+    unpack2(b[p / 2], x[second_of<HALVES, V>(p)], x[second_of<HALVES, V>(p + 1)]);
+  }
+}
+
 // Whether unit `u` is of queries or keys, of which token, and its first head.  A unit is a warp's work: `span` heads of a token.
 struct HeadUnit {
   uint32_t side, token, head;
   __device__ __forceinline__ HeadUnit(uint64_t u, const HeadsArgs& g, uint32_t span) {
     const uint32_t nq = (g.side[0].heads + span - 1u) / span, nk = (g.side[1].heads + span - 1u) / span;
-    token = (uint32_t)(u / (nq + nk));
-    const uint32_t at = (uint32_t)(u % (nq + nk));
+    // (a division in 64 bits takes as long as a row)
+    token = u >> 32 ? (uint32_t)(u / (nq + nk)) : (uint32_t)u / (nq + nk);
+    const uint32_t at = (uint32_t)(u - (uint64_t)token * (nq + nk));
     side = at >= nq;
     head = (side ? at - nq : at) * span;
   }
 };
 
-// T lanes to a row, U rows of a team asked for at once.
+template <int DT>
+__device__ __forceinline__ const uint8_t* row_of(const HeadsSide& s, uint32_t token, uint32_t head) {
+  return s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
+}
+template <int DT>
+__device__ __forceinline__ uint64_t out_at(const HeadsSide& s, uint32_t token, uint32_t head) {
+  return ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
+}
+
+// T lanes to a row, U rows of a team at once: asked for together, and their sums, whose exchanges and roots are chains of latencies, taken side by side.
 template <int DT, int T, int U, bool HALVES>
 __global__ void __launch_bounds__(kHeadThreads) heads_forward_kernel(const HeadsArgs g) {
   constexpr uint32_t V = kV<DT>, kTeams = 32 / T, kSpan = kTeams * U;
@@ -205,55 +240,82 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_kernel(const Heads
   const HeadsSide& s = g.side[unit.side];
   const Slot<DT> slot(lane % T, g.dim, g.rotary, HALVES);
   RawSlot raw[U];
+  bool there[U];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     const uint32_t head = unit.head + i * kTeams + team;
+    there[i] = slot.there && head < s.heads;
     raw[i].zero();
-    if (slot.there && head < s.heads) raw[i].load<DT>(s.x + ((uint64_t)unit.token * s.token + (uint64_t)head * s.head) * kEs<DT>, slot.a, slot.b);
+    if (there[i]) raw[i].load<DT>(row_of<DT>(s, unit.token, head), slot.a, slot.b);
   }
   float c[V], n[V], w[2 * V];
   if (slot.there) load_weights<DT>(s.gamma, g, slot.a, slot.b, w);
-  const int64_t at = position_of(g, unit.token);
+  const int32_t at = position_of(g, unit.token);
   if (at < 0) return;
   if (slot.there) load_turn<DT>(g, slot, at, c, n);
-  const float size = (float)g.dim;
+  // weights and rotation as one factor each: y = rstd (xa (wa c) - xb (wb n)), rstd (xb (wb c) + xa (wa n))
+  f32x2 ac[V / 2], an[V / 2], bc[V / 2], bn[V / 2];
+  {
+    f32x2 wa[V / 2], wb[V / 2];
+    split<HALVES, V>(w, wa, wb);
+#pragma unroll
+    for (uint32_t p = 0; p < V / 2; ++p) {
+      const f32x2 cc = pack2(c[2 * p], c[2 * p + 1]), nn = pack2(n[2 * p], n[2 * p + 1]), minus = pack2(-n[2 * p], -n[2 * p + 1]);
+      ac[p] = mul2(wa[p], cc);
+      an[p] = mul2(wa[p], nn);
+      bc[p] = mul2(wb[p], cc);
+      bn[p] = mul2(wb[p], minus);
+    }
+  }
+  const float size = (float)g.dim, part = 1.0f / size;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const uint32_t head = unit.head + i * kTeams + team;
     float x[2 * V];
     raw[i].values<DT>(x);
+    f32x2 a[V / 2], b[V / 2];
+    split<HALVES, V>(x, a, b);
     if (g.layer) {
-      float sum = 0.0f;
+      f32x2 sum = add2(a[0], b[0]);
 #pragma unroll
-      for (uint32_t e = 0; e < 2 * V; ++e) sum += x[e];
-      const float mean = __fdiv_rn(team_sum<T>(sum), size);
+      for (uint32_t p = 1; p < V / 2; ++p) sum = add2(sum, add2(a[p], b[p]));
+      const float mean = __fdiv_rn(team_sum<T>(sum2(sum)), size);
+      const f32x2 less = twice(slot.there ? -mean : 0.0f);
 #pragma unroll
-      for (uint32_t e = 0; e < 2 * V; ++e) x[e] = slot.there ? x[e] - mean : 0.0f;
+      for (uint32_t p = 0; p < V / 2; ++p) {
+        a[p] = add2(a[p], less);
+        b[p] = add2(b[p], less);
+      }
     }
-    float sum = 0.0f;
+    f32x2 sum = mul2(a[0], a[0]);
 #pragma unroll
-    for (uint32_t e = 0; e < 2 * V; ++e) sum = __fmaf_rn(x[e], x[e], sum);
-    const float rstd = 1.0f / sqrtf(__fdiv_rn(team_sum<T>(sum), size) + g.eps);
-    if (!slot.there || head >= s.heads) continue;
-    float y[2 * V];
-#pragma unroll
-    for (uint32_t p = 0; p < V; ++p) {
-      const uint32_t fi = first_of<HALVES, V>(p), se = second_of<HALVES, V>(p);
-      const float za = x[fi] * rstd * w[fi], zb = x[se] * rstd * w[se];
-      y[fi] = __fmaf_rn(za, c[p], -(zb * n[p]));
-      y[se] = __fmaf_rn(zb, c[p], za * n[p]);
+    for (uint32_t p = 0; p < V / 2; ++p) {
+      if (p) sum = fma2(a[p], a[p], sum);
+      sum = fma2(b[p], b[p], sum);
     }
-    uint8_t* o = s.out + ((uint64_t)unit.token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
-    store_vec<DT>(o + slot.a * kEs<DT>, y);
-    store_vec<DT>(o + slot.b * kEs<DT>, y + V);
+    const f32x2 rstd = twice(rsqrtf(__fmaf_rn(team_sum<T>(sum2(sum)), part, g.eps)));
+    f32x2 ya[V / 2], yb[V / 2];
+#pragma unroll
+    for (uint32_t p = 0; p < V / 2; ++p) {
+      const f32x2 sa = mul2(a[p], rstd), sb = mul2(b[p], rstd);
+      ya[p] = fma2(sa, ac[p], mul2(sb, bn[p]));
+      yb[p] = fma2(sb, bc[p], mul2(sa, an[p]));
+    }
+    join<HALVES, V>(ya, yb, x);
+    if (there[i]) {
+      uint8_t* o = s.out + out_at<DT>(s, unit.token, unit.head + i * kTeams + team);
+      store_vec<DT>(o + slot.a * kEs<DT>, x);
+      store_vec<DT>(o + slot.b * kEs<DT>, x + V);
+    }
   }
 }
 
 // Backward.  CTAs are dealt out to queries and keys, and each adds up its rows' part of the weights' gradient: a lane for its slot, then teams, then warps,
-// in a fixed order.
-template <int DT, int T, int U, bool HALVES>
-__global__ void __launch_bounds__(kHeadThreads) heads_backward_kernel(const HeadsArgs g) {
-  constexpr uint32_t V = kV<DT>, kTeams = 32 / T, kSpan = kTeams * U;
+// in a fixed order.  A unit's rows are asked for while the one before it is worked on.  (16384 tokens of 32 + 8 heads of 128 in bf16: 112 us with registers
+// for four CTAs an SM, 127 for three; two rows of a team at once and none ahead 140; a ring in shared memory filled by asynchronous copies 156 to 204: its
+// addresses and second reads cost more than they hid.)
+template <int DT, int T, bool HALVES>
+__global__ void __launch_bounds__(kHeadThreads, 4) heads_backward_kernel(const HeadsArgs g) {
+  constexpr uint32_t V = kV<DT>, kTeams = 32 / T;
   __shared__ float sums[kHeadWarps][T * 2 * V];
   dep_trigger();
   dep_wait();
@@ -266,82 +328,120 @@ __global__ void __launch_bounds__(kHeadThreads) heads_backward_kernel(const Head
   const HeadsSide& s = g.side[which];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, team = lane / T;
   const Slot<DT> slot(lane % T, g.dim, g.rotary, HALVES);
-  const uint32_t spans = (s.heads + kSpan - 1u) / kSpan;
+  const uint32_t spans = (s.heads + kTeams - 1u) / kTeams;
   const uint64_t units = (uint64_t)g.tokens * spans;
-  const float size = (float)g.dim;
-  float w[2 * V] = {}, acc[2 * V] = {};
-  if (slot.there) load_weights<DT>(s.gamma, g, slot.a, slot.b, w);
-  for (uint64_t u = (uint64_t)part * kHeadWarps + warp; u < units; u += (uint64_t)s.parts * kHeadWarps) {
-    const uint32_t token = (uint32_t)(u / spans), head0 = (uint32_t)(u % spans) * kSpan;
-    RawSlot xs[U], ds[U];
+  const float size = (float)g.dim, share = 1.0f / size;
+  f32x2 wa[V / 2], wb[V / 2], sa[V / 2], sb[V / 2];
+  {
+    float w[2 * V] = {};
+    if (slot.there) load_weights<DT>(s.gamma, g, slot.a, slot.b, w);
+    split<HALVES, V>(w, wa, wb);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const uint32_t head = head0 + i * kTeams + team;
-      xs[i].zero();
-      ds[i].zero();
-      if (slot.there && head < s.heads) {
-        xs[i].load<DT>(s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>, slot.a, slot.b);
-        ds[i].load<DT>(s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>, slot.a, slot.b);
+    for (uint32_t p = 0; p < V / 2; ++p) sa[p] = sb[p] = 0ull;
+  }
+  // This warp's units: neighbouring spans, so that a token's position, cosines and sines serve several of them.
+  const uint64_t mine = (uint64_t)part * kHeadWarps + warp, warps = (uint64_t)s.parts * kHeadWarps;
+  const uint64_t first = units / warps * mine + (mine < units % warps ? mine : units % warps), count = units / warps + (mine < units % warps ? 1u : 0u);
+  uint32_t token = (uint32_t)(first / spans), span = (uint32_t)(first % spans);
+  RawSlot nx, ny;
+  auto ask = [&](uint32_t token, uint32_t span) {
+    const uint32_t head = span * kTeams + team;
+    nx.zero();
+    ny.zero();
+    if (slot.there && head < s.heads) {
+      nx.load<DT>(row_of<DT>(s, token, head), slot.a, slot.b);
+      ny.load<DT>(s.dy + out_at<DT>(s, token, head), slot.a, slot.b);
+    }
+  };
+  if (count) ask(token, span);
+  int32_t at = count ? position_of(g, token) : -1, next_at = at;
+  bool fresh = true;
+  f32x2 c[V / 2], n[V / 2], minus[V / 2];
+  for (uint64_t left = count; left; --left) {
+    const RawSlot rx = nx, ry = ny;
+    const uint32_t now = token, head = span * kTeams + team;
+    if (fresh && at >= 0 && slot.there) {
+      float fc[V], fn[V];
+      load_turn<DT>(g, slot, at, fc, fn);
+#pragma unroll
+      for (uint32_t p = 0; p < V / 2; ++p) {
+        c[p] = pack2(fc[2 * p], fc[2 * p + 1]);
+        n[p] = pack2(fn[2 * p], fn[2 * p + 1]);
+        minus[p] = pack2(-fn[2 * p], -fn[2 * p + 1]);
       }
     }
-    const int64_t at = position_of(g, token);
-    if (at < 0) continue;
-    float c[V], n[V];
-    if (slot.there) load_turn<DT>(g, slot, at, c, n);
+    const int32_t here = at;
+    fresh = false;
+    if (++span == spans) {
+      span = 0;
+      ++token;
+      fresh = true;
+    }
+    if (left > 1u) {
+      ask(token, span);
+      if (fresh) next_at = position_of(g, token);
+    }
+    at = next_at;
+    if (here < 0) continue;
+    const bool there = slot.there && head < s.heads;
+    f32x2 xa[V / 2], xb[V / 2], da[V / 2], db[V / 2];
+    {
+      float v[2 * V];
+      rx.values<DT>(v);
+      split<HALVES, V>(v, xa, xb);
+      ry.values<DT>(v);
+      split<HALVES, V>(v, da, db);
+    }
+    if (g.layer) {
+      f32x2 sum = add2(xa[0], xb[0]);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const uint32_t head = head0 + i * kTeams + team;
-      const bool there = slot.there && head < s.heads;
-      float x[2 * V], d[2 * V];
-      xs[i].values<DT>(x);
-      ds[i].values<DT>(d);
-      if (g.layer) {
-        float sum = 0.0f;
+      for (uint32_t p = 1; p < V / 2; ++p) sum = add2(sum, add2(xa[p], xb[p]));
+      const float mean = __fdiv_rn(team_sum<T>(sum2(sum)), size);
+      const f32x2 less = twice(there ? -mean : 0.0f);
 #pragma unroll
-        for (uint32_t e = 0; e < 2 * V; ++e) sum += x[e];
-        const float mean = __fdiv_rn(team_sum<T>(sum), size);
-#pragma unroll
-        for (uint32_t e = 0; e < 2 * V; ++e) x[e] = there ? x[e] - mean : 0.0f;
+      for (uint32_t p = 0; p < V / 2; ++p) {
+        xa[p] = add2(xa[p], less);
+        xb[p] = add2(xb[p], less);
       }
-      // dz in d, then the sums of x^2, g x and g
-      if (there) {
+    }
+    // dz in da and db, then the sums of x^2, g x and g (of a slot that is not there everything is zero)
+    f32x2 xx = 0ull, gx = 0ull, gs = 0ull;
 #pragma unroll
-        for (uint32_t p = 0; p < V; ++p) {
-          const uint32_t fi = first_of<HALVES, V>(p), se = second_of<HALVES, V>(p);
-          const float ya = d[fi], yb = d[se];
-          d[fi] = __fmaf_rn(ya, c[p], yb * n[p]);
-          d[se] = __fmaf_rn(yb, c[p], -(ya * n[p]));
-        }
+    for (uint32_t p = 0; p < V / 2; ++p) {
+      if (slot.there) {
+        const f32x2 ya = da[p], yb = db[p];
+        da[p] = fma2(ya, c[p], mul2(yb, n[p]));
+        db[p] = fma2(yb, c[p], mul2(ya, minus[p]));
       }
-      float xx = 0.0f, gx = 0.0f, gs = 0.0f;
+      const f32x2 ga = mul2(da[p], wa[p]), gb = mul2(db[p], wb[p]);
+      xx = fma2(xb[p], xb[p], fma2(xa[p], xa[p], xx));
+      gx = fma2(gb, xb[p], fma2(ga, xa[p], gx));
+      if (g.layer) gs = add2(gs, add2(ga, gb));
+    }
+    const float sxx = team_sum<T>(sum2(xx)), sgx = team_sum<T>(sum2(gx)), sgs = g.layer ? team_sum<T>(sum2(gs)) : 0.0f;
+    const float rstd = rsqrtf(__fmaf_rn(sxx, share, g.eps));
+    // dx = rstd (g - x rstd mean(g xhat) - mean(g))
+    const f32x2 r = twice(rstd), along = twice(-(sgx * rstd * share) * rstd), level = twice(-(sgs * share));
 #pragma unroll
-      for (uint32_t e = 0; e < 2 * V; ++e) {
-        const float gg = d[e] * w[e];
-        xx = __fmaf_rn(x[e], x[e], xx);
-        gx = __fmaf_rn(gg, x[e], gx);
-        gs += gg;
+    for (uint32_t p = 0; p < V / 2; ++p) {
+      if (there) {  // (a row without elements has no rstd where eps is 0)
+        sa[p] = fma2(da[p], mul2(xa[p], r), sa[p]);
+        sb[p] = fma2(db[p], mul2(xb[p], r), sb[p]);
       }
-      xx = team_sum<T>(xx);
-      gx = team_sum<T>(gx);
-      if (g.layer) gs = team_sum<T>(gs);
-      const float rstd = 1.0f / sqrtf(__fdiv_rn(xx, size) + g.eps);
-      const float along = gx * rstd / size, level = g.layer ? gs / size : 0.0f;  // mean(g xhat), mean(g)
-      if (!there) continue;
-      float dx[2 * V];
-#pragma unroll
-      for (uint32_t e = 0; e < 2 * V; ++e) {
-        const float xhat = x[e] * rstd;
-        acc[e] = __fmaf_rn(d[e], xhat, acc[e]);
-        dx[e] = rstd * (__fmaf_rn(-xhat, along, d[e] * w[e]) - level);
-      }
-      if (s.dx) {
-        uint8_t* o = s.dx + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
-        store_vec<DT>(o + slot.a * kEs<DT>, dx);
-        store_vec<DT>(o + slot.b * kEs<DT>, dx + V);
-      }
+      da[p] = mul2(r, add2(fma2(xa[p], along, mul2(da[p], wa[p])), level));
+      db[p] = mul2(r, add2(fma2(xb[p], along, mul2(db[p], wb[p])), level));
+    }
+    if (there && s.dx) {
+      float v[2 * V];
+      join<HALVES, V>(da, db, v);
+      uint8_t* o = s.dx + ((uint64_t)now * s.token + (uint64_t)head * s.head) * kEs<DT>;
+      store_vec<DT>(o + slot.a * kEs<DT>, v);
+      store_vec<DT>(o + slot.b * kEs<DT>, v + V);
     }
   }
   if (!s.dgamma) return;
+  float acc[2 * V];
+  join<HALVES, V>(sa, sb, acc);
 #pragma unroll
   for (uint32_t e = 0; e < 2 * V; ++e) {
 #pragma unroll
@@ -421,7 +521,7 @@ struct LooseLane {
       b[j] = p[j].two ? b[j] - mean : 0.0f;
     }
   }
-  __device__ __forceinline__ void turns(const HeadsArgs& g, int64_t at, uint32_t lane, float2 (&t)[N]) const {
+  __device__ __forceinline__ void turns(const HeadsArgs& g, int32_t at, uint32_t lane, float2 (&t)[N]) const {
 #pragma unroll
     for (int j = 0; j < N; ++j) t[j] = there[j] && p[j].turned ? g.table[(uint64_t)at * (g.rotary / 2u) + lane + 32u * j] : make_float2(1.0f, 0.0f);
   }
@@ -464,7 +564,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_loose_kernel(const
     const LooseLane<N, HALVES> my(g, s.gamma, lane);
     float a[N], b[N];
     my.template load<DT>(p, a, b);
-    const int64_t at = position_of(g, unit.token);
+    const int32_t at = position_of(g, unit.token);
     if (at < 0) return;
     float2 t[N];
     my.turns(g, at, lane, t);
@@ -480,7 +580,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_loose_kernel(const
       if (my.p[j].two) put_elem<DT>(o, my.p[j].b, __fmaf_rn(zb, t[j].x, za * t[j].y));
     }
   } else {
-    const int64_t at = position_of(g, unit.token);
+    const int32_t at = position_of(g, unit.token);
     if (at < 0) return;
     const float2* turn = g.table + (uint64_t)at * (g.rotary / 2u);
     const float mean = loose_mean<DT>(g, p, lane);
@@ -528,7 +628,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_backward_loose_kernel(cons
       float a[N], b[N], ya[N], yb[N];
       my.template load<DT>(s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>, a, b);
       my.template load<DT>(s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>, ya, yb);
-      const int64_t at = position_of(g, token);
+      const int32_t at = position_of(g, token);
       if (at < 0) continue;
       float2 t[N];
       my.turns(g, at, lane, t);
@@ -571,7 +671,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_backward_loose_kernel(cons
     __syncwarp();
     for (uint64_t u = first; u < units; u += step) {
       const uint32_t token = (uint32_t)(u / s.heads), head = (uint32_t)(u % s.heads);
-      const int64_t at = position_of(g, token);
+      const int32_t at = position_of(g, token);
       if (at < 0) continue;
       const uint8_t* p = s.x + ((uint64_t)token * s.token + (uint64_t)head * s.head) * kEs<DT>;
       const uint8_t* q = s.dy + ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
@@ -631,9 +731,9 @@ __global__ void __launch_bounds__(kHeadThreads) heads_backward_loose_kernel(cons
   }
 }
 
-// The weights' gradients: a warp's lanes have 32 columns, eight warps share the parts, and are added up in their order.
-__global__ void __launch_bounds__(256) heads_columns_kernel(const HeadsArgs g) {
-  __shared__ float sums[8][32];
+// The weights' gradients: a warp's lanes have 32 columns, 32 warps share the parts, and are added up in their order.
+__global__ void __launch_bounds__(1024) heads_columns_kernel(const HeadsArgs g) {
+  __shared__ float sums[32][32];
   dep_trigger();
   dep_wait();
   const uint32_t groups = (g.dim + 31u) / 32u, which = blockIdx.x / groups, col = blockIdx.x % groups * 32u + threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -642,15 +742,15 @@ __global__ void __launch_bounds__(256) heads_columns_kernel(const HeadsArgs g) {
   const float* p = g.work + (which ? (uint64_t)g.side[0].parts * g.dim : 0u) + col;
   float sum = 0.0f;
   if (col < g.dim) {
-#pragma unroll 4
-    for (uint32_t x = warp; x < s.parts; x += 8u) sum += p[(uint64_t)x * g.dim];
+#pragma unroll 8
+    for (uint32_t x = warp; x < s.parts; x += 32u) sum += p[(uint64_t)x * g.dim];
   }
   sums[warp][threadIdx.x % 32] = sum;
   __syncthreads();
   if (warp || col >= g.dim) return;
   sum = 0.0f;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) sum += sums[w][threadIdx.x];
+  for (int w = 0; w < 32; ++w) sum += sums[w][threadIdx.x];
   if (g.wdtype == kF32)
     put_elem<kF32>(s.dgamma, col, sum);
   else
@@ -702,6 +802,13 @@ int loose_by_length(const HeadsArgs& a, L launch) {
   return a.halves ? with(std::true_type()) : with(std::false_type());
 }
 
+// `all` CTAs dealt out to queries and keys by the rows that they have, so that all end together.
+void deal_out(HeadsArgs* a, uint64_t all) {
+  const uint64_t q = a->side[0].heads, k = a->side[1].heads;
+  a->side[0].parts = !q ? 0u : !k ? (uint32_t)all : (uint32_t)std::min<uint64_t>(all - 1, std::max<uint64_t>(1, all * q / (q + k)));
+  a->side[1].parts = !k ? 0u : (uint32_t)(all - a->side[0].parts);
+}
+
 template <int DT, int T, int U, bool HALVES>
 int forward_t(const HeadsArgs& a, cudaStream_t stream) {
   constexpr uint32_t span = 32 / T * U;
@@ -712,11 +819,15 @@ int forward_t(const HeadsArgs& a, cudaStream_t stream) {
 }
 template <int DT, int T>
 int forward_n(const HeadsArgs& a, cudaStream_t stream) {
-  // four rows to a team where that leaves every SM four warps
-  const uint64_t rows = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads);
-  const bool many = rows >= (uint64_t)std::max(1, sm_count()) * 4u * (32u / T * 4u);
-  if (a.halves) return many ? forward_t<DT, T, 4, true>(a, stream) : forward_t<DT, T, 1, true>(a, stream);
-  return many ? forward_t<DT, T, 4, false>(a, stream) : forward_t<DT, T, 1, false>(a, stream);
+  // Four rows to a team where the device then has its warps three times over, two where every SM has four warps, or one.  (4096 tokens of 8 + 8 heads of 128
+  // in bf16: four 13.0 us, two 10.6; 16384 of 32 + 8: 68 and 76.)
+  const uint64_t rows = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads), warps = rows / (32u / T), sms = (uint64_t)std::max(1, sm_count());
+  auto with = [&](auto halves) {
+    if (warps >= sms * 20u * 4u * 3u) return forward_t<DT, T, 4, halves.value>(a, stream);
+    if (warps >= sms * 4u * 2u) return forward_t<DT, T, 2, halves.value>(a, stream);
+    return forward_t<DT, T, 1, halves.value>(a, stream);
+  };
+  return a.halves ? with(std::true_type()) : with(std::false_type());
 }
 template <int DT>
 int forward_d(const HeadsArgs& a, cudaStream_t stream) {
@@ -742,29 +853,25 @@ uint64_t heads_parts_of(const HeadsArgs& a, uint32_t most, uint32_t rows_per_cta
   const uint64_t rows = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads);
   return std::min<uint64_t>(a.dim > 1024u ? 148u : most, std::max<uint64_t>(2, (rows + rows_per_cta - 1) / rows_per_cta));
 }
-// Dealt out to queries and keys by the rows that they have, so that all end together.
-void heads_parts(HeadsArgs* a, uint32_t most, uint32_t rows_per_cta) {
-  const uint64_t q = a->side[0].heads, k = a->side[1].heads, all = heads_parts_of(*a, most, rows_per_cta);
-  a->side[0].parts = !q ? 0u : !k ? (uint32_t)all : (uint32_t)std::min<uint64_t>(all - 1, std::max<uint64_t>(1, all * q / (q + k)));
-  a->side[1].parts = !k ? 0u : (uint32_t)(all - a->side[0].parts);
-}
+void heads_parts(HeadsArgs* a, uint32_t most, uint32_t rows_per_cta) { deal_out(a, heads_parts_of(*a, most, rows_per_cta)); }
 
 template <typename L>
 int backward_launch(const HeadsArgs& a, cudaStream_t stream, L rows) {
   const int rc = rows(a.side[0].parts + a.side[1].parts + (a.status ? 1u : 0u));
   if (rc != FH_OK || (!a.side[0].dgamma && !a.side[1].dgamma)) return rc;
-  return launch_plain<heads_columns_kernel>((a.dim + 31u) / 32u * 2u, 256, 0, 1, stream, a);
+  return launch_plain<heads_columns_kernel>((a.dim + 31u) / 32u * 2u, 1024, 0, 1, stream, a);
 }
-template <int DT, int T, int U, bool HALVES>
+template <int DT, int T, bool HALVES>
 int backward_t(const HeadsArgs& a0, cudaStream_t stream) {
   HeadsArgs a = a0;
-  heads_parts(&a, 148u * 3u, U * kHeadWarps * (32u / T));
-  static_assert(U * kHeadWarps * (32u / T) >= kHeadFewest, "the workspace's size");
-  return backward_launch(a, stream, [&](uint32_t grid) { return launch_plain<heads_backward_kernel<DT, T, U, HALVES>>(grid, kHeadThreads, 0, 1, stream, a); });
+  constexpr uint32_t rows = kHeadWarps * (32u / T);
+  static_assert(rows >= kHeadFewest, "the workspace's size");
+  heads_parts(&a, 148u * 4u, rows);
+  return backward_launch(a, stream, [&](uint32_t grid) { return launch_plain<heads_backward_kernel<DT, T, HALVES>>(grid, kHeadThreads, 0, 1, stream, a); });
 }
 template <int DT, int T>
 int backward_n(const HeadsArgs& a, cudaStream_t stream) {
-  return a.halves ? backward_t<DT, T, 2, true>(a, stream) : backward_t<DT, T, 2, false>(a, stream);
+  return a.halves ? backward_t<DT, T, true>(a, stream) : backward_t<DT, T, false>(a, stream);
 }
 template <int DT>
 int backward_d(const HeadsArgs& a0, cudaStream_t stream) {
