@@ -496,10 +496,10 @@ int fh_layer_norm_backward(const fh_norm_desc* desc, const void* d_dy, const voi
 size_t fh_i8_bytes(int32_t rows, int32_t cols); /* 0 for invalid arguments.  Host-only, no CUDA call. */
 
 /*
- * Compress a matrix: one kernel for each container.
+ * Compress a matrix: one kernel for d_rows; for d_cols one, or where there are many rows three.
  *   d_rows   container of the matrix (a scale for each row: for tokens), 16-byte aligned, rows_capacity bytes; may be NULL
  *   d_cols   container of its transpose (a scale for each column: for channels), cols_capacity bytes; may be NULL, but not both
- * Elements are read twice where a row (column) does not fit the registers of the CTAs that work on it.
+ * Columns are read twice, and rows that do not fit a CTA's registers.
  * FH_ERR_CAPACITY when a container has less than fh_i8_bytes, FH_ERR_ARG when input and containers overlap.
  */
 int fh_i8_compress(const fh_matrix* matrix, const void* d_src, void* d_rows, size_t rows_capacity, void* d_cols, size_t cols_capacity, void* stream);

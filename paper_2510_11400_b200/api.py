@@ -623,10 +623,16 @@ def _sides(d: fh_heads_desc, dev: int, q, k, q_out, k_out):
 
 def _turn(d: fh_heads_desc, table, at, dev: int):
     """The addresses of the table and the positions."""
-    if at is not None and (at.dtype.is_floating_point or at.element_size() != 4):
-        raise ValueError(f"positions of {at.dtype}, where int32 is wanted")
     n, tokens = d.positions * d.rotary, d.tokens
-    return _dense(table, dev, 1, n, n, FH_F32), _ptr(at, dev, tokens, 4, (1, tokens, tokens))
+    place = None
+    if at is not None:
+        if _torch is not None and at.dtype is _torch.int32 and at.get_device() == dev and at.is_contiguous() and at.numel() >= tokens:
+            place = at.data_ptr()
+        else:
+            if at.dtype.is_floating_point or at.element_size() != 4:
+                raise ValueError(f"positions of {at.dtype}, where int32 is wanted")
+            place = _ptr(at, dev, tokens, 4, (1, tokens, tokens))
+    return _dense(table, dev, 1, n, n, FH_F32), place
 
 
 def fh_head_norm(d: fh_heads_desc, q, k, gamma_q, gamma_k, table, positions, q_out, k_out, status=None, stream=None) -> int:

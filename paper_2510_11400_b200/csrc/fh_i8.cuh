@@ -79,7 +79,7 @@ constexpr float kI8Magic23 = 12582912.0f;  // 1.5 * 2^23
 // least 1 / (2 M 2^(q - p)), which is fifty times what t may be off by (127 * 255 / (M 2^(q - p)) times 2^-21).  Nothing: 127 divides M, which then
 // is 254, so that s is a power of two and everything is exact; or it divides 2 k + 1, which then is 127: x is half of the magnitude.  So inv is moved
 // by a last place where half the magnitude would come out on the wrong side, and no element is looked at again.  (Half of the magnitude is no rare
-// value: looking again at 16 elements where one of them is near a middle made 8192 x 4096 take 60 us instead of @@.)
+// value: looking again at 16 elements where one of them is near a middle made 8192 x 4096 by rows take 60 us instead of 29.)
 template <int DT>
 struct I8Coder {
   float inv, s, edge;

@@ -304,26 +304,25 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
   if (warp == 5) tmem_free(tmem, S::kCols);
 }
 
-// More rows of A: a pair of CTAs on a tile of 256 columns of C, 128 rows of B (and of U) in the shared memory of each, and half of the tile's rows of A.
-// Pairs take tiles one after the other, and accumulators alternate between two halves of tensor memory, so that the next tile's matrix instructions run
-// while the eight warps for the result write this one's.  With a split, a cluster's pairs share one tile.
+// More rows of A: a pair of CTAs on a tile of 256 columns of C, 128 rows of B (and of U) and 128 of the tile's 256 rows of A in the shared memory of each.
+// Pairs take tiles one after the other.  The eight warps for the result take the accumulators into registers, 128 columns at a time, before they write: the
+// word that tensor memory is free would wait for what the thread has stored.  A product's accumulators alternate between the halves of tensor memory, so that
+// the next tile's matrix instructions run meanwhile; two weights' take all of it.  (With 128 rows of A to a tile they alternated too, but a stage then moved
+// 80 bytes a clock from L2 to an SM instead of 48: 4096 x 8192 x 4096 253 us and 194.)  With a split, a cluster's pairs share one tile.
 constexpr int kI8PairThreads = 320;  // eight warps for the result, then one each for loads and matrix instructions
 
-#ifndef GATED_Q
-#define GATED_Q 256
-#endif
 template <bool GATED>
 struct I8PairShape {
   static constexpr int kW = GATED ? 2 : 1;
-  static constexpr uint32_t kQ = GATED ? GATED_Q : 256;  // rows of A to a tile
+  static constexpr uint32_t kQ = 256;                              // rows of A to a tile
   static constexpr uint32_t kSums = kW * kQ, kBufs = 512 / kSums;  // columns of tensor memory that a tile takes, tiles that have room
-  static constexpr uint32_t kP = 128 * kI8Step, kA = kQ / 2 * kI8Step;
-  static constexpr uint32_t kStage = kW * kP + kA;
+  static constexpr uint32_t kP = 128 * kI8Step;
+  static constexpr uint32_t kStage = (kW + 1) * kP;
   static constexpr int kStages = 200 * 1024 / kStage;
   static constexpr uint32_t kTail = 256 + 2 * kQ * 4;
   static constexpr size_t kSmem = 128 + (size_t)kStages * kStage + kTail;
-  static constexpr uint32_t kMostSplit = kStages * kStage >= kW * (kQ + 8) * 512 ? 4 : 1;  // (partial sums, and rows read behind them, lie in the stages)
-  static_assert(kSmem <= kMxSmemLimit, "room");
+  static constexpr uint32_t kMostSplit = GATED ? 1 : 4;  // (two weights' partial sums do not fit the stages)
+  static_assert(kSmem <= kMxSmemLimit && (GATED || kStages * kStage >= (kQ + 8) * 512), "room; partial sums, and rows read behind them");
   // the barriers behind the stages
   static constexpr int kEmpty = kStages;          // a stage may be loaded again
   static constexpr int kDone = 2 * kStages;       // an accumulator is complete (one for each of the two)
@@ -342,16 +341,14 @@ struct I8PairArgs {
   I8ProductArgs g;
 };
 
-// Where a CTA's rows of an operand are: a block of 128 rows, or `high` groups of eight from group `y` on.  A block that the matrix does not have is
-// behind the end of the map: its copies bring zeros.
+// Where a block of 128 rows of an operand is.  One that the matrix does not have is behind the end of the map: its copies bring zeros.
 struct I8Source {
   const CUtensorMap* map;
-  uint32_t y, z;
-  __device__ __forceinline__ I8Source(const I8Maps& m, const I8Layout& l, uint32_t block, uint32_t group) {
+  uint32_t z;
+  __device__ __forceinline__ I8Source(const I8Maps& m, const I8Layout& l, uint32_t block) {
     const uint32_t whole = l.r8 / 128u, c = l.chunks();
     const bool rest = whole == 0u || (block == whole && l.r8 % 128u != 0u);
     map = rest ? &m.rest : &m.codes;
-    y = group;
     z = rest ? (block == whole ? 0u : c) : min(block, whole) * c;
   }
 };
@@ -411,8 +408,8 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
       Turn<S::kStages> turn;
       for (uint32_t tile = pair; tile < tiles && good; tile += pairs) {
         const PairTile where(tile, g.tiles_m, g.tiles_n);
-        const I8Source p(pa.b, lp, where.n * 2u + half, 0u), u(pa.up, lp, where.n * 2u + half, 0u);
-        const I8Source q(pa.a, lq, S::kQ == 128u ? where.m : where.m * 2u + half, S::kQ == 128u ? half * 8u : 0u);
+        const I8Source p(pa.b, lp, where.n * 2u + half), u(pa.up, lp, where.n * 2u + half);
+        const I8Source q(pa.a, lq, where.m * 2u + half);
         for (uint32_t it = first; it < last; ++it, ++loaded, turn.next()) {
           if (loaded == silent) {
             good = false;
@@ -425,9 +422,9 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
           }
           const uint32_t st = smem_u32(smem) + turn.stage * S::kStage, bar = at_rank(full + turn.stage, even), z = it * kI8Chunks;
           if (half == 0u) mbar_expect_tx(full + turn.stage, 2u * S::kStage);
-          tma_pair_3d(st, p.map, 0u, p.y, p.z + z, bar);
-          if (GATED) tma_pair_3d(st + S::kP, u.map, 0u, u.y, u.z + z, bar);
-          tma_pair_3d(st + S::kW * S::kP, q.map, 0u, q.y, q.z + z, bar);
+          tma_pair_3d(st, p.map, 0u, 0u, p.z + z, bar);
+          if (GATED) tma_pair_3d(st + S::kP, u.map, 0u, 0u, u.z + z, bar);
+          tma_pair_3d(st + S::kW * S::kP, q.map, 0u, 0u, q.z + z, bar);
         }
       }
       *loads = loaded;
@@ -454,12 +451,12 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
           tc_fence_after();
           const uint32_t nc = min((uint32_t)kI8Chunks, chunks - it * kI8Chunks);
           const uint32_t st = smem_u32(smem) + s * S::kStage;
-          const uint64_t dp = smem_desc(st, 2048u, 128u), du = smem_desc(st + S::kP, 2048u, 128u), dq = smem_desc(st + S::kW * S::kP, S::kQ / 2u * 16u, 128u);
+          const uint64_t dp = smem_desc(st, 2048u, 128u), du = smem_desc(st + S::kP, 2048u, 128u), dq = smem_desc(st + S::kW * S::kP, 2048u, 128u);
 #pragma unroll
           for (uint32_t x = 0; x < kI8Chunks / 2u; ++x)
             if (2u * x < nc) {
-              tc_mma_i8<true>(acc, dp + 256u * x, dq + S::kQ * x, i8_idesc(256u, S::kQ), it > first || x > 0u);
-              if (GATED) tc_mma_i8<true>(acc + S::kQ, du + 256u * x, dq + S::kQ * x, i8_idesc(256u, S::kQ), it > first || x > 0u);
+              tc_mma_i8<true>(acc, dp + 256u * x, dq + 256u * x, i8_idesc(256u, S::kQ), it > first || x > 0u);
+              if (GATED) tc_mma_i8<true>(acc + S::kQ, du + 256u * x, dq + 256u * x, i8_idesc(256u, S::kQ), it > first || x > 0u);
             }
           if (it + (uint32_t)S::kStages < last || tile + pairs < tiles) tc_commit_pair(empty + s, both);
         }
@@ -502,7 +499,7 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
       }
       tc_fence_after();
       const uint32_t at = tmem + buf * S::kSums + (warp % 4u * 32u << 16) + side;
-      if (wide && g.split == 1u) {
+      if (wide && (GATED || g.split == 1u)) {
 #pragma unroll 1
         for (uint32_t q = 0; q < kSide; ++q) {
           const uint32_t v = tc_load1(at + q), w = GATED ? tc_load1(at + S::kQ + q) : 0u;
@@ -528,7 +525,7 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
           __syncwarp();
           if (lane == 0) mbar_arrive_at(taken + buf, even);
         }
-        if (g.split == 1u) {
+        if (GATED || g.split == 1u) {
 #pragma unroll
           for (uint32_t x = 0; x < kRun / 16u; ++x) {
             const uint32_t q = side + run + 16u * x;
@@ -539,25 +536,22 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
 #pragma unroll
           for (uint32_t x = 0; x < kRun / 16u; ++x)
 #pragma unroll
-            for (uint32_t y = 0; y < 16u; ++y) {
-              part[(16u * x + y) * 128u] = v[x][y];
-              if (GATED) part[(S::kQ + 16u * x + y) * 128u] = w[x][y];
-            }
+            for (uint32_t y = 0; y < 16u; ++y) part[(16u * x + y) * 128u] = v[x][y];
         }
       }
     }
   }
   __syncwarp();
   tc_fence_before();
-  if (g.split > 1u) {
+  if (!GATED && g.split > 1u) {
     cluster_sync();
     if (warp < 8u && tiles && !*abort) {
       const PairTile where(pair, g.tiles_m, g.tiles_n);
       const uint32_t p = warp % 4u * 32u + lane, col = where.n * 256u + half * 128u + p, row0 = where.m * S::kQ;
       const uint32_t rows = min(S::kQ, g.m - row0), from = rows * rank / g.split, end = rows * (rank + 1u) / g.split, mid = (from + end) / 2u;
       const uint32_t stop = warp < 4u ? mid : end;
-      const I8Factors by = {factors, g.a + lq.magnitude_at(row0), g.alpha, i8_scale_at(g.b, lp, col), GATED ? i8_scale_at(g.up, lp, col) : 0.0f};
-      bool wide = !i8_plain(by.col) || !i8_plain(by.up);
+      const I8Factors by = {factors, g.a + lq.magnitude_at(row0), g.alpha, i8_scale_at(g.b, lp, col), 0.0f};
+      bool wide = !i8_plain(by.col);
       for (uint32_t q = lane; q < rows; q += 32u) wide = wide || factors[q] != factors[q];
       wide = __any_sync(0xFFFFFFFFu, wide);
       const uint32_t step = wide ? 1u : 8u;
@@ -565,7 +559,6 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
       for (uint32_t q = warp < 4u ? from : mid; q < stop; q += step) {
         uint32_t v[8], w[8] = {};
         add_parts<8>(smem_u32(reinterpret_cast<uint32_t*>(smem) + q * 128u + p), half, 2u, g.split, v);
-        if (GATED) add_parts<8>(smem_u32(reinterpret_cast<uint32_t*>(smem) + (S::kQ + q) * 128u + p), half, 2u, g.split, w);
         if (wide)
           i8_put_wide<DT, ACT>(g, by, v[0], w[0], row0, q, col);
         else
@@ -604,10 +597,10 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
   if (warp == 9) tmem_free_pair(tmem, 512u);
 }
 
-bool encode_i8(I8Maps* m, const uint8_t* c, uint32_t rows, uint32_t k, uint32_t groups) {
+bool encode_i8(I8Maps* m, const uint8_t* c, uint32_t rows, uint32_t k) {
   const I8Layout l(rows, k);
   const uint32_t whole = l.r8 / 128u, rest = l.r8 % 128u, chunks = l.chunks();
-  const cuuint32_t box[3] = {128, groups, (cuuint32_t)kI8Chunks};
+  const cuuint32_t box[3] = {128, 16, (cuuint32_t)kI8Chunks};
   // (coordinates are signed 32-bit numbers, one tile's steps behind the end included)
   if ((uint64_t)(whole + 2u) * chunks + kI8Chunks > 0x7FFFFFFFull) return false;
   bool ok = true;
@@ -623,7 +616,7 @@ int launch_i8_pair(const I8ProductArgs& a, cudaStream_t stream) {
   p.g = a;
   p.g.tiles_m = (uint32_t)(((uint64_t)a.m + S::kQ - 1u) / S::kQ);
   p.g.tiles_n = (a.n + 255u) / 256u;
-  if (!encode_i8(&p.a, a.a, a.m, a.k, S::kQ / 16u) || !encode_i8(&p.b, a.b, a.n, a.k, 16u) || (ACT >= 0 && !encode_i8(&p.up, a.up, a.n, a.k, 16u)))
+  if (!encode_i8(&p.a, a.a, a.m, a.k) || !encode_i8(&p.b, a.b, a.n, a.k) || (ACT >= 0 && !encode_i8(&p.up, a.up, a.n, a.k)))
     return FH_ERR_UNSUPPORTED;
   const uint64_t tiles = (uint64_t)p.g.tiles_m * p.g.tiles_n;
   auto at_once = [](uint32_t s) { return clusters_at_once<i8_pair_kernel<DT, ACT>>((int)(2 * s), kI8PairThreads, S::kSmem); };

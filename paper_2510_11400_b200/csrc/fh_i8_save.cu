@@ -112,10 +112,11 @@ int rows_by_group(const I8SaveArgs& a, cudaStream_t stream) {
 // ---- by columns ------------------------------------------------------------------------------------
 // The container of the transpose: its rows are the matrix's columns, its chunks 16 of the matrix's rows.  A lane has C neighbouring columns and 16 rows at
 // a time, whose codes are C times 16 bytes side by side in the container, 32 C columns to a warp: both sides are in whole sectors without a detour through
-// shared memory.  A cluster's CTAs share the rows of a group of columns, put their maxima together and then read their rows again, from L2 as a
-// rule.
+// shared memory.  The scales need whole columns first.
+//  Matrices of few rows: one kernel, a cluster's CTAs share the rows of a group of columns, put their maxima together and read their rows again.
+//  Others: the maxima by a kernel of their own, bands of rows side by side, which leaves them in the container (a maximum does not depend on the order), then
+//  the codes.  (In clusters 8192 x 4096 bf16 took 40 us, 34 in two passes; 65536 x 256, with eight CTAs to a group of columns, 122 and 24.)
 constexpr int kColWarps = 8;
-
 template <int DT, int C, bool VEC>
 struct ColChunk {
   static constexpr int kWords = C * (int)kEs<DT> / 4 ? C * (int)kEs<DT> / 4 : 1;
@@ -171,17 +172,19 @@ __global__ void __launch_bounds__(kColWarps * 32) i8_cols_kernel(const I8SaveArg
   dep_trigger();
   dep_wait();
   if (blockIdx.x == 0 && tid < 32) i8_write_header(g.dst, l, tid);
-  ColChunk<DT, C, VEC> x;
-  uint32_t top[C] = {};
+  using Chunk = ColChunk<DT, C, VEC>;
+  Chunk x;
+  uint32_t top[Chunk::kWords] = {};  // (in bf16 two columns' maxima side by side)
   for (uint32_t j = first; j < last; j += kColWarps) {
     x.load(g, j, col, n);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
 #pragma unroll
-      for (int c = 0; c < C; ++c) top[c] = max(top[c], __float_as_uint(x.at(i, c)) & 0x7FFFFFFFu);
+      for (int w = 0; w < Chunk::kWords; ++w)
+        top[w] = DT == kF32 ? max(top[w], x.w[i][w] & 0x7FFFFFFFu) : __vmaxu2(top[w], x.w[i][w] & 0x7FFF7FFFu);
   }
 #pragma unroll
-  for (int c = 0; c < C; ++c) tops[warp][lane * C + c] = top[c];
+  for (int c = 0; c < C; ++c) tops[warp][lane * C + c] = DT == kF32 ? top[c] : c % 2 ? top[c / 2] & 0x7FFF0000u : top[c / 2] << 16;
   __syncthreads();
   if (tid < kCols) {
     uint32_t t = 0;
@@ -220,15 +223,132 @@ __global__ void __launch_bounds__(kColWarps * 32) i8_cols_kernel(const I8SaveArg
   }
 }
 
+// The container's header, and zeros where the maxima are gathered.
+__global__ void __launch_bounds__(kI8Threads) i8_cols_start_kernel(const I8SaveArgs g) {
+  const I8Layout l(g.cols, g.rows);
+  dep_trigger();
+  dep_wait();
+  if (blockIdx.x == 0 && threadIdx.x < 32) i8_write_header(g.dst, l, threadIdx.x);
+  uint32_t* top = reinterpret_cast<uint32_t*>(g.dst + l.magnitude_at(0));
+  for (uint64_t i = (uint64_t)blockIdx.x * kI8Threads + threadIdx.x; i < l.r8; i += (uint64_t)gridDim.x * kI8Threads) top[i] = 0u;
+}
+
+// A CTA takes 256 columns of a band of rows: a lane eight columns (VEC: side by side, in 16-byte vectors), a warp every eighth row.
+constexpr uint32_t kBand = 64;
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kI8Threads) i8_cols_max_kernel(const I8SaveArgs g) {
+  __shared__ uint32_t tops[kI8Threads / 32][256];
+  const I8Layout l(g.cols, g.rows);
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, groups = (g.cols + 255u) / 256u, c0 = blockIdx.x % groups * 256u;
+  const uint32_t r0 = blockIdx.x / groups * kBand, end = min(g.rows, r0 + kBand);
+  uint32_t top[8] = {};
+  dep_trigger();
+  dep_wait();
+  const uint8_t* p = g.src + ((uint64_t)r0 * g.ld + c0) * kEs<DT>;
+  if (VEC) {
+    const uint32_t n = c0 + lane * 8u < g.cols ? min(8u, g.cols - c0 - lane * 8u) : 0u;
+    constexpr int kWords = DT == kF32 ? 8 : 4;
+    uint32_t m[kWords] = {};
+#pragma unroll 4
+    for (uint32_t r = r0 + warp; r < end; r += kI8Threads / 32) {
+      const uint8_t* q = p + ((uint64_t)(r - r0) * g.ld + lane * 8u) * kEs<DT>;
+      uint32_t w[kWords] = {};
+      if (n == 8u) {
+#pragma unroll
+        for (int x = 0; x < kWords; x += 4) {
+          const uint4 v = reinterpret_cast<const uint4*>(q)[x / 4];
+          w[x] = v.x;
+          w[x + 1] = v.y;
+          w[x + 2] = v.z;
+          w[x + 3] = v.w;
+        }
+      } else {
+#pragma unroll
+        for (uint32_t x = 0; x < 8u; ++x)
+          if (x < n) {
+            if (DT == kF32)
+              w[x] = reinterpret_cast<const uint32_t*>(q)[x];
+            else
+              w[x / 2u] |= (uint32_t) reinterpret_cast<const uint16_t*>(q)[x] << (x % 2u * 16u);
+          }
+      }
+#pragma unroll
+      for (int x = 0; x < kWords; ++x) m[x] = DT == kF32 ? max(m[x], w[x] & 0x7FFFFFFFu) : __vmaxu2(m[x], w[x] & 0x7FFF7FFFu);
+    }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) top[x] = DT == kF32 ? m[x % kWords] : x % 2 ? m[x / 2 % kWords] & 0x7FFF0000u : m[x / 2 % kWords] << 16;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) tops[warp][lane * 8 + x] = top[x];
+  } else {
+#pragma unroll 2
+    for (uint32_t r = r0 + warp; r < end; r += kI8Threads / 32) {
+      const uint8_t* q = p + (uint64_t)(r - r0) * g.ld * kEs<DT>;
+#pragma unroll
+      for (uint32_t x = 0; x < 8u; ++x) {
+        const uint32_t c = x * 32u + lane;
+        if (c0 + c < g.cols)
+          top[x] = max(top[x], DT == kF32 ? reinterpret_cast<const uint32_t*>(q)[c] & 0x7FFFFFFFu : (uint32_t)(reinterpret_cast<const uint16_t*>(q)[c] & 0x7FFFu) << 16);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) tops[warp][x * 32 + lane] = top[x];
+  }
+  __syncthreads();
+  uint32_t t = 0;
+#pragma unroll
+  for (int w = 0; w < kI8Threads / 32; ++w) t = max(t, tops[w][threadIdx.x]);
+  if (c0 + threadIdx.x < g.cols && t) atomicMax(reinterpret_cast<uint32_t*>(g.dst + l.magnitude_at(c0 + threadIdx.x)), i8_magnitude_bits(t));
+}
+
+// A warp takes a chunk of 32 C columns.  (Several, each asked for while the one before it is worked on: 8192 x 4096 bf16 34 -> 35 us with two, 47 with four.  Panels
+// of columns that stay in L2 from one pass to the other, 16384 x 8192 with 48 MB to a panel: 121 -> 159.)
+template <int DT, int C, bool VEC>
+__global__ void __launch_bounds__(kI8Threads) i8_cols_codes_kernel(const I8SaveArgs g) {
+  const I8Layout l(g.cols, g.rows);
+  const uint32_t lane = threadIdx.x % 32, groups = (l.r8 + 32u * C - 1u) / (32u * C);
+  const uint32_t col = blockIdx.x % groups * 32u * C + lane * C, j = blockIdx.x / groups * (kI8Threads / 32) + threadIdx.x / 32;
+  const int n = col < g.cols ? (int)min((uint32_t)C, g.cols - col) : 0;
+  dep_trigger();
+  dep_wait();
+  if (j >= l.chunks() || col >= l.r8) return;
+  ColChunk<DT, C, VEC> x;
+  x.load(g, j, col, n);
+  uint8_t* dst = g.dst + l.code_at(col, j);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    if (col + c >= l.r8) break;
+    const I8Coder<DT> coder(*reinterpret_cast<const uint32_t*>(g.dst + l.magnitude_at(col + c)));
+    float f[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] = x.at(i, c);
+    *reinterpret_cast<uint4*>(dst + c * 16u) = i8_codes16(f, coder);
+  }
+}
+
 template <int DT, int C, bool VEC>
 int cols_launch(const I8SaveArgs& a0, cudaStream_t stream) {
   I8SaveArgs a = a0;
-  const uint32_t chunks = I8Layout(a.cols, a.rows).chunks();
+  const I8Layout l(a.cols, a.rows);
+  const uint32_t chunks = l.chunks();
   const uint64_t groups = ((uint64_t)a.cols + 32u * C - 1u) / (32u * C);
   a.parts = 1u;
   while (a.parts < 8u && chunks >= 2u * kColWarps * a.parts) a.parts *= 2u;
-  if (groups * a.parts > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
-  return launch_plain<i8_cols_kernel<DT, C, VEC>>((uint32_t)(groups * a.parts), kColWarps * 32, 0, (int)a.parts, stream, a);
+  // (the cluster kernel where a CTA has few rows: 1024 x 4096 bf16 8 us; or not many and the device several CTAs an SM: 4096 x 16384 59 us, in two passes 65)
+  if (a.rows <= 1024u || (a.rows <= 4096u && groups * a.parts >= 8ull * std::max(1, sm_count()))) {
+    if (groups * a.parts > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
+    return launch_plain<i8_cols_kernel<DT, C, VEC>>((uint32_t)(groups * a.parts), kColWarps * 32, 0, (int)a.parts, stream, a);
+  }
+  const uint64_t max_ctas = ((uint64_t)a.cols + 255u) / 256u * (((uint64_t)a.rows + kBand - 1u) / kBand);
+  const uint64_t code_ctas = (l.r8 + 32ull * C - 1u) / (32u * C) * ((chunks + kI8Threads / 32 - 1ull) / (kI8Threads / 32));
+  if (max_ctas > 0x7FFFFFFFull || code_ctas > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
+  int rc = launch_plain<i8_cols_start_kernel>((uint32_t)std::min<uint64_t>((l.r8 + kI8Threads - 1ull) / kI8Threads, 148u), kI8Threads, 0, 1, stream, a);
+  if (rc != FH_OK) return rc;
+  if (((uintptr_t)a.src | a.ld * kEs<DT>) % 16u == 0u)
+    rc = launch_plain<i8_cols_max_kernel<DT, true>>((uint32_t)max_ctas, kI8Threads, 0, 1, stream, a);
+  else
+    rc = launch_plain<i8_cols_max_kernel<DT, false>>((uint32_t)max_ctas, kI8Threads, 0, 1, stream, a);
+  if (rc != FH_OK) return rc;
+  return launch_plain<i8_cols_codes_kernel<DT, C, VEC>>((uint32_t)code_ctas, kI8Threads, 0, 1, stream, a);
 }
 
 // ---- and back --------------------------------------------------------------------------------------
