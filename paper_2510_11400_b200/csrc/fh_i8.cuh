@@ -91,8 +91,9 @@ struct I8Coder {
     inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
     edge = s > 0.0f ? s * 0.49997f : __uint_as_float(0x7F800000u);
     if (DT == kBF16 && s > 1.17549435e-38f) {  // (the smallest scale is a power of two)
-      const float half = 0.5f * __uint_as_float(bits);
-      const bool up = __fmaf_rn(-63.5f, s, half) >= 0.0f, got = __fmaf_rn(half, inv, -63.5f) >= 0.0f;
+      // (127 s, not 63.5: what is left over of the smallest scales would be half of the smallest number)
+      const float a = __uint_as_float(bits);
+      const bool up = __fmaf_rn(-127.0f, s, a) >= 0.0f, got = __fmaf_rn(0.5f * a, inv, -63.5f) >= 0.0f;
       if (up != got) inv = __uint_as_float(__float_as_uint(inv) + (up ? 1u : ~0u));
     }
   }

@@ -62,8 +62,8 @@ def cuda(x, dtype=None):
 
 
 def sums_slack(dim):
-    """Relative error of a sum of `dim` numbers of one sign, and of what rstd is made of it: chains of at most dim / 32 + 16 additions to a lane, five
-    across lanes, division, addition, root and reciprocal."""
+    """Relative error of a sum of `dim` numbers of one sign, and of what rstd is made of it, which halves it: chains of at most dim / 32 + 16 additions to a lane,
+    five across lanes, one for the division, one for the addition, four for a reciprocal root within two places."""
     return (dim / 32 + 32) * U
 
 
