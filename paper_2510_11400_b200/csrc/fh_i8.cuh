@@ -52,7 +52,7 @@ __device__ __forceinline__ void i8_write_header(uint8_t* dst, const I8Layout& l,
   if (i == 7u) w = (uint32_t)(l.total >> 32);
   reinterpret_cast<uint32_t*>(dst)[i] = w;
 }
-// Whether a container is the one expected.
+// Whether a container is the one expected.  (That it is large enough the host knows too: then the header is there to be read, and what the layout has.)
 __device__ __forceinline__ bool i8_header_ok(const uint8_t* src, uint64_t src_bytes, const I8Layout& l) {
   if (src_bytes < l.total) return false;  // (so that the header is there to be read)
   const uint4 a = *reinterpret_cast<const uint4*>(src), b = *reinterpret_cast<const uint4*>(src + 16);

@@ -165,13 +165,13 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
   const uint32_t tmem = *tmem_at;
   dep_trigger();  // (behind the allocation: no later kernel takes tensor memory that this one still wants)
   dep_wait();
-  const bool ok_a = i8_header_ok(g.a, g.a_bytes, lq), ok_b = i8_header_ok(g.b, g.b_bytes, lp), ok_u = !GATED || i8_header_ok(g.up, g.up_bytes, lp);
-  const bool ok = ok_a && ok_b && ok_u;
-  if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
+  // Containers that are large enough are multiplied, whatever their headers say, and the result is written when those are right: waiting for them first is a
+  // latency that a single token's product would see.
+  const bool sized = g.a_bytes >= lq.total && g.b_bytes >= lp.total && (!GATED || g.up_bytes >= lp.total);
   const uint32_t chunks = lp.chunks(), steps = (chunks + kI8Chunks - 1u) / kI8Chunks;
   const uint32_t first = (uint32_t)((uint64_t)steps * rank / g.split), last = (uint32_t)((uint64_t)steps * (rank + 1u) / g.split);
   const uint32_t rp = lp.block_rows(tp), rq = lq.block_rows(tq);
-  if (ok && warp == 4) {
+  if (sized && warp == 4) {
     if (lane == 0) {
       const uint64_t at = lp.code_at(tp * 128u, 0);
       const uint8_t* q = g.a + lq.code_at(tq * 128u, 0);
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
       }
       *loads = loaded;
     }
-  } else if (ok && warp == 5) {
+  } else if (sized && warp == 5) {
     if (lane == 0) {
       Turn<S::kStages> turn;
       for (uint32_t it = first; it < last; ++it, turn.next()) {
@@ -219,10 +219,15 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
   }
   __syncwarp();
   // the accumulator: lane i of warp w has row 32 w + i of the tile of B, QT columns for the rows of A
-  const bool mine = ok && warp < 4;
+  const bool mine = sized && warp < 4;
   const uint32_t col = tp * 128u + warp * 32u + lane, rows = min((uint32_t)QT, g.m - tq * 128u);
   I8Factors by = {factors, g.a + lq.magnitude_at(tq * 128u), g.alpha, 0.0f, 0.0f};
-  bool good = mine, wide = false;
+  bool good = mine, wide = false, ok = false;
+  if (warp < 4) {
+    const bool ok_a = i8_header_ok(g.a, g.a_bytes, lq), ok_b = i8_header_ok(g.b, g.b_bytes, lp), ok_u = !GATED || i8_header_ok(g.up, g.up_bytes, lp);
+    ok = ok_a && ok_b && ok_u;
+    if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
+  }
   if (mine) {
     by.col = i8_scale_at(g.b, lp, col);
     if (GATED) by.up = i8_scale_at(g.up, lp, col);
@@ -240,7 +245,7 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
   constexpr int NR = 16;
   const uint32_t at = tmem + (warp * 32u << 16);
   if (g.split == 1u) {
-    if (good && !wide) {
+    if (good && ok && !wide) {
 #pragma unroll 1
       for (uint32_t q = 0; q < rows; q += NR) {
         uint32_t v[NR], w[NR] = {};
@@ -249,7 +254,7 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
         tc_load_wait();
         i8_put_sums<DT, NR, ACT>(g, by, v, w, tq * 128u, g.m, q, col);
       }
-    } else if (good) {
+    } else if (good && ok) {
 #pragma unroll 1
       for (uint32_t q = 0; q < rows; ++q) {
         const uint32_t v = tc_load1(at + q), w = GATED ? tc_load1(at + QT + q) : 0u;
@@ -272,7 +277,7 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
       }
     }
     cluster_sync();
-    if (good) {
+    if (good && ok) {
       const uint32_t end = rows * (rank + 1u) / g.split;
       constexpr int N = QT < 32 ? 2 : 8;
       const uint32_t step = wide ? 1u : N;
@@ -292,9 +297,9 @@ __global__ void __launch_bounds__(kI8Threads) i8_product_kernel(const I8ProductA
   tc_fence_before();
   __syncthreads();
   if (*abort) {  // (see "Waits" in fh_product.cuh)
-    if (ok && lane == 0 && warp == 4)
+    if (sized && lane == 0 && warp == 4)
       for (uint32_t n = *loads, w = n > (uint32_t)S::kStages ? n - S::kStages : 0u; w < n; ++w) mbar_wait(full + w % S::kStages, w / S::kStages & 1u, kDrainPolls);
-    if (ok && lane == 0 && warp == 5) {
+    if (sized && lane == 0 && warp == 5) {
       tc_commit(idle);
       mbar_wait(idle, 0u, kDrainPolls);
     }
