@@ -399,13 +399,11 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
   const uint32_t tmem = *tmem_at;
   dep_trigger();  // (behind the allocation: no later kernel takes tensor memory that this one still wants)
   dep_wait();
-  const bool ok_a = i8_header_ok(g.a, g.a_bytes, lq), ok_b = i8_header_ok(g.b, g.b_bytes, lp), ok_u = !GATED || i8_header_ok(g.up, g.up_bytes, lp);
-  const bool ok = ok_a && ok_b && ok_u;
-  if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
+  const bool sized = g.a_bytes >= lq.total && g.b_bytes >= lp.total && (!GATED || g.up_bytes >= lp.total);  // (as in the kernel for few rows)
   const uint32_t chunks = lp.chunks(), steps = (chunks + kI8Chunks - 1u) / kI8Chunks;
   const uint32_t first = (uint32_t)((uint64_t)steps * rank / g.split), last = (uint32_t)((uint64_t)steps * (rank + 1u) / g.split);
-  const uint32_t tiles = ok ? g.tiles_m * g.tiles_n : 0u;
-  bool good = true;
+  const uint32_t tiles = sized ? g.tiles_m * g.tiles_n : 0u;
+  bool good = true, ok = false;
   if (warp == 8) {
     if (lane == 0) {
       uint32_t loaded = 0;
@@ -471,6 +469,9 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
   } else {
     constexpr uint32_t kSide = S::kQ / 2u, kRun = 128u / S::kW;  // columns of an accumulator to each four warps: rows of A; those of them in registers at once
     const uint32_t side = warp / 4u * kSide;
+    const bool ok_a = i8_header_ok(g.a, g.a_bytes, lq), ok_b = i8_header_ok(g.b, g.b_bytes, lp), ok_u = !GATED || i8_header_ok(g.up, g.up_bytes, lp);
+    ok = ok_a && ok_b && ok_u;
+    if (blockIdx.x == 0 && tid == 0 && g.status) *g.status = ok ? 0ull : status_word(kErrCorrupt);
     // The magnitudes of a tile are asked for a tile ahead.
     float next_col = 0.0f, next_up = 0.0f, next_row = 0.0f;
     auto ask = [&](uint32_t tile) {
@@ -509,7 +510,7 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
         for (uint32_t q = 0; q < kSide; ++q) {
           const uint32_t v = tc_load1(at + q), w = GATED ? tc_load1(at + S::kQ + q) : 0u;
           tc_load_wait();
-          if (side + q < rows) i8_put_wide<DT, ACT>(g, by, v, w, row0, side + q, col);
+          if (ok && side + q < rows) i8_put_wide<DT, ACT>(g, by, v, w, row0, side + q, col);
         }
         tc_fence_before();
         __syncwarp();
@@ -534,7 +535,7 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
 #pragma unroll
           for (uint32_t x = 0; x < kRun / 16u; ++x) {
             const uint32_t q = side + run + 16u * x;
-            if (q < rows) i8_put_sums<DT, 16, ACT>(g, by, v[x], w[GATED ? x : 0u], row0, g.m, q, col);
+            if (ok && q < rows) i8_put_sums<DT, 16, ACT>(g, by, v[x], w[GATED ? x : 0u], row0, g.m, q, col);
           }
         } else {  // (one tile only: all copies into shared memory have been used)
           uint32_t* part = reinterpret_cast<uint32_t*>(smem) + (side + run) * 128u + warp % 4u * 32u + lane;
@@ -550,7 +551,7 @@ __global__ void __launch_bounds__(kI8PairThreads, 1) i8_pair_kernel(const __grid
   tc_fence_before();
   if (!GATED && g.split > 1u) {
     cluster_sync();
-    if (warp < 8u && tiles && !*abort) {
+    if (warp < 8u && tiles && ok && !*abort) {
       const PairTile where(pair, g.tiles_m, g.tiles_n);
       const uint32_t p = warp % 4u * 32u + lane, col = where.n * 256u + half * 128u + p, row0 = where.m * S::kQ;
       const uint32_t rows = min(S::kQ, g.m - row0), from = rows * rank / g.split, end = rows * (rank + 1u) / g.split, mid = (from + end) / 2u;
