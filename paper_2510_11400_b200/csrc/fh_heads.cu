@@ -145,8 +145,10 @@ __device__ __forceinline__ void report_positions(const HeadsArgs& g) {
   if (threadIdx.x == 0) bad = 0u;
   __syncthreads();
   bool mine = false;
-  if (g.at && g.rotary)
-    for (uint32_t t = threadIdx.x; t < g.tokens; t += blockDim.x) mine = mine || position_of(g, t) < 0;
+  if (g.at && g.rotary) {
+#pragma unroll 16
+    for (uint32_t t = threadIdx.x; t < g.tokens; t += blockDim.x) mine |= (uint32_t)g.at[t] >= g.positions;
+  }
   if (mine) bad = 1u;
   __syncthreads();
   if (threadIdx.x == 0) *g.status = bad ? status_word(kErrCorrupt) : 0ull;
