@@ -223,10 +223,11 @@ __device__ __forceinline__ uint64_t out_at(const HeadsSide& s, uint32_t token, u
   return ((uint64_t)token * s.out_token + (uint64_t)head * s.out_head) * kEs<DT>;
 }
 
-// T lanes to a row, U rows of a team at once: asked for together, and their sums, whose exchanges and roots are chains of latencies, taken side by side.
+// T lanes to a row.  A team takes U heads of a token at once, which are asked for together and share what the token and the side have; the teams of a warp go on
+// where their neighbours end, at the next heads or the next tokens.
 template <int DT, int T, int U, bool HALVES>
 __global__ void __launch_bounds__(kHeadThreads) heads_forward_kernel(const HeadsArgs g) {
-  constexpr uint32_t V = kV<DT>, kTeams = 32 / T, kSpan = kTeams * U;
+  constexpr uint32_t V = kV<DT>, kTeams = 32 / T;
   dep_trigger();
   dep_wait();
   const uint32_t extra = g.status ? 1u : 0u;
@@ -234,27 +235,25 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_kernel(const Heads
     report_positions(g);
     return;
   }
-  const uint32_t lane = threadIdx.x % 32, team = lane / T;
-  const uint64_t units = (uint64_t)g.tokens * ((g.side[0].heads + kSpan - 1u) / kSpan + (g.side[1].heads + kSpan - 1u) / kSpan);
-  const uint64_t u = (uint64_t)(blockIdx.x - extra) * kHeadWarps + threadIdx.x / 32;
-  if (u >= units) return;
-  const HeadUnit unit(u, g, kSpan);
-  const HeadsSide& s = g.side[unit.side];
+  const uint32_t cta = blockIdx.x - extra, which = cta >= g.side[0].parts, lane = threadIdx.x % 32;
+  const HeadsSide& s = g.side[which];
+  const uint32_t blocks = (s.heads + U - 1u) / U;
+  const uint64_t units = (uint64_t)g.tokens * blocks, u = ((uint64_t)(cta - (which ? g.side[0].parts : 0u)) * kHeadWarps + threadIdx.x / 32) * kTeams + lane / T;
+  // (a division in 64 bits takes as long as a row)
+  const uint32_t token = u >> 32 ? (uint32_t)(u / blocks) : (uint32_t)u / blocks, head0 = (uint32_t)(u - (uint64_t)token * blocks) * U;
   const Slot<DT> slot(lane % T, g.dim, g.rotary, HALVES);
   RawSlot raw[U];
   bool there[U];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const uint32_t head = unit.head + i * kTeams + team;
-    there[i] = slot.there && head < s.heads;
+    there[i] = slot.there && u < units && head0 + i < s.heads;
     raw[i].zero();
-    if (there[i]) raw[i].load<DT>(row_of<DT>(s, unit.token, head), slot.a, slot.b);
+    if (there[i]) raw[i].load<DT>(row_of<DT>(s, token, head0 + i), slot.a, slot.b);
   }
   float c[V], n[V], w[2 * V];
   if (slot.there) load_weights<DT>(s.gamma, g, slot.a, slot.b, w);
-  const int32_t at = position_of(g, unit.token);
-  if (at < 0) return;
-  if (slot.there) load_turn<DT>(g, slot, at, c, n);
+  const int32_t at = u < units ? position_of(g, token) : -1;
+  if (slot.there && at >= 0) load_turn<DT>(g, slot, at, c, n);
   // weights and rotation as one factor each: y = rstd (xa (wa c) - xb (wb n)), rstd (xb (wb c) + xa (wa n))
   f32x2 ac[V / 2], an[V / 2], bc[V / 2], bn[V / 2];
   {
@@ -272,6 +271,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_kernel(const Heads
   const float size = (float)g.dim, part = 1.0f / size;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
+    if (i && !__any_sync(0xFFFFFFFFu, there[i])) break;
     float x[2 * V];
     raw[i].values<DT>(x);
     f32x2 a[V / 2], b[V / 2];
@@ -303,8 +303,8 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_kernel(const Heads
       yb[p] = fma2(sb, bc[p], mul2(sa, an[p]));
     }
     join<HALVES, V>(ya, yb, x);
-    if (there[i]) {
-      uint8_t* o = s.out + out_at<DT>(s, unit.token, unit.head + i * kTeams + team);
+    if (there[i] && at >= 0) {
+      uint8_t* o = s.out + out_at<DT>(s, token, head0 + i);
       store_vec<DT>(o + slot.a * kEs<DT>, x);
       store_vec<DT>(o + slot.b * kEs<DT>, x + V);
     }
@@ -330,8 +330,6 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_backward_kernel(const H
   const HeadsSide& s = g.side[which];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, team = lane / T;
   const Slot<DT> slot(lane % T, g.dim, g.rotary, HALVES);
-  const uint32_t spans = (s.heads + kTeams - 1u) / kTeams;
-  const uint64_t units = (uint64_t)g.tokens * spans;
   const float size = (float)g.dim, share = 1.0f / size;
   f32x2 wa[V / 2], wb[V / 2], sa[V / 2], sb[V / 2];
   {
@@ -341,27 +339,29 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_backward_kernel(const H
 #pragma unroll
     for (uint32_t p = 0; p < V / 2; ++p) sa[p] = sb[p] = 0ull;
   }
-  // This warp's units: neighbouring spans, so that a token's position, cosines and sines serve several of them.
-  const uint64_t mine = (uint64_t)part * kHeadWarps + warp, warps = (uint64_t)s.parts * kHeadWarps;
-  const uint64_t first = units / warps * mine + (mine < units % warps ? mine : units % warps), count = units / warps + (mine < units % warps ? 1u : 0u);
-  uint32_t token = (uint32_t)(first / spans), span = (uint32_t)(first % spans);
+  // Each team's rows are neighbours, so that a token's position, cosines and sines serve several heads.
+  const uint64_t rows = (uint64_t)g.tokens * s.heads, teams = (uint64_t)s.parts * kHeadWarps * kTeams, me = ((uint64_t)part * kHeadWarps + warp) * kTeams + team;
+  const uint64_t each = rows / teams, over = rows % teams, first = each * me + (me < over ? me : over);
+  const uint32_t count = (uint32_t)each + (me < over ? 1u : 0u), most = (uint32_t)each + (over ? 1u : 0u);
+  uint32_t token = (uint32_t)(first / s.heads), head = (uint32_t)(first % s.heads);
   RawSlot nx, ny;
-  auto ask = [&](uint32_t token, uint32_t span) {
-    const uint32_t head = span * kTeams + team;
+  auto ask = [&](bool more) {
     nx.zero();
     ny.zero();
-    if (slot.there && head < s.heads) {
+    if (slot.there && more) {
       nx.load<DT>(row_of<DT>(s, token, head), slot.a, slot.b);
       ny.load<DT>(s.dy + out_at<DT>(s, token, head), slot.a, slot.b);
     }
   };
-  if (count) ask(token, span);
+  ask(count != 0u);
   int32_t at = count ? position_of(g, token) : -1, next_at = at;
   bool fresh = true;
-  f32x2 c[V / 2], n[V / 2], minus[V / 2];
-  for (uint64_t left = count; left; --left) {
+  f32x2 c[V / 2], n[V / 2];
+#pragma unroll
+  for (uint32_t p = 0; p < V / 2; ++p) c[p] = n[p] = 0ull;
+  for (uint32_t k = 0; k < most; ++k) {  // (all teams of a warp as often)
     const RawSlot rx = nx, ry = ny;
-    const uint32_t now = token, head = span * kTeams + team;
+    const uint32_t now = token, row = head;
     if (fresh && at >= 0 && slot.there) {
       float fc[V], fn[V];
       load_turn<DT>(g, slot, at, fc, fn);
@@ -369,23 +369,18 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_backward_kernel(const H
       for (uint32_t p = 0; p < V / 2; ++p) {
         c[p] = pack2(fc[2 * p], fc[2 * p + 1]);
         n[p] = pack2(fn[2 * p], fn[2 * p + 1]);
-        minus[p] = pack2(-fn[2 * p], -fn[2 * p + 1]);
       }
     }
-    const int32_t here = at;
+    const bool there = slot.there && k < count && at >= 0;
     fresh = false;
-    if (++span == spans) {
-      span = 0;
+    if (++head == s.heads) {
+      head = 0;
       ++token;
       fresh = true;
     }
-    if (left > 1u) {
-      ask(token, span);
-      if (fresh) next_at = position_of(g, token);
-    }
+    ask(k + 1u < count);
+    if (fresh && k + 1u < count) next_at = position_of(g, token);
     at = next_at;
-    if (here < 0) continue;
-    const bool there = slot.there && head < s.heads;
     f32x2 xa[V / 2], xb[V / 2], da[V / 2], db[V / 2];
     {
       float v[2 * V];
@@ -410,11 +405,9 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_backward_kernel(const H
     f32x2 xx = 0ull, gx = 0ull, gs = 0ull;
 #pragma unroll
     for (uint32_t p = 0; p < V / 2; ++p) {
-      if (slot.there) {
-        const f32x2 ya = da[p], yb = db[p];
-        da[p] = fma2(ya, c[p], mul2(yb, n[p]));
-        db[p] = fma2(yb, c[p], mul2(ya, minus[p]));
-      }
+      const f32x2 ya = da[p], yb = db[p];
+      da[p] = fma2(ya, c[p], mul2(yb, n[p]));
+      db[p] = fma2(mul2(ya, n[p]), twice(-1.0f), mul2(yb, c[p]));
       const f32x2 ga = mul2(da[p], wa[p]), gb = mul2(db[p], wb[p]);
       xx = fma2(xb[p], xb[p], fma2(xa[p], xa[p], xx));
       gx = fma2(gb, xb[p], fma2(ga, xa[p], gx));
@@ -436,7 +429,7 @@ __global__ void __launch_bounds__(kHeadThreads, 4) heads_backward_kernel(const H
     if (there && s.dx) {
       float v[2 * V];
       join<HALVES, V>(da, db, v);
-      uint8_t* o = s.dx + ((uint64_t)now * s.token + (uint64_t)head * s.head) * kEs<DT>;
+      uint8_t* o = s.dx + ((uint64_t)now * s.token + (uint64_t)row * s.head) * kEs<DT>;
       store_vec<DT>(o + slot.a * kEs<DT>, v);
       store_vec<DT>(o + slot.b * kEs<DT>, v + V);
     }
@@ -812,21 +805,27 @@ void deal_out(HeadsArgs* a, uint64_t all) {
 }
 
 template <int DT, int T, int U, bool HALVES>
-int forward_t(const HeadsArgs& a, cudaStream_t stream) {
-  constexpr uint32_t span = 32 / T * U;
-  const uint64_t units = (uint64_t)a.tokens * ((a.side[0].heads + span - 1u) / span + (a.side[1].heads + span - 1u) / span);
-  const uint64_t grid = (units + kHeadWarps - 1u) / kHeadWarps + (a.status ? 1u : 0u);
-  if (grid > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
+int forward_t(const HeadsArgs& a0, cudaStream_t stream) {
+  HeadsArgs a = a0;
+  constexpr uint32_t per_cta = kHeadWarps * (32 / T);
+  uint64_t grid = a.status ? 1u : 0u;
+  for (HeadsSide& s : a.side) {
+    const uint64_t ctas = ((uint64_t)a.tokens * ((s.heads + U - 1u) / U) + per_cta - 1u) / per_cta;
+    if (ctas > 0x3FFFFFFFull) return FH_ERR_UNSUPPORTED;
+    s.parts = (uint32_t)ctas;
+    grid += ctas;
+  }
   return launch_plain<heads_forward_kernel<DT, T, U, HALVES>>((uint32_t)grid, kHeadThreads, 0, 1, stream, a);
 }
 template <int DT, int T>
 int forward_n(const HeadsArgs& a, cudaStream_t stream) {
-  // Four rows to a team where the device then has its warps three times over, two where every SM has four warps, or one.  (4096 tokens of 8 + 8 heads of 128
-  // in bf16: four 13.0 us, two 10.6; 16384 of 32 + 8: 68 and 76.)
+  // Heads to a team: four where the device then has its warps three times over, two where every SM has four warps, or one; no more than there are.  (4096
+  // tokens of 8 + 8 heads of 128 in bf16: four 13.0 us, two 10.6; 16384 of 32 + 8: 68 and 76.)
   const uint64_t rows = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads), warps = rows / (32u / T), sms = (uint64_t)std::max(1, sm_count());
+  const uint32_t heads = std::max(a.side[0].heads, a.side[1].heads);
   auto with = [&](auto halves) {
-    if (warps >= sms * 20u * 4u * 3u) return forward_t<DT, T, 4, halves.value>(a, stream);
-    if (warps >= sms * 4u * 2u) return forward_t<DT, T, 2, halves.value>(a, stream);
+    if (heads > 2u && warps >= sms * 20u * 4u * 3u) return forward_t<DT, T, 4, halves.value>(a, stream);
+    if (heads > 1u && warps >= sms * 4u * 2u) return forward_t<DT, T, 2, halves.value>(a, stream);
     return forward_t<DT, T, 1, halves.value>(a, stream);
   };
   return a.halves ? with(std::true_type()) : with(std::false_type());
