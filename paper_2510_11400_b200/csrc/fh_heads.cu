@@ -312,11 +312,13 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_kernel(const Heads
 }
 
 // Backward.  CTAs are dealt out to queries and keys, and each adds up its rows' part of the weights' gradient: a lane for its slot, then teams, then warps,
-// in a fixed order.  A unit's rows are asked for while the one before it is worked on.  (16384 tokens of 32 + 8 heads of 128 in bf16: 112 us with registers
-// for four CTAs an SM, 127 for three; two rows of a team at once and none ahead 140; a ring in shared memory filled by asynchronous copies 156 to 204: its
-// addresses and second reads cost more than they hid.)
+// in a fixed order.  A team's next row is asked for while it works on one.  (16384 tokens of 32 + 8 heads of 128 in bf16: 108 us with registers for four CTAs
+// an SM, 127 for three; in fp32 8192 of 16 + 16: 73 for five, 77 for four.  Before, in bf16: two rows of a team at once and none ahead 140; a ring in shared
+// memory filled by asynchronous copies 156 to 204, as its addresses and second reads cost more than they hid.)
+template <int DT>
+constexpr uint32_t kBackCtas = DT == kF32 ? 5 : 4;
 template <int DT, int T, bool HALVES>
-__global__ void __launch_bounds__(kHeadThreads, 4) heads_backward_kernel(const HeadsArgs g) {
+__global__ void __launch_bounds__(kHeadThreads, kBackCtas<DT>) heads_backward_kernel(const HeadsArgs g) {
   constexpr uint32_t V = kV<DT>, kTeams = 32 / T;
   __shared__ float sums[kHeadWarps][T * 2 * V];
   dep_trigger();
@@ -819,13 +821,13 @@ int forward_t(const HeadsArgs& a0, cudaStream_t stream) {
 }
 template <int DT, int T>
 int forward_n(const HeadsArgs& a, cudaStream_t stream) {
-  // Heads to a team: four where the device then has its warps three times over, two where every SM has four warps, or one; no more than there are.  (4096
-  // tokens of 8 + 8 heads of 128 in bf16: four 13.0 us, two 10.6; 16384 of 32 + 8: 68 and 76.)
-  const uint64_t rows = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads), warps = rows / (32u / T), sms = (uint64_t)std::max(1, sm_count());
+  // Heads to a team: four, or two where there are no more, if every SM then has eight warps; else one.  (16384 tokens of 32 + 8 heads of 128 in bf16: four 62 us,
+  // two 73, one 93; 1024: 6.3, 7.2 and 8.1; 64: 3.0, 2.6 and 2.5.)
+  const uint64_t rows = (uint64_t)a.tokens * (a.side[0].heads + a.side[1].heads), warps = rows / (32u / T), enough = 8ull * std::max(1, sm_count());
   const uint32_t heads = std::max(a.side[0].heads, a.side[1].heads);
   auto with = [&](auto halves) {
-    if (heads > 2u && warps >= sms * 20u * 4u * 3u) return forward_t<DT, T, 4, halves.value>(a, stream);
-    if (heads > 1u && warps >= sms * 4u * 2u) return forward_t<DT, T, 2, halves.value>(a, stream);
+    if (heads > 2u && warps / 4u >= enough) return forward_t<DT, T, 4, halves.value>(a, stream);
+    if (heads > 1u && warps / 2u >= enough) return forward_t<DT, T, 2, halves.value>(a, stream);
     return forward_t<DT, T, 1, halves.value>(a, stream);
   };
   return a.halves ? with(std::true_type()) : with(std::false_type());
@@ -867,7 +869,7 @@ int backward_t(const HeadsArgs& a0, cudaStream_t stream) {
   HeadsArgs a = a0;
   constexpr uint32_t rows = kHeadWarps * (32u / T);
   static_assert(rows >= kHeadFewest, "the workspace's size");
-  heads_parts(&a, 148u * 4u, rows);
+  heads_parts(&a, 148u * kBackCtas<DT>, rows);
   return backward_launch(a, stream, [&](uint32_t grid) { return launch_plain<heads_backward_kernel<DT, T, HALVES>>(grid, kHeadThreads, 0, 1, stream, a); });
 }
 template <int DT, int T>
