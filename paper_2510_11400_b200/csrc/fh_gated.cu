@@ -18,13 +18,15 @@ constexpr uint32_t kEs = DT == kF32 ? 4u : 2u;
 //
 // Where the width is no multiple of 16, du's chunks begin inside a chunk of the container.  The row's codes are then put together in shared memory (`room`
 // bytes), or written byte by byte where there is no room.
+//
+// Registers for three CTAs an SM in bf16 (4096 x 8192 83 us, for two 101, for four 92), for two in fp32 (4096 x 4096 78, three 82).
 struct GatedPlan {
   GatedArgs g;
   uint32_t room;
 };
 
 template <int DT, int ACT, int I, bool VEC>
-__global__ void __launch_bounds__(256, 2) gated_backward_kernel(const GatedPlan plan) {
+__global__ void __launch_bounds__(256, DT == kF32 ? 2 : 3) gated_backward_kernel(const GatedPlan plan) {
   const GatedArgs& g = plan.g;
   using Loose = LooseRows<DT, 1>;
   extern __shared__ __align__(16) uint8_t joined[];
@@ -163,8 +165,8 @@ int gated_start(const GatedArgs& a, uint32_t warps, cudaStream_t stream) {
   if (a.packed && a.width % 16u && room <= 64 * 1024) p.room = (uint32_t)room;
   return launch_plain<gated_backward_kernel<DT, ACT, I, VEC>>((uint32_t)grid, (int)warps * 32, p.room, 1, stream, p);
 }
-// A row to a CTA (two rows, whose codes are written in whole sectors: 4096 x 8192 bf16 101 -> 94 us, but 4096 x 2048 22.6 -> 27, 16384 x 1024 41 -> 46), of up to eight
-// warps, and as few chunks to a lane as hold it; in fp32, whose chunks take twice the registers, two where there are two (4096 x 4096 90 us with one, 78).
+// A row to a CTA (with two, whose codes are written in whole sectors, 4096 x 8192 bf16 took 6 % less, but 4096 x 2048 22.6 -> 27 us, 16384 x 1024 41 -> 46), of up
+// to eight warps, and as few chunks to a lane as hold it; in fp32, whose chunks take twice the registers, two where there are two (4096 x 4096 90 us with one, 78).
 template <int DT, int ACT, bool VEC>
 int gated_by_length(const GatedArgs& a, cudaStream_t stream) {
   const uint32_t need = (a.width + 511u) / 512u;  // steps of a warp in all
