@@ -117,6 +117,7 @@ int rows_by_group(const I8SaveArgs& a, cudaStream_t stream) {
 //  Others: the maxima by a kernel of their own, bands of rows side by side, which leaves them in the container (a maximum does not depend on the order), then
 //  the codes.  (In clusters 8192 x 4096 bf16 took 40 us, 34 in two passes; 65536 x 256, with eight CTAs to a group of columns, 122 and 24.)
 constexpr int kColWarps = 8;
+
 template <int DT, int C, bool VEC>
 struct ColChunk {
   static constexpr int kWords = C * (int)kEs<DT> / 4 ? C * (int)kEs<DT> / 4 : 1;
