@@ -539,7 +539,8 @@ int fh_i8_product(const fh_i8_product_desc* desc, const void* d_a, size_t a_byte
  * The gated feed-forward block: both projections, the activation and the product in one kernel.
  *
  *   g = x Wg^T, u = x Wu^T, h = act(g) * u
- * with x (rows x k), Wg and Wu (width x k) held in 8 bits.  The projection behind it is fh_i8_product of h, compressed.
+ * with x (rows x k), Wg and Wu (width x k) held in 8 bits.  The projection behind it is fh_i8_product of h, compressed.  An fp32 h has the activation to a few of
+ * its last places (relative to its own size, next to nothing too); for a bf16 h the exponentials are fast ones, a hundredth of its rounding off.
  */
 typedef enum { FH_SILU = 0, FH_GELU = 1, FH_GELU_TANH = 2, FH_RELU = 3 } fh_activation;
 typedef struct {

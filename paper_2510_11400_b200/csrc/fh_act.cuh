@@ -4,20 +4,24 @@
 #include <cuda_runtime.h>
 
 #include "../../include/fh.h"
+#include "fh_device.cuh"
 
 namespace fh {
 
 constexpr float kTanhC = 0.7978845608028654f, kTanhK = 0.044715f;  // tanh's form of the gelu: sqrt(2 / pi), and the cube's factor
+constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.07135481627260025f;  // 2 sqrt(2 / pi), and that times the cube's factor
 
-// act(g).
-template <int ACT>
+// act(g), for a result of type DT.  silu and tanh's form of the gelu are g / (1 + exp(-v)), v = g and g (A + B g^2).  The exponential is that of -|v|, which
+// never overflows, so that values next to nothing are not lost, and the fast quotient, two places off at most, has denominators from 1 to 2 (an exact one, 4096 x
+// 8192 x 4096 in fp32 412 us, 210 so).  For bf16 the exponential is the fast one too, up to 1e-5 of the value off, a hundredth of what rounding it is.
+template <int ACT, int DT>
 __device__ __forceinline__ float act_of(float g) {
-  if (ACT == FH_SILU) return __fdividef(g, 1.0f + __expf(-g));
-  if (ACT == FH_GELU) return 0.5f * g * (1.0f + erff(g * 0.7071067811865476f));
-  if (ACT == FH_GELU_TANH) {  // 0.5 g (1 + tanh w) = g / (1 + exp(-2 w))
-    const float w = kTanhC * __fmaf_rn(kTanhK * g * g, g, g);
-    return __fdividef(g, 1.0f + __expf(-2.0f * w));
+  if (ACT == FH_SILU || ACT == FH_GELU_TANH) {
+    const float v = ACT == FH_SILU ? g : g * __fmaf_rn(kTanhB, g * g, kTanhA);
+    const float e = DT == kF32 ? expf(-fabsf(v)) : __expf(-fabsf(v)), top = v < 0.0f ? g * e : g;
+    return __fdividef(top, 1.0f + e);
   }
+  if (ACT == FH_GELU) return 0.5f * g * (1.0f + erff(g * 0.7071067811865476f));
   return g > 0.0f ? g : (g != g ? g : 0.0f);
 }
 

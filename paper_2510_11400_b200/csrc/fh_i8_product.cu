@@ -79,7 +79,7 @@ __device__ __forceinline__ void i8_put(const I8ProductArgs& g, float (&f)[NR], c
     }
     if (g.c) {
 #pragma unroll
-      for (int x = 0; x < NR; ++x) f[x] = act_of<ACT>(f[x]) * u[x];
+      for (int x = 0; x < NR; ++x) f[x] = act_of<ACT, DT>(f[x]) * u[x];
       store_c<DT, NR>(g.c, g.ldc, row, end, col, f);
     }
   }
