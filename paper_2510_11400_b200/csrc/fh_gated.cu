@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(256, DT == kF32 ? 2 : 3) gated_backward_kernel
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       float act, slope;
-      act_and_slope<ACT>(fg[i], act, slope);
+      act_and_slope<ACT, DT>(fg[i], act, slope);
       fg[i] = fd[i] * fu[i] * slope;
       fu[i] = fd[i] * act;
     }

@@ -13,7 +13,7 @@ torch = pytest.importorskip("torch")
 U = 2.0 ** -24                                                       # half a step of fp32, relative
 HALF = {api.FH_F32: U, api.FH_BF16: 2.0 ** -8}
 TYPES = {api.FH_F32: torch.float32, api.FH_BF16: torch.bfloat16}
-KINDS = [api.FH_SILU, api.FH_GELU_TANH, api.FH_RELU]
+KINDS = [api.FH_SILU, api.FH_GELU, api.FH_GELU_TANH, api.FH_RELU]
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -40,10 +40,10 @@ def exact(g, kind):
     return np.maximum(g, 0), (g > 0).astype(np.float64)
 
 
-def slack(g, kind):
+def slack(g, kind, dtype=api.FH_F32):
     """How far the activation and its derivative may be off in fp32.  Functions: exponential and quotient within two steps (4 U), complementary error function within four
-    (8 U); every product and sum rounds once.  A rounded argument moves an exponential by the argument's error: 4 U of it for gelu_tanh's g (A + B g^2), A and B
-    rounded, 1.5 U for the error function's (whose logarithm has a slope of at most 2 x + 1.2), U for the density's square.  Where an exponential is below the normal
+    (8 U), the normal distribution of bf16 results within 16 U besides its exponential; every product and sum rounds once.  A rounded argument moves an
+    exponential by the argument's error: 4 U of it for gelu_tanh's g (A + B g^2), A and B rounded, 1.5 U for the error function's (whose logarithm has a slope of at most 2 x + 1.2), U for the density's square.  Where an exponential is below the normal
     numbers it is a multiple of 2^-149."""
     a, d = (np.abs(v) for v in exact(g, kind))
     c = np.clip(np.abs(g), 0, 1e3)
@@ -57,7 +57,8 @@ def slack(g, kind):
             arg = np.where(g < 0, (2 * x + 1.2) * 1.5 * U * x, 1.5 * U * x * np.exp(-x * x) * 1.2)
             p = a / np.where(c == 0, 1, np.abs(g))
             dens = c * np.exp(-0.5 * c * c) * 0.4
-            return (12 * U + arg) * a + least, (10 * U + arg) * p + (8 * U + 0.5 * c * c * 2 * U) * dens + U * d + 40 * least
+            phi = 8 * U if dtype == api.FH_F32 else 20 * U
+            return (phi + 4 * U + arg) * a + least, (phi + 2 * U + arg) * p + (8 * U + 0.5 * c * c * 2 * U) * dens + U * d + 40 * least
         if kind == i8.GELU_TANH:
             v = 2 * math.sqrt(2 / math.pi) * (c + 0.044715 * c ** 3)
             e = 4 * U + np.minimum(v, 110.0) * 4 * U                 # of exp(-|v|)
@@ -98,6 +99,27 @@ def test_forward(rows, kind, dtype):
         eg, eu = (np.broadcast_to((127 * q[:, 0] * i8.scales(m).astype(np.float64))[None, :], (rows, f)) for q, m in ((qg, mg), (qu, mu)))
         want = exact(eg, kind)[0]
         wide = np.minimum(np.abs(eg), 110.0) ** (3 if kind == i8.GELU_TANH else 2 if kind == i8.GELU else 1) + 1
-        bound = np.abs(want * eu) * (HALF[dtype] * (1 + 1e-6) + 40 * U * np.minimum(wide, 200.0)) + np.abs(eu) * slack(eg, kind)[0] + 2.0 ** -133
+        bound = np.abs(want * eu) * (HALF[dtype] * (1 + 1e-6) + 40 * U * np.minimum(wide, 200.0)) + np.abs(eu) * slack(eg, kind, dtype)[0] + 2.0 ** -133
     assert np.isfinite(got).all()
     assert (np.abs(got - want * eu) <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", [api.FH_F32, api.FH_BF16])
+@pytest.mark.parametrize("kind", [api.FH_GELU, api.FH_RELU])
+@pytest.mark.parametrize("extra", [0, 1])
+def test_backward(extra, kind, dtype):
+    """dh = u = 1: the derivative, and the activation.  On to the largest numbers."""
+    far = np.exp2(np.arange(7, 128)).astype(np.float32) * np.float32(1.3)
+    g = torch.from_numpy(np.concatenate([grid(), far, -far])).to(TYPES[dtype])
+    f = g.numel()
+    pre = torch.ones(2, 2 * f + extra, dtype=TYPES[dtype], device="cuda")
+    pre[:, :f] = g.cuda()
+    dh, out = torch.ones(2, f, dtype=TYPES[dtype], device="cuda"), torch.empty_like(pre)
+    d = api.gated_desc(2, f, 1, kind, dtype, f, 2 * f + extra)
+    assert api.fh_gated_backward(d, dh, pre[:, :2 * f], out[:, :2 * f]) == api.FH_OK
+    v = g.double().numpy()
+    (a, slope), (ea, es) = exact(v, kind), slack(v, kind, dtype)
+    for row in out.double().cpu().numpy():
+        for got, want, e in ((row[:f], slope, es), (row[f:2 * f], a, ea)):
+            assert np.isfinite(got).all()
+            assert (np.abs(got - want) <= e + HALF[dtype] * (1 + 1e-6) * np.abs(want) + 2.0 ** -133 * (dtype == api.FH_BF16)).all()
