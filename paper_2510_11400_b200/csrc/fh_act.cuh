@@ -8,8 +8,7 @@
 
 namespace fh {
 
-constexpr float kTanhC = 0.7978845608028654f, kTanhK = 0.044715f;  // tanh's form of the gelu: sqrt(2 / pi), and the cube's factor
-constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.07135481627260025f;  // 2 sqrt(2 / pi), and that times the cube's factor
+constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.07135481627260025f;  // tanh's form of the gelu: 2 sqrt(2 / pi), and that times the cube's factor, 0.044715
 
 // The normal distribution below g, Phi(g) = 1 - Phi(-g), for results of type DT, given e = exp(-g^2 / 2).  (1 + erf would leave nothing of it below -5.)
 // In fp32 by the complementary error function.  In bf16 that made the gated backward pass of 4096 x 8192 take 122 us instead of 88: there Phi(-a) = e R(a),
@@ -47,21 +46,21 @@ __device__ __forceinline__ float act_of(float g) {
 }
 
 // act(g) and its derivative.  (Full-precision functions: behind this a gradient may be rounded to whole numbers, where an error in the last
-// places turns over more of them than it has to.)
+// places turns over more of them than it has to; the quotient of 1 and 1 to 2 is a fast one where the gradient is rounded to bf16 first: 4096 x 8192 102 us and 79.)
 template <int ACT, int DT>
 __device__ __forceinline__ void act_and_slope(float g, float& a, float& slope) {
-  if (ACT == FH_SILU) {
-    const float p = 1.0f / (1.0f + expf(-g));
+  if (ACT == FH_SILU || ACT == FH_GELU_TANH) {
+    // p = 1 / (1 + exp(-v)) and q = 1 - p, both from exp(-|v|), so that neither is what is left of 1; the derivative is p (1 + g v' q).  From 64 on tanh's p
+    // is 0 or 1 whatever g is, and beyond some 1e19 its v' would be infinite.
+    const float c = ACT == FH_SILU ? g : max_nan(min_nan(g, 64.0f), -64.0f), cc = c * c;
+    const float v = ACT == FH_SILU ? g : c * __fmaf_rn(kTanhB, cc, kTanhA), along = ACT == FH_SILU ? g : c * __fmaf_rn(3.0f * kTanhB, cc, kTanhA);
+    const float e = expf(-fabsf(v)), r = DT == kF32 ? 1.0f / (1.0f + e) : __fdividef(1.0f, 1.0f + e), p = v < 0.0f ? e * r : r, q = v < 0.0f ? r : e * r;
     a = g * p;
-    slope = p * __fmaf_rn(g, 1.0f - p, 1.0f);
+    slope = p * __fmaf_rn(along, q, 1.0f);
   } else if (ACT == FH_GELU) {
     const float e = expf(-0.5f * g * g), p = normal_below<DT>(g, e);
     a = g * p;
     slope = __fmaf_rn(g * 0.3989422804014327f, e, p);
-  } else if (ACT == FH_GELU_TANH) {  // (1 + tanh w) / 2 = p, (1 - tanh w) / 2 = q
-    const float e = expf(-2.0f * kTanhC * __fmaf_rn(kTanhK * g * g, g, g)), p = 1.0f / (1.0f + e), q = e <= 1.0f ? e * p : 1.0f - p;
-    a = g * p;
-    slope = __fmaf_rn(2.0f * g * p * q, kTanhC * __fmaf_rn(3.0f * kTanhK * g, g, 1.0f), p);
   } else {
     const bool on = g > 0.0f;
     a = on ? g : (g != g ? g : 0.0f);

@@ -105,7 +105,7 @@ def test_forward(rows, kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", [api.FH_F32, api.FH_BF16])
-@pytest.mark.parametrize("kind", [api.FH_GELU, api.FH_RELU])
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("extra", [0, 1])
 def test_backward(extra, kind, dtype):
     """dh = u = 1: the derivative, and the activation.  On to the largest numbers."""
@@ -123,3 +123,13 @@ def test_backward(extra, kind, dtype):
         for got, want, e in ((row[:f], slope, es), (row[f:2 * f], a, ea)):
             assert np.isfinite(got).all()
             assert (np.abs(got - want) <= e + HALF[dtype] * (1 + 1e-6) * np.abs(want) + 2.0 ** -133 * (dtype == api.FH_BF16)).all()
+
+
+@pytest.mark.parametrize("dtype", [api.FH_F32, api.FH_BF16])
+@pytest.mark.parametrize("kind", KINDS)
+def test_nan_stays_in_its_place(kind, dtype):
+    pre, dh, out = (torch.ones(3, n, dtype=TYPES[dtype], device="cuda") for n in (64, 32, 64))
+    pre[1, 5] = float("nan")
+    assert api.fh_gated_backward(api.gated_desc(3, 32, 1, kind, dtype), dh, pre, out) == api.FH_OK
+    bad = out.isnan().nonzero().tolist()
+    assert [1, 32 + 5] in bad and ([1, 5] in bad or kind == api.FH_RELU) and len(bad) <= 2    # (relu's derivative: not above zero)
