@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(256, DT == kF32 ? 2 : 3) gated_backward_kernel
     for (int i = 0; i < 16; ++i) {
       float act, slope;
       act_and_slope<ACT, DT>(fg[i], act, slope);
-      fg[i] = fd[i] * fu[i] * slope;
+      fg[i] = fd[i] * (fu[i] * slope);  // (dh u may be beyond the largest number where the derivative is 0)
       fu[i] = fd[i] * act;
     }
     dg.take(fg);

@@ -133,3 +133,12 @@ def test_nan_stays_in_its_place(kind, dtype):
     assert api.fh_gated_backward(api.gated_desc(3, 32, 1, kind, dtype), dh, pre, out) == api.FH_OK
     bad = out.isnan().nonzero().tolist()
     assert [1, 32 + 5] in bad and ([1, 5] in bad or kind == api.FH_RELU) and len(bad) <= 2    # (relu's derivative: not above zero)
+
+
+@pytest.mark.parametrize("dtype", [api.FH_F32, api.FH_BF16])
+def test_what_relu_takes_out_is_zero(dtype):
+    """dh u is beyond the largest number there."""
+    pre, dh, out = torch.full((2, 64), 1e30, dtype=TYPES[dtype], device="cuda"), torch.full((2, 32), 1e30, dtype=TYPES[dtype], device="cuda"), torch.empty(2, 64, dtype=TYPES[dtype], device="cuda")
+    pre[:, :32] = -1.0
+    assert api.fh_gated_backward(api.gated_desc(2, 32, 1, api.FH_RELU, dtype), dh, pre, out) == api.FH_OK
+    assert (out == 0).all()
