@@ -582,11 +582,11 @@ def heads_desc(tokens: int, q_heads: int, k_heads: int, dim: int, rotary: Option
 
 
 def rotation_table(positions: int, rotary: int, base: float = 10000.0, scale: float = 1.0, out=None, stream=None):
-    """A table of cosines and sines, fp32 [positions, rotary / 2, 2]."""
-    dev = _device()
+    """A table of cosines and sines, fp32 [positions, rotary / 2, 2]; in `out` its elements have to lie side by side."""
+    dev, n = _device(), positions * rotary
     if out is None:
-        out = _torch.empty(positions, rotary // 2, 2, dtype=_torch.float32, device=f"cuda:{dev}")
-    rc = lib().fh_rotation_table(positions, rotary, base, scale, _ptr(out, dev, positions * rotary, 4), _on(stream, dev))
+        out = _torch.empty(max(0, positions), max(0, rotary) // 2, 2, dtype=_torch.float32, device=f"cuda:{dev}")
+    rc = lib().fh_rotation_table(positions, rotary, base, scale, _dense(out, dev, 1, n, n, FH_F32), _on(stream, dev))
     if rc != FH_OK:
         raise FhError(rc, "fh_rotation_table")
     return out
