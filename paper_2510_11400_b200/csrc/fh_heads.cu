@@ -201,16 +201,16 @@ __device__ __forceinline__ void join(const f32x2 (&a)[V / 2], const f32x2 (&b)[V
   }
 }
 
-// Whether unit `u` is of queries or keys, of which token, and its first head.  A unit is a warp's work: `span` heads of a token.
+// Row `u` of all: whether it is of queries or keys, its token and its head.
 struct HeadUnit {
   uint32_t side, token, head;
-  __device__ __forceinline__ HeadUnit(uint64_t u, const HeadsArgs& g, uint32_t span) {
-    const uint32_t nq = (g.side[0].heads + span - 1u) / span, nk = (g.side[1].heads + span - 1u) / span;
+  __device__ __forceinline__ HeadUnit(uint64_t u, const HeadsArgs& g) {
+    const uint32_t nq = g.side[0].heads, n = nq + g.side[1].heads;
     // (a division in 64 bits takes as long as a row)
-    token = u >> 32 ? (uint32_t)(u / (nq + nk)) : (uint32_t)u / (nq + nk);
-    const uint32_t at = (uint32_t)(u - (uint64_t)token * (nq + nk));
+    token = u >> 32 ? (uint32_t)(u / n) : (uint32_t)u / n;
+    const uint32_t at = (uint32_t)(u - (uint64_t)token * n);
     side = at >= nq;
-    head = (side ? at - nq : at) * span;
+    head = side ? at - nq : at;
   }
 };
 
@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(kHeadThreads) heads_forward_loose_kernel(const
   const uint64_t units = (uint64_t)g.tokens * (g.side[0].heads + g.side[1].heads);
   const uint64_t u = (uint64_t)(blockIdx.x - extra) * kHeadWarps + threadIdx.x / 32;
   if (u >= units) return;
-  const HeadUnit unit(u, g, 1u);
+  const HeadUnit unit(u, g);
   const HeadsSide& s = g.side[unit.side];
   const uint8_t* p = s.x + ((uint64_t)unit.token * s.token + (uint64_t)unit.head * s.head) * kEs<DT>;
   uint8_t* o = s.out + ((uint64_t)unit.token * s.out_token + (uint64_t)unit.head * s.out_head) * kEs<DT>;
@@ -849,7 +849,7 @@ int forward_d(const HeadsArgs& a, cudaStream_t stream) {
 }
 
 // CTAs of the backward pass: a rule's most, and another for every so many rows.  The workspace is sized for kHeadMost and kHeadFewest, which no rule is
-// beyond.
+// beyond.  (148 SMs, whatever the device says: the workspace's size is asked for without one, and sums do not depend on it.)
 constexpr uint32_t kHeadMost = 148 * 8, kHeadFewest = 4;
 
 uint64_t heads_parts_of(const HeadsArgs& a, uint32_t most, uint32_t rows_per_cta) {

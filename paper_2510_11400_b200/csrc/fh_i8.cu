@@ -34,7 +34,6 @@ struct HeadRows {
     if (heads > 1 && head < dim) return false;
     return tokens == 1 || heads == 1 || token >= (heads - 1) * head + dim || head >= (tokens - 1) * token + dim;
   }
-  int64_t bytes() const { return ((tokens - 1) * token + (heads - 1) * head + dim) * (int64_t)esize_of(dtype); }
   // The rows with what lies between the heads of a token, or the tokens of a head.
   Rows coarse() const {
     if (tokens == 1) return Rows(p, heads, dim, std::max(head, dim), dtype);

@@ -94,19 +94,19 @@ int rows_by_length(const I8SaveArgs& a, bool many, cudaStream_t stream) {
   // CTA: 16 warps 26 us, 8 18.5, 4 17.4); as many warps as the row has work for where there are few.
   const uint32_t most = many ? 4u : 16u;
   if (need <= most) return rows_launch<DT, R, 1, VEC>(a, need, stream);
-  if (need <= 2u * most || (kMost == 2 && need <= 32u)) return rows_launch<DT, R, 2, VEC>(a, (need + 1u) / 2u, stream);
-  if (kMost == 4 && need <= 64u) return rows_launch<DT, R, kMost, VEC>(a, (need + 3u) / 4u, stream);
-  return rows_launch<DT, R, 0, VEC>(a, 16u, stream);
+  if (kMost == 4 && need <= 2u * most) return rows_launch<DT, R, 2, VEC>(a, (need + 1u) / 2u, stream);
+  if (R == 2 || need <= 16u * kMost) return rows_launch<DT, R, kMost, VEC>(a, (need + kMost - 1u) / kMost, stream);
+  return rows_launch<DT, 1, 0, VEC>(a, 16u, stream);  // (R is 1)
 }
 template <int DT, bool VEC>
 int rows_by_group(const I8SaveArgs& a, cudaStream_t stream) {
   // Two rows to a CTA write whole sectors of codes (one row 16384 x 512 17.8 us, two 9.3, four 6.8; 8192 x 4096 20.8, 17.4 and 18.5); one where there are not
-  // enough rows for every SM, or where two do not fit the registers of 16 warps.
+  // enough rows for every SM, or where two do not fit the registers of 16 warps.  Four rows have a chunk to a lane.
   const uint32_t chunks = I8Layout(a.rows, a.cols).chunks(), most = DT == kF32 ? 32u : 64u;
   const bool many = a.rows / 2u >= (uint32_t)std::max(1, sm_count());
   if (!many || (chunks + 15u) / 16u > most) return rows_by_length<DT, 1, VEC>(a, many, stream);
   if (chunks > 32u) return rows_by_length<DT, 2, VEC>(a, true, stream);
-  return rows_by_length<DT, 4, VEC>(a, true, stream);
+  return rows_launch<DT, 4, 1, VEC>(a, (chunks + 7u) / 8u, stream);
 }
 
 // ---- by columns ------------------------------------------------------------------------------------
@@ -121,6 +121,7 @@ constexpr int kColWarps = 8;
 template <int DT, int C, bool VEC>
 struct ColChunk {
   static constexpr int kWords = C * (int)kEs<DT> / 4 ? C * (int)kEs<DT> / 4 : 1;
+  static_assert(!VEC || C * kEs<DT> == 4u, "a word to a row");
   uint32_t w[16][kWords];
   // Rows 16 j ... of the columns from `col` on (n of them there), zeros elsewhere.
   __device__ __forceinline__ void load(const I8SaveArgs& g, uint32_t j, uint32_t col, int n) {
@@ -133,12 +134,7 @@ struct ColChunk {
       for (int x = 0; x < kWords; ++x) w[i][x] = 0u;
       if (VEC) {
         if (there && n == C) {
-          if (kWords == 1) w[i][0] = *reinterpret_cast<const uint32_t*>(p);
-          if (kWords == 2) {
-            const uint2 v = *reinterpret_cast<const uint2*>(p);
-            w[i][0] = v.x;
-            w[i][kWords - 1] = v.y;
-          }
+          w[i][0] = *reinterpret_cast<const uint32_t*>(p);  // (two columns of bf16)
           continue;
         }
       }
@@ -342,7 +338,7 @@ int cols_launch(const I8SaveArgs& a0, cudaStream_t stream) {
   const uint64_t max_ctas = ((uint64_t)a.cols + 255u) / 256u * (((uint64_t)a.rows + kBand - 1u) / kBand);
   const uint64_t code_ctas = (l.r8 + 32ull * C - 1u) / (32u * C) * ((chunks + kI8Threads / 32 - 1ull) / (kI8Threads / 32));
   if (max_ctas > 0x7FFFFFFFull || code_ctas > 0x7FFFFFFFull) return FH_ERR_UNSUPPORTED;
-  int rc = launch_plain<i8_cols_start_kernel>((uint32_t)std::min<uint64_t>((l.r8 + kI8Threads - 1ull) / kI8Threads, 148u), kI8Threads, 0, 1, stream, a);
+  int rc = launch_plain<i8_cols_start_kernel>((uint32_t)std::min<uint64_t>((l.r8 + kI8Threads - 1ull) / kI8Threads, (uint64_t)std::max(1, sm_count())), kI8Threads, 0, 1, stream, a);
   if (rc != FH_OK) return rc;
   if (((uintptr_t)a.src | a.ld * kEs<DT>) % 16u == 0u)
     rc = launch_plain<i8_cols_max_kernel<DT, true>>((uint32_t)max_ctas, kI8Threads, 0, 1, stream, a);
