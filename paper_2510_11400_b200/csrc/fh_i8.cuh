@@ -76,7 +76,7 @@ constexpr float kI8Magic23 = 12582912.0f;  // 1.5 * 2^23
 //
 // bf16: only half of the row's magnitude is that near to a middle (63.5), and elements whose quotient is a middle exactly.  With x = X 2^p and the
 // magnitude M 2^q, X and M of eight bits, 127 x / magnitude is |254 X - (2 k + 1) M 2^(q - p)| / (2 M 2^(q - p)) away from the middle above k: nothing, or at
-// least 1 / (2 M 2^(q - p)), which is fifty times what t may be off by (127 * 255 / (M 2^(q - p)) times 2^-21).  Nothing: 127 divides M, which then
+// least 1 / (2 M 2^(q - p)), which is thirty times what t may be off by (127 * 255 / (M 2^(q - p)) times 2^-21).  Nothing: 127 divides M, which then
 // is 254, so that s is a power of two and everything is exact; or it divides 2 k + 1, which then is 127: x is half of the magnitude.  So inv is moved
 // by a last place where half the magnitude would come out on the wrong side, and no element is looked at again.  (Half of the magnitude is no rare
 // value: looking again at 16 elements where one of them is near a middle made 8192 x 4096 by rows take 60 us instead of 29.)

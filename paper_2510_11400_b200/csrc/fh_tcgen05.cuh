@@ -1,5 +1,5 @@
-// Tensor-core instructions of sm_100a as the product kernels use them: tensor memory, scale copies, block-scaled matrix
-// instructions on 4-bit operands, clusters.
+// Tensor-core instructions of sm_100a as the product kernels use them: tensor memory, scale copies, matrix instructions on 4-bit
+// operands with block scales and on 8-bit integers, clusters.
 #pragma once
 
 #include <stdint.h>
