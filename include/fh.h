@@ -580,7 +580,7 @@ int fh_gated_backward(const fh_gated_desc* desc, const void* d_dh, const void* d
  * Norms of queries and keys for each head, with the rotation by position in the same pass.
  *
  * For each token and head, x of `dim` elements:  xhat = x * rstd, rstd = 1 / sqrt(mean(x^2) + eps)  (FH_HEADS_RMS), or xhat = (x - mean) * rstd with
- * the variance instead (FH_HEADS_LAYER);  z = xhat * gamma;  and of the first `rotary` elements the pairs (a, b) become
+ * the variance instead (FH_HEADS_LAYER; squares are summed up in fp32, unscaled);  z = xhat * gamma;  and of the first `rotary` elements the pairs (a, b) become
  * (a c - b n, b c + a n), c and n the cosine and sine that the table has for the token's position and the pair.
  */
 typedef enum { FH_HEADS_RMS = 0, FH_HEADS_LAYER = 1 } fh_heads_kind;
@@ -615,7 +615,7 @@ int fh_rotation_table(int32_t positions, int32_t rotary, double base, double sca
  *   d_gamma_q, d_gamma_k dim weights, either may be NULL (1)
  *   d_table              positions x rotary / 2 pairs (cos, sin), 8-byte aligned; may be NULL when rotary is 0
  *   d_positions          a position for each token; NULL: 0, 1, 2 ...  A token whose position is negative or not in the table is left out: nothing of
- *                        it is written, and the status is FH_ERR_CORRUPT
+ *                        it is written, and the status is FH_ERR_CORRUPT.  (Not read when rotary is 0: then no token is left out)
  *   d_q_out, d_k_out     may be d_q (d_k) where the strides are the same
  *   d_status             optional uint64 in device (or mapped pinned) memory: (uint64)(int64) status
  * FH_ERR_ARG when an output or the status has a byte in common with an input or another of them, other than in place as above.

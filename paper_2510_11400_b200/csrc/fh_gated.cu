@@ -19,7 +19,8 @@ constexpr uint32_t kEs = DT == kF32 ? 4u : 2u;
 // Where the width is no multiple of 16, du's chunks begin inside a chunk of the container.  The row's codes are then put together in shared memory (`room`
 // bytes), or written byte by byte where there is no room.
 //
-// Registers for three CTAs an SM in bf16 (4096 x 8192 83 us, for two 101, for four 92), for two in fp32 (4096 x 4096 78, three 82).
+// Registers for three CTAs an SM in bf16 (4096 x 8192 76 to 81 us; with earlier activations 83, for two 101, for four 92), for two in fp32 (4096 x 4096 78, three
+// 82).  Four chunks to a lane, widths from 8193 to 16384, do not fit those: up to 124 bytes a thread are spilled there, and 4096 x 11008 takes 130 us.
 struct GatedPlan {
   GatedArgs g;
   uint32_t room;
